@@ -179,7 +179,7 @@ def prepare(case, seed):
     return s
 
 
-MUON = dict(lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.01, steps=5, rms=0.2)
+MUON = dict(lr=0.02, beta=0.95, nesterov=True, weight_decay=0.01, steps=5, rms=0.2)
 
 
 def _own():
@@ -268,8 +268,8 @@ def _plain_muon(s):
     a, b, c = NS
     for at, r, k in s["matrices"].tolist():
         w, g, m = (s[n][at:at + r * k].view(r, k) for n in ("weights", "grads", "momentum"))
-        m.mul_(MUON["momentum"]).add_(g)
-        u = g + MUON["momentum"] * m
+        m.mul_(MUON["beta"]).add_(g)
+        u = g + MUON["beta"] * m
         x = u.T if r > k else u
         x = x / ((x * x).sum().sqrt() + 1e-7)
         for _ in range(MUON["steps"]):
@@ -339,8 +339,8 @@ def exact(case, seed):
     if c["op"] == "muon":
         p1, p3, p5 = NS
         W, M = s["weights"].double(), s["momentum"].double()
-        M = MUON["momentum"] * M + s["grads"].double()
-        U = s["grads"].double() + MUON["momentum"] * M
+        M = MUON["beta"] * M + s["grads"].double()
+        U = s["grads"].double() + MUON["beta"] * M
         for at, r, k in s["matrices"].tolist():
             u = U[at:at + r * k].view(r, k)
             u = u / (u.norm() + 1e-7)
