@@ -332,6 +332,84 @@ int xrl_ppo_objective(xrl_ctx *ctx, const xrl_batch *b, const float *d_logp, con
 int xrl_edge_features_from_shapes(const int32_t *shape_ptr, const int64_t *dims, int64_t n_edges,
                                   double M, float *edge_feat);
 
+/* ---- operators over a vocabulary -------------------------------------------------------------
+ * What a program needs beside the encoder to train and run a policy over a vocabulary (operator types, rewrite
+ * rules, tokens), and to step the weights. They use the context's stream and a workspace of its own, which only grows (a call that
+ * grows it waits for the stream; one under capture is refused with HIP if it would). Types are XRL_PREC_FP32 or XRL_PREC_BF16.
+ * All arrays are device memory unless said; a stride is the number of elements from one row to the next. Any alignment of the
+ * elements' own size is accepted; rows that begin at multiples of 16 bytes are the fastest. Results do not change from run to run. */
+
+/* xrl_embedding: out[t, :] = scale * table[ids[t], :], rounded once to the output's type; zeros for an id outside [0, vocab)
+ * (padding). d_table [vocab, dim] and d_out [n, dim] must not overlap. Errors: NULL, SHAPE, UNSUPPORTED (type), HIP. */
+int xrl_embedding(xrl_ctx *ctx, const void *d_table, int32_t table_type, int64_t table_stride, int64_t vocab, int64_t dim,
+                  const int32_t *d_ids, int64_t n, float scale, void *d_out, int32_t out_type, int64_t out_stride);
+
+/* xrl_embedding_backward: dtable[v, :] += scale * sum of dout[t, :] over the t with ids[t] = v, added up in fp32 in a fixed order; ids
+ * outside [0, vocab) add nothing, and rows that no id names are neither read nor written. d_dout [n, dim] of dout_type, d_dtable
+ * [vocab, dim] fp32. Errors: NULL, SHAPE, UNSUPPORTED (type; n from 2^27 or vocab from 2^30 on), OOM, HIP. */
+int xrl_embedding_backward(xrl_ctx *ctx, const void *d_dout, int32_t dout_type, int64_t dout_stride, const int32_t *d_ids,
+                           int64_t n, int64_t vocab, int64_t dim, float scale, float *d_dtable, int64_t dtable_stride);
+
+/* Rows of logits. Dense: n_rows rows of n_cols logits, `stride` apart. Ragged (d_row_ptr not NULL): row r is elements
+ * [d_row_ptr[r], d_row_ptr[r + 1]) of one flat array of n_cols elements in all (the slots of packed states: state_graph_ptr), `stride`
+ * and mask_stride are ignored, and what a d_row_ptr says outside the array counts as not there. A logit may be chosen if its mask byte is not 0 and it is not
+ * -inf; what stands in masked places is not looked at. */
+typedef struct xrl_logits_desc {
+  int64_t n_rows, n_cols, stride;
+  const void *d_logits;
+  const int32_t *d_row_ptr;   /* [n_rows + 1], or NULL                                                       */
+  const uint8_t *d_mask;      /* laid out like the logits, rows mask_stride apart (0: one row for all); or NULL */
+  int64_t mask_stride;
+  int32_t type;               /* of the logits                                                                  */
+  float temperature;          /* logits are divided by it; > 0                                                  */
+} xrl_logits_desc;
+
+/* xrl_token_logp: of every row the log-probability of a given entry, the entropy and the best entries, in one pass over the logits with sums
+ * in fp32. With x the logits over the temperature, over the entries that may be chosen:
+ *   logp = x[id] - ln sum exp x,  entropy = -sum p ln p,  top_ids / top_logp [n_rows, top_k] = the entries of the largest logits in
+ *   falling order, the lowest index first among equals, and their log-probabilities.
+ * d_ids [n_rows] (NULL: none is given, and d_logp may be NULL): index inside the row. A negative id is no token: logp 0. An id behind the row's
+ * end, or of an entry that may not be chosen: -inf. Alternatives that a row does not have are -1 and -inf. A row with
+ * nothing to choose has logp -inf and entropy 0. A NaN or +inf that may be chosen makes the row's logp, entropy and top_logp NaN.
+ * d_stats [n_rows, 2] (or NULL): the largest logit and ln sum exp(x - largest), for the backward call. top_k: 0 (the two arrays
+ * may be NULL) to 64. Errors: NULL, SHAPE, UNSUPPORTED (type, top_k), VALUE (temperature), OOM, HIP. */
+int xrl_token_logp(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d_ids, int32_t top_k, float *d_logp,
+                   float *d_entropy, float *d_stats, int32_t *d_top_ids, float *d_top_logp);
+
+/* xrl_token_logp_backward: writes dJ/dlogits (type and layout of the logits, rows dlogits_stride apart; it may be the logits' own
+ * memory at their own stride) for dJ/dlogp = d_dlogp [n_rows] and dJ/dentropy = d_dentropy [n_rows] (NULL: zeros), from the logits and what
+ * xrl_token_logp wrote of them (d_stats and d_entropy; the same ids, mask and temperature):
+ *   dlogits_j = (dlogp ([j = id] - p_j) - dentropy p_j (ln p_j + entropy)) / temperature.
+ * Exactly 0 at entries that may not be chosen. A row whose logp is 0 or -inf by the rules above takes nothing from d_dlogp.
+ * Errors: as above. */
+int xrl_token_logp_backward(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_entropy,
+                            const float *d_stats, const float *d_dlogp, const float *d_dentropy, void *d_dlogits,
+                            int64_t dlogits_stride);
+
+/* A matrix inside a flat vector of weights, row-major (what xrl_weight_tensor says of a tensor with cols > 0). */
+typedef struct xrl_matrix {
+  int64_t offset, rows, cols;
+} xrl_matrix;
+
+typedef struct xrl_muon_desc {
+  float lr, momentum, weight_decay;
+  float rms;          /* root mean square that the update of a matrix of full rank has before lr (usually 0.2) */
+  int32_t nesterov;   /* not 0: the update looks one momentum step ahead                                        */
+  int32_t steps;      /* Newton-Schulz steps, 1 to 16 (usually 5)                                              */
+} xrl_muon_desc;
+
+/* xrl_muon_step: one step of momentum with orthogonalised updates on each of the listed matrices (host array; they must
+ * not overlap) of a flat weight vector; the other entries of the vectors are not touched. Per matrix, all fp32:
+ *   M = momentum M + G;  U = nesterov ? G + momentum M : M;  X = U / (|U|_F + 1e-7), transposed if it has more rows than columns;
+ *   `steps` times: A = X X^T, X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;
+ *   W = (1 - lr weight_decay) W - lr rms sqrt(max(rows, cols)) X.
+ * The products run on the matrix cores on entries split in two halves of 11 bits each (22 bits of each factor count), with fp32 sums. |U|
+ * is summed in 64 bits. The vectors have n_weights entries each and must not overlap. A NaN or infinity in a matrix's gradient
+ * makes that matrix NaN, no other. Errors: NULL, SHAPE (a matrix outside the vector, overlapping ones), VALUE (not finite, negative
+ * lr, ...), UNSUPPORTED (more than 32768 rows or columns), OOM, HIP. */
+int xrl_muon_step(xrl_ctx *ctx, const xrl_muon_desc *desc, int32_t n_matrices, const xrl_matrix *matrices, int64_t n_weights,
+                  float *d_weights, const float *d_grads, float *d_momentum);
+
 /* ---- building blocks exposed for measurement and per-step checks ----------------------------
  * xrl_segment_sum: out[i, :] = sum of values[r, :] over rows r in [d_ptr[i], d_ptr[i+1]) -- the
  * receiver-side aggregation of Section 3.4's first two equations on receiver-ordered rows, and

@@ -59,13 +59,25 @@ class PackedView(C.Structure):
                 ("n_graph_tiles", C.c_int64), ("graph_tile_ptr", C.c_void_p), ("gtile_ptr", C.c_void_p)]
 
 
+class LogitsDesc(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("n_cols", C.c_int64), ("stride", C.c_int64), ("d_logits", C.c_void_p),
+                ("d_row_ptr", C.c_void_p), ("d_mask", C.c_void_p), ("mask_stride", C.c_int64), ("type", C.c_int32),
+                ("temperature", C.c_float)]
+
+
+class MuonDesc(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("rms", C.c_float),
+                ("nesterov", C.c_int32), ("steps", C.c_int32)]
+
+
 EXPORTS = ["xrl_weight_count", "xrl_weight_tensor_count", "xrl_weight_tensor", "xrl_pack_state", "xrl_pack_state_edits",
            "xrl_batch_dims", "xrl_batch_level", "xrl_batch_host_view", "xrl_batch_free", "xrl_create",
            "xrl_set_weights", "xrl_destroy", "xrl_batch_upload", "xrl_encode", "xrl_policy_value",
            "xrl_policy_value_static",
            "xrl_policy_value_backward", "xrl_encode_backward", "xrl_ppo_objective", "xrl_segment_sum",
            "xrl_get_activation", "xrl_set_timing", "xrl_read_timing", "xrl_measure_peaks",
-           "xrl_edge_features_from_shapes", "xrl_weight_gradient", "xrl_mlp_backward", "xrl_last_error", "xrl_version"]
+           "xrl_edge_features_from_shapes", "xrl_weight_gradient", "xrl_mlp_backward", "xrl_embedding",
+           "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_muon_step", "xrl_last_error", "xrl_version"]
 
 
 def load_library():
@@ -107,6 +119,11 @@ def load_library():
     lib.xrl_read_timing.argtypes = [vp, C.c_char_p, C.POINTER(C.c_double), C.POINTER(i64)]
     lib.xrl_measure_peaks.argtypes = [vp, i64, C.POINTER(C.c_double), C.POINTER(C.c_double)]
     lib.xrl_ppo_objective.argtypes = [vp] * 9 + [C.c_float] * 3 + [vp] * 4
+    lib.xrl_embedding.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, C.c_float, vp, i32, i64]
+    lib.xrl_embedding_backward.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, C.c_float, vp, i64]
+    lib.xrl_token_logp.argtypes = [vp, C.POINTER(LogitsDesc), vp, i32] + [vp] * 5
+    lib.xrl_token_logp_backward.argtypes = [vp, C.POINTER(LogitsDesc)] + [vp] * 6 + [i64]
+    lib.xrl_muon_step.argtypes = [vp, C.POINTER(MuonDesc), i32, vp, i64, vp, vp, vp]
     lib.xrl_last_error.restype = C.c_char_p
     lib.xrl_version.restype = C.c_char_p
     _lib = lib
@@ -148,6 +165,16 @@ def weight_layout(model):
         expect += int(np.prod(shape))
         out.append((name.value.decode(), shape))
     return out
+
+
+def weight_matrices(model):
+    """[count, 3] int64 (offset, rows, cols) of the flat vector's matrices, for Encoder.muon_step."""
+    at, out = 0, []
+    for _, shape in weight_layout(model):
+        if len(shape) == 2:
+            out.append((at,) + shape)
+        at += int(np.prod(shape))
+    return np.array(out, dtype=np.int64).reshape(-1, 3)
 
 
 def _arr(a, dtype):
@@ -358,6 +385,135 @@ class Encoder:
         _check(self.lib.xrl_segment_sum(self.handle, values.data_ptr(), ptr.data_ptr(), n_rows, n_seg,
                                         width, o.data_ptr()))
         return o
+
+    # ---- operators over a vocabulary (see xrl.h). Tensors that a method makes belong to the context's stream, as its kernels do: a
+    # program that works on another stream orders the two as it does for every call here.
+
+    def _made(self, shape, dtype):
+        t = self.torch
+        if t.cuda.current_stream() == self.stream:
+            return t.empty(shape, dtype=dtype, device="cuda")
+        with t.cuda.stream(self.stream):
+            return t.empty(shape, dtype=dtype, device="cuda")
+
+    def _type(self, x, name):
+        t = self.torch
+        if x.dtype == t.float32:
+            return 0
+        if x.dtype == t.bfloat16:
+            return 1
+        raise ValueError(f"{name}: {x.dtype}, float32 or bfloat16 is needed")
+
+    @staticmethod
+    def _rows(x, name, shape=None):
+        """Elements from row to row of a matrix on the GPU whose rows are contiguous."""
+        if not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+            raise ValueError(f"{name}: a matrix on the GPU with contiguous rows is needed")
+        if shape is not None and tuple(x.shape) != tuple(shape):
+            raise ValueError(f"{name}: shape {tuple(x.shape)}, {tuple(shape)} is needed")
+        return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], x.stride(0))
+
+    @staticmethod
+    def _flat(x, name, dtype, n):
+        """Address of a contiguous tensor on the GPU of n elements (None: none)."""
+        if x is None:
+            return None
+        if not x.is_cuda or x.dtype != dtype or x.numel() != n or not x.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous elements of {dtype} on the GPU are needed")
+        return x.data_ptr()
+
+    def embedding(self, table, ids, scale=1.0, dtype=None, out=None):
+        """[n, dim] rows scale * table[ids], zeros for ids outside the table; ids int32, out of `dtype` (the table's)."""
+        t = self.torch
+        stride, n = self._rows(table, "table"), ids.numel()
+        if out is None:
+            out = self._made((n, table.shape[1]), dtype or table.dtype)
+        elif dtype is not None and out.dtype != dtype:
+            raise ValueError(f"out: {out.dtype}, {dtype} is asked for")
+        _check(self.lib.xrl_embedding(self.handle, table.data_ptr(), self._type(table, "table"), stride, table.shape[0],
+                                      table.shape[1], self._flat(ids, "ids", t.int32, n), n, scale, out.data_ptr(),
+                                      self._type(out, "out"), self._rows(out, "out", (n, table.shape[1]))))
+        return out
+
+    def embedding_backward(self, dout, ids, dtable, scale=1.0):
+        """dtable[v] += scale * sum of the rows of dout whose id is v (dtable float32); returns dtable."""
+        t = self.torch
+        n, dim = dout.shape[0], dtable.shape[1]
+        stride, tstride = self._rows(dout, "dout", (n, dim)), self._rows(dtable, "dtable")
+        if dtable.dtype != t.float32:
+            raise ValueError(f"dtable: {dtable.dtype}, float32 is needed")
+        _check(self.lib.xrl_embedding_backward(self.handle, dout.data_ptr(), self._type(dout, "dout"), stride,
+                                               self._flat(ids, "ids", t.int32, n), n, dtable.shape[0], dim, scale,
+                                               dtable.data_ptr(), tstride))
+        return dtable
+
+    def _logits(self, logits, mask, row_ptr, temperature):
+        t = self.torch
+        if row_ptr is not None:
+            n, total = row_ptr.numel() - 1, logits.numel()
+            if n < 0:
+                raise ValueError("row_ptr: at least one element is needed")
+            self._flat(logits, "logits", logits.dtype, total)
+            return LogitsDesc(n, total, 0, logits.data_ptr(), self._flat(row_ptr, "row_ptr", t.int32, n + 1),
+                              self._flat(mask, "mask", t.uint8, total), 0, self._type(logits, "logits"), temperature)
+        stride, mstride = self._rows(logits, "logits"), 0
+        if mask is not None:
+            if mask.dtype != t.uint8:
+                raise ValueError(f"mask: {mask.dtype}, uint8 is needed")
+            if mask.dim() == 1:
+                self._flat(mask, "mask", t.uint8, logits.shape[1])
+            else:
+                mstride = self._rows(mask, "mask", logits.shape)
+        return LogitsDesc(logits.shape[0], logits.shape[1], stride, logits.data_ptr(), None,
+                          None if mask is None else mask.data_ptr(), mstride, self._type(logits, "logits"), temperature)
+
+    def token_logp(self, logits, ids=None, mask=None, row_ptr=None, top_k=0, temperature=1.0):
+        """Of every row of logits [n, cols] -- or, with row_ptr [n + 1] int32, of every range of flat logits --: dict(logp, entropy
+        [n], stats [n, 2] for the backward call, and with top_k: top_ids, top_logp [n, top_k]). ids int32 (None: no logp), mask
+        uint8 like the logits or, dense, one row for all. See xrl_token_logp."""
+        t = self.torch
+        d = self._logits(logits, mask, row_ptr, temperature)
+        n, f = d.n_rows, t.float32
+        o = dict(entropy=self._made((n,), f), stats=self._made((n, 2), f))
+        if ids is not None:
+            o["logp"] = self._made((n,), f)
+        if top_k:
+            o["top_ids"], o["top_logp"] = self._made((n, top_k), t.int32), self._made((n, top_k), f)
+        p = lambda k: o[k].data_ptr() if k in o else None  # noqa: E731
+        _check(self.lib.xrl_token_logp(self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), top_k, p("logp"),
+                                       p("entropy"), p("stats"), p("top_ids"), p("top_logp")))
+        return o
+
+    def token_logp_backward(self, logits, ids, forward, dlogp, dentropy=None, mask=None, row_ptr=None, temperature=1.0,
+                            out=None):
+        """dJ/dlogits, like the logits, from `forward` (what token_logp gave), dJ/dlogp and dJ/dentropy [n]; out may be the
+        logits' own memory. See xrl_token_logp_backward."""
+        t, f = self.torch, self.torch.float32
+        d = self._logits(logits, mask, row_ptr, temperature)
+        n = d.n_rows
+        if out is None:
+            out = self._made(tuple(logits.shape), logits.dtype)
+        if out.dtype != logits.dtype:
+            raise ValueError(f"out: {out.dtype}, {logits.dtype} is needed")
+        if row_ptr is not None:
+            self._flat(out, "out", logits.dtype, d.n_cols)
+        _check(self.lib.xrl_token_logp_backward(
+            self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), self._flat(forward["entropy"], "entropy", f, n),
+            self._flat(forward["stats"], "stats", f, 2 * n), self._flat(dlogp, "dlogp", f, n),
+            self._flat(dentropy, "dentropy", f, n), out.data_ptr(),
+            0 if row_ptr is not None else self._rows(out, "out", logits.shape)))
+        return out
+
+    def muon_step(self, weights, grads, momentum, matrices, lr, beta=0.95, nesterov=True, weight_decay=0.0, steps=5,
+                  rms=0.2):
+        """One step of momentum with orthogonalised updates, in place, on the matrices of flat float32 vectors (see
+        xrl_muon_step): matrices = [(offset, rows, cols)], a list or an int64 array (see weight_matrices)."""
+        f, n = self.torch.float32, weights.numel()
+        m = np.ascontiguousarray(matrices, dtype=np.int64).reshape(-1, 3)
+        d = MuonDesc(lr, beta, weight_decay, rms, int(nesterov), steps)
+        _check(self.lib.xrl_muon_step(self.handle, C.byref(d), m.shape[0], m.ctypes.data, n,
+                                      self._flat(weights, "weights", f, n), self._flat(grads, "grads", f, n),
+                                      self._flat(momentum, "momentum", f, n)))
 
     def get_activation(self, batch, what, rnd=0):
         shape = {"a0": (batch.N, self.model["d_edge"]), "pool": (batch.G, self.H)}.get(what, (batch.N, self.H))

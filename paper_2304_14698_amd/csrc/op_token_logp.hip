@@ -1,0 +1,432 @@
+// Log-probabilities of given entries of rows of logits, with entropy and the best entries, and their gradient.
+#include "op_common.h"
+
+#include <algorithm>
+#include <cmath>
+
+using namespace xrl;
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLowest = -3.402823466e38f;        // a maximum that no entry has reached yet: -inf - kLowest is -inf, not NaN
+constexpr int kMaxTop = 64;                        // one alternative a lane
+
+struct LogpArgs {
+  const void *logits;
+  const int32_t *row_ptr;
+  const uint8_t *mask;
+  const int32_t *ids;
+  int64_t row0, n_rows, n_cols, stride, mask_stride;   // row0: first row of this launch
+  float inv_t;
+  int top_k, parts;
+  float *logp, *entropy, *stats, *top_logp;
+  int32_t *top_ids;
+  // rows in several parts: of each part the maximum, the two sums and its best entries
+  float *part_sums;             // [rows][parts][3]
+  float *part_top;              // [rows][parts][top_k]
+  int32_t *part_ids;
+  // gradient
+  const float *dlogp, *dentropy;
+  void *dlogits;
+  int64_t dstride;
+};
+
+template <typename T>
+struct Row {
+  const T *x;
+  const uint8_t *mask;
+  int64_t begin;                // ragged: of the flat arrays
+  int len;
+};
+
+// Row r. What a row's ends say outside the array counts as not there.
+template <typename T>
+__device__ __forceinline__ Row<T> row_of(const LogpArgs &a, int64_t r) {
+  Row<T> o;
+  if (a.row_ptr) {
+    int64_t b = a.row_ptr[r], e = a.row_ptr[r + 1];
+    b = b < 0 ? 0 : b;
+    e = e > a.n_cols ? a.n_cols : e;
+    o.begin = b;
+    o.len = e > b ? (int)(e - b) : 0;
+    if (o.len == 0) o.begin = 0;
+    o.x = (const T *)a.logits + o.begin;
+    o.mask = a.mask ? a.mask + o.begin : nullptr;
+  } else {
+    o.begin = r * a.stride;
+    o.len = (int)a.n_cols;
+    o.x = (const T *)a.logits + o.begin;
+    o.mask = a.mask ? a.mask + r * a.mask_stride : nullptr;
+  }
+  return o;
+}
+
+// Running sums of the entries seen so far, m their largest logit: S = sum 2^t and W = sum 2^t t, t = (x - m) c with c = log2(e) / temperature.
+// A t of -inf counts as -200: 2^-200 is 0 in fp32, and 0 times it is 0.
+struct Sums {
+  float m, s, w;
+};
+__device__ __forceinline__ void add_sums(Sums &a, const Sums &b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  const float ta = (a.m - m) * c, tb = (b.m - m) * c;
+  const float ea = __builtin_amdgcn_exp2f(ta), eb = __builtin_amdgcn_exp2f(tb);
+  a.w = ea * (a.w + a.s * fmaxf(ta, -200.f)) + eb * (b.w + b.s * fmaxf(tb, -200.f));
+  a.s = ea * a.s + eb * b.s;
+  a.m = m;
+}
+
+// The best entries of a wave, lane i the i-th: by falling logit, then by rising index. An entry that is not there: kNone.
+constexpr int kNone = 0x7fffffff;
+struct Best {
+  float x;
+  int id;
+};
+__device__ __forceinline__ bool better(float xa, int ia, float xb, int ib) { return xa > xb || (xa == xb && ia < ib); }
+// One entry that all lanes hold the same goes into the list of k.
+__device__ __forceinline__ void insert_best(Best &b, float x, int id, int lane) {
+  const bool before = better(b.x, b.id, x, id);
+  const int at = __popcll(__ballot(before));
+  const float px = __shfl_up(b.x, 1);
+  const int pi = __shfl_up(b.id, 1);
+  if (lane == at) { b.x = x; b.id = id; }
+  if (lane > at) { b.x = px; b.id = pi; }
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+  for (int s = 32; s; s /= 2) v = fmaxf(v, __shfl_xor(v, s));
+  return v;
+}
+
+// What a wave does with VEC logits a lane: columns c .. c + VEC - 1 of the row, -inf where nothing may be chosen.
+template <int VEC, bool TOP>
+__device__ __forceinline__ void take(const float *x, int col, int lane, float c, int top_k, Sums &u, Best &best, float &bar) {
+  float mx = x[0];
+#pragma unroll
+  for (int j = 1; j < VEC; ++j) mx = fmaxf(mx, x[j]);
+  if (mx > u.m) {
+    const float t = (u.m - mx) * c, e = __builtin_amdgcn_exp2f(t);
+    u.w = e * (u.w + u.s * fmaxf(t, -200.f));
+    u.s *= e;
+    u.m = mx;
+  }
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) {
+    const float t = (x[j] - u.m) * c, e = __builtin_amdgcn_exp2f(t);
+    u.s += e;
+    u.w += e * fmaxf(t, -200.f);
+  }
+  if (TOP) {
+    // entries over the k-th best: the largest first, at most k of them. (One that equals it has a higher index than it.)
+    if (!__any(mx > bar)) return;
+    float y[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) y[j] = x[j];
+    for (int n = 0; n < top_k; ++n) {
+      float v = y[0];
+      int at = 0;
+#pragma unroll
+      for (int j = 1; j < VEC; ++j)
+        if (y[j] > v || !(v == v)) { v = y[j]; at = j; }
+      if (!(v == v)) v = -INFINITY;                       // NaN is no alternative
+      const float top = wave_max(v);
+      if (!(top > bar)) break;
+      const int from = __ffsll((unsigned long long)__ballot(v == top)) - 1;
+      const int id = __shfl(col + at, from);
+      insert_best(best, top, id, lane);
+      bar = __shfl(best.x, top_k - 1);
+      if (lane == from)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (j == at) y[j] = -INFINITY;
+    }
+  }
+}
+
+// The row's results from its sums (the same in all lanes) and its best entries.
+template <typename T>
+__device__ __forceinline__ void finish(const LogpArgs &a, int64_t r, const Row<T> &row, const Sums &u, const Best &best, int lane) {
+  const bool any = !(u.s == 0.f);                         // (NaN: yes)
+  const float ln_s = logf(u.s);
+  if (lane == 0) {
+    a.entropy[r] = any ? ln_s - kLn2 * (u.w / u.s) : 0.f;
+    if (a.stats) {
+      a.stats[2 * r] = any ? u.m : -INFINITY;
+      a.stats[2 * r + 1] = any ? ln_s : -INFINITY;
+    }
+    if (a.logp) {
+      const int id = a.ids ? a.ids[r] : -1;
+      float v = 0.f;
+      if (id >= 0) {
+        v = -INFINITY;
+        if (any && id < row.len && (!row.mask || row.mask[id])) v = ((float)row.x[id] - u.m) * a.inv_t - ln_s;
+      }
+      a.logp[r] = v;
+    }
+  }
+  if (lane < a.top_k) {
+    const bool there = best.id != kNone;
+    a.top_ids[r * a.top_k + lane] = there ? best.id : -1;
+    a.top_logp[r * a.top_k + lane] = !any || (!there && u.s == u.s) ? -INFINITY : (best.x - u.m) * a.inv_t - ln_s;
+  }
+}
+
+// k rounds: the best of the heads of `lists` lists of k entries each, which lie in memory one after another.
+template <typename GetX, typename GetId>
+__device__ __forceinline__ Best merge_best(int lists, int k, int lane, GetX get_x, GetId get_id) {
+  Best out = {-INFINITY, kNone};
+  int head = 0;
+  float x = lane < lists ? get_x(lane, 0) : -INFINITY;
+  int id = lane < lists ? get_id(lane, 0) : kNone;
+  for (int n = 0; n < k; ++n) {
+    float bx = x;
+    int bi = id;
+    for (int s = 32; s; s /= 2) {
+      const float ox = __shfl_xor(bx, s);
+      const int oi = __shfl_xor(bi, s);
+      if (better(ox, oi, bx, bi)) { bx = ox; bi = oi; }
+    }
+    if (lane == n) { out.x = bx; out.id = bi; }
+    if (bi == kNone) break;
+    if (id == bi) {
+      ++head;
+      x = head < k ? get_x(lane, head) : -INFINITY;
+      id = head < k ? get_id(lane, head) : kNone;
+    }
+  }
+  return out;
+}
+
+// A team of WAVES waves takes one part of one row.
+template <typename T, int WAVES, bool TOP>
+__global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
+  constexpr int VEC = 16 / (int)sizeof(T), TEAM = WAVES * 64, TEAMS = 256 / TEAM;
+  const int t = threadIdx.x % TEAM, lane = threadIdx.x & 63, wave = t >> 6;
+  const int64_t job = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
+  const int64_t r = a.row0 + job / a.parts;
+  const int part = (int)(job % a.parts);
+  if (r >= a.n_rows) return;                              // (a whole wave, and with WAVES > 1 the whole block)
+  const Row<T> row = row_of<T>(a, r);
+  const float c = a.inv_t * kLog2e;
+  // part `part`: columns [c0, c1), whole steps of the team
+  const int steps = (row.len + TEAM * VEC - 1) / (TEAM * VEC), per = (steps + a.parts - 1) / a.parts;
+  const int64_t b0 = (int64_t)part * per * (TEAM * VEC), b1 = b0 + (int64_t)per * (TEAM * VEC);
+  const int c0 = (int)(b0 < row.len ? b0 : row.len), c1 = (int)(b1 < row.len ? b1 : row.len);
+  Sums u = {kLowest, 0.f, 0.f};
+  Best best = {-INFINITY, kNone};
+  float bar = -INFINITY;
+  for (int col = c0 + t * VEC; col - lane * VEC < c1; col += TEAM * VEC) {
+    float x[VEC];
+    if (col + VEC <= c1) {
+      const Piece<T, VEC> p = load_piece<T, VEC>(row.x + col);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j];
+      if (row.mask) {
+        const Piece<uint8_t, VEC> m = load_piece<uint8_t, VEC>(row.mask + col);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[j] = m.v[j] ? x[j] : -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = col + j < c1 && (!row.mask || row.mask[col + j]) ? (float)row.x[col + j] : -INFINITY;
+    }
+    take<VEC, TOP>(x, col, lane, c, a.top_k, u, best, bar);
+  }
+  for (int s = 32; s; s /= 2) add_sums(u, {__shfl_xor(u.m, s), __shfl_xor(u.s, s), __shfl_xor(u.w, s)}, c);
+  if constexpr (WAVES > 1) {
+    __shared__ float sums[WAVES][3], bx[WAVES][kMaxTop];
+    __shared__ int bi[WAVES][kMaxTop];
+    if (lane == 0) { sums[wave][0] = u.m; sums[wave][1] = u.s; sums[wave][2] = u.w; }
+    bx[wave][lane] = best.x;
+    bi[wave][lane] = best.id;
+    __syncthreads();
+    if (wave) return;
+    for (int k = 1; k < WAVES; ++k) add_sums(u, {sums[k][0], sums[k][1], sums[k][2]}, c);
+    if (TOP)
+      best = merge_best(WAVES, a.top_k, lane, [&](int l, int i) { return bx[l][i]; }, [&](int l, int i) { return bi[l][i]; });
+  }
+  if (a.parts == 1) {
+    finish<T>(a, r, row, u, best, lane);
+    return;
+  }
+  if (lane == 0) {
+    float *p = a.part_sums + job * 3;
+    p[0] = u.m; p[1] = u.s; p[2] = u.w;
+  }
+  if (TOP && lane < a.top_k) {
+    a.part_top[job * a.top_k + lane] = best.x;
+    a.part_ids[job * a.top_k + lane] = best.id;
+  }
+}
+
+// A wave per row: its parts (at most 64), in order.
+template <typename T>
+__global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
+  const int64_t r = blockIdx.x;
+  const int lane = threadIdx.x;
+  const Row<T> row = row_of<T>(a, r);
+  const int64_t job = r * a.parts + lane;
+  const bool in = lane < a.parts;
+  const float *p = a.part_sums + (in ? job : 0) * 3;
+  Sums u = {in ? p[0] : kLowest, in ? p[1] : 0.f, in ? p[2] : 0.f};
+  for (int s = 32; s; s /= 2) add_sums(u, {__shfl_xor(u.m, s), __shfl_xor(u.s, s), __shfl_xor(u.w, s)}, a.inv_t * kLog2e);
+  Best best = {-INFINITY, kNone};
+  if (a.top_k)
+    best = merge_best(a.parts, a.top_k, lane, [&](int l, int i) { return a.part_top[(r * a.parts + l) * a.top_k + i]; },
+                      [&](int l, int i) { return a.part_ids[(r * a.parts + l) * a.top_k + i]; });
+  finish<T>(a, r, row, u, best, lane);
+}
+
+// dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
+template <typename T>
+__global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs a) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  const int64_t r = a.row0 + blockIdx.y + (int64_t)blockIdx.z * 32768;
+  if (r >= a.n_rows) return;
+  const Row<T> row = row_of<T>(a, r);
+  const float m = a.stats[2 * r], ln_s = a.stats[2 * r + 1], H = a.entropy[r];
+  const float c = a.inv_t * kLog2e, log2_s = ln_s * kLog2e;
+  const bool any = !(m == -INFINITY);
+  const int id0 = a.ids ? a.ids[r] : -1;
+  float g = 0.f;
+  int id = -1;
+  if (id0 >= 0 && id0 < row.len && (!row.mask || row.mask[id0]) && !((float)row.x[id0] == -INFINITY)) {
+    id = id0;
+    g = a.dlogp[r];
+  }
+  const float h = a.dentropy ? a.dentropy[r] : 0.f;
+  const float A = -a.inv_t * (g + h * H), B = -a.inv_t * h * kLn2;
+  T *out = (T *)a.dlogits + (a.row_ptr ? row.begin : r * a.dstride);
+  for (int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; col < row.len; col += (int64_t)gridDim.x * 256 * VEC) {
+    const int n = row.len - col < VEC ? (int)(row.len - col) : VEC;
+    float x[VEC], d[VEC];
+    bool ok[VEC];
+    if (n == VEC) {
+      const Piece<T, VEC> p = load_piece<T, VEC>(row.x + col);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j];
+      if (row.mask) {
+        const Piece<uint8_t, VEC> k = load_piece<uint8_t, VEC>(row.mask + col);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) ok[j] = k.v[j] != 0;
+      } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) ok[j] = true;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        ok[j] = j < n && (!row.mask || row.mask[col + j]);
+        x[j] = j < n ? (float)row.x[col + j] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const float q = (x[j] - m) * c - log2_s;
+      float v = __builtin_amdgcn_exp2f(q) * (A + B * fmaxf(q, -200.f));
+      if (col + j == id) v += a.inv_t * g;
+      d[j] = ok[j] && any && !(x[j] == -INFINITY) ? v : 0.f;
+    }
+    if (n == VEC) store_piece<T, VEC>(out + col, d);
+    else
+#pragma unroll
+      for (int j = 0; j < VEC; ++j)
+        if (j < n) out[col + j] = (T)d[j];
+  }
+}
+
+int check_logits(const xrl_ctx *c, const xrl_logits_desc *l, const char *who, LogpArgs &a) {
+  if (!c || !l) return fail(XRL_ERR_NULL, "%s: ctx or logits is NULL", who);
+  if (!op_type_ok(l->type)) return fail(XRL_ERR_UNSUPPORTED, "%s: type %d", who, l->type);
+  if (!(l->temperature > 0.f) || !std::isfinite(l->temperature)) return fail(XRL_ERR_VALUE, "%s: temperature %g", who, (double)l->temperature);
+  if (!std::isfinite(1.f / l->temperature * kLog2e)) return fail(XRL_ERR_VALUE, "%s: temperature %g", who, (double)l->temperature);
+  if (l->n_rows < 0 || l->n_cols < 0 || (!l->d_row_ptr && (l->stride < l->n_cols || (l->d_mask && l->mask_stride != 0 && l->mask_stride < l->n_cols))))
+    return fail(XRL_ERR_SHAPE, "%s: %lld rows of %lld columns, strides %lld and %lld", who, (long long)l->n_rows, (long long)l->n_cols,
+                (long long)l->stride, (long long)l->mask_stride);
+  if (l->n_cols > INT32_MAX - 65536 || l->n_rows > INT32_MAX)
+    return fail(XRL_ERR_UNSUPPORTED, "%s: %lld rows of %lld columns", who, (long long)l->n_rows, (long long)l->n_cols);
+  if (l->n_rows > 0 && l->n_cols > 0 && !l->d_logits) return fail(XRL_ERR_NULL, "%s: d_logits is NULL", who);
+  if ((uintptr_t)l->d_logits % (l->type == XRL_PREC_BF16 ? 2 : 4) || (uintptr_t)l->d_row_ptr % 4)
+    return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
+  a = LogpArgs{};
+  a.logits = l->d_logits; a.row_ptr = l->d_row_ptr; a.mask = l->d_mask;
+  a.n_rows = l->n_rows; a.n_cols = l->n_cols; a.stride = l->stride; a.mask_stride = l->mask_stride;
+  a.inv_t = 1.f / l->temperature;
+  return XRL_OK;
+}
+
+template <typename T, bool TOP>
+void launch_logp(const xrl_ctx *c, LogpArgs &a, bool wave_rows) {
+  for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMaxBlocks) {
+    const int64_t jobs = std::min(a.n_rows - a.row0, kMaxBlocks) * a.parts;    // (parts > 1: of a few rows)
+    if (wave_rows)
+      token_logp_kernel<T, 1, TOP><<<dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, op_stream(c)>>>(a);
+    else
+      token_logp_kernel<T, 4, TOP><<<dim3((unsigned)jobs), dim3(256), 0, op_stream(c)>>>(a);
+  }
+  if (a.parts > 1) token_logp_join_kernel<T><<<dim3((unsigned)a.n_rows), dim3(64), 0, op_stream(c)>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int xrl_token_logp(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_ids, int32_t top_k, float *d_logp,
+                   float *d_entropy, float *d_stats, int32_t *d_top_ids, float *d_top_logp) {
+  const char *who = "xrl_token_logp";
+  LogpArgs a;
+  if (int rc = check_logits(c, logits, who, a)) return rc;
+  if (top_k < 0 || top_k > kMaxTop) return fail(XRL_ERR_UNSUPPORTED, "%s: top_k = %d (at most %d)", who, top_k, kMaxTop);
+  if (a.n_rows == 0) return XRL_OK;
+  if ((d_ids && !d_logp) || !d_entropy || (top_k > 0 && (!d_top_ids || !d_top_logp))) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
+  if (((uintptr_t)d_ids | (uintptr_t)d_logp | (uintptr_t)d_entropy | (uintptr_t)d_stats | (uintptr_t)d_top_ids | (uintptr_t)d_top_logp) % 4)
+    return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
+  a.ids = d_ids; a.top_k = top_k; a.logp = d_logp; a.entropy = d_entropy; a.stats = d_stats; a.top_ids = d_top_ids; a.top_logp = d_top_logp;
+  const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols;      // (ragged: on average)
+  const bool wave_rows = cols <= 1024;
+  a.parts = 1;
+  if (!wave_rows) {
+    const int64_t want = 4 * (int64_t)op_compute_units(c) / a.n_rows, most = cols / 2048;
+    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+  }
+  if (a.parts > 1) {
+    const size_t jobs = (size_t)a.n_rows * a.parts, o_t = op_align(jobs * 12), o_i = o_t + op_align(jobs * top_k * 4);
+    char *ws = nullptr;
+    if (int rc = op_workspace(c, o_i + jobs * top_k * 4, &ws, who)) return rc;
+    a.part_sums = (float *)ws; a.part_top = (float *)(ws + o_t); a.part_ids = (int32_t *)(ws + o_i);
+  }
+  if (logits->type == XRL_PREC_BF16) top_k ? launch_logp<bf16_t, true>(c, a, wave_rows) : launch_logp<bf16_t, false>(c, a, wave_rows);
+  else top_k ? launch_logp<float, true>(c, a, wave_rows) : launch_logp<float, false>(c, a, wave_rows);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}
+
+int xrl_token_logp_backward(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_entropy,
+                            const float *d_stats, const float *d_dlogp, const float *d_dentropy, void *d_dlogits,
+                            int64_t dlogits_stride) {
+  const char *who = "xrl_token_logp_backward";
+  LogpArgs a;
+  if (int rc = check_logits(c, logits, who, a)) return rc;
+  if (a.n_rows == 0 || a.n_cols == 0) return XRL_OK;
+  if (!d_entropy || !d_stats || !d_dlogits || (d_ids && !d_dlogp)) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
+  if (!a.row_ptr && dlogits_stride < a.n_cols) return fail(XRL_ERR_SHAPE, "%s: dlogits_stride = %lld", who, (long long)dlogits_stride);
+  if (d_dlogits == logits->d_logits && !a.row_ptr && dlogits_stride != a.stride)
+    return fail(XRL_ERR_SHAPE, "%s: in place, but at another stride", who);
+  if (((uintptr_t)d_ids | (uintptr_t)d_entropy | (uintptr_t)d_stats | (uintptr_t)d_dlogp | (uintptr_t)d_dentropy) % 4 ||
+      (uintptr_t)d_dlogits % (logits->type == XRL_PREC_BF16 ? 2 : 4))
+    return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
+  a.ids = d_ids; a.entropy = (float *)d_entropy; a.stats = (float *)d_stats; a.dlogp = d_dlogp; a.dentropy = d_dentropy;
+  a.dlogits = d_dlogits; a.dstride = dlogits_stride;
+  const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, vec = logits->type == XRL_PREC_BF16 ? 8 : 4;
+  const int64_t chunks = std::max<int64_t>(1, (cols + 256 * vec * 2 - 1) / (256 * vec * 2));
+  for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMaxBlocks) {
+    const int64_t rows = std::min(a.n_rows - a.row0, kMaxBlocks);
+    const dim3 grid((unsigned)chunks, (unsigned)std::min<int64_t>(rows, 32768), (unsigned)((rows + 32767) / 32768));
+    if (logits->type == XRL_PREC_BF16) token_logp_backward_kernel<bf16_t><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+    else token_logp_backward_kernel<float><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  }
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}
+
+}  // extern "C"

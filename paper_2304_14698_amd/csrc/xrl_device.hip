@@ -240,6 +240,10 @@ struct xrl_ctx {
   size_t hws_bytes = 0;
   char *bws = nullptr;          // backward scratch
   size_t bws_bytes = 0;
+  char *ows = nullptr;          // the operators' (op_workspace), whether graphs hold addresses in it, and those it has outgrown
+  size_t ows_bytes = 0;
+  bool ows_captured = false;
+  std::vector<char *> ows_kept;
   bool room_refused = false;    // (see fit_room)
   size_t levels_refused = SIZE_MAX;   // least size of ws with levels in it that there was no memory for
   // buffers of the last encode (inside ws)
@@ -910,6 +914,34 @@ bool is_capturing(const xrl_ctx *c) {
   hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
   return went_well(hipStreamIsCapturing(c->stream, &cap)) && cap != hipStreamCaptureStatusNone;
 }
+
+}  // namespace
+namespace xrl {
+hipStream_t op_stream(const xrl_ctx *c) { return c->stream; }
+int op_compute_units(const xrl_ctx *c) { return c->n_cu; }
+int op_workspace(xrl_ctx *c, size_t bytes, char **ws, const char *who) {
+  const bool capturing = is_capturing(c);
+  if (bytes > c->ows_bytes) {
+    if (capturing)
+      return fail(XRL_ERR_HIP, "%s: the stream is being captured and the workspace would have to grow to %zu bytes: call it once before", who, bytes);
+    if (c->ows && c->ows_captured) {
+      try {
+        c->ows_kept.push_back(c->ows);
+      } catch (const std::bad_alloc &) {
+        return fail(XRL_ERR_OOM, "%s: out of host memory", who);
+      }
+      c->ows = nullptr;
+      c->ows_bytes = 0;
+      c->ows_captured = false;
+    }
+    if (int rc = ensure_buf(c, &c->ows, &c->ows_bytes, bytes, who)) return rc;
+  }
+  if (capturing) c->ows_captured = true;
+  *ws = c->ows;
+  return XRL_OK;
+}
+}  // namespace xrl
+namespace {
 
 int check_batch(xrl_ctx *c, const xrl_batch *b, const char *who) {
   if (!c || !b) return fail(XRL_ERR_NULL, "%s: ctx or batch is NULL", who);
@@ -3181,6 +3213,8 @@ int xrl_destroy(xrl_ctx *c) {
   if (c->ws) (void)hipFree(c->ws);
   if (c->hws) (void)hipFree(c->hws);
   if (c->bws) (void)hipFree(c->bws);
+  if (c->ows) (void)hipFree(c->ows);
+  for (char *p : c->ows_kept) (void)hipFree(p);
   for (auto &sp : c->spans) { (void)hipEventDestroy(sp.a); (void)hipEventDestroy(sp.b); }
   for (auto &e : c->free_events) (void)hipEventDestroy(e);
   c->blocks->close();
