@@ -389,12 +389,13 @@ class Encoder:
     # ---- operators over a vocabulary (see xrl.h). Tensors that a method makes belong to the context's stream, as its kernels do: a
     # program that works on another stream orders the two as it does for every call here.
 
-    def _made(self, shape, dtype):
+    def _made(self, *specs):
         t = self.torch
-        if t.cuda.current_stream() == self.stream:
-            return t.empty(shape, dtype=dtype, device="cuda")
+        # (the stream's handle: an object of it takes 3 us to make, the call to the library 4)
+        if t._C._cuda_getCurrentRawStream(self.stream.device_index) == self.stream.cuda_stream:
+            return [t.empty(shape, dtype=dtype, device="cuda") for shape, dtype in specs]
         with t.cuda.stream(self.stream):
-            return t.empty(shape, dtype=dtype, device="cuda")
+            return [t.empty(shape, dtype=dtype, device="cuda") for shape, dtype in specs]
 
     def _type(self, x, name):
         t = self.torch
@@ -427,7 +428,7 @@ class Encoder:
         t = self.torch
         stride, n = self._rows(table, "table"), ids.numel()
         if out is None:
-            out = self._made((n, table.shape[1]), dtype or table.dtype)
+            out, = self._made(((n, table.shape[1]), dtype or table.dtype))
         elif dtype is not None and out.dtype != dtype:
             raise ValueError(f"out: {out.dtype}, {dtype} is asked for")
         _check(self.lib.xrl_embedding(self.handle, table.data_ptr(), self._type(table, "table"), stride, table.shape[0],
@@ -467,21 +468,20 @@ class Encoder:
         return LogitsDesc(logits.shape[0], logits.shape[1], stride, logits.data_ptr(), None,
                           None if mask is None else mask.data_ptr(), mstride, self._type(logits, "logits"), temperature)
 
-    def token_logp(self, logits, ids=None, mask=None, row_ptr=None, top_k=0, temperature=1.0):
+    def token_logp(self, logits, ids=None, mask=None, row_ptr=None, top_k=0, temperature=1.0, out=None):
         """Of every row of logits [n, cols] -- or, with row_ptr [n + 1] int32, of every range of flat logits --: dict(logp, entropy
         [n], stats [n, 2] for the backward call, and with top_k: top_ids, top_logp [n, top_k]). ids int32 (None: no logp), mask
-        uint8 like the logits or, dense, one row for all. See xrl_token_logp."""
+        uint8 like the logits or, dense, one row for all; out: a dict that an earlier call of these sizes gave, written again. See
+        xrl_token_logp."""
         t = self.torch
         d = self._logits(logits, mask, row_ptr, temperature)
         n, f = d.n_rows, t.float32
-        o = dict(entropy=self._made((n,), f), stats=self._made((n, 2), f))
-        if ids is not None:
-            o["logp"] = self._made((n,), f)
-        if top_k:
-            o["top_ids"], o["top_logp"] = self._made((n, top_k), t.int32), self._made((n, top_k), f)
-        p = lambda k: o[k].data_ptr() if k in o else None  # noqa: E731
-        _check(self.lib.xrl_token_logp(self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), top_k, p("logp"),
-                                       p("entropy"), p("stats"), p("top_ids"), p("top_logp")))
+        keys = ["entropy", "stats"] + (["logp"] if ids is not None else []) + (["top_ids", "top_logp"] if top_k > 0 else [])
+        spec = dict(logp=((n,), f), entropy=((n,), f), stats=((n, 2), f), top_ids=((n, top_k), t.int32), top_logp=((n, top_k), f))
+        o = dict(zip(keys, self._made(*[spec[k] for k in keys]))) if out is None else out
+        p = [self._flat(o[k], k, spec[k][1], n * (1 if len(spec[k][0]) == 1 else spec[k][0][1])) if k in keys else None
+             for k in ("logp", "entropy", "stats", "top_ids", "top_logp")]
+        _check(self.lib.xrl_token_logp(self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), top_k, *p))
         return o
 
     def token_logp_backward(self, logits, ids, forward, dlogp, dentropy=None, mask=None, row_ptr=None, temperature=1.0,
@@ -492,7 +492,7 @@ class Encoder:
         d = self._logits(logits, mask, row_ptr, temperature)
         n = d.n_rows
         if out is None:
-            out = self._made(tuple(logits.shape), logits.dtype)
+            out, = self._made((logits.shape, logits.dtype))
         if out.dtype != logits.dtype:
             raise ValueError(f"out: {out.dtype}, {logits.dtype} is needed")
         if row_ptr is not None:

@@ -59,4 +59,29 @@ __device__ __forceinline__ void store_piece(T *p, const float *v) {
   __builtin_memcpy(p, &x, sizeof(x));
 }
 
+// Reductions over a wave by lane moves within the vector registers (a row of 16 lanes, then rows onto the next), the result in all lanes.
+// A shuffle goes through the LDS, about 100 clocks each way: six of them for a maximum, two dozen for a row's sums.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int lane_move(int old, int x) { return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xf, false); }
+constexpr int kShr1 = 0x111, kShr2 = 0x112, kShr4 = 0x114, kShr8 = 0x118, kBcast15 = 0x142, kBcast31 = 0x143, kWaveShr1 = 0x138;
+__device__ __forceinline__ float last_lane(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
+__device__ __forceinline__ float wave_max(float x) {
+#define STEP(CTRL) x = fmaxf(x, __int_as_float(lane_move<CTRL, 0xf>(__float_as_int(x), __float_as_int(x))))
+  STEP(kShr1); STEP(kShr2); STEP(kShr4); STEP(kShr8); STEP(kBcast15); STEP(kBcast31);
+#undef STEP
+  return last_lane(x);
+}
+__device__ __forceinline__ int wave_min(int x) {
+#define STEP(CTRL) { const int o = lane_move<CTRL, 0xf>(x, x); x = o < x ? o : x; }
+  STEP(kShr1) STEP(kShr2) STEP(kShr4) STEP(kShr8) STEP(kBcast15) STEP(kBcast31)
+#undef STEP
+  return __builtin_amdgcn_readlane(x, 63);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#define STEP(CTRL, ROWS) x += __int_as_float(lane_move<CTRL, ROWS>(0, __float_as_int(x)))
+  STEP(kShr1, 0xf); STEP(kShr2, 0xf); STEP(kShr4, 0xf); STEP(kShr8, 0xf); STEP(kBcast15, 0xa); STEP(kBcast31, 0xc);
+#undef STEP
+  return last_lane(x);
+}
+
 }  // namespace

@@ -87,15 +87,16 @@ __device__ __forceinline__ bool better(float xa, int ia, float xb, int ib) { ret
 __device__ __forceinline__ void insert_best(Best &b, float x, int id, int lane) {
   const bool before = better(b.x, b.id, x, id);
   const int at = __popcll(__ballot(before));
-  const float px = __shfl_up(b.x, 1);
-  const int pi = __shfl_up(b.id, 1);
+  const float px = __int_as_float(lane_move<kWaveShr1, 0xf>(0, __float_as_int(b.x)));
+  const int pi = lane_move<kWaveShr1, 0xf>(0, b.id);
   if (lane == at) { b.x = x; b.id = id; }
   if (lane > at) { b.x = px; b.id = pi; }
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-  for (int s = 32; s; s /= 2) v = fmaxf(v, __shfl_xor(v, s));
-  return v;
+// The sums of all lanes of a wave, in all lanes.
+__device__ __forceinline__ Sums wave_sums(const Sums &u, float c) {
+  const float m = wave_max(u.m), t = (u.m - m) * c, e = __builtin_amdgcn_exp2f(t);
+  return {m, wave_sum(e * u.s), wave_sum(e * (u.w + u.s * fmaxf(t, -200.f)))};
 }
 
 // What a wave does with VEC logits a lane: columns c .. c + VEC - 1 of the row, -inf where nothing may be chosen.
@@ -132,9 +133,9 @@ __device__ __forceinline__ void take(const float *x, int col, int lane, float c,
       const float top = wave_max(v);
       if (!(top > bar)) break;
       const int from = __ffsll((unsigned long long)__ballot(v == top)) - 1;
-      const int id = __shfl(col + at, from);
+      const int id = __builtin_amdgcn_readlane(col + at, from);
       insert_best(best, top, id, lane);
-      bar = __shfl(best.x, top_k - 1);
+      bar = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(best.x), top_k - 1));
       if (lane == from)
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
@@ -179,13 +180,10 @@ __device__ __forceinline__ Best merge_best(int lists, int k, int lane, GetX get_
   float x = lane < lists ? get_x(lane, 0) : -INFINITY;
   int id = lane < lists ? get_id(lane, 0) : kNone;
   for (int n = 0; n < k; ++n) {
-    float bx = x;
-    int bi = id;
-    for (int s = 32; s; s /= 2) {
-      const float ox = __shfl_xor(bx, s);
-      const int oi = __shfl_xor(bi, s);
-      if (better(ox, oi, bx, bi)) { bx = ox; bi = oi; }
-    }
+    const float bx = wave_max(x);
+    const unsigned long long tied = __ballot(x == bx);
+    int bi = __builtin_amdgcn_readlane(id, __ffsll(tied) - 1);
+    if (tied & (tied - 1)) bi = wave_min(x == bx ? id : kNone);
     if (lane == n) { out.x = bx; out.id = bi; }
     if (bi == kNone) break;
     if (id == bi) {
@@ -232,7 +230,7 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
     }
     take<VEC, TOP>(x, col, lane, c, a.top_k, u, best, bar);
   }
-  for (int s = 32; s; s /= 2) add_sums(u, {__shfl_xor(u.m, s), __shfl_xor(u.s, s), __shfl_xor(u.w, s)}, c);
+  u = wave_sums(u, c);
   if constexpr (WAVES > 1) {
     __shared__ float sums[WAVES][3], bx[WAVES][kMaxTop];
     __shared__ int bi[WAVES][kMaxTop];
@@ -269,7 +267,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
   const bool in = lane < a.parts;
   const float *p = a.part_sums + (in ? job : 0) * 3;
   Sums u = {in ? p[0] : kLowest, in ? p[1] : 0.f, in ? p[2] : 0.f};
-  for (int s = 32; s; s /= 2) add_sums(u, {__shfl_xor(u.m, s), __shfl_xor(u.s, s), __shfl_xor(u.w, s)}, a.inv_t * kLog2e);
+  u = wave_sums(u, a.inv_t * kLog2e);
   Best best = {-INFINITY, kNone};
   if (a.top_k)
     best = merge_best(a.parts, a.top_k, lane, [&](int l, int i) { return a.part_top[(r * a.parts + l) * a.top_k + i]; },
