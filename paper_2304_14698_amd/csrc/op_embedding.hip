@@ -58,15 +58,80 @@ int launch_embed(const xrl_ctx *c, EmbedArgs &a) {
 }
 
 // ---- gradient
-// Sorted pairs (id, t): a stable radix sort by up to kDigitBits bits a pass. Ids outside the vocabulary sort behind all others, as `vocab`.
+// Few ids: a block per place t and slab of columns. It ends at once if the id stands before t; else it adds up all places of the id, wave w those of the
+// w-th quarter of the places from t on, and the four sums in order. One launch and no workspace.
+constexpr int kFewIds = 2048;
+
+struct FewArgs {
+  const int32_t *ids;
+  const void *dout;
+  float *dtable;
+  int64_t dout_stride, dtable_stride;
+  int n, vocab, dim;
+  float scale;
+};
+
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void embed_few_kernel(const FewArgs a) {
+  touch_args(a);
+  const int t = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int id = a.ids[t];
+  if ((unsigned)id >= (unsigned)a.vocab) return;
+  int before = 0;
+  for (int i = threadIdx.x; i < t; i += 256) before |= a.ids[i] == id;
+  if (__syncthreads_or(before)) return;
+  const int c = ((int)blockIdx.y * 64 + lane) * VEC, nv = a.dim - c < VEC ? a.dim - c : VEC;
+  const int chunks = (a.n - t + 63) / 64, per = (chunks + 3) / 4;
+  const int i0 = t + w * per * 64, i1 = i0 + per * 64 < a.n ? i0 + per * 64 : a.n;
+  float acc[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+  for (int i = i0; i < i1; i += 64) {
+    unsigned long long here = __ballot(i + lane < i1 && a.ids[i + lane < i1 ? i + lane : i] == id);
+    while (here) {
+      constexpr int BATCH = 8;
+      Piece<T, VEC> v[BATCH];
+      int got = 0;
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        if (!here) break;
+        const T *p = (const T *)a.dout + (int64_t)(i + __ffsll(here) - 1) * a.dout_stride + c;
+        here &= here - 1;
+        got = k + 1;
+        if (nv == VEC) v[k] = load_piece<T, VEC>(p);
+        else
+          for (int j = 0; j < VEC; ++j) v[k].v[j] = j < nv ? p[j] : (T)0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k)
+        if (k < got)
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) acc[j] += (float)v[k].v[j];
+    }
+  }
+  __shared__ float part[3][64][VEC + 1];
+  if (w)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) part[w - 1][lane][j] = acc[j];
+  __syncthreads();
+  if (w) return;
+  float *p = a.dtable + (int64_t)id * a.dtable_stride + c;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j)
+    if (j < nv) p[j] += a.scale * (((acc[j] + part[0][lane][j]) + part[1][lane][j]) + part[2][lane][j]);
+}
+
+// More ids: sorted pairs (id, t) by a stable radix sort of up to kDigitBits bits a pass. Ids outside the vocabulary sort behind all others, as
+// `vocab`. A pass takes one launch: its scatter counts, for the pass behind it, the digits that each block of that will find; only the first has a launch that counts.
 constexpr int kDigitBits = 10, kSortBlocks = 64, kSortThreads = 512, kSortWaves = kSortThreads / 64;
 
 struct SortArgs {
   const int32_t *ids;           // first pass: the items are (ids[t], t)
   const uint2 *in;              // later passes
   uint2 *out;
-  int32_t *hist;                // [blocks][1 << bits]
-  int64_t n;
+  int32_t *hist, *next_hist;    // [blocks][1 << bits] of this pass and of the one behind it (nullptr: none)
+  int32_t *clear;               // counting launch: zeroed, clear_n of them
+  int64_t n, clear_n;
   int vocab, shift, bits, per_wave;   // per_wave: consecutive items of a wave, a multiple of 64
 };
 
@@ -77,9 +142,11 @@ __device__ __forceinline__ uint2 sort_item(const SortArgs &a, int64_t i) {
 }
 
 __global__ __launch_bounds__(kSortThreads) void embed_sort_count_kernel(const SortArgs a) {
+  touch_args(a);
   __shared__ int cnt[1 << kDigitBits];
   const int digits = 1 << a.bits;
   for (int d = threadIdx.x; d < digits; d += kSortThreads) cnt[d] = 0;
+  for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < a.clear_n; i += (int64_t)gridDim.x * kSortThreads) a.clear[i] = 0;
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * kSortWaves * a.per_wave;
   const int64_t i1 = i0 + (int64_t)kSortWaves * a.per_wave < a.n ? i0 + (int64_t)kSortWaves * a.per_wave : a.n;
@@ -89,29 +156,35 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_count_kernel(const So
 }
 
 __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const SortArgs a) {
+  touch_args(a);
   __shared__ int off[kSortWaves][1 << kDigitBits];
-  __shared__ int total[1 << kDigitBits], wave_sum[kSortWaves];
+  __shared__ int total[1 << kDigitBits], before[1 << kDigitBits], wave_sum[kSortWaves];
   const int digits = 1 << a.bits, t = threadIdx.x, lane = t & 63, w = t >> 6;
   for (int k = 0; k < kSortWaves; ++k)
     for (int d = t; d < digits; d += kSortThreads) off[k][d] = 0;
+  for (int d = t; d < digits; d += kSortThreads) total[d] = before[d] = 0;
   __syncthreads();
   const int64_t w0 = ((int64_t)blockIdx.x * kSortWaves + w) * a.per_wave;
   for (int k = lane; k < a.per_wave; k += 64)
     if (w0 + k < a.n) atomicAdd(&off[w][(sort_item(a, w0 + k).x >> a.shift) & (digits - 1)], 1);
-  // of each digit: the items of all blocks, and those of the blocks before
-  int before[(1 << kDigitBits) / kSortThreads];
+  // of each digit: the items of all blocks, and those of the blocks before; digits x blocks dealt to the threads, eight requests at a time
+  {
+    const int d = t & (digits - 1), slices = digits < kSortThreads ? kSortThreads / digits : 1;
+    for (int dd = d; dd < digits; dd += kSortThreads) {
+      int sum = 0, mine = 0;
+      for (int b = digits < kSortThreads ? t / digits : 0; b < (int)gridDim.x; b += 8 * slices) {
+        int h[8];
 #pragma unroll
-  for (int q = 0; q < (1 << kDigitBits) / kSortThreads; ++q) {
-    const int d = t + q * kSortThreads;
-    int sum = 0, mine = 0;
-    if (d < digits)
-      for (int b = 0; b < (int)gridDim.x; ++b) {
-        const int h = a.hist[(size_t)b * digits + d];
-        mine += b < (int)blockIdx.x ? h : 0;
-        sum += h;
+        for (int k = 0; k < 8; ++k) h[k] = b + k * slices < (int)gridDim.x ? a.hist[(size_t)(b + k * slices) * digits + dd] : 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          sum += h[k];
+          mine += b + k * slices < (int)blockIdx.x ? h[k] : 0;
+        }
       }
-    before[q] = mine;
-    if (d < digits) total[d] = sum;
+      atomicAdd(&total[dd], sum);
+      atomicAdd(&before[dd], mine);
+    }
   }
   __syncthreads();
   // exclusive sums over the digits: thread t takes digits [t * per, ...)
@@ -127,27 +200,21 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
   __syncthreads();
   int base = inc - own;
   for (int k = 0; k < w; ++k) base += wave_sum[k];
-  for (int k = 0; k < per; ++k)
-    if (t * per + k < digits) {
-      const int x = total[t * per + k];
-      total[t * per + k] = base;
-      base += x;
-    }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < (1 << kDigitBits) / kSortThreads; ++q) {
-    const int d = t + q * kSortThreads;
+  for (int k = 0; k < per; ++k) {
+    const int d = t * per + k;
     if (d < digits) {
-      int at = total[d] + before[q];
-      for (int k = 0; k < kSortWaves; ++k) {       // digit d's first place for each wave
-        const int x = off[k][d];
-        off[k][d] = at;
+      int at = base + before[d];
+      base += total[d];
+      for (int q = 0; q < kSortWaves; ++q) {             // digit d's first place for each wave
+        const int x = off[q][d];
+        off[q][d] = at;
         at += x;
       }
     }
   }
   __syncthreads();
   volatile int *mine = off[w];
+  const int64_t per_block = (int64_t)kSortWaves * a.per_wave;
   for (int k = 0; k < a.per_wave; k += 64) {
     const int64_t i = w0 + k + lane;
     const bool in = i < a.n;
@@ -164,26 +231,34 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
     if (in && rank == 0) mine[d] = place + __popcll(same);
     __threadfence_block();
     __builtin_amdgcn_wave_barrier();
-    if (in) a.out[place] = x;
+    if (in) {
+      a.out[place] = x;
+      if (a.next_hist)                                    // (integers: the same in any order)
+        atomicAdd(&a.next_hist[(size_t)(place / per_block) * digits + ((x.x >> (a.shift + a.bits)) & (unsigned)(digits - 1))], 1);
+    }
   }
 }
 
-// Sums over runs of equal ids. A group of `lanes` threads takes kWindow consecutive sorted pairs, in their order. A run inside the window is
-// added to its row of the table; the piece of a run that began before goes to carry[window][0], that of one that goes on behind it to
-// carry[window][1], and embed_join_kernel adds up the pieces of each such run.
-constexpr int kWindow = 32;
+// Sums over runs of equal ids. A group of `lanes` threads takes kWindow consecutive sorted pairs, in their order; a batch's rows, and the rows of the
+// table that its runs are added to, are requested together. A run inside the window is added to its row of the table. The piece of a run that began
+// before goes to carry[window][0], that of one that goes on behind it to carry[window][1]; a window that such a run begins in is listed, and
+// embed_join_kernel adds up the run's pieces.
+constexpr int kWindow = 16;
 
 struct SumArgs {
   const uint2 *items;
   const void *dout;
   float *dtable, *carry;        // carry [windows][2][dim]
+  int32_t *listed, *list;       // how many windows are listed, and which (in any order)
   int64_t dout_stride, dtable_stride, n;
   int vocab, dim, lanes;
   float scale;
 };
 
-template <typename T, int VEC, int BATCH>
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
+  touch_args(a);
+  constexpr int BATCH = 8;
   const int lane = threadIdx.x & (a.lanes - 1);
   const int64_t w = (int64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
   const int64_t i0 = w * kWindow;
@@ -191,76 +266,136 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   const int c = ((int)blockIdx.y * a.lanes + lane) * VEC;
   if (c >= a.dim) return;
   const int nv = a.dim - c < VEC ? a.dim - c : VEC;     // columns of this thread
-  const int len = (int)(a.n - i0 < kWindow ? a.n - i0 : kWindow);
+  const unsigned vocab = (unsigned)a.vocab;
   const uint2 *it = a.items + i0;
-  const unsigned before = i0 > 0 ? it[-1].x : ~0u, behind = i0 + len < a.n ? it[len].x : ~0u;
+  // the window's pairs, and the ids around it (behind the last pair: no row's)
+  unsigned id[kWindow + 2];
+  int at[kWindow];
+  id[0] = i0 > 0 ? it[-1].x : ~0u;
+#pragma unroll
+  for (int i = 0; i < kWindow + 1; ++i) {
+    const uint2 x = i0 + i < a.n ? it[i] : make_uint2(vocab, 0);
+    id[i + 1] = x.x;
+    if (i < kWindow) at[i] = (int)x.y;
+  }
   float acc[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
-  bool first = true;                                     // in the window's first run
-  for (int b0 = 0; b0 < len; b0 += BATCH) {
-    uint2 x[BATCH];
+  bool head = id[0] == id[1];                            // the run at hand began before the window
+#pragma unroll
+  for (int b0 = 0; b0 < kWindow; b0 += BATCH) {
     Piece<T, VEC> v[BATCH];
+    Piece<float, VEC> old[BATCH];
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) x[i] = b0 + i < len ? it[b0 + i] : make_uint2((unsigned)a.vocab, 0);
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = b0 + k;
+      if (id[i + 1] >= vocab) continue;
+      const T *p = (const T *)a.dout + (int64_t)at[i] * a.dout_stride + c;
+      if (nv == VEC) v[k] = load_piece<T, VEC>(p);
+      else
+        for (int j = 0; j < VEC; ++j) v[k].v[j] = j < nv ? p[j] : (T)0.f;
+      if (id[i + 2] != id[i + 1] && nv == VEC) old[k] = load_piece<float, VEC>(a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c);
+    }
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i)
-      if (x[i].x < (unsigned)a.vocab) {
-        const T *p = (const T *)a.dout + (int64_t)x[i].y * a.dout_stride + c;
-        if (nv == VEC) v[i] = load_piece<T, VEC>(p);
-        else
-          for (int j = 0; j < VEC; ++j) v[i].v[j] = j < nv ? p[j] : (T)0.f;
-      }
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = b0 + k;
+      if (id[i + 1] >= vocab) continue;
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-      if (x[i].x >= (unsigned)a.vocab) continue;         // behind the end, or no row's id
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) acc[j] += (float)v[i].v[j];
-      const bool last = b0 + i == len - 1;
-      const unsigned next = last ? behind : it[b0 + i + 1].x;
-      if (next == x[i].x && !last) continue;
-      const bool head = first && before == x[i].x, goes_on = next == x[i].x;
-      float *p = head || goes_on ? a.carry + ((size_t)w * 2 + (head ? 0 : 1)) * a.dim + c
-                                 : a.dtable + (int64_t)x[i].x * a.dtable_stride + c;
+      for (int j = 0; j < VEC; ++j) acc[j] += (float)v[k].v[j];
+      const bool goes_on = id[i + 2] == id[i + 1];
+      if (goes_on && i < kWindow - 1) continue;
       if (head || goes_on) {
-        for (int j = 0; j < nv; ++j) p[j] = acc[j];
+        float *p = a.carry + ((size_t)w * 2 + (head ? 0 : 1)) * a.dim + c;
+        if (nv == VEC) store_piece<float, VEC>(p, acc);
+        else
+          for (int j = 0; j < nv; ++j) p[j] = acc[j];
+        if (!head && lane == 0 && blockIdx.y == 0) a.list[atomicAdd(a.listed, 1)] = (int)w;
       } else {
-        for (int j = 0; j < nv; ++j) p[j] += a.scale * acc[j];
+        float *p = a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c;
+        if (nv == VEC) {
+          float s[VEC];
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) s[j] = old[k].v[j] + a.scale * acc[j];
+          store_piece<float, VEC>(p, s);
+        } else {
+          for (int j = 0; j < nv; ++j) p[j] += a.scale * acc[j];
+        }
       }
-      first = false;
+      head = false;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
     }
   }
 }
 
-// A block per window: if its last run begins in it and goes on, the run's pieces in sixteen parts, and the parts in order.
-__global__ __launch_bounds__(1024) void embed_join_kernel(const SumArgs a) {
-  const int64_t w = blockIdx.x, i1 = (w + 1) * kWindow;
-  if (i1 >= a.n) return;
-  const unsigned id = a.items[i1 - 1].x;
-  if (id >= (unsigned)a.vocab || a.items[i1].x != id) return;
-  if (a.items[i1 - kWindow].x == id && w > 0 && a.items[i1 - kWindow - 1].x == id) return;   // began before
-  // the first pair behind the run
-  int64_t lo = i1, hi = a.n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (a.items[mid].x <= id) lo = mid + 1; else hi = mid;
+// The runs that go over windows: a block takes listed windows and 256 columns, each of its four waves a quarter of the run's pieces, eight requests
+// at a time, and adds up the four sums in order.
+__global__ __launch_bounds__(256) void embed_join_kernel(const SumArgs a) {
+  touch_args(a);
+  __shared__ float part[3][256];
+  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, listed = *a.listed;
+  const int c = (int)blockIdx.y * 256 + lane * 4;
+  const int nv = a.dim - c < 4 ? a.dim - c : 4;
+  for (int q = blockIdx.x; q < listed; q += gridDim.x) {
+    const int64_t w = a.list[q], i1 = (w + 1) * kWindow;
+    const unsigned id = a.items[i1 - 1].x;
+    // the first pair behind the run: steps of growing size, then halves
+    int64_t lo = i1, step = kWindow;
+    while (lo + step < a.n && a.items[lo + step].x == id) {
+      lo += step;
+      step *= 2;
+    }
+    int64_t hi = lo + step < a.n ? lo + step : a.n;      // items[lo] is the run's (i1 is: it goes on), items[hi] is not
+    while (hi - lo > 1) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (a.items[mid].x == id) lo = mid; else hi = mid;
+    }
+    const int64_t n = lo / kWindow + 1 - w, per = (n + 3) / 4, p0 = g * per, p1 = p0 + per < n ? p0 + per : n;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (nv == 4) {
+      int64_t k = p0;
+      const float *src = a.carry + (size_t)w * 2 * a.dim + c;
+      if (k == 0 && k < p1) {                             // the run's first piece
+        const Piece<float, 4> x = load_piece<float, 4>(src + a.dim);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = x.v[j];
+        ++k;
+      }
+      for (; k < p1; k += 8) {
+        Piece<float, 4> x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (k + u < p1) x[u] = load_piece<float, 4>(src + (size_t)(k + u) * 2 * a.dim);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (k + u < p1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += x[u].v[j];
+      }
+    } else {
+      for (int64_t k = p0; k < p1; ++k)
+        for (int j = 0; j < nv; ++j) sum[j] += a.carry[((size_t)(w + k) * 2 + (k == 0 ? 1 : 0)) * a.dim + c + j];
+    }
+    __syncthreads();
+    if (g)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) part[g - 1][lane * 4 + j] = sum[j];
+    __syncthreads();
+    if (g == 0) {
+      float *p = a.dtable + (int64_t)id * a.dtable_stride + c;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < nv) p[j] += a.scale * (((sum[j] + part[0][lane * 4 + j]) + part[1][lane * 4 + j]) + part[2][lane * 4 + j]);
+    }
   }
-  const int64_t w_end = (lo + kWindow - 1) / kWindow;   // windows w + 1 .. w_end - 1 hold its other pieces
-  __shared__ float part[16][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int c = (int)blockIdx.y * 64 + lane;
-  const int64_t n = w_end - w, per = (n + 15) / 16, p0 = g * per, p1 = p0 + per < n ? p0 + per : n;
-  float sum = 0.f;
-  if (c < a.dim)
-    for (int64_t k = p0; k < p1; ++k) sum += a.carry[((size_t)(w + k) * 2 + (k == 0 ? 1 : 0)) * a.dim + c];
-  part[g][lane] = sum;
-  __syncthreads();
-  if (g || c >= a.dim) return;
-  for (int k = 1; k < 16; ++k) sum += part[k][lane];
-  float *p = a.dtable + (int64_t)id * a.dtable_stride + c;
-  *p += a.scale * sum;
+}
+
+template <typename T>
+int launch_embed_few(const xrl_ctx *c, const FewArgs &a) {
+  constexpr int VEC = sizeof(T) == 2 ? 8 : 4;
+  embed_few_kernel<T, VEC><<<dim3((unsigned)a.n, (unsigned)((a.dim + 64 * VEC - 1) / (64 * VEC))), dim3(256), 0, op_stream(c)>>>(a);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
 }
 
 template <typename T>
@@ -270,9 +405,10 @@ int launch_embed_sums(const xrl_ctx *c, SumArgs &a) {
   a.lanes = 1;
   while (a.lanes < pieces && a.lanes < 256) a.lanes *= 2;
   const int64_t windows = (a.n + kWindow - 1) / kWindow, per = 256 / a.lanes;
-  embed_sum_kernel<T, VEC, 4><<<dim3((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes)), dim3(256), 0,
-                                op_stream(c)>>>(a);
-  embed_join_kernel<<<dim3((unsigned)windows, (unsigned)((a.dim + 63) / 64)), dim3(1024), 0, op_stream(c)>>>(a);
+  embed_sum_kernel<T, VEC><<<dim3((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes)), dim3(256), 0,
+                             op_stream(c)>>>(a);
+  embed_join_kernel<<<dim3((unsigned)std::min<int64_t>(windows, 4 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256)), dim3(256), 0,
+                      op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
@@ -314,6 +450,10 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   if (!d_ids || !d_dout || !d_dtable) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
   if ((uintptr_t)d_dout % (dout_type == XRL_PREC_BF16 ? 2 : 4) || (uintptr_t)d_dtable % 4 || (uintptr_t)d_ids % 4)
     return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
+  if (n <= kFewIds) {
+    const FewArgs a = {d_ids, d_dout, d_dtable, dout_stride, dtable_stride, (int)n, (int)vocab, (int)dim, scale};
+    return dout_type == XRL_PREC_BF16 ? launch_embed_few<bf16_t>(c, a) : launch_embed_few<float>(c, a);
+  }
   int bits = 1;
   while ((vocab >> bits) > 0) ++bits;                   // of the largest key, `vocab`
   const int passes = (bits + kDigitBits - 1) / kDigitBits, per_pass = (bits + passes - 1) / passes;
@@ -323,20 +463,26 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   s.per_wave = (int)((per_wave + 63) / 64 * 64);
   const int blocks = (int)((n + (int64_t)s.per_wave * kSortWaves - 1) / ((int64_t)s.per_wave * kSortWaves));
   const int64_t windows = (n + kWindow - 1) / kWindow;
-  const size_t o_b = op_align((size_t)n * 8), o_h = 2 * o_b, o_c = o_h + op_align((size_t)blocks * ((size_t)4 << per_pass));
+  const int64_t hist = (int64_t)blocks << per_pass;      // counters of one pass
+  const size_t o_b = op_align((size_t)n * 8), o_h = 2 * o_b, o_l = o_h + op_align((size_t)(passes * hist + 1) * 4),
+               o_c = o_l + op_align((size_t)windows * 4);
   char *ws = nullptr;
   if (int rc = op_workspace(c, o_c + (size_t)windows * 2 * dim * 4, &ws, who)) return rc;
   uint2 *x = (uint2 *)ws, *y = (uint2 *)(ws + o_b);
-  s.hist = (int32_t *)(ws + o_h);
+  int32_t *counters = (int32_t *)(ws + o_h);             // the first pass's, the others' (cleared), the list's length (cleared)
+  s.hist = counters; s.clear = counters + hist; s.clear_n = (passes - 1) * hist + 1;
+  s.ids = d_ids;
+  embed_sort_count_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);
   for (int p = 0; p < passes; ++p) {
     s.ids = p == 0 ? d_ids : nullptr;
     s.in = x; s.out = y; s.shift = p * per_pass;
-    embed_sort_count_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);
+    s.hist = counters + p * hist; s.next_hist = p + 1 < passes ? s.hist + hist : nullptr;
     embed_sort_scatter_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);
     std::swap(x, y);
   }
   OP_TRY(hipGetLastError());
-  SumArgs a = {x, d_dout, d_dtable, (float *)(ws + o_c), dout_stride, dtable_stride, n, (int)vocab, (int)dim, 0, scale};
+  SumArgs a = {x, d_dout, d_dtable, (float *)(ws + o_c), counters + passes * hist, (int32_t *)(ws + o_l), dout_stride, dtable_stride, n,
+               (int)vocab, (int)dim, 0, scale};
   return dout_type == XRL_PREC_BF16 ? launch_embed_sums<bf16_t>(c, a) : launch_embed_sums<float>(c, a);
 }
 

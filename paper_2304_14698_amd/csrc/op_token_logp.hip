@@ -99,54 +99,19 @@ __device__ __forceinline__ Sums wave_sums(const Sums &u, float c) {
   return {m, wave_sum(e * u.s), wave_sum(e * (u.w + u.s * fmaxf(t, -200.f)))};
 }
 
-// What a wave does with VEC logits a lane: columns c .. c + VEC - 1 of the row, -inf where nothing may be chosen.
-template <int VEC, bool TOP>
-__device__ __forceinline__ void take(const float *x, int col, int lane, float c, int top_k, Sums &u, Best &best, float &bar) {
-  float mx = x[0];
-#pragma unroll
-  for (int j = 1; j < VEC; ++j) mx = fmaxf(mx, x[j]);
-  if (mx > u.m) {
-    const float t = (u.m - mx) * c, e = __builtin_amdgcn_exp2f(t);
-    u.w = e * (u.w + u.s * fmaxf(t, -200.f));
-    u.s *= e;
-    u.m = mx;
-  }
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) {
-    const float t = (x[j] - u.m) * c, e = __builtin_amdgcn_exp2f(t);
-    u.s += e;
-    u.w += e * fmaxf(t, -200.f);
-  }
-  if (TOP) {
-    // entries over the k-th best: the largest first, at most k of them. (One that equals it has a higher index than it.)
-    if (!__any(mx > bar)) return;
-    float y[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) y[j] = x[j];
-    for (int n = 0; n < top_k; ++n) {
-      float v = y[0];
-      int at = 0;
-#pragma unroll
-      for (int j = 1; j < VEC; ++j)
-        if (y[j] > v || !(v == v)) { v = y[j]; at = j; }
-      if (!(v == v)) v = -INFINITY;                       // NaN is no alternative
-      const float top = wave_max(v);
-      if (!(top > bar)) break;
-      const int from = __ffsll((unsigned long long)__ballot(v == top)) - 1;
-      const int id = __builtin_amdgcn_readlane(col + at, from);
-      insert_best(best, top, id, lane);
-      bar = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(best.x), top_k - 1));
-      if (lane == from)
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-          if (j == at) y[j] = -INFINITY;
-    }
-  }
+// The row's given entry: whether there is one, and its logit, -inf if it may not be chosen.
+struct Given {
+  bool none;
+  float x;
+};
+template <typename T>
+__device__ __forceinline__ Given given_entry(const LogpArgs &a, int64_t r, const Row<T> &row) {
+  const int id = a.ids ? a.ids[r] : -1;
+  return {id < 0, id >= 0 && id < row.len && (!row.mask || row.mask[id]) ? (float)row.x[id] : -INFINITY};
 }
 
-// The row's results from its sums (the same in all lanes) and its best entries.
-template <typename T>
-__device__ __forceinline__ void finish(const LogpArgs &a, int64_t r, const Row<T> &row, const Sums &u, const Best &best, int lane) {
+// The row's results from its sums (the same in all lanes), its given logit (lane 0) and its best entries.
+__device__ __forceinline__ void finish(const LogpArgs &a, int64_t r, const Given &given, const Sums &u, const Best &best, int lane) {
   const bool any = !(u.s == 0.f);                         // (NaN: yes)
   const float ln_s = logf(u.s);
   if (lane == 0) {
@@ -156,13 +121,8 @@ __device__ __forceinline__ void finish(const LogpArgs &a, int64_t r, const Row<T
       a.stats[2 * r + 1] = any ? ln_s : -INFINITY;
     }
     if (a.logp) {
-      const int id = a.ids ? a.ids[r] : -1;
-      float v = 0.f;
-      if (id >= 0) {
-        v = -INFINITY;
-        if (any && id < row.len && (!row.mask || row.mask[id])) v = ((float)row.x[id] - u.m) * a.inv_t - ln_s;
-      }
-      a.logp[r] = v;
+      const float v = (given.x - u.m) * a.inv_t - ln_s;
+      a.logp[r] = given.none ? 0.f : any && given.x != -INFINITY ? v : -INFINITY;
     }
   }
   if (lane < a.top_k) {
@@ -195,10 +155,66 @@ __device__ __forceinline__ Best merge_best(int lists, int k, int lane, GetX get_
   return out;
 }
 
-// A team of WAVES waves takes one part of one row.
+// Columns col .. col + VEC - 1 of the row as fp32, -inf where nothing may be chosen and from c1 on.
+template <typename T, int VEC>
+__device__ __forceinline__ void fetch(const Row<T> &row, int col, int c1, float *x) {
+  if (col + VEC <= c1) {
+    const Piece<T, VEC> p = load_piece<T, VEC>(row.x + col);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j];
+    if (row.mask) {
+      const Piece<uint8_t, VEC> m = load_piece<uint8_t, VEC>(row.mask + col);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = m.v[j] ? x[j] : -INFINITY;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] = col + j < c1 && (!row.mask || row.mask[col + j]) ? (float)row.x[col + j] : -INFINITY;
+  }
+}
+
+// The entries of x over the wave's k-th best: the largest first, so at most k of them whatever their order, the lowest column first among equals (by
+// piece, then lane, then place). mx: the pieces' maxima. Entries that are taken are overwritten. One that equals the k-th best has a higher column than it.
+template <int VEC, int PIECES>
+__device__ __forceinline__ void take_best(float (*x)[VEC], float *mx, int n_pieces, int col, int step, int lane, int top_k, Best &best, float &bar) {
+  for (int n = 0; n < top_k; ++n) {
+    float v = mx[0];
+#pragma unroll
+    for (int p = 1; p < PIECES; ++p) v = fmaxf(v, mx[p]);
+    const float top = wave_max(v);
+    if (!(top > bar)) return;
+    bool done = false;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      if (done || p >= n_pieces) continue;
+      const unsigned long long have = __ballot(mx[p] == top);
+      if (!have) continue;
+      done = true;
+      const int from = __ffsll(have) - 1;
+      int at = VEC - 1;
+#pragma unroll
+      for (int j = VEC - 2; j >= 0; --j) at = x[p][j] == top ? j : at;
+      insert_best(best, top, __builtin_amdgcn_readlane(col + p * step + at, from), lane);
+      bar = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(best.x), top_k - 1));
+      const int gone = lane == from ? at : -1;
+      float m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        x[p][j] = j == gone ? -INFINITY : x[p][j];
+        m = fmaxf(m, x[p][j]);
+      }
+      mx[p] = m;
+    }
+    if (!done) return;
+  }
+}
+
+// A team of WAVES waves takes one part of one row, 32 entries a lane at a time: their maximum first, then the two sums against the largest so
+// far, then the best of them.
 template <typename T, int WAVES, bool TOP>
 __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
-  constexpr int VEC = 16 / (int)sizeof(T), TEAM = WAVES * 64, TEAMS = 256 / TEAM;
+  touch_args(a);
+  constexpr int VEC = 16 / (int)sizeof(T), PIECES = 32 / VEC, TEAM = WAVES * 64, TEAMS = 256 / TEAM, STEP = TEAM * VEC;
   const int t = threadIdx.x % TEAM, lane = threadIdx.x & 63, wave = t >> 6;
   const int64_t job = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
   const int64_t r = a.row0 + job / a.parts;
@@ -207,28 +223,46 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
   const Row<T> row = row_of<T>(a, r);
   const float c = a.inv_t * kLog2e;
   // part `part`: columns [c0, c1), whole steps of the team
-  const int steps = (row.len + TEAM * VEC - 1) / (TEAM * VEC), per = (steps + a.parts - 1) / a.parts;
-  const int64_t b0 = (int64_t)part * per * (TEAM * VEC), b1 = b0 + (int64_t)per * (TEAM * VEC);
+  const int steps = (row.len + STEP - 1) / STEP, per = (steps + a.parts - 1) / a.parts;
+  const int64_t b0 = (int64_t)part * per * STEP, b1 = b0 + (int64_t)per * STEP;
   const int c0 = (int)(b0 < row.len ? b0 : row.len), c1 = (int)(b1 < row.len ? b1 : row.len);
+  const Given given = a.parts == 1 && lane == 0 ? given_entry<T>(a, r, row) : Given{true, 0.f};
   Sums u = {kLowest, 0.f, 0.f};
   Best best = {-INFINITY, kNone};
   float bar = -INFINITY;
-  for (int col = c0 + t * VEC; col - lane * VEC < c1; col += TEAM * VEC) {
-    float x[VEC];
-    if (col + VEC <= c1) {
-      const Piece<T, VEC> p = load_piece<T, VEC>(row.x + col);
+  for (int w = c0 + wave * 64 * VEC; w < c1; w += PIECES * STEP) {   // w: the wave's first column
+    const int col = w + lane * VEC, left = (c1 - w + STEP - 1) / STEP, n_pieces = left < PIECES ? left : PIECES;
+    float x[PIECES][VEC], mx[PIECES];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j];
-      if (row.mask) {
-        const Piece<uint8_t, VEC> m = load_piece<uint8_t, VEC>(row.mask + col);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) x[j] = m.v[j] ? x[j] : -INFINITY;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[j] = col + j < c1 && (!row.mask || row.mask[col + j]) ? (float)row.x[col + j] : -INFINITY;
+    for (int p = 0; p < PIECES; ++p) {
+      if (p < n_pieces) fetch<T, VEC>(row, col + p * STEP, c1, x[p]);
     }
-    take<VEC, TOP>(x, col, lane, c, a.top_k, u, best, bar);
+    float m = u.m;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      mx[p] = -INFINITY;
+      if (p < n_pieces) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) mx[p] = fmaxf(mx[p], x[p][j]);
+        m = fmaxf(m, mx[p]);
+      }
+    }
+    const float t0 = (u.m - m) * c, e0 = __builtin_amdgcn_exp2f(t0);
+    u.w = e0 * (u.w + u.s * fmaxf(t0, -200.f));
+    u.s *= e0;
+    u.m = m;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      if (p < n_pieces) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float q = (x[p][j] - m) * c, e = __builtin_amdgcn_exp2f(q);
+          u.s += e;
+          u.w += e * fmaxf(q, -200.f);
+        }
+      }
+    }
+    if (TOP) take_best<VEC, PIECES>(x, mx, n_pieces, col, STEP, lane, a.top_k, best, bar);
   }
   u = wave_sums(u, c);
   if constexpr (WAVES > 1) {
@@ -244,7 +278,7 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
       best = merge_best(WAVES, a.top_k, lane, [&](int l, int i) { return bx[l][i]; }, [&](int l, int i) { return bi[l][i]; });
   }
   if (a.parts == 1) {
-    finish<T>(a, r, row, u, best, lane);
+    finish(a, r, given, u, best, lane);
     return;
   }
   if (lane == 0) {
@@ -262,7 +296,9 @@ template <typename T>
 __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
   const int64_t r = blockIdx.x;
   const int lane = threadIdx.x;
+  touch_args(a);
   const Row<T> row = row_of<T>(a, r);
+  const Given given = lane == 0 ? given_entry<T>(a, r, row) : Given{true, 0.f};
   const int64_t job = r * a.parts + lane;
   const bool in = lane < a.parts;
   const float *p = a.part_sums + (in ? job : 0) * 3;
@@ -272,7 +308,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
   if (a.top_k)
     best = merge_best(a.parts, a.top_k, lane, [&](int l, int i) { return a.part_top[(r * a.parts + l) * a.top_k + i]; },
                       [&](int l, int i) { return a.part_ids[(r * a.parts + l) * a.top_k + i]; });
-  finish<T>(a, r, row, u, best, lane);
+  finish(a, r, given, u, best, lane);
 }
 
 // dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
