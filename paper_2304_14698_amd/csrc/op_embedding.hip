@@ -59,8 +59,8 @@ int launch_embed(const xrl_ctx *c, EmbedArgs &a) {
 
 // ---- gradient
 // Few ids: a block per place t and slab of columns. It ends at once if the id stands before t; else it adds up all places of the id, wave w those of the
-// w-th quarter of the places from t on, and the four sums in order. One launch and no workspace.
-constexpr int kFewIds = 2048;
+// w-th eighth of the places from t on, and the eight sums in order. One launch and no workspace.
+constexpr int kFewIds = 1024, kFewWaves = 8;
 
 struct FewArgs {
   const int32_t *ids;
@@ -72,16 +72,16 @@ struct FewArgs {
 };
 
 template <typename T, int VEC>
-__global__ __launch_bounds__(256) void embed_few_kernel(const FewArgs a) {
+__global__ __launch_bounds__(kFewWaves * 64) void embed_few_kernel(const FewArgs a) {
   touch_args(a);
   const int t = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int id = a.ids[t];
   if ((unsigned)id >= (unsigned)a.vocab) return;
   int before = 0;
-  for (int i = threadIdx.x; i < t; i += 256) before |= a.ids[i] == id;
+  for (int i = threadIdx.x; i < t; i += kFewWaves * 64) before |= a.ids[i] == id;
   if (__syncthreads_or(before)) return;
   const int c = ((int)blockIdx.y * 64 + lane) * VEC, nv = a.dim - c < VEC ? a.dim - c : VEC;
-  const int chunks = (a.n - t + 63) / 64, per = (chunks + 3) / 4;
+  const int chunks = (a.n - t + 63) / 64, per = (chunks + kFewWaves - 1) / kFewWaves;
   const int i0 = t + w * per * 64, i1 = i0 + per * 64 < a.n ? i0 + per * 64 : a.n;
   float acc[VEC];
 #pragma unroll
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256) void embed_few_kernel(const FewArgs a) {
           for (int j = 0; j < VEC; ++j) acc[j] += (float)v[k].v[j];
     }
   }
-  __shared__ float part[3][64][VEC + 1];
+  __shared__ float part[kFewWaves - 1][64][VEC + 1];
   if (w)
 #pragma unroll
     for (int j = 0; j < VEC; ++j) part[w - 1][lane][j] = acc[j];
@@ -117,21 +117,24 @@ __global__ __launch_bounds__(256) void embed_few_kernel(const FewArgs a) {
   if (w) return;
   float *p = a.dtable + (int64_t)id * a.dtable_stride + c;
 #pragma unroll
-  for (int j = 0; j < VEC; ++j)
-    if (j < nv) p[j] += a.scale * (((acc[j] + part[0][lane][j]) + part[1][lane][j]) + part[2][lane][j]);
+  for (int j = 0; j < VEC; ++j) {
+#pragma unroll
+    for (int k = 0; k < kFewWaves - 1; ++k) acc[j] += part[k][lane][j];
+    if (j < nv) p[j] += a.scale * acc[j];
+  }
 }
 
 // More ids: sorted pairs (id, t) by a stable radix sort of up to kDigitBits bits a pass. Ids outside the vocabulary sort behind all others, as
-// `vocab`. A pass takes one launch: its scatter counts, for the pass behind it, the digits that each block of that will find; only the first has a launch that counts.
+// `vocab`. A pass is two launches: one counts each block's digits, one moves the pairs.
 constexpr int kDigitBits = 10, kSortBlocks = 64, kSortThreads = 512, kSortWaves = kSortThreads / 64;
 
 struct SortArgs {
   const int32_t *ids;           // first pass: the items are (ids[t], t)
   const uint2 *in;              // later passes
   uint2 *out;
-  int32_t *hist, *next_hist;    // [blocks][1 << bits] of this pass and of the one behind it (nullptr: none)
-  int32_t *clear;               // counting launch: zeroed, clear_n of them
-  int64_t n, clear_n;
+  int32_t *hist;                // [blocks][1 << bits]
+  int32_t *clear;               // zeroed by the counting launch
+  int64_t n;
   int vocab, shift, bits, per_wave;   // per_wave: consecutive items of a wave, a multiple of 64
 };
 
@@ -146,7 +149,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_count_kernel(const So
   __shared__ int cnt[1 << kDigitBits];
   const int digits = 1 << a.bits;
   for (int d = threadIdx.x; d < digits; d += kSortThreads) cnt[d] = 0;
-  for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < a.clear_n; i += (int64_t)gridDim.x * kSortThreads) a.clear[i] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * kSortWaves * a.per_wave;
   const int64_t i1 = i0 + (int64_t)kSortWaves * a.per_wave < a.n ? i0 + (int64_t)kSortWaves * a.per_wave : a.n;
@@ -214,7 +217,6 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
   }
   __syncthreads();
   volatile int *mine = off[w];
-  const int64_t per_block = (int64_t)kSortWaves * a.per_wave;
   for (int k = 0; k < a.per_wave; k += 64) {
     const int64_t i = w0 + k + lane;
     const bool in = i < a.n;
@@ -231,11 +233,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
     if (in && rank == 0) mine[d] = place + __popcll(same);
     __threadfence_block();
     __builtin_amdgcn_wave_barrier();
-    if (in) {
-      a.out[place] = x;
-      if (a.next_hist)                                    // (integers: the same in any order)
-        atomicAdd(&a.next_hist[(size_t)(place / per_block) * digits + ((x.x >> (a.shift + a.bits)) & (unsigned)(digits - 1))], 1);
-    }
+    if (in) a.out[place] = x;
   }
 }
 
@@ -243,7 +241,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
 // table that its runs are added to, are requested together. A run inside the window is added to its row of the table. The piece of a run that began
 // before goes to carry[window][0], that of one that goes on behind it to carry[window][1]; a window that such a run begins in is listed, and
 // embed_join_kernel adds up the run's pieces.
-constexpr int kWindow = 16;
+constexpr int kWindow = 16, kJoinWaves = 8;
 
 struct SumArgs {
   const uint2 *items;
@@ -255,10 +253,9 @@ struct SumArgs {
   float scale;
 };
 
-template <typename T, int VEC>
+template <typename T, int VEC, int BATCH>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   touch_args(a);
-  constexpr int BATCH = 8;
   const int lane = threadIdx.x & (a.lanes - 1);
   const int64_t w = (int64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
   const int64_t i0 = w * kWindow;
@@ -328,64 +325,100 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   }
 }
 
-// The runs that go over windows: a block takes listed windows and 256 columns, each of its four waves a quarter of the run's pieces, eight requests
-// at a time, and adds up the four sums in order.
-__global__ __launch_bounds__(256) void embed_join_kernel(const SumArgs a) {
+// The run that the listed window w begins: its id, and its pieces, one in each window from w on that it reaches.
+struct Run {
+  int64_t w, pieces;
+  unsigned id;
+};
+__device__ __forceinline__ Run run_of(const SumArgs &a, int listed, int lane) {
+  Run r;
+  r.w = a.list[listed];
+  r.id = a.items[(r.w + 1) * kWindow - 1].x;
+  // windows behind w that begin with the id: 64 probes at once, each level 64 times as fine
+  const int64_t windows = (a.n + kWindow - 1) / kWindow;
+  int64_t more = 0;
+  for (int64_t s = (int64_t)1 << 18; s; s >>= 6)
+    if (s == 1 || s < windows) {
+      const int64_t k = r.w + more + (lane + 1) * s;
+      more += s * __popcll(__ballot(k < windows && a.items[k < windows ? k * kWindow : 0].x == r.id));
+    }
+  r.pieces = more + 1;
+  return r;
+}
+// Pieces [p0, p1) of a run added up in their order, eight requests at a time: four columns from c on.
+__device__ __forceinline__ void add_pieces(const SumArgs &a, const Run &r, int64_t p0, int64_t p1, int c, int nv, float *sum) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum[j] = 0.f;
+  const float *src = a.carry + (size_t)r.w * 2 * a.dim + c;
+  for (int64_t k = p0; k < p1; k += 8) {
+    Piece<float, 4> x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (k + u < p1) {
+        const float *p = src + ((size_t)(k + u) * 2 + (k + u == 0)) * a.dim;
+        if (nv == 4) x[u] = load_piece<float, 4>(p);
+        else
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[u].v[j] = j < nv ? p[j] : 0.f;
+      }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (k + u < p1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += x[u].v[j];
+  }
+}
+__device__ __forceinline__ void add_run(const SumArgs &a, const Run &r, int c, int nv, const float *sum) {
+  float *p = a.dtable + (int64_t)r.id * a.dtable_stride + c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (j < nv) p[j] += a.scale * sum[j];
+}
+
+// The runs that go over windows, 256 columns a block: each wave takes a listed window and adds up the run's pieces if they are few; the runs of many
+// pieces are then taken by all waves of the block, a part of the pieces each, and their sums in order. A block for every run leaves most of its waves
+// idle, a wave for every run is long at an id that fills the batch: us of this kernel at 65536 long-tailed ids of 1024 columns, and of the whole
+// call at 131072 times the same id of 128 columns: sixteen waves a run 49 and 113, four 17 and 263, this 19 and 197.
+constexpr int kFewPieces = 32;
+__global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumArgs a) {
   touch_args(a);
-  __shared__ float part[3][256];
+  __shared__ float part[kJoinWaves - 1][256];
+  __shared__ int many[kJoinWaves];
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, listed = *a.listed;
   const int c = (int)blockIdx.y * 256 + lane * 4;
   const int nv = a.dim - c < 4 ? a.dim - c : 4;
-  for (int q = blockIdx.x; q < listed; q += gridDim.x) {
-    const int64_t w = a.list[q], i1 = (w + 1) * kWindow;
-    const unsigned id = a.items[i1 - 1].x;
-    // the first pair behind the run: steps of growing size, then halves
-    int64_t lo = i1, step = kWindow;
-    while (lo + step < a.n && a.items[lo + step].x == id) {
-      lo += step;
-      step *= 2;
-    }
-    int64_t hi = lo + step < a.n ? lo + step : a.n;      // items[lo] is the run's (i1 is: it goes on), items[hi] is not
-    while (hi - lo > 1) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (a.items[mid].x == id) lo = mid; else hi = mid;
-    }
-    const int64_t n = lo / kWindow + 1 - w, per = (n + 3) / 4, p0 = g * per, p1 = p0 + per < n ? p0 + per : n;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    if (nv == 4) {
-      int64_t k = p0;
-      const float *src = a.carry + (size_t)w * 2 * a.dim + c;
-      if (k == 0 && k < p1) {                             // the run's first piece
-        const Piece<float, 4> x = load_piece<float, 4>(src + a.dim);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] = x.v[j];
-        ++k;
+  for (int q0 = blockIdx.x; q0 < listed; q0 += gridDim.x * kJoinWaves) {   // neighbours in the list go to different blocks
+    bool left = false;
+    const int q = q0 + g * (int)gridDim.x;
+    if (q < listed) {
+      const Run r = run_of(a, q, lane);
+      left = r.pieces > kFewPieces;
+      if (!left) {
+        float sum[4];
+        add_pieces(a, r, 0, r.pieces, c, nv, sum);
+        add_run(a, r, c, nv, sum);
       }
-      for (; k < p1; k += 8) {
-        Piece<float, 4> x[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (k + u < p1) x[u] = load_piece<float, 4>(src + (size_t)(k + u) * 2 * a.dim);
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (k + u < p1)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += x[u].v[j];
-      }
-    } else {
-      for (int64_t k = p0; k < p1; ++k)
-        for (int j = 0; j < nv; ++j) sum[j] += a.carry[((size_t)(w + k) * 2 + (k == 0 ? 1 : 0)) * a.dim + c + j];
     }
+    if (!__syncthreads_or(left)) continue;
+    if (lane == 0) many[g] = left;
     __syncthreads();
-    if (g)
+    for (int k = 0; k < kJoinWaves; ++k) {
+      if (!many[k]) continue;
+      const Run r = run_of(a, q0 + k * (int)gridDim.x, lane);
+      const int64_t per = (r.pieces + kJoinWaves - 1) / kJoinWaves, p0 = g * per, p1 = p0 + per < r.pieces ? p0 + per : r.pieces;
+      float sum[4];
+      add_pieces(a, r, p0, p1, c, nv, sum);
+      if (g)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) part[g - 1][lane * 4 + j] = sum[j];
-    __syncthreads();
-    if (g == 0) {
-      float *p = a.dtable + (int64_t)id * a.dtable_stride + c;
+        for (int j = 0; j < 4; ++j) part[g - 1][lane * 4 + j] = sum[j];
+      __syncthreads();
+      if (g == 0) {
+        for (int u = 0; u < kJoinWaves - 1; ++u)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j < nv) p[j] += a.scale * (((sum[j] + part[0][lane * 4 + j]) + part[1][lane * 4 + j]) + part[2][lane * 4 + j]);
+          for (int j = 0; j < 4; ++j) sum[j] += part[u][lane * 4 + j];
+        add_run(a, r, c, nv, sum);
+      }
+      __syncthreads();
     }
   }
 }
@@ -393,22 +426,22 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const SumArgs a) {
 template <typename T>
 int launch_embed_few(const xrl_ctx *c, const FewArgs &a) {
   constexpr int VEC = sizeof(T) == 2 ? 8 : 4;
-  embed_few_kernel<T, VEC><<<dim3((unsigned)a.n, (unsigned)((a.dim + 64 * VEC - 1) / (64 * VEC))), dim3(256), 0, op_stream(c)>>>(a);
+  embed_few_kernel<T, VEC><<<dim3((unsigned)a.n, (unsigned)((a.dim + 64 * VEC - 1) / (64 * VEC))), dim3(kFewWaves * 64), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
 
 template <typename T>
 int launch_embed_sums(const xrl_ctx *c, SumArgs &a) {
-  constexpr int VEC = sizeof(T) == 2 ? 8 : 4;
+  constexpr int VEC = sizeof(T) == 2 ? 8 : 4, BATCH = 4;
   const int pieces = (a.dim + VEC - 1) / VEC;
   a.lanes = 1;
   while (a.lanes < pieces && a.lanes < 256) a.lanes *= 2;
   const int64_t windows = (a.n + kWindow - 1) / kWindow, per = 256 / a.lanes;
-  embed_sum_kernel<T, VEC><<<dim3((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes)), dim3(256), 0,
+  embed_sum_kernel<T, VEC, BATCH><<<dim3((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes)), dim3(256), 0,
                              op_stream(c)>>>(a);
-  embed_join_kernel<<<dim3((unsigned)std::min<int64_t>(windows, 4 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256)), dim3(256), 0,
-                      op_stream(c)>>>(a);
+  embed_join_kernel<<<dim3((unsigned)std::min<int64_t>(windows, 2 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256)),
+                      dim3(kJoinWaves * 64), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
@@ -464,24 +497,22 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   const int blocks = (int)((n + (int64_t)s.per_wave * kSortWaves - 1) / ((int64_t)s.per_wave * kSortWaves));
   const int64_t windows = (n + kWindow - 1) / kWindow;
   const int64_t hist = (int64_t)blocks << per_pass;      // counters of one pass
-  const size_t o_b = op_align((size_t)n * 8), o_h = 2 * o_b, o_l = o_h + op_align((size_t)(passes * hist + 1) * 4),
+  const size_t o_b = op_align((size_t)n * 8), o_h = 2 * o_b, o_l = o_h + op_align((size_t)(hist + 1) * 4),
                o_c = o_l + op_align((size_t)windows * 4);
   char *ws = nullptr;
   if (int rc = op_workspace(c, o_c + (size_t)windows * 2 * dim * 4, &ws, who)) return rc;
   uint2 *x = (uint2 *)ws, *y = (uint2 *)(ws + o_b);
-  int32_t *counters = (int32_t *)(ws + o_h);             // the first pass's, the others' (cleared), the list's length (cleared)
-  s.hist = counters; s.clear = counters + hist; s.clear_n = (passes - 1) * hist + 1;
-  s.ids = d_ids;
-  embed_sort_count_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);
+  s.hist = (int32_t *)(ws + o_h);
+  s.clear = s.hist + hist;                               // the list's length
   for (int p = 0; p < passes; ++p) {
     s.ids = p == 0 ? d_ids : nullptr;
     s.in = x; s.out = y; s.shift = p * per_pass;
-    s.hist = counters + p * hist; s.next_hist = p + 1 < passes ? s.hist + hist : nullptr;
+    embed_sort_count_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);
     embed_sort_scatter_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);
     std::swap(x, y);
   }
   OP_TRY(hipGetLastError());
-  SumArgs a = {x, d_dout, d_dtable, (float *)(ws + o_c), counters + passes * hist, (int32_t *)(ws + o_l), dout_stride, dtable_stride, n,
+  SumArgs a = {x, d_dout, d_dtable, (float *)(ws + o_c), s.clear, (int32_t *)(ws + o_l), dout_stride, dtable_stride, n,
                (int)vocab, (int)dim, 0, scale};
   return dout_type == XRL_PREC_BF16 ? launch_embed_sums<bf16_t>(c, a) : launch_embed_sums<float>(c, a);
 }
