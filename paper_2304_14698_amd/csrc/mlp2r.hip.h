@@ -29,22 +29,6 @@
 #pragma once
 #include "mlp2.hip.h"
 
-// 16 bytes per lane from global memory straight into LDS: lane i's piece lands at LDS byte
-// lds_base + 16 i (lds_base uniform across the wave). Written as inline assembly on purpose:
-// the compiler makes every later LDS access wait for its own LDS-direct loads, whichever
-// buffer they target, which would serialise the prefetch with the compute it is meant to
-// overlap. Whoever reads the destination must wait for vmcnt(0) and a barrier first.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_direct_load16(const void *g, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(lds_base)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-__device__ __forceinline__ unsigned lds_address(const void *p) {
-  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
-}
-
 template <int H, int KIND>
 struct RTile {
   static constexpr int MB = H / 32, NT = 64 * MB;                          // waves, threads per block

@@ -368,3 +368,19 @@ __device__ __forceinline__ void mma_split3(const Split3 &a, const Split3 &b, f32
   corr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[0], b.p[1], corr, 0, 0, 0);
   corr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[1], b.p[0], corr, 0, 0, 0);
 }
+
+// 16 bytes per lane from global memory straight into LDS: lane i's piece lands at LDS byte
+// lds_base + 16 i (lds_base uniform across the wave). Written as inline assembly on purpose:
+// the compiler makes every later LDS access wait for its own LDS-direct loads, whichever
+// buffer they target, which would serialise the prefetch with the compute it is meant to
+// overlap. Whoever reads the destination must wait for vmcnt(0) and a barrier first.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void lds_direct_load16(const void *g, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(lds_base)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+__device__ __forceinline__ unsigned lds_address(const void *p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}

@@ -28,7 +28,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;
 constexpr int kGroup = 32;             // matrices of one launch: their list is a kernel argument
-constexpr int kTile = 64;              // a block's output, four waves of 32 x 32
+constexpr int kTile = 64;              // sizes are padded to multiples of this
 constexpr int kMaxSums = 1024;         // partial sums of squares of a matrix
 
 struct Mat {
@@ -57,17 +57,17 @@ __host__ __device__ inline int64_t x_halves(int m, int n) {
   return (int64_t)((m + kTile - 1) / kTile * kTile) * ((n + kTile - 1) / kTile * kTile) * 2;
 }
 struct Buffers {
-  _Float16 *x, *xt[2], *a, *b;
+  _Float16 *x, *xt, *next_xt, *a, *b;   // X; X^T as it is, and as the step's last product makes it; A; B
 };
 __device__ __forceinline__ Buffers buffers(const MuonArgs &p, const Mat &q) {
   const int64_t nx = x_halves(q.m, q.n), na = x_halves(q.m, q.m);
   _Float16 *w = p.ws + q.ws;
-  return {w, {w + nx, w + 2 * nx}, w + 3 * nx, w + 3 * nx + na};
+  return {w, w + (p.flip ? 2 : 1) * nx, w + (p.flip ? 1 : 2) * nx, w + 3 * nx, w + 3 * nx + na};
 }
+// The matrix that a block belongs to: a lane looks at one.
 __device__ __forceinline__ int matrix_of(const MuonArgs &p, int block) {
-  int k = 0;
-  while (k + 1 < p.count && p.first[k + 1] <= block) ++k;
-  return k;
+  const int lane = threadIdx.x & 63;
+  return __popcll(__ballot(lane < p.count && p.first[lane < p.count ? lane : 0] <= block)) - 1;
 }
 __device__ __forceinline__ void split(float y, _Float16 &hi, _Float16 &lo) {
   hi = (_Float16)y;
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
       split(x[c + e][row], h, l);
       hi[e] = h; lo[e] = l;
     }
-    o = buf.xt[0] + ((int64_t)(tj * 2 + rb) * (mp / 16) + ti * 4 + kb) * 1024 + lane * 8;
+    o = buf.xt + ((int64_t)(tj * 2 + rb) * (mp / 16) + ti * 4 + kb) * 1024 + lane * 8;
     *(f16x8 *)o = hi;
     *(f16x8 *)(o + 512) = lo;
   }
@@ -143,53 +143,85 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
 
 enum { STEP_GRAM, STEP_POLY, STEP_APPLY, STEP_LAST };
 
-// One product of a step. D[i][j] = sum over k of P[i][k] Q[j][k], both in fragment order along k.
-template <int STEP>
-__global__ __launch_bounds__(256) void muon_product_kernel(const MuonArgs p) {
-  const int k = matrix_of(p, blockIdx.x), tile = blockIdx.x - p.first[k], lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Mat &q = p.mat[k];
-  const int mp = padded(q.m), np = padded(q.n);
-  const Buffers buf = buffers(p, q);
-  int ti, tj, kbs;
+// One product of a step, D[i][j] = sum over k of P[i][k] Q[j][k], both in fragment order along k: the block's tile, of T x T.
+struct Product {
+  int k, ti, tj, mp, np, kbs;          // matrix; tile; padded sizes; fragments along k
   const _Float16 *P, *Q;
+  Buffers buf;
+};
+template <int STEP, int T>
+__device__ __forceinline__ Product product_of(const MuonArgs &p) {
+  Product d;
+  // Blocks are dealt to the eight XCDs in turn: an XCD takes neighbouring tiles, whose operands its L2 then holds
+  const int all = p.first[p.count], xcd = blockIdx.x % 8, per = all / 8, rem = all % 8;
+  const int block = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / 8;
+  d.k = matrix_of(p, block);
+  const Mat &q = p.mat[d.k];
+  const int tile = block - p.first[d.k];
+  d.mp = padded(q.m);
+  d.np = padded(q.n);
+  d.buf = buffers(p, q);
   if (STEP == STEP_GRAM || STEP == STEP_POLY) {           // symmetric: tiles with tj <= ti
-    ti = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
+    int ti = (int)((sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
     while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
     while (ti * (ti + 1) / 2 > tile) --ti;
-    tj = tile - ti * (ti + 1) / 2;
-    P = Q = STEP == STEP_GRAM ? buf.x : buf.a;
-    kbs = (STEP == STEP_GRAM ? np : mp) / 16;
-  } else {
-    ti = tile / (np / kTile);
-    tj = tile % (np / kTile);
-    P = buf.b;
-    Q = buf.xt[p.flip];
-    kbs = mp / 16;
+    d.ti = ti;
+    d.tj = tile - ti * (ti + 1) / 2;
+    d.P = d.Q = STEP == STEP_GRAM ? d.buf.x : d.buf.a;
+    d.kbs = (STEP == STEP_GRAM ? d.np : d.mp) / 16;
+  } else {                                                 // strips of eight tiles' height, column by column
+    const int th = (d.mp + T - 1) / T, tw = (d.np + T - 1) / T, strip = tile / (8 * tw), in = tile - strip * 8 * tw;
+    const int h = th - strip * 8 < 8 ? th - strip * 8 : 8;
+    d.ti = strip * 8 + in % h;
+    d.tj = in / h;
+    d.P = d.buf.b;
+    d.Q = d.buf.xt;
+    d.kbs = d.mp / 16;
   }
-  const int ib = ti * 2 + (wave >> 1), jb = tj * 2 + (wave & 1);
-  const _Float16 *pa = P + (int64_t)ib * kbs * 1024 + lane * 8, *qa = Q + (int64_t)jb * kbs * 1024 + lane * 8;
-  f32x16 acc;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  for (int kb = 0; kb < kbs; ++kb) {
-    const f16x8 ph = *(const f16x8 *)(pa + (int64_t)kb * 1024), pl = *(const f16x8 *)(pa + (int64_t)kb * 1024 + 512);
-    const f16x8 qh = *(const f16x8 *)(qa + (int64_t)kb * 1024), ql = *(const f16x8 *)(qa + (int64_t)kb * 1024 + 512);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
-  }
+  return d;
+}
+
+// What becomes of a wave's 32 x 32 of a product, block (ib, jb). turn: the wave's own 32 x 33 floats of LDS.
+template <int STEP>
+__device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f32x16 &acc, int ib, int jb, float (*turn)[33]) {
+  const Mat &q = p.mat[d.k];
   // register r of a lane: D[i][j] with i = ib 32 + 8 (r / 4) + 4 (lane / 32) + r % 4, j = jb 32 + lane % 32
-  const int g = lane >> 5, jl = lane & 31;
+  const int lane = threadIdx.x & 63, g = lane >> 5, jl = lane & 31;
   if (STEP == STEP_LAST) {
-    const int j = jb * 32 + jl;
     const float step = p.step * sqrtf((float)q.n) * (kDown * kDown);
+    float *w = p.w + q.offset;
+    if (!q.t) {
+      const int j = jb * 32 + jl;
+      float old[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int i = ib * 32 + acc_row(r, g);
-      if (i < q.m && j < q.n) {
-        float *w = p.w + q.offset + (q.t ? (int64_t)j * q.m + i : (int64_t)i * q.n + j);
-        *w = p.decay * *w - step * acc[r];
+      for (int r = 0; r < 16; ++r) {
+        const int i = ib * 32 + acc_row(r, g);
+        old[r] = i < q.m && j < q.n ? w[(int64_t)i * q.n + j] : 0.f;
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = ib * 32 + acc_row(r, g);
+        if (i < q.m && j < q.n) w[(int64_t)i * q.n + j] = p.decay * old[r] - step * acc[r];
+      }
+    } else {                                               // rows j of the vector's matrix, along i
+#pragma unroll
+      for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = acc[r];
+      __builtin_amdgcn_wave_barrier();
+      __threadfence_block();
+      const int i = ib * 32 + jl;
+      float old[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = jb * 32 + 2 * r + g;
+        old[r] = i < q.m && j < q.n ? w[(int64_t)j * q.m + i] : 0.f;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = jb * 32 + 2 * r + g;
+        if (i < q.m && j < q.n) w[(int64_t)j * q.m + i] = p.decay * old[r] - step * turn[jl][2 * r + g];
+      }
+      __threadfence_block();
+      __builtin_amdgcn_wave_barrier();
     }
     return;
   }
@@ -199,7 +231,7 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonArgs p) {
   if (STEP == STEP_POLY) {
 #pragma unroll
     for (int s = 0; s < 4; ++s) {                          // A[i][j] = A[j][i]: four i of one j lie side by side
-      const _Float16 *at = buf.a + ((int64_t)jb * kbs + ib * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
+      const _Float16 *at = d.buf.a + ((int64_t)jb * d.kbs + ib * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
       const f16x4 h = *(const f16x4 *)at, l = *(const f16x4 *)(at + 512);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -209,7 +241,7 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonArgs p) {
     }
   }
   // rows j, along i: a lane has four i side by side
-  _Float16 *by_j = STEP == STEP_GRAM ? buf.a : STEP == STEP_POLY ? buf.b : buf.xt[p.flip ^ 1];
+  _Float16 *by_j = STEP == STEP_GRAM ? d.buf.a : STEP == STEP_POLY ? d.buf.b : d.buf.next_xt;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     f16x4 hi, lo;
@@ -219,63 +251,180 @@ __global__ __launch_bounds__(256) void muon_product_kernel(const MuonArgs p) {
       split(v[4 * s + e], h, l);
       hi[e] = h; lo[e] = l;
     }
-    _Float16 *o = by_j + ((int64_t)jb * (mp / 16) + ib * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
+    _Float16 *o = by_j + ((int64_t)jb * (d.mp / 16) + ib * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
     *(f16x4 *)o = hi;
     *(f16x4 *)(o + 512) = lo;
   }
   // rows i, along j: turned round in LDS. (A block on the diagonal of a symmetric product has written both already.)
-  if (STEP != STEP_APPLY && ti == tj) return;
-  __shared__ float turn[4][32][33];
-  float (*x)[33] = turn[wave];
+  if (STEP != STEP_APPLY && d.ti == d.tj) return;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) x[acc_row(r, g)][jl] = v[r];
+  for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = v[r];
   __builtin_amdgcn_wave_barrier();
   __threadfence_block();
-  _Float16 *by_i = STEP == STEP_GRAM ? buf.a : STEP == STEP_POLY ? buf.b : buf.x;
-  const int kdim = STEP == STEP_APPLY ? np : mp;
+  _Float16 *by_i = STEP == STEP_GRAM ? d.buf.a : STEP == STEP_POLY ? d.buf.b : d.buf.x;
+  const int kdim = STEP == STEP_APPLY ? d.np : d.mp;
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     f16x8 hi, lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       _Float16 h, l;
-      split(x[jl][kb * 16 + g * 8 + e], h, l);
+      split(turn[jl][kb * 16 + g * 8 + e], h, l);
       hi[e] = h; lo[e] = l;
     }
     _Float16 *o = by_i + ((int64_t)ib * (kdim / 16) + jb * 2 + kb) * 1024 + lane * 8;
     *(f16x8 *)o = hi;
     *(f16x8 *)(o + 512) = lo;
   }
+  __threadfence_block();
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Both halves of two factors of a 32 x 32 x 16 product; the small terms first.
+__device__ __forceinline__ void add_product(f32x16 &acc, const f16x8 &ph, const f16x8 &pl, const f16x8 &qh, const f16x8 &ql) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
+}
+
+// Few tiles: 64 x 64 a block, 32 x 32 a wave, fragments requested in place from L2 and kAhead of them ahead.
+template <int STEP>
+__global__ __launch_bounds__(256) void muon_product_kernel(const MuonArgs p) {
+  constexpr int kAhead = 4;                                // (there are a multiple of four along k)
+  __shared__ float turn[4][32][33];
+  const Product d = product_of<STEP, kTile>(p);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ib = d.ti * 2 + (wave >> 1), jb = d.tj * 2 + (wave & 1);
+  const _Float16 *pa = d.P + (int64_t)ib * d.kbs * 1024 + lane * 8, *qa = d.Q + (int64_t)jb * d.kbs * 1024 + lane * 8;
+  f32x16 acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  f16x8 ph[kAhead], pl[kAhead], qh[kAhead], ql[kAhead];
+  auto request = [&](int u, int kb) {
+    const _Float16 *a = pa + (int64_t)kb * 1024, *b = qa + (int64_t)kb * 1024;
+    ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 512);
+    qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 512);
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) request(u, u);
+  __builtin_amdgcn_sched_barrier(0);
+  for (int kb = 0; kb < d.kbs; kb += kAhead) {
+    const int next = kb + kAhead < d.kbs ? kb + kAhead : kb;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      add_product(acc, ph[u], pl[u], qh[u], ql[u]);
+      request(u, next + u);
+      __builtin_amdgcn_sched_barrier(0);                   // (else the requests sink to where they are needed)
+    }
+  }
+  put<STEP>(p, d, acc, ib, jb, turn[wave]);
+}
+
+// Many tiles: 128 x 128 a block, 64 x 64 a wave. 32 of the summed dimension at a time go from L2 straight into LDS, where two waves each read them;
+// while they are multiplied the next 32 are on their way into the other half of the LDS. Two blocks a compute unit.
+constexpr int kWide = 128;
+constexpr unsigned kStage = 32 * 1024;                     // bytes: 2 factors x 4 blocks of 32 rows x 2 fragments x (hi, lo)
+template <int STEP>
+__global__ __launch_bounds__(256, 2) void muon_product_wide_kernel(const MuonArgs p) {
+  extern __shared__ __align__(16) char lds[];
+  const Product d = product_of<STEP, kWide>(p);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wi = wave >> 1, wj = wave & 1;
+  const int rows_q = (STEP == STEP_GRAM || STEP == STEP_POLY ? d.mp : d.np) / 32;
+  // wave w fills 8 KB of a stage: two blocks of 32 rows of P (w = 0, 1) or Q, 4 KB each, which lie side by side along k. (Rows behind the
+  // padded matrix are read from its last block and never stored.)
+  const char *src[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int rb = (wave & 1) * 2 + u;
+    int at = (wave < 2 ? d.ti : d.tj) * 4 + rb;
+    const int last = (wave < 2 ? d.mp / 32 : rows_q) - 1;
+    at = at < last ? at : last;
+    src[u] = (const char *)((wave < 2 ? d.P : d.Q) + (int64_t)at * d.kbs * 1024) + lane * 16;
+  }
+  const unsigned base = lds_address(lds), mine = (unsigned)__builtin_amdgcn_readfirstlane(wave) * 8192;
+  auto request = [&](int s) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) lds_direct_load16(src[u] + (int64_t)s * 4096 + k * 1024, base + (s & 1) * kStage + mine + u * 4096 + k * 1024);
+  };
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+  const int stages = d.kbs / 2;
+  request(0);
+  for (int s = 0; s < stages; ++s) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's part of stage s is there, and behind the barrier all of it;
+    __syncthreads();                                        // and nobody reads the other half any more
+    if (s + 1 < stages) request(s + 1);
+    const char *at = lds + (s & 1) * kStage + lane * 16;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      f16x8 ph[2], pl[2], qh[2], ql[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const char *a = at + (wi * 2 + u) * 4096 + k * 2048, *b = at + 16384 + (wj * 2 + u) * 4096 + k * 2048;
+        ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 1024);
+        qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 1024);
+      }
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) add_product(acc[a][b], ph[a], pl[a], qh[b], ql[b]);
+    }
+  }
+  __syncthreads();                                          // the LDS becomes the waves' turning space
+  float (*turn)[33] = (float (*)[33])(lds + wave * 32 * 33 * 4);
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int ib = d.ti * 4 + wi * 2 + a, jb = d.tj * 4 + wj * 2 + b;
+      if (ib < d.mp / 32 && jb < rows_q) put<STEP>(p, d, acc[a][b], ib, jb, turn);
+    }
+}
+
+// A launch of product STEP over all matrices.
+template <int STEP>
+int launch_product(const xrl_ctx *c, MuonArgs &p) {
+  auto blocks = [&](int T) {
+    int64_t at = 0;
+    for (int k = 0; k < p.count; ++k) {
+      const int64_t th = (p.mat[k].m + T - 1) / T, tw = (p.mat[k].n + T - 1) / T;
+      p.first[k] = (int)at;
+      at += STEP == STEP_GRAM || STEP == STEP_POLY ? th * (th + 1) / 2 : th * tw;
+    }
+    p.first[p.count] = (int)at;
+    return at;
+  };
+  if (blocks(kWide) >= op_compute_units(c)) {
+    constexpr int lds = 2 * (int)kStage;
+    muon_product_wide_kernel<STEP><<<dim3((unsigned)p.first[p.count]), dim3(256), lds, op_stream(c)>>>(p);
+  } else {
+    muon_product_kernel<STEP><<<dim3((unsigned)blocks(kTile)), dim3(256), 0, op_stream(c)>>>(p);
+  }
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
 }
 
 int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
-  const hipStream_t stream = op_stream(c);
-  // blocks of a launch whose matrix k has of(k) of them
-  auto blocks = [&](auto of) {
-    int64_t at = 0;
-    for (int k = 0; k < p.count; ++k) {
-      p.first[k] = (int)at;
-      at += of(k);
-    }
-    p.first[p.count] = (int)at;
-    return dim3((unsigned)at);
-  };
-  auto tiles = [](int x) { return (int64_t)(x + kTile - 1) / kTile; };
-  const dim3 all = dim3(256);
-  const dim3 sums = blocks([&](int k) { return (int64_t)p.first_sum[k + 1] - p.first_sum[k]; });
-  muon_momentum_kernel<<<sums, all, 0, stream>>>(p);
-  const dim3 whole = blocks([&](int k) { return tiles(p.mat[k].m) * tiles(p.mat[k].n); });
-  muon_begin_kernel<<<whole, all, 0, stream>>>(p);
+  for (int k = 0; k <= p.count; ++k) p.first[k] = p.first_sum[k];
+  muon_momentum_kernel<<<dim3((unsigned)p.first[p.count]), dim3(256), 0, op_stream(c)>>>(p);
+  p.first[0] = 0;
+  for (int k = 0; k < p.count; ++k)
+    p.first[k + 1] = p.first[k] + (p.mat[k].m + kTile - 1) / kTile * ((p.mat[k].n + kTile - 1) / kTile);
+  muon_begin_kernel<<<dim3((unsigned)p.first[p.count]), dim3(256), 0, op_stream(c)>>>(p);
+  OP_TRY(hipGetLastError());
   for (int s = 0; s < steps; ++s) {
-    const dim3 half = blocks([&](int k) { return tiles(p.mat[k].m) * (tiles(p.mat[k].m) + 1) / 2; });
-    muon_product_kernel<STEP_GRAM><<<half, all, 0, stream>>>(p);
-    muon_product_kernel<STEP_POLY><<<half, all, 0, stream>>>(p);
-    blocks([&](int k) { return tiles(p.mat[k].m) * tiles(p.mat[k].n); });
-    if (s + 1 < steps) muon_product_kernel<STEP_APPLY><<<whole, all, 0, stream>>>(p);
-    else muon_product_kernel<STEP_LAST><<<whole, all, 0, stream>>>(p);
+    if (int rc = launch_product<STEP_GRAM>(c, p)) return rc;
+    if (int rc = launch_product<STEP_POLY>(c, p)) return rc;
+    if (int rc = s + 1 < steps ? launch_product<STEP_APPLY>(c, p) : launch_product<STEP_LAST>(c, p)) return rc;
     p.flip ^= 1;
   }
-  OP_TRY(hipGetLastError());
   return XRL_OK;
 }
 
