@@ -42,6 +42,7 @@ struct MuonArgs {
   int first[kGroup + 1];               // first block of each matrix in this launch
   Mat mat[kGroup];
   int first_sum[kGroup + 1];           // first partial sum of each
+  int share[9];                        // products: first tile of each XCD's share
   float *w, *mom;
   const float *g;
   _Float16 *ws;
@@ -82,11 +83,34 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
   float *mom = p.mom + q.offset;
   const float *g = p.g + q.offset;
   double sum = 0.;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += 256) {
-    const float gi = g[i], mi = p.mu * mom[i] + gi;
-    mom[i] = mi;
-    const float u = p.nesterov ? gi + p.mu * mi : mi;
-    sum += (double)u * (double)u;
+  for (int64_t i = i0 + threadIdx.x * 4; i < i1; i += 4 * 256 * 4) {
+    Piece<float, 4> gi[4], mi[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * 1024 + 4 <= i1) {
+        gi[u] = load_piece<float, 4>(g + i + u * 1024);
+        mi[u] = load_piece<float, 4>(mom + i + u * 1024);
+      }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t at = i + u * 1024;
+      if (at + 4 <= i1) {
+        float m[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          m[e] = p.mu * mi[u].v[e] + gi[u].v[e];
+          const float x = p.nesterov ? gi[u].v[e] + p.mu * m[e] : m[e];
+          sum += (double)x * (double)x;
+        }
+        store_piece<float, 4>(mom + at, m);
+      } else {
+        for (int64_t k = at; k < i1; ++k) {
+          const float m = p.mu * mom[k] + g[k], x = p.nesterov ? g[k] + p.mu * m : m;
+          mom[k] = m;
+          sum += (double)x * (double)x;
+        }
+      }
+    }
   }
   for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
   __shared__ double part_sum[4];
@@ -95,28 +119,34 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
   if (threadIdx.x == 0) p.sums[p.first_sum[k] + part] = part_sum[0] + part_sum[1] + part_sum[2] + part_sum[3];
 }
 
+__device__ __forceinline__ int wave_of(int t) { return t >> 6; }
+
 // X = U / (|U| + 1e-7) in both orders, a 64 x 64 tile a block
 __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
   const int k = matrix_of(p, blockIdx.x), tile = blockIdx.x - p.first[k], t = threadIdx.x, lane = t & 63;
   const Mat &q = p.mat[k];
   const int mp = padded(q.m), np = padded(q.n), ti = tile / (np / kTile), tj = tile % (np / kTile);
   const Buffers buf = buffers(p, q);
+  const int ld = q.t ? q.m : q.n;
+  float g[kTile * kTile / 256], m[kTile * kTile / 256];
+#pragma unroll
+  for (int u = 0; u < kTile * kTile / 256; ++u) {         // rows and columns of the tile as the vector has them: lanes along a row
+    const int a = wave_of(t) + u * 4, b = lane, i = ti * kTile + (q.t ? b : a), j = tj * kTile + (q.t ? a : b);
+    const bool in = i < q.m && j < q.n;
+    const int64_t at = q.offset + (q.t ? (int64_t)j * ld + i : (int64_t)i * ld + j);
+    m[u] = in ? p.mom[at] : 0.f;
+    g[u] = in && p.nesterov ? p.g[at] : 0.f;
+  }
   double sum = 0.;
   const int n_sums = p.first_sum[k + 1] - p.first_sum[k];
   for (int i = lane; i < n_sums; i += 64) sum += p.sums[p.first_sum[k] + i];
   for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
   const float inv = (float)(1. / (sqrt(sum) + 1e-7));
   __shared__ float x[kTile][kTile + 1];
-  const int ld = q.t ? q.m : q.n;
-  for (int s = t; s < kTile * kTile; s += 256) {
-    const int a = s / kTile, b = s % kTile, i = ti * kTile + (q.t ? b : a), j = tj * kTile + (q.t ? a : b);
-    float u = 0.f;
-    if (i < q.m && j < q.n) {
-      const int64_t at = q.offset + (q.t ? (int64_t)j * ld + i : (int64_t)i * ld + j);
-      const float mi = p.mom[at];
-      u = (p.nesterov ? p.g[at] + p.mu * mi : mi) * inv;
-    }
-    x[q.t ? b : a][q.t ? a : b] = u * kUp;
+#pragma unroll
+  for (int u = 0; u < kTile * kTile / 256; ++u) {
+    const int a = wave_of(t) + u * 4, b = lane;
+    x[q.t ? b : a][q.t ? a : b] = (p.nesterov ? g[u] + p.mu * m[u] : m[u]) * inv * kUp;
   }
   __syncthreads();
   for (int s = t; s < 512; s += 256) {
@@ -152,9 +182,10 @@ struct Product {
 template <int STEP, int T>
 __device__ __forceinline__ Product product_of(const MuonArgs &p) {
   Product d;
-  // Blocks are dealt to the eight XCDs in turn: an XCD takes neighbouring tiles, whose operands its L2 then holds
-  const int all = p.first[p.count], xcd = blockIdx.x % 8, per = all / 8, rem = all % 8;
-  const int block = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / 8;
+  // Blocks are dealt to the eight XCDs in turn; an XCD takes consecutive tiles, whose operands its L2 then holds
+  const int xcd = blockIdx.x % 8, block = p.share[xcd] + (int)(blockIdx.x / 8);
+  d.k = -1;
+  if (block >= p.share[xcd + 1]) return d;
   d.k = matrix_of(p, block);
   const Mat &q = p.mat[d.k];
   const int tile = block - p.first[d.k];
@@ -280,115 +311,117 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
   __builtin_amdgcn_wave_barrier();
 }
 
-// Both halves of two factors of a 32 x 32 x 16 product; the small terms first.
-__device__ __forceinline__ void add_product(f32x16 &acc, const f16x8 &ph, const f16x8 &pl, const f16x8 &qh, const f16x8 &ql) {
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, ql, acc, 0, 0, 0);
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl, qh, acc, 0, 0, 0);
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph, qh, acc, 0, 0, 0);
-}
-
-// Few tiles: 64 x 64 a block, 32 x 32 a wave, fragments requested in place from L2 and kAhead of them ahead.
-template <int STEP>
-__global__ __launch_bounds__(256) void muon_product_kernel(const MuonArgs p) {
-  constexpr int kAhead = 4;                                // (there are a multiple of four along k)
-  __shared__ float turn[4][32][33];
-  const Product d = product_of<STEP, kTile>(p);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ib = d.ti * 2 + (wave >> 1), jb = d.tj * 2 + (wave & 1);
-  const _Float16 *pa = d.P + (int64_t)ib * d.kbs * 1024 + lane * 8, *qa = d.Q + (int64_t)jb * d.kbs * 1024 + lane * 8;
-  f32x16 acc;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  f16x8 ph[kAhead], pl[kAhead], qh[kAhead], ql[kAhead];
-  auto request = [&](int u, int kb) {
-    const _Float16 *a = pa + (int64_t)kb * 1024, *b = qa + (int64_t)kb * 1024;
-    ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 512);
-    qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 512);
-  };
-#pragma unroll
-  for (int u = 0; u < kAhead; ++u) request(u, u);
-  __builtin_amdgcn_sched_barrier(0);
-  for (int kb = 0; kb < d.kbs; kb += kAhead) {
-    const int next = kb + kAhead < d.kbs ? kb + kAhead : kb;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      add_product(acc, ph[u], pl[u], qh[u], ql[u]);
-      request(u, next + u);
-      __builtin_amdgcn_sched_barrier(0);                   // (else the requests sink to where they are needed)
-    }
-  }
-  put<STEP>(p, d, acc, ib, jb, turn[wave]);
-}
-
-// Many tiles: 128 x 128 a block, 64 x 64 a wave. 32 of the summed dimension at a time go from L2 straight into LDS, where two waves each read them;
-// while they are multiplied the next 32 are on their way into the other half of the LDS. Two blocks a compute unit.
-constexpr int kWide = 128;
-constexpr unsigned kStage = 32 * 1024;                     // bytes: 2 factors x 4 blocks of 32 rows x 2 fragments x (hi, lo)
-template <int STEP>
-__global__ __launch_bounds__(256, 2) void muon_product_wide_kernel(const MuonArgs p) {
+// A block takes T x T of a product, each of its four waves a quarter. 32 of the summed dimension at a time (a stage) go from L2 straight into LDS, where two
+// waves each read them; while a stage is multiplied the STAGES - 1 behind it are on their way.
+template <int STEP, int T, int STAGES>
+__global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) {
+  constexpr int NB = T / 64;                               // blocks of 32 of a wave, in each direction
+  constexpr unsigned kFactor = T / 32 * 4096, kStage = 2 * kFactor;   // bytes: T / 32 blocks of rows x 2 fragments x (hi, lo) of 1 KB
+  constexpr int kLoads = (int)(kStage / 4096);             // of a wave, 1 KB each: half of one factor's blocks
   extern __shared__ __align__(16) char lds[];
-  const Product d = product_of<STEP, kWide>(p);
+  const Product d = product_of<STEP, T>(p);
+  if (d.k < 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wi = wave >> 1, wj = wave & 1;
   const int rows_q = (STEP == STEP_GRAM || STEP == STEP_POLY ? d.mp : d.np) / 32;
-  // wave w fills 8 KB of a stage: two blocks of 32 rows of P (w = 0, 1) or Q, 4 KB each, which lie side by side along k. (Rows behind the
-  // padded matrix are read from its last block and never stored.)
-  const char *src[2];
+  // waves 0 and 1 fill in P, 2 and 3 Q, NB blocks of rows each, 4 KB that lie side by side along k. (Rows behind the padded matrix
+  // are read from its last block and never stored.)
+  const char *src[NB];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int rb = (wave & 1) * 2 + u;
-    int at = (wave < 2 ? d.ti : d.tj) * 4 + rb;
+  for (int u = 0; u < NB; ++u) {
+    int at = (wave < 2 ? d.ti : d.tj) * (T / 32) + (wave & 1) * NB + u;
     const int last = (wave < 2 ? d.mp / 32 : rows_q) - 1;
     at = at < last ? at : last;
     src[u] = (const char *)((wave < 2 ? d.P : d.Q) + (int64_t)at * d.kbs * 1024) + lane * 16;
   }
-  const unsigned base = lds_address(lds), mine = (unsigned)__builtin_amdgcn_readfirstlane(wave) * 8192;
-  auto request = [&](int s) {
+  const unsigned base = lds_address(lds) + (unsigned)__builtin_amdgcn_readfirstlane(wave) * (NB * 4096);
+  auto request = [&](int s, int buffer) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < NB; ++u)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) lds_direct_load16(src[u] + (int64_t)s * 4096 + k * 1024, base + (s & 1) * kStage + mine + u * 4096 + k * 1024);
+      for (int k = 0; k < 4; ++k) lds_direct_load16(src[u] + (int64_t)s * 4096 + k * 1024, base + buffer * kStage + u * 4096 + k * 1024);
   };
-  f32x16 acc[2][2];
+  f32x16 acc[NB][NB];
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+  for (int a = 0; a < NB; ++a)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-  const int stages = d.kbs / 2;
-  request(0);
+  const int stages = d.kbs / 2;                            // (kbs is a multiple of four)
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < stages) request(s, s);
+  int buffer = 0;
   for (int s = 0; s < stages; ++s) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's part of stage s is there, and behind the barrier all of it;
-    __syncthreads();                                        // and nobody reads the other half any more
-    if (s + 1 < stages) request(s + 1);
-    const char *at = lds + (s & 1) * kStage + lane * 16;
+    // this wave's part of stage s is there (loads arrive in order), and behind the barrier all of it; and nobody reads the buffer of stage s - 1 any more
+    if (STAGES > 2 && s + STAGES - 2 < stages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    if (s + STAGES - 1 < stages) request(s + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);
+    const char *at = lds + buffer * kStage + lane * 16;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      f16x8 ph[2], pl[2], qh[2], ql[2];
+      f16x8 ph[NB], pl[NB], qh[NB], ql[NB];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const char *a = at + (wi * 2 + u) * 4096 + k * 2048, *b = at + 16384 + (wj * 2 + u) * 4096 + k * 2048;
+      for (int u = 0; u < NB; ++u) {
+        const char *a = at + (wi * NB + u) * 4096 + k * 2048, *b = at + kFactor + (wj * NB + u) * 4096 + k * 2048;
         ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 1024);
         qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 1024);
       }
+      // (an instruction that adds to the sums of the one before it waits for that: the three products of a block apart)
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+      for (int a = 0; a < NB; ++a)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) add_product(acc[a][b], ph[a], pl[a], qh[b], ql[b]);
+        for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], ql[b], acc[a][b], 0, 0, 0);
+#pragma unroll
+      for (int a = 0; a < NB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[a], qh[b], acc[a][b], 0, 0, 0);
+#pragma unroll
+      for (int a = 0; a < NB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], qh[b], acc[a][b], 0, 0, 0);
     }
+    buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
   }
   __syncthreads();                                          // the LDS becomes the waves' turning space
   float (*turn)[33] = (float (*)[33])(lds + wave * 32 * 33 * 4);
 #pragma unroll
-  for (int a = 0; a < 2; ++a)
+  for (int a = 0; a < NB; ++a)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int ib = d.ti * 4 + wi * 2 + a, jb = d.tj * 4 + wj * 2 + b;
+    for (int b = 0; b < NB; ++b) {
+      const int ib = (d.ti * 2 + wi) * NB + a, jb = (d.tj * 2 + wj) * NB + b;
       if (ib < d.mp / 32 && jb < rows_q) put<STEP>(p, d, acc[a][b], ib, jb, turn);
     }
 }
 
-// A launch of product STEP over all matrices.
+// A launch of product STEP over all matrices. An XCD's share of the tiles is an eighth of the work, in the order of the matrices: a small matrix is
+// one XCD's in all products of a step, a large one is cut into few pieces.
+template <int STEP, int T, int STAGES>
+int launch_tiles(const xrl_ctx *c, MuonArgs &p) {
+  constexpr int kFixed = 256;                              // what a tile costs beside its products, as a sum's length
+  auto length = [&](int k) { return (int64_t)(STEP == STEP_GRAM ? p.mat[k].n : p.mat[k].m) + kFixed; };
+  int64_t work = 0, done = 0;
+  for (int k = 0; k < p.count; ++k) work += (p.first[k + 1] - p.first[k]) * length(k);
+  int x = 1, most = 0;
+  for (int k = 0; k < p.count; ++k) {
+    const int64_t tiles = p.first[k + 1] - p.first[k], each = length(k);
+    for (; x < 8; ++x) {                                   // share x ends inside matrix k, at a whole tile
+      const int64_t n = std::max<int64_t>(0, (work * x / 8 - done + each / 2) / each);
+      if (n > tiles) break;
+      p.share[x] = p.first[k] + (int)n;
+    }
+    done += tiles * each;
+  }
+  p.share[0] = 0;
+  for (; x <= 8; ++x) p.share[x] = p.first[p.count];
+  for (int s = 0; s < 8; ++s) most = std::max(most, p.share[s + 1] - p.share[s]);
+  muon_product_kernel<STEP, T, STAGES><<<dim3((unsigned)most * 8), dim3(256), STAGES * T * 256, op_stream(c)>>>(p);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}
+
 template <int STEP>
 int launch_product(const xrl_ctx *c, MuonArgs &p) {
   auto blocks = [&](int T) {
@@ -401,18 +434,13 @@ int launch_product(const xrl_ctx *c, MuonArgs &p) {
     p.first[p.count] = (int)at;
     return at;
   };
-  if (blocks(kWide) >= op_compute_units(c)) {
-    constexpr int lds = 2 * (int)kStage;
-    muon_product_wide_kernel<STEP><<<dim3((unsigned)p.first[p.count]), dim3(256), lds, op_stream(c)>>>(p);
-  } else {
-    muon_product_kernel<STEP><<<dim3((unsigned)blocks(kTile)), dim3(256), 0, op_stream(c)>>>(p);
-  }
-  OP_TRY(hipGetLastError());
-  return XRL_OK;
+  if (blocks(128) >= op_compute_units(c)) return launch_tiles<STEP, 128, 2>(c, p);
+  blocks(64);
+  return launch_tiles<STEP, 64, 3>(c, p);
 }
 
 int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
-  for (int k = 0; k <= p.count; ++k) p.first[k] = p.first_sum[k];
+  for (int k = 0; k <= p.count; ++k) p.first[k] = p.first_sum[k];   // (one partial sum a block)
   muon_momentum_kernel<<<dim3((unsigned)p.first[p.count]), dim3(256), 0, op_stream(c)>>>(p);
   p.first[0] = 0;
   for (int k = 0; k < p.count; ++k)
@@ -460,6 +488,10 @@ int xrl_muon_step(xrl_ctx *c, const xrl_muon_desc *desc, int32_t n_matrices, con
       const xrl_matrix &q = matrices[order[i]];
       if (q.offset + q.rows * q.cols > matrices[order[i + 1]].offset) return fail(XRL_ERR_SHAPE, "%s: matrices %d and %d overlap", who, order[i], order[i + 1]);
     }
+    // the longest sums first, so that a launch does not end with them
+    std::stable_sort(order.begin(), order.end(), [&](int x, int y) {
+      return std::max(matrices[x].rows, matrices[x].cols) > std::max(matrices[y].rows, matrices[y].cols);
+    });
     for (int k : order) {
       const xrl_matrix &q = matrices[k];
       Mat x = {};
