@@ -42,7 +42,11 @@ struct MuonArgs {
   int first[kGroup + 1];               // first block of each matrix in this launch
   Mat mat[kGroup];
   int first_sum[kGroup + 1];           // first partial sum of each
-  int share[9];                        // products: first tile of each XCD's share
+  int parts[kGroup];                   // products: parts that the sums of each matrix's tiles are cut into, a block each
+  int share[9];                        // products: first block of each XCD's share
+  float *partial;                      // [blocks of a launch][T * T] sums of parts
+  int *arrived;                        // [blocks of a launch] parts of a tile that are there, zero between launches
+  int n_arrived;
   float *w, *mom;
   const float *g;
   _Float16 *ws;
@@ -77,6 +81,7 @@ __device__ __forceinline__ void split(float y, _Float16 &hi, _Float16 &lo) {
 
 // M = mu M + G, and of each chunk the sum of squares of U
 __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < p.n_arrived; i += gridDim.x * 256) p.arrived[i] = 0;
   const int k = matrix_of(p, blockIdx.x), part = blockIdx.x - p.first[k];
   const Mat &q = p.mat[k];
   const int64_t size = (int64_t)q.m * q.n, i0 = (int64_t)part * q.chunk, i1 = i0 + q.chunk < size ? i0 + q.chunk : size;
@@ -176,6 +181,7 @@ enum { STEP_GRAM, STEP_POLY, STEP_APPLY, STEP_LAST };
 // One product of a step, D[i][j] = sum over k of P[i][k] Q[j][k], both in fragment order along k: the block's tile, of T x T.
 struct Product {
   int k, ti, tj, mp, np, kbs;          // matrix; tile; padded sizes; fragments along k
+  int block, part, parts;              // block of the launch, which part of the tile's sums it adds up
   const _Float16 *P, *Q;
   Buffers buf;
 };
@@ -188,7 +194,10 @@ __device__ __forceinline__ Product product_of(const MuonArgs &p) {
   if (block >= p.share[xcd + 1]) return d;
   d.k = matrix_of(p, block);
   const Mat &q = p.mat[d.k];
-  const int tile = block - p.first[d.k];
+  d.parts = p.parts[d.k];
+  d.block = block;
+  const int tile = (block - p.first[d.k]) / d.parts;
+  d.part = block - p.first[d.k] - tile * d.parts;
   d.mp = padded(q.m);
   d.np = padded(q.n);
   d.buf = buffers(p, q);
@@ -311,6 +320,24 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
   __builtin_amdgcn_wave_barrier();
 }
 
+// Three products of the halves of two factors, 32 x 32 x 16, into NB x NB blocks; an instruction that adds to the sums of the one before it waits for
+// that, so the three of a block stand apart.
+template <int NB>
+__device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *ph, const f16x8 *pl, const f16x8 *qh, const f16x8 *ql) {
+#pragma unroll
+  for (int a = 0; a < NB; ++a)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], ql[b], acc[a][b], 0, 0, 0);
+#pragma unroll
+  for (int a = 0; a < NB; ++a)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[a], qh[b], acc[a][b], 0, 0, 0);
+#pragma unroll
+  for (int a = 0; a < NB; ++a)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], qh[b], acc[a][b], 0, 0, 0);
+}
+
 // A block takes T x T of a product, each of its four waves a quarter. 32 of the summed dimension at a time (a stage) go from L2 straight into LDS, where two
 // waves each read them; while a stage is multiplied the STAGES - 1 behind it are on their way.
 template <int STEP, int T, int STAGES>
@@ -348,7 +375,10 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-  const int stages = d.kbs / 2;                            // (kbs is a multiple of four)
+  // this block's part of the sums (kbs is a multiple of four)
+  const int per = (d.kbs / 2 + d.parts - 1) / d.parts, first = d.part * per, stages = first + per < d.kbs / 2 ? per : d.kbs / 2 - first;
+#pragma unroll
+  for (int u = 0; u < NB; ++u) src[u] += (int64_t)first * 4096;
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s)
     if (s < stages) request(s, s);
@@ -369,21 +399,45 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
         ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 1024);
         qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 1024);
       }
-      // (an instruction that adds to the sums of the one before it waits for that: the three products of a block apart)
-#pragma unroll
-      for (int a = 0; a < NB; ++a)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], ql[b], acc[a][b], 0, 0, 0);
-#pragma unroll
-      for (int a = 0; a < NB; ++a)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[a], qh[b], acc[a][b], 0, 0, 0);
-#pragma unroll
-      for (int a = 0; a < NB; ++a)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], qh[b], acc[a][b], 0, 0, 0);
+      add_products<NB>(acc, ph, pl, qh, ql);
     }
     buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+  }
+  if (d.parts > 1) {
+    // The part is laid down, past the L2 that other XCDs do not see; the block that comes last adds up all of them in order.
+    constexpr int kTileFloats = T * T;
+    const int64_t mine = (int64_t)wave * NB * NB * 1024 + lane;
+    float *to = p.partial + (int64_t)d.block * kTileFloats + mine;
+#pragma unroll
+    for (int a = 0; a < NB; ++a)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          __hip_atomic_store(to + ((a * NB + b) * 16 + r) * 64, acc[a][b][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __shared__ int last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int *arrived = p.arrived + d.block - d.part;
+    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == d.parts - 1;
+    __syncthreads();
+    if (!last) return;
+    if (threadIdx.x == 0) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int a = 0; a < NB; ++a)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+    for (int k = 0; k < d.parts; ++k) {
+      const float *from = p.partial + (int64_t)(d.block - d.part + k) * kTileFloats + mine;
+#pragma unroll
+      for (int a = 0; a < NB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[a][b][r] += __hip_atomic_load(from + ((a * NB + b) * 16 + r) * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
   }
   __syncthreads();                                          // the LDS becomes the waves' turning space
   float (*turn)[33] = (float (*)[33])(lds + wave * 32 * 33 * 4);
@@ -396,50 +450,312 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     }
 }
 
-// A launch of product STEP over all matrices. An XCD's share of the tiles is an eighth of the work, in the order of the matrices: a small matrix is
-// one XCD's in all products of a step, a large one is cut into few pieces.
-template <int STEP, int T, int STAGES>
-int launch_tiles(const xrl_ctx *c, MuonArgs &p) {
-  constexpr int kFixed = 256;                              // what a tile costs beside its products, as a sum's length
-  auto length = [&](int k) { return (int64_t)(STEP == STEP_GRAM ? p.mat[k].n : p.mat[k].m) + kFixed; };
+// ---- matrices of at most 64 x 512: a whole step of one matrix in one block, nothing but the vectors' entries read and written.
+// Wave w keeps columns 32 w .. 32 w + 31 of X in registers, as the products leave them: x[b][r] is row 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of column
+// 32 w + lane % 32, times 2^12, in fp32. For A = X X^T the waves lay X down in LDS in fragment order (turned round on the way) and share out the four
+// 32 x 32 blocks of A, a quarter of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
+constexpr int kSmallRows = 64, kSmallCols = 512, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+constexpr int kSmallX = kSmallWaves * 8192, kSmallLds = kSmallX + 2 * 16384;   // X, and the quarters of A after it; A; B
+
+__device__ __forceinline__ unsigned two_halves(_Float16 a, _Float16 b) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, f16x2{a, b});
+}
+// Four rows of one column, as a lane has them in a product, into a fragment-ordered 64 x 64 matrix: rows along the summed dimension.
+__device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, int lane, const float *v) {
+  f16x4 hi, lo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    _Float16 h, l;
+    split(v[e], h, l);
+    hi[e] = h; lo[e] = l;
+  }
+  _Float16 *o = to + (jb * 4 + ib * 2 + (s >> 1)) * 1024 + ((lane & 31) + 32 * (s & 1)) * 8 + 4 * (lane >> 5);
+  *(f16x4 *)o = hi;
+  *(f16x4 *)(o + 512) = lo;
+}
+
+__global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArgs p, int steps) {
+  extern __shared__ __align__(16) char lds[];
+  const Mat &q = p.mat[blockIdx.x];
+  const int m = q.m, n = q.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, jl = lane & 31;
+  const int j = wave * 32 + jl, used = (n + 31) / 32;     // waves that have columns
+  _Float16 *X = (_Float16 *)lds, *A = (_Float16 *)(lds + kSmallX), *B = A + 8192;
+  float *quarters = (float *)lds;
+  float *w = p.w + q.offset, *mom = p.mom + q.offset;
+  const float *grad = p.g + q.offset;
+  // entry (b, r) of a lane in the vector: lanes along its rows, which for a matrix that is taken transposed is another order than x's
+  float (*turn)[33] = (float (*)[33])(lds + wave * 8192);
+  auto at = [&](int b, int r) {
+    const int i = 32 * b + (q.t ? jl : acc_row(r, g)), c = q.t ? wave * 32 + 2 * r + g : j;
+    return i < m && c < n ? (q.t ? c * m + i : i * n + c) : -1;
+  };
+  // M = mu M + G, U and |U|
+  float x[2][16];
+  double sum = 0.;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    float gi[16], mi[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int k = at(b, r);
+      gi[r] = k >= 0 ? grad[k] : 0.f;
+      mi[r] = k >= 0 ? mom[k] : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int k = at(b, r);
+      const float mr = p.mu * mi[r] + gi[r];
+      if (k >= 0) mom[k] = mr;
+      const float u = p.nesterov ? gi[r] + p.mu * mr : mr;
+      x[b][r] = u;
+      sum += (double)u * (double)u;
+    }
+  }
+  for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
+  double *sums = (double *)lds;
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  sum = 0.;
+  for (int k = 0; k < kSmallWaves; ++k) sum += sums[k];
+  const float inv = (float)(1. / (sqrt(sum) + 1e-7));
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[b][r] = x[b][r] * inv * kUp;
+  __syncthreads();
+  if (q.t)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) turn[jl][2 * r + g] = x[b][r];
+      __builtin_amdgcn_wave_barrier();
+      __threadfence_block();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = turn[acc_row(r, g)][jl];
+      __builtin_amdgcn_wave_barrier();
+      __threadfence_block();
+    }
+  for (int step = 0; step < steps; ++step) {
+    // X in fragment order, rows along the columns: turned round 32 x 32 at a time in the wave's own 8 KB
+    if (wave < used) {
+      f16x8 hi[2][2], lo[2][2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = x[b][r];
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            _Float16 h, l;
+            split(turn[jl][kb * 16 + g * 8 + e], h, l);
+            hi[b][kb][e] = h; lo[b][kb][e] = l;
+          }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
+      }
+      // [wave][kb][row block][hi, lo]
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          _Float16 *o = X + ((wave * 2 + kb) * 2 + b) * 1024 + lane * 8;
+          *(f16x8 *)o = hi[b][kb];
+          *(f16x8 *)(o + 512) = lo[b][kb];
+        }
+    }
+    __syncthreads();
+    // A: wave 4 t + s the s-th quarter of the sum of block t
+    const int ib = wave >> 3, jb = (wave >> 2) & 1, quarter = wave & 3;
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+    const int kbs = 2 * used, per = (kbs + 3) / 4, k0 = quarter * per, k1 = k0 + per < kbs ? k0 + per : kbs;
+    for (int kb = k0; kb < k1; ++kb) {
+      const _Float16 *a = X + (kb * 2 + ib) * 1024 + lane * 8, *b = X + (kb * 2 + jb) * 1024 + lane * 8;
+      const f16x8 ah = *(const f16x8 *)a, al = *(const f16x8 *)(a + 512), bh = *(const f16x8 *)b, bl = *(const f16x8 *)(b + 512);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
+    }
+    __syncthreads();                                       // (the quarters take X's place)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) quarters[(wave * 16 + r) * 64 + lane] = acc[r];
+    __syncthreads();
+    {
+      float v[4];                                          // the same waves: four rows each of the sums of the four quarters
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float *o = quarters + ((wave & ~3) * 16 + quarter * 4 + e) * 64 + lane;
+        v[e] = (((o[0] + o[1024]) + o[2048]) + o[3072]) * kDown;
+      }
+      put_four(A, ib, jb, quarter, lane, v);
+    }
+    __syncthreads();
+    if (wave < 4) {                                        // B = a I + b A + c A A, a block a wave
+      const int bi = wave >> 1, bj = wave & 1;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        const _Float16 *a = A + (bi * 4 + kb) * 1024 + lane * 8, *b = A + (bj * 4 + kb) * 1024 + lane * 8;
+        const f16x8 ah = *(const f16x8 *)a, al = *(const f16x8 *)(a + 512), bh = *(const f16x8 *)b, bl = *(const f16x8 *)(b + 512);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const _Float16 *o = A + (bj * 4 + bi * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
+        const f16x4 h = *(const f16x4 *)o, l = *(const f16x4 *)(o + 512);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = kNsC * (acc[4 * s + e] * kDown) + (kNsB * ((float)h[e] + (float)l[e]) + (bi == bj && 8 * s + 4 * g + e == jl ? kNsA * kUp : 0.f));
+        put_four(B, bi, bj, s, lane, v);
+      }
+    }
+    __syncthreads();
+    if (wave < used) {                                     // X = B X, the wave's columns
+      f16x8 xh[4], xl[4];
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) {
+        // rows 16 kb .. 16 kb + 15 of the column lie in registers 8 (kb % 2) .. of the lane (rows 0-3 and 8-11) and of its
+        // partner in the other half (4-7, 12-15); the operand wants rows 0-7 in the lower half's lane and 8-15 in the upper's
+        _Float16 h[8], l[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split(x[kb >> 1][8 * (kb & 1) + e], h[e], l[e]);
+        typedef unsigned u32x4v __attribute__((ext_vector_type(4)));
+        u32x4v ph, pl;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const auto a = __builtin_amdgcn_permlane32_swap(two_halves(h[2 * u], h[2 * u + 1]), two_halves(h[4 + 2 * u], h[5 + 2 * u]), false, false);
+          const auto b = __builtin_amdgcn_permlane32_swap(two_halves(l[2 * u], l[2 * u + 1]), two_halves(l[4 + 2 * u], l[5 + 2 * u]), false, false);
+          ph[u] = a[0]; ph[2 + u] = a[1];
+          pl[u] = b[0]; pl[2 + u] = b[1];
+        }
+        xh[kb] = __builtin_bit_cast(f16x8, ph);
+        xl[kb] = __builtin_bit_cast(f16x8, pl);
+      }
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+          const _Float16 *o = B + (b * 4 + kb) * 1024 + lane * 8;
+          const f16x8 bh = *(const f16x8 *)o, bl = *(const f16x8 *)(o + 512);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh, xl[kb], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(bl, xh[kb], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh, xh[kb], acc, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[b][r] = acc[r] * kDown;
+      }
+    }
+    __syncthreads();                                       // (B and the quarters are read no more)
+  }
+  const float step = p.step * sqrtf((float)n) * kDown;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    if (q.t) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = x[b][r];
+      __builtin_amdgcn_wave_barrier();
+      __threadfence_block();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = turn[jl][2 * r + g];
+      __builtin_amdgcn_wave_barrier();
+      __threadfence_block();
+    }
+    float old[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int k = at(b, r);
+      old[r] = k >= 0 ? w[k] : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int k = at(b, r);
+      if (k >= 0) w[k] = p.decay * old[r] - step * x[b][r];
+    }
+  }
+}
+
+// The blocks of product `step` of all matrices, in p: tiles of 128 x 128 where they fill the chip, else of 64 x 64; a sum that is long beside what each
+// compute unit has to do is cut into parts. Returns the tile's size.
+int plan_product(MuonArgs &p, int step, int n_cu) {
+  const bool half = step == STEP_GRAM || step == STEP_POLY;
+  auto sum_length = [&](int k) { return (int64_t)((step == STEP_GRAM ? p.mat[k].n : p.mat[k].m) + kTile - 1) / kTile * kTile; };
+  auto tiles = [&](int k, int T) {
+    const int64_t th = (p.mat[k].m + T - 1) / T, tw = (p.mat[k].n + T - 1) / T;
+    return half ? th * (th + 1) / 2 : th * tw;
+  };
+  int64_t wide = 0, work = 0;
+  for (int k = 0; k < p.count; ++k) wide += tiles(k, 128);
+  const int T = wide >= n_cu ? 128 : 64;
+  for (int k = 0; k < p.count; ++k) work += tiles(k, T) * sum_length(k);
+  // What cutting costs, laying down and adding up, is 2 to 4 us; 64 of a sum take a lone block of 64 x 64 0.8 us. One step of a 1 x 2342 matrix
+  // 31 / 19 us, of 2859 x 89 37 / 22. (Tiles of 128 x 128 are cut nowhere: X X^T of 2048 x 8192, three parts, 336 / 392.)
+  const int64_t least = std::max<int64_t>(384, work / n_cu);
+  int64_t at = 0;
+  for (int k = 0; k < p.count; ++k) {
+    p.parts[k] = half && T == 64 ? (int)std::min<int64_t>(16, std::max<int64_t>(1, sum_length(k) / least)) : 1;
+    const int64_t stages = sum_length(k) / 32, per = (stages + p.parts[k] - 1) / p.parts[k];
+    p.parts[k] = (int)((stages + per - 1) / per);          // none is empty
+    p.first[k] = (int)at;
+    at += tiles(k, T) * p.parts[k];
+  }
+  p.first[p.count] = (int)at;
+  return T;
+}
+
+// An XCD's share of the blocks is an eighth of the work, in the order of the matrices: a small matrix is one XCD's in all products of a step, a large
+// one is cut into few pieces. Returns the blocks of the launch.
+int deal_blocks(MuonArgs &p, int step) {
+  constexpr int kFixed = 256;                              // what a block costs beside its products, as a sum's length
   int64_t work = 0, done = 0;
+  auto length = [&](int k) { return (int64_t)(step == STEP_GRAM ? p.mat[k].n : p.mat[k].m) / p.parts[k] + kFixed; };
   for (int k = 0; k < p.count; ++k) work += (p.first[k + 1] - p.first[k]) * length(k);
   int x = 1, most = 0;
   for (int k = 0; k < p.count; ++k) {
-    const int64_t tiles = p.first[k + 1] - p.first[k], each = length(k);
-    for (; x < 8; ++x) {                                   // share x ends inside matrix k, at a whole tile
+    const int64_t blocks = p.first[k + 1] - p.first[k], each = length(k);
+    for (; x < 8; ++x) {                                   // share x ends inside matrix k
       const int64_t n = std::max<int64_t>(0, (work * x / 8 - done + each / 2) / each);
-      if (n > tiles) break;
+      if (n > blocks) break;
       p.share[x] = p.first[k] + (int)n;
     }
-    done += tiles * each;
+    done += blocks * each;
   }
   p.share[0] = 0;
   for (; x <= 8; ++x) p.share[x] = p.first[p.count];
   for (int s = 0; s < 8; ++s) most = std::max(most, p.share[s + 1] - p.share[s]);
-  muon_product_kernel<STEP, T, STAGES><<<dim3((unsigned)most * 8), dim3(256), STAGES * T * 256, op_stream(c)>>>(p);
-  OP_TRY(hipGetLastError());
-  return XRL_OK;
+  return most * 8;
 }
 
 template <int STEP>
 int launch_product(const xrl_ctx *c, MuonArgs &p) {
-  auto blocks = [&](int T) {
-    int64_t at = 0;
-    for (int k = 0; k < p.count; ++k) {
-      const int64_t th = (p.mat[k].m + T - 1) / T, tw = (p.mat[k].n + T - 1) / T;
-      p.first[k] = (int)at;
-      at += STEP == STEP_GRAM || STEP == STEP_POLY ? th * (th + 1) / 2 : th * tw;
-    }
-    p.first[p.count] = (int)at;
-    return at;
-  };
-  if (blocks(128) >= op_compute_units(c)) return launch_tiles<STEP, 128, 2>(c, p);
-  blocks(64);
-  return launch_tiles<STEP, 64, 3>(c, p);
+  const int T = plan_product(p, STEP, op_compute_units(c));
+  const dim3 grid((unsigned)deal_blocks(p, STEP)), block(256);
+  if (T == 128) muon_product_kernel<STEP, 128, 2><<<grid, block, 2 * 32 * 1024, op_stream(c)>>>(p);
+  else muon_product_kernel<STEP, 64, 3><<<grid, block, 3 * 16 * 1024, op_stream(c)>>>(p);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
 }
 
 int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
+  bool small = true;
+  for (int k = 0; k < p.count; ++k) small = small && p.mat[k].m <= kSmallRows && p.mat[k].n <= kSmallCols;
+  if (small) {
+    static const hipError_t allowed = hipFuncSetAttribute((const void *)muon_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);
+    if (allowed != hipSuccess) return fail(XRL_ERR_HIP, "xrl_muon_step: %d bytes of LDS: %s", kSmallLds, hipGetErrorString(allowed));
+    muon_small_kernel<<<dim3((unsigned)p.count), dim3(kSmallThreads), kSmallLds, op_stream(c)>>>(p, steps);
+    OP_TRY(hipGetLastError());
+    return XRL_OK;
+  }
   for (int k = 0; k <= p.count; ++k) p.first[k] = p.first_sum[k];   // (one partial sum a block)
   muon_momentum_kernel<<<dim3((unsigned)p.first[p.count]), dim3(256), 0, op_stream(c)>>>(p);
   p.first[0] = 0;
@@ -508,29 +824,42 @@ int xrl_muon_step(xrl_ctx *c, const xrl_muon_desc *desc, int32_t n_matrices, con
   if (list.empty()) return XRL_OK;
   if (!d_weights || !d_grads || !d_momentum) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
   if (((uintptr_t)d_weights | (uintptr_t)d_grads | (uintptr_t)d_momentum) % 4) return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of 4", who);
-  // the largest group's workspace: every group uses it from the start
-  size_t most = 0;
-  for (size_t i = 0; i < list.size(); i += kGroup) {
-    int64_t halves = 0;
-    for (size_t k = i; k < std::min(list.size(), i + kGroup); ++k) {
-      list[k].ws = halves;
-      halves += 3 * x_halves(list[k].m, list[k].n) + 2 * x_halves(list[k].m, list[k].m);
+  // Groups run one after another in the same workspace: operands, sums of squares, parts of sums and their counters
+  std::vector<MuonArgs> groups;
+  size_t most = 0, floats = 0, counters = 0;
+  try {
+    for (size_t i = 0; i < list.size(); i += kGroup) {
+      MuonArgs p = {};
+      p.count = (int)std::min<size_t>(kGroup, list.size() - i);
+      int64_t halves = 0;
+      for (int k = 0; k < p.count; ++k) {
+        Mat &q = p.mat[k] = list[i + k];
+        const int64_t size = (int64_t)q.m * q.n;
+        q.ws = halves;
+        halves += 3 * x_halves(q.m, q.n) + 2 * x_halves(q.m, q.m);
+        p.first_sum[k + 1] = p.first_sum[k] + (int)((size + q.chunk - 1) / q.chunk);
+      }
+      most = std::max(most, (size_t)halves * 2);
+      for (int step : {STEP_GRAM, STEP_POLY}) {
+        const int T = plan_product(p, step, op_compute_units(c));
+        bool cut = false;
+        for (int k = 0; k < p.count; ++k) cut = cut || p.parts[k] > 1;
+        if (!cut) continue;
+        counters = std::max(counters, (size_t)p.first[p.count]);
+        floats = std::max(floats, (size_t)p.first[p.count] * T * T);
+      }
+      groups.push_back(p);
     }
-    most = std::max(most, (size_t)halves * 2);
+  } catch (const std::bad_alloc &) {
+    return fail(XRL_ERR_OOM, "%s: out of host memory", who);
   }
-  const size_t o_sums = op_align(most);
+  const size_t o_sums = op_align(most), o_part = o_sums + op_align((size_t)kGroup * kMaxSums * 8), o_count = o_part + op_align(floats * 4);
   char *ws = nullptr;
-  if (int rc = op_workspace(c, o_sums + (size_t)kGroup * kMaxSums * 8, &ws, who)) return rc;
-  for (size_t i = 0; i < list.size(); i += kGroup) {
-    MuonArgs p = {};
-    p.count = (int)std::min<size_t>(kGroup, list.size() - i);
-    for (int k = 0; k < p.count; ++k) {
-      p.mat[k] = list[i + k];
-      const int64_t size = (int64_t)p.mat[k].m * p.mat[k].n;
-      p.first_sum[k + 1] = p.first_sum[k] + (int)((size + p.mat[k].chunk - 1) / p.mat[k].chunk);
-    }
+  if (int rc = op_workspace(c, o_count + counters * 4, &ws, who)) return rc;
+  for (MuonArgs &p : groups) {
     p.w = d_weights; p.mom = d_momentum; p.g = d_grads;
     p.ws = (_Float16 *)ws; p.sums = (double *)(ws + o_sums);
+    p.partial = (float *)(ws + o_part); p.arrived = (int *)(ws + o_count); p.n_arrived = (int)counters;
     p.mu = desc->momentum; p.decay = 1.f - desc->lr * desc->weight_decay; p.step = desc->lr * desc->rms; p.nesterov = desc->nesterov != 0;
     if (int rc = run_group(c, p, desc->steps)) return rc;
   }
