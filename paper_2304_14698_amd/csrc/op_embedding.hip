@@ -237,27 +237,33 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
   }
 }
 
-// Sums over runs of equal ids. A group of `lanes` threads takes kWindow consecutive sorted pairs, in their order; a batch's rows, and the rows of the
+// Sums over runs of equal ids. A group of `lanes` threads takes a window of consecutive sorted pairs, in their order; a batch's rows, and the rows of the
 // table that its runs are added to, are requested together. A run inside the window is added to its row of the table. The piece of a run that began
 // before goes to carry[window][0], that of one that goes on behind it to carry[window][1]; a window that such a run begins in is listed, and
 // embed_join_kernel adds up the run's pieces.
-constexpr int kWindow = 16, kJoinWaves = 8;
+// Groups that are whole waves keep their pairs in scalar registers; there a window is of 32 pairs from eight waves a compute unit on, else of 16. us of
+// this kernel and the next, 32 / 16: 65536 long-tailed ids of 1024 columns in bf16 52 + 16 / 53 + 19, 77013 ids of 128 columns in fp32 (no whole waves)
+// 18 + 7 / 11 + 9; whole calls of 8192 and 16384 ids of 1024 columns 56 / 47 and 60 / 55.
+constexpr int kJoinWaves = 8;
 
 struct SumArgs {
   const uint2 *items;
   const void *dout;
   float *dtable, *carry;        // carry [windows][2][dim]
-  int32_t *listed, *list;       // how many windows are listed, and which (in any order)
+  int32_t *listed;              // how many windows are listed,
+  int2 *list;                   // and which, with the run's id (in any order)
   int64_t dout_stride, dtable_stride, n;
-  int vocab, dim, lanes;
+  int vocab, dim, lanes, window;
   float scale;
 };
 
-template <typename T, int VEC, int BATCH>
+template <typename T, int VEC, int BATCH, bool WHOLE, int kWindow>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   touch_args(a);
   const int lane = threadIdx.x & (a.lanes - 1);
-  const int64_t w = (int64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
+  int in_block = threadIdx.x / a.lanes;
+  if (WHOLE) in_block = __builtin_amdgcn_readfirstlane(in_block);   // whole waves: their pairs are in scalar registers
+  const int64_t w = (int64_t)blockIdx.x * (256 / a.lanes) + in_block;
   const int64_t i0 = w * kWindow;
   if (i0 >= a.n) return;
   const int c = ((int)blockIdx.y * a.lanes + lane) * VEC;
@@ -269,11 +275,12 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   unsigned id[kWindow + 2];
   int at[kWindow];
   id[0] = i0 > 0 ? it[-1].x : ~0u;
+  if (WHOLE) id[0] = __builtin_amdgcn_readfirstlane(id[0]);
 #pragma unroll
   for (int i = 0; i < kWindow + 1; ++i) {
     const uint2 x = i0 + i < a.n ? it[i] : make_uint2(vocab, 0);
-    id[i + 1] = x.x;
-    if (i < kWindow) at[i] = (int)x.y;
+    id[i + 1] = WHOLE ? __builtin_amdgcn_readfirstlane(x.x) : x.x;
+    if (i < kWindow) at[i] = WHOLE ? __builtin_amdgcn_readfirstlane((int)x.y) : (int)x.y;
   }
   float acc[VEC];
 #pragma unroll
@@ -306,7 +313,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
         if (nv == VEC) store_piece<float, VEC>(p, acc);
         else
           for (int j = 0; j < nv; ++j) p[j] = acc[j];
-        if (!head && lane == 0 && blockIdx.y == 0) a.list[atomicAdd(a.listed, 1)] = (int)w;
+        if (!head && lane == 0 && blockIdx.y == 0) a.list[atomicAdd(a.listed, 1)] = make_int2((int)w, (int)id[i + 1]);
       } else {
         float *p = a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c;
         if (nv == VEC) {
@@ -332,15 +339,16 @@ struct Run {
 };
 __device__ __forceinline__ Run run_of(const SumArgs &a, int listed, int lane) {
   Run r;
-  r.w = a.list[listed];
-  r.id = a.items[(r.w + 1) * kWindow - 1].x;
+  const int2 x = a.list[listed];
+  r.w = x.x;
+  r.id = (unsigned)x.y;
   // windows behind w that begin with the id: 64 probes at once, each level 64 times as fine
-  const int64_t windows = (a.n + kWindow - 1) / kWindow;
+  const int64_t windows = (a.n + a.window - 1) / a.window;
   int64_t more = 0;
   for (int64_t s = (int64_t)1 << 18; s; s >>= 6)
     if (s == 1 || s < windows) {
       const int64_t k = r.w + more + (lane + 1) * s;
-      more += s * __popcll(__ballot(k < windows && a.items[k < windows ? k * kWindow : 0].x == r.id));
+      more += s * __popcll(__ballot(k < windows && a.items[k < windows ? k * a.window : 0].x == r.id));
     }
   r.pieces = more + 1;
   return r;
@@ -431,15 +439,23 @@ int launch_embed_few(const xrl_ctx *c, const FewArgs &a) {
   return XRL_OK;
 }
 
+// Threads that share a row of the gradient, and pairs of a window.
+void sum_shape(const xrl_ctx *c, int elem, int dim, int64_t n, int *lanes, int *window) {
+  const int vec = 16 / elem, pieces = (dim + vec - 1) / vec;
+  *lanes = 1;
+  while (*lanes < pieces && *lanes < 256) *lanes *= 2;
+  *window = *lanes >= 64 && n / 32 * (*lanes / 64) >= 8 * op_compute_units(c) ? 32 : 16;
+}
+
 template <typename T>
 int launch_embed_sums(const xrl_ctx *c, SumArgs &a) {
   constexpr int VEC = sizeof(T) == 2 ? 8 : 4, BATCH = 4;
   const int pieces = (a.dim + VEC - 1) / VEC;
-  a.lanes = 1;
-  while (a.lanes < pieces && a.lanes < 256) a.lanes *= 2;
-  const int64_t windows = (a.n + kWindow - 1) / kWindow, per = 256 / a.lanes;
-  embed_sum_kernel<T, VEC, BATCH><<<dim3((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes)), dim3(256), 0,
-                             op_stream(c)>>>(a);
+  const int64_t windows = (a.n + a.window - 1) / a.window, per = 256 / a.lanes;
+  const dim3 grid((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes));
+  if (a.window == 32) embed_sum_kernel<T, VEC, BATCH, true, 32><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else if (a.lanes >= 64) embed_sum_kernel<T, VEC, BATCH, true, 16><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else embed_sum_kernel<T, VEC, BATCH, false, 16><<<grid, dim3(256), 0, op_stream(c)>>>(a);
   embed_join_kernel<<<dim3((unsigned)std::min<int64_t>(windows, 2 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256)),
                       dim3(kJoinWaves * 64), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
@@ -495,10 +511,12 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   const int64_t per_wave = std::max<int64_t>(256, (n + (int64_t)kSortBlocks * kSortWaves - 1) / ((int64_t)kSortBlocks * kSortWaves));
   s.per_wave = (int)((per_wave + 63) / 64 * 64);
   const int blocks = (int)((n + (int64_t)s.per_wave * kSortWaves - 1) / ((int64_t)s.per_wave * kSortWaves));
-  const int64_t windows = (n + kWindow - 1) / kWindow;
+  int lanes, window;
+  sum_shape(c, dout_type == XRL_PREC_BF16 ? 2 : 4, (int)dim, n, &lanes, &window);
+  const int64_t windows = (n + window - 1) / window;
   const int64_t hist = (int64_t)blocks << per_pass;      // counters of one pass
   const size_t o_b = op_align((size_t)n * 8), o_h = 2 * o_b, o_l = o_h + op_align((size_t)(hist + 1) * 4),
-               o_c = o_l + op_align((size_t)windows * 4);
+               o_c = o_l + op_align((size_t)windows * 8);
   char *ws = nullptr;
   if (int rc = op_workspace(c, o_c + (size_t)windows * 2 * dim * 4, &ws, who)) return rc;
   uint2 *x = (uint2 *)ws, *y = (uint2 *)(ws + o_b);
@@ -512,8 +530,8 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
     std::swap(x, y);
   }
   OP_TRY(hipGetLastError());
-  SumArgs a = {x, d_dout, d_dtable, (float *)(ws + o_c), s.clear, (int32_t *)(ws + o_l), dout_stride, dtable_stride, n,
-               (int)vocab, (int)dim, 0, scale};
+  SumArgs a = {x, d_dout, d_dtable, (float *)(ws + o_c), s.clear, (int2 *)(ws + o_l), dout_stride, dtable_stride, n,
+               (int)vocab, (int)dim, lanes, window, scale};
   return dout_type == XRL_PREC_BF16 ? launch_embed_sums<bf16_t>(c, a) : launch_embed_sums<float>(c, a);
 }
 
