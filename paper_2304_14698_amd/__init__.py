@@ -476,11 +476,25 @@ class Encoder:
         t = self.torch
         d = self._logits(logits, mask, row_ptr, temperature)
         n, f = d.n_rows, t.float32
-        keys = ["entropy", "stats"] + (["logp"] if ids is not None else []) + (["top_ids", "top_logp"] if top_k > 0 else [])
-        spec = dict(logp=((n,), f), entropy=((n,), f), stats=((n, 2), f), top_ids=((n, top_k), t.int32), top_logp=((n, top_k), f))
-        o = dict(zip(keys, self._made(*[spec[k] for k in keys]))) if out is None else out
-        p = [self._flat(o[k], k, spec[k][1], n * (1 if len(spec[k][0]) == 1 else spec[k][0][1])) if k in keys else None
-             for k in ("logp", "entropy", "stats", "top_ids", "top_logp")]
+        have, best = ids is not None, top_k > 0
+        o = out
+        if o is None:
+            spec = [((n,), f), ((n, 2), f)]
+            if have:
+                spec.append(((n,), f))
+            if best:
+                spec += [((n, top_k), t.int32), ((n, top_k), f)]
+            made = self._made(*spec)
+            o = dict(entropy=made[0], stats=made[1])
+            if have:
+                o["logp"] = made[2]
+            if best:
+                o["top_ids"], o["top_logp"] = made[-2:]
+            p = [o[k].data_ptr() if k in o else None for k in ("logp", "entropy", "stats", "top_ids", "top_logp")]
+        else:
+            p = [self._flat(o["logp"], "logp", f, n) if have else None, self._flat(o["entropy"], "entropy", f, n),
+                 self._flat(o["stats"], "stats", f, 2 * n), self._flat(o["top_ids"], "top_ids", t.int32, n * top_k) if best else None,
+                 self._flat(o["top_logp"], "top_logp", f, n * top_k) if best else None]
         _check(self.lib.xrl_token_logp(self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), top_k, *p))
         return o
 

@@ -74,9 +74,20 @@ __device__ __forceinline__ int matrix_of(const MuonArgs &p, int block) {
   const int lane = threadIdx.x & 63;
   return __popcll(__ballot(lane < p.count && p.first[lane < p.count ? lane : 0] <= block)) - 1;
 }
-__device__ __forceinline__ void split(float y, _Float16 &hi, _Float16 &lo) {
-  hi = (_Float16)y;
-  lo = (_Float16)(y - (float)hi);
+// N values split in two halves each: pairs, so that one instruction rounds two.
+template <int N, typename V>
+__device__ __forceinline__ void split(const float *y, V &hi, V &lo) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  f16x2 h[N / 2], l[N / 2];
+#pragma unroll
+  for (int e = 0; e < N / 2; ++e) {
+    const f32x2 x = {y[2 * e], y[2 * e + 1]};
+    h[e] = __builtin_convertvector(x, f16x2);
+    l[e] = __builtin_convertvector(x - __builtin_convertvector(h[e], f32x2), f16x2);
+  }
+  __builtin_memcpy(&hi, h, sizeof(hi));
+  __builtin_memcpy(&lo, l, sizeof(lo));
 }
 
 // M = mu M + G, and of each chunk the sum of squares of U
@@ -157,19 +168,16 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
   for (int s = t; s < 512; s += 256) {
     const int rb = s >> 8, kb = (s >> 6) & 3, row = rb * 32 + (lane & 31), c = kb * 16 + (lane >> 5) * 8;
     f16x8 hi, lo;
-    for (int e = 0; e < 8; ++e) {
-      _Float16 h, l;
-      split(x[row][c + e], h, l);
-      hi[e] = h; lo[e] = l;
-    }
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[row][c + e];
+    split<8>(v, hi, lo);
     _Float16 *o = buf.x + ((int64_t)(ti * 2 + rb) * (np / 16) + tj * 4 + kb) * 1024 + lane * 8;
     *(f16x8 *)o = hi;
     *(f16x8 *)(o + 512) = lo;
-    for (int e = 0; e < 8; ++e) {
-      _Float16 h, l;
-      split(x[c + e][row], h, l);
-      hi[e] = h; lo[e] = l;
-    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[c + e][row];
+    split<8>(v, hi, lo);
     o = buf.xt + ((int64_t)(tj * 2 + rb) * (mp / 16) + ti * 4 + kb) * 1024 + lane * 8;
     *(f16x8 *)o = hi;
     *(f16x8 *)(o + 512) = lo;
@@ -285,12 +293,7 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     f16x4 hi, lo;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      _Float16 h, l;
-      split(v[4 * s + e], h, l);
-      hi[e] = h; lo[e] = l;
-    }
+    split<4>(v + 4 * s, hi, lo);
     _Float16 *o = by_j + ((int64_t)jb * (d.mp / 16) + ib * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
     *(f16x4 *)o = hi;
     *(f16x4 *)(o + 512) = lo;
@@ -306,12 +309,10 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
 #pragma unroll
   for (int kb = 0; kb < 2; ++kb) {
     f16x8 hi, lo;
+    float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      _Float16 h, l;
-      split(turn[jl][kb * 16 + g * 8 + e], h, l);
-      hi[e] = h; lo[e] = l;
-    }
+    for (int e = 0; e < 8; ++e) y[e] = turn[jl][kb * 16 + g * 8 + e];
+    split<8>(y, hi, lo);
     _Float16 *o = by_i + ((int64_t)ib * (kdim / 16) + jb * 2 + kb) * 1024 + lane * 8;
     *(f16x8 *)o = hi;
     *(f16x8 *)(o + 512) = lo;
@@ -457,19 +458,10 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 constexpr int kSmallRows = 64, kSmallCols = 512, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 constexpr int kSmallX = kSmallWaves * 8192, kSmallLds = kSmallX + 2 * 16384;   // X, and the quarters of A after it; A; B
 
-__device__ __forceinline__ unsigned two_halves(_Float16 a, _Float16 b) {
-  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(unsigned, f16x2{a, b});
-}
 // Four rows of one column, as a lane has them in a product, into a fragment-ordered 64 x 64 matrix: rows along the summed dimension.
 __device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, int lane, const float *v) {
   f16x4 hi, lo;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    _Float16 h, l;
-    split(v[e], h, l);
-    hi[e] = h; lo[e] = l;
-  }
+  split<4>(v, hi, lo);
   _Float16 *o = to + (jb * 4 + ib * 2 + (s >> 1)) * 1024 + ((lane & 31) + 32 * (s & 1)) * 8 + 4 * (lane >> 5);
   *(f16x4 *)o = hi;
   *(f16x4 *)(o + 512) = lo;
@@ -547,13 +539,12 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
         __builtin_amdgcn_wave_barrier();
         __threadfence_block();
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb) {
+          float y[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            _Float16 h, l;
-            split(turn[jl][kb * 16 + g * 8 + e], h, l);
-            hi[b][kb][e] = h; lo[b][kb][e] = l;
-          }
+          for (int e = 0; e < 8; ++e) y[e] = turn[jl][kb * 16 + g * 8 + e];
+          split<8>(y, hi[b][kb], lo[b][kb]);
+        }
         __builtin_amdgcn_wave_barrier();
         __threadfence_block();
       }
@@ -625,15 +616,13 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
       for (int kb = 0; kb < 4; ++kb) {
         // rows 16 kb .. 16 kb + 15 of the column lie in registers 8 (kb % 2) .. of the lane (rows 0-3 and 8-11) and of its
         // partner in the other half (4-7, 12-15); the operand wants rows 0-7 in the lower half's lane and 8-15 in the upper's
-        _Float16 h[8], l[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) split(x[kb >> 1][8 * (kb & 1) + e], h[e], l[e]);
         typedef unsigned u32x4v __attribute__((ext_vector_type(4)));
-        u32x4v ph, pl;
+        u32x4v h, l, ph, pl;
+        split<8>(x[kb >> 1] + 8 * (kb & 1), h, l);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const auto a = __builtin_amdgcn_permlane32_swap(two_halves(h[2 * u], h[2 * u + 1]), two_halves(h[4 + 2 * u], h[5 + 2 * u]), false, false);
-          const auto b = __builtin_amdgcn_permlane32_swap(two_halves(l[2 * u], l[2 * u + 1]), two_halves(l[4 + 2 * u], l[5 + 2 * u]), false, false);
+          const auto a = __builtin_amdgcn_permlane32_swap(h[u], h[2 + u], false, false);
+          const auto b = __builtin_amdgcn_permlane32_swap(l[u], l[2 + u], false, false);
           ph[u] = a[0]; ph[2 + u] = a[1];
           pl[u] = b[0]; pl[2 + u] = b[1];
         }
