@@ -44,7 +44,8 @@ __device__ __forceinline__ Piece<T, N> load_piece(const T *p) {
   __builtin_memcpy(&x, p, sizeof(x));
   return x;
 }
-template <typename T, int N>
+// N floats to p, rounded to T. STREAM: stores that leave no copy in the caches (16-byte pieces), for results that are larger than these.
+template <typename T, int N, bool STREAM = false>
 __device__ __forceinline__ void store_piece(T *p, const float *v) {
   Piece<T, N> x;
   if constexpr (sizeof(T) == 2 && N % 2 == 0) {
@@ -56,8 +57,18 @@ __device__ __forceinline__ void store_piece(T *p, const float *v) {
 #pragma unroll
     for (int i = 0; i < N; ++i) x.v[i] = (T)v[i];
   }
-  __builtin_memcpy(p, &x, sizeof(x));
+  if constexpr (STREAM) {
+    typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    u32x4 u[sizeof(x) / 16];
+    __builtin_memcpy(u, &x, sizeof(x));
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(x) / 16); ++i) __builtin_nontemporal_store(u[i], (u32x4_any *)p + i);
+  } else {
+    __builtin_memcpy(p, &x, sizeof(x));
+  }
 }
+// Results of more bytes than all L2s together hold (eight of 4 MB) are stored past the caches.
+inline bool streams(int64_t bytes) { return bytes > (int64_t)32 << 20; }
 
 // Reductions over a wave by lane moves within the vector registers (a row of 16 lanes, then rows onto the next), the result in all lanes.
 // A shuffle goes through the LDS, about 100 clocks each way: six of them for a maximum, two dozen for a row's sums.

@@ -339,12 +339,12 @@ __device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *ph,
     for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], qh[b], acc[a][b], 0, 0, 0);
 }
 
-// A block takes T x T of a product, each of its four waves a quarter. 32 of the summed dimension at a time (a stage) go from L2 straight into LDS, where two
+// A block takes T x T of a product, each of its four waves a quarter. KB fragments along the summed dimension at a time (a stage) go from L2 straight into LDS, where two
 // waves each read them; while a stage is multiplied the STAGES - 1 behind it are on their way.
-template <int STEP, int T, int STAGES>
+template <int STEP, int T, int STAGES, int KB = 2>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) {
   constexpr int NB = T / 64;                               // blocks of 32 of a wave, in each direction
-  constexpr unsigned kFactor = T / 32 * 4096, kStage = 2 * kFactor;   // bytes: T / 32 blocks of rows x 2 fragments x (hi, lo) of 1 KB
+  constexpr unsigned kRows = KB * 2048, kFactor = T / 32 * kRows, kStage = 2 * kFactor;   // bytes: T / 32 blocks of rows x KB fragments x (hi, lo) of 1 KB
   constexpr int kLoads = (int)(kStage / 4096);             // of a wave, 1 KB each: half of one factor's blocks
   extern __shared__ __align__(16) char lds[];
   const Product d = product_of<STEP, T>(p);
@@ -362,12 +362,12 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     at = at < last ? at : last;
     src[u] = (const char *)((wave < 2 ? d.P : d.Q) + (int64_t)at * d.kbs * 1024) + lane * 16;
   }
-  const unsigned base = lds_address(lds) + (unsigned)__builtin_amdgcn_readfirstlane(wave) * (NB * 4096);
+  const unsigned base = lds_address(lds) + (unsigned)__builtin_amdgcn_readfirstlane(wave) * (NB * kRows);
   auto request = [&](int s, int buffer) {
 #pragma unroll
     for (int u = 0; u < NB; ++u)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) lds_direct_load16(src[u] + (int64_t)s * 4096 + k * 1024, base + buffer * kStage + u * 4096 + k * 1024);
+      for (int k = 0; k < 2 * KB; ++k) lds_direct_load16(src[u] + (int64_t)s * kRows + k * 1024, base + buffer * kStage + u * kRows + k * 1024);
   };
   f32x16 acc[NB][NB];
 #pragma unroll
@@ -377,9 +377,9 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
   // this block's part of the sums (kbs is a multiple of four)
-  const int per = (d.kbs / 2 + d.parts - 1) / d.parts, first = d.part * per, stages = first + per < d.kbs / 2 ? per : d.kbs / 2 - first;
+  const int per = (d.kbs / KB + d.parts - 1) / d.parts, first = d.part * per, stages = first + per < d.kbs / KB ? per : d.kbs / KB - first;
 #pragma unroll
-  for (int u = 0; u < NB; ++u) src[u] += (int64_t)first * 4096;
+  for (int u = 0; u < NB; ++u) src[u] += (int64_t)first * kRows;
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s)
     if (s < stages) request(s, s);
@@ -392,11 +392,11 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     if (s + STAGES - 1 < stages) request(s + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);
     const char *at = lds + buffer * kStage + lane * 16;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < KB; ++k) {
       f16x8 ph[NB], pl[NB], qh[NB], ql[NB];
 #pragma unroll
       for (int u = 0; u < NB; ++u) {
-        const char *a = at + (wi * NB + u) * 4096 + k * 2048, *b = at + kFactor + (wj * NB + u) * 4096 + k * 2048;
+        const char *a = at + (wi * NB + u) * kRows + k * 2048, *b = at + kFactor + (wj * NB + u) * kRows + k * 2048;
         ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 1024);
         qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 1024);
       }
@@ -729,7 +729,10 @@ template <int STEP>
 int launch_product(const xrl_ctx *c, MuonArgs &p) {
   const int T = plan_product(p, STEP, op_compute_units(c));
   const dim3 grid((unsigned)deal_blocks(p, STEP)), block(256);
-  if (T == 128) muon_product_kernel<STEP, 128, 2><<<grid, block, 2 * 32 * 1024, op_stream(c)>>>(p);
+  // (the last product reads and writes the weights besides: four blocks of half the LDS a compute unit, 555 / 516 us for two 2048^2 and two 2048 x 8192;
+  // X X^T so 331 / 365, the others alike)
+  constexpr int KB = STEP == STEP_LAST ? 1 : 2;
+  if (T == 128) muon_product_kernel<STEP, 128, 2, KB><<<grid, block, 2 * KB * 16 * 1024, op_stream(c)>>>(p);
   else muon_product_kernel<STEP, 64, 3><<<grid, block, 3 * 16 * 1024, op_stream(c)>>>(p);
   OP_TRY(hipGetLastError());
   return XRL_OK;

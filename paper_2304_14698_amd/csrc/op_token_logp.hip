@@ -312,7 +312,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
 }
 
 // dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T);
   const int64_t r = a.row0 + blockIdx.y + (int64_t)blockIdx.z * 32768;
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs
       if (col + j == id) v += a.inv_t * g;
       d[j] = ok[j] && any && !(x[j] == -INFINITY) ? v : 0.f;
     }
-    if (n == VEC) store_piece<T, VEC>(out + col, d);
+    if (n == VEC) store_piece<T, VEC, STREAM>(out + col, d);
     else
 #pragma unroll
       for (int j = 0; j < VEC; ++j)
@@ -399,6 +399,11 @@ void launch_logp(const xrl_ctx *c, LogpArgs &a, bool wave_rows) {
       token_logp_kernel<T, 4, TOP><<<dim3((unsigned)jobs), dim3(256), 0, op_stream(c)>>>(a);
   }
   if (a.parts > 1) token_logp_join_kernel<T><<<dim3((unsigned)a.n_rows), dim3(64), 0, op_stream(c)>>>(a);
+}
+
+template <typename T, bool STREAM>
+void launch_backward(const xrl_ctx *c, const LogpArgs &a, dim3 grid) {
+  token_logp_backward_kernel<T, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
 }
 
 }  // namespace
@@ -453,11 +458,12 @@ int xrl_token_logp_backward(xrl_ctx *c, const xrl_logits_desc *logits, const int
   a.dlogits = d_dlogits; a.dstride = dlogits_stride;
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, vec = logits->type == XRL_PREC_BF16 ? 8 : 4;
   const int64_t chunks = std::max<int64_t>(1, (cols + 256 * vec * 2 - 1) / (256 * vec * 2));
+  const bool stream = streams(a.n_cols * (a.row_ptr ? 1 : a.n_rows) * (logits->type == XRL_PREC_BF16 ? 2 : 4));
   for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMaxBlocks) {
     const int64_t rows = std::min(a.n_rows - a.row0, kMaxBlocks);
     const dim3 grid((unsigned)chunks, (unsigned)std::min<int64_t>(rows, 32768), (unsigned)((rows + 32767) / 32768));
-    if (logits->type == XRL_PREC_BF16) token_logp_backward_kernel<bf16_t><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-    else token_logp_backward_kernel<float><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+    if (logits->type == XRL_PREC_BF16) stream ? launch_backward<bf16_t, true>(c, a, grid) : launch_backward<bf16_t, false>(c, a, grid);
+    else stream ? launch_backward<float, true>(c, a, grid) : launch_backward<float, false>(c, a, grid);
   }
   OP_TRY(hipGetLastError());
   return XRL_OK;
