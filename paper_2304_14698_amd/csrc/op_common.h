@@ -33,15 +33,24 @@ inline bool op_type_ok(int32_t type) { return type == XRL_PREC_FP32 || type == X
 // Whether rows of `stride` elements of `elem` bytes from p on all begin at multiples of 16 bytes.
 inline bool rows_aligned(const void *p, int64_t stride, int elem) { return ((uintptr_t)p | (uintptr_t)(stride * elem)) % 16 == 0; }
 
-// N elements from p, which may lie at any multiple of the element's size.
+// N elements from p, which may lie at any multiple of the element's size. STREAM: what is read for the last time, 16-byte pieces that leave no copy in
+// the caches.
 template <typename T, int N>
 struct Piece {
   T v[N];
 };
-template <typename T, int N>
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T, int N, bool STREAM = false>
 __device__ __forceinline__ Piece<T, N> load_piece(const T *p) {
   Piece<T, N> x;
-  __builtin_memcpy(&x, p, sizeof(x));
+  if constexpr (STREAM) {
+    u32x4 u[sizeof(x) / 16];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(x) / 16); ++i) u[i] = __builtin_nontemporal_load((const u32x4_any *)p + i);
+    __builtin_memcpy(&x, u, sizeof(x));
+  } else {
+    __builtin_memcpy(&x, p, sizeof(x));
+  }
   return x;
 }
 // N floats to p, rounded to T. STREAM: stores that leave no copy in the caches (16-byte pieces), for results that are larger than these.
@@ -58,7 +67,6 @@ __device__ __forceinline__ void store_piece(T *p, const float *v) {
     for (int i = 0; i < N; ++i) x.v[i] = (T)v[i];
   }
   if constexpr (STREAM) {
-    typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
     u32x4 u[sizeof(x) / 16];
     __builtin_memcpy(u, &x, sizeof(x));
 #pragma unroll

@@ -421,12 +421,16 @@ int xrl_token_logp(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_i
   if (((uintptr_t)d_ids | (uintptr_t)d_logp | (uintptr_t)d_entropy | (uintptr_t)d_stats | (uintptr_t)d_top_ids | (uintptr_t)d_top_logp) % 4)
     return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
   a.ids = d_ids; a.top_k = top_k; a.logp = d_logp; a.entropy = d_entropy; a.stats = d_stats; a.top_ids = d_top_ids; a.top_logp = d_top_logp;
-  const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols;      // (ragged: on average)
-  const bool wave_rows = cols <= 1024;
+  // A wave a row up to 1024 columns (on average, where they are ragged), else a block a row. Few long rows are cut into parts, at most 64, which a second
+  // launch joins: of 2048 columns and a wave each where such parts do not fill the chip by themselves, else of a block each.
+  const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, n_cu = op_compute_units(c), fine = (cols + 2047) / 2048;
+  bool wave_rows = cols <= 1024;
   a.parts = 1;
-  if (!wave_rows) {
-    const int64_t want = 4 * (int64_t)op_compute_units(c) / a.n_rows, most = cols / 2048;
-    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+  if (!wave_rows && fine <= 64 && fine * a.n_rows <= 8 * n_cu) {
+    wave_rows = true;
+    a.parts = (int)fine;
+  } else if (!wave_rows) {
+    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({4 * n_cu / a.n_rows, cols / 2048, 64}));
   }
   if (a.parts > 1) {
     const size_t jobs = (size_t)a.n_rows * a.parts, o_t = op_align(jobs * 12), o_i = o_t + op_align(jobs * top_k * 4);
