@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 using namespace xrl;
@@ -31,29 +32,31 @@ constexpr int kGroup = 32;             // matrices of one launch: their list is 
 constexpr int kTile = 64;              // sizes are padded to multiples of this
 constexpr int kMaxSums = 1024;         // partial sums of squares of a matrix
 
+// A matrix of a launch. A lane of each wave reads one, all at once, and what the block needs of its own matrix is then passed on from that lane: kernel arguments
+// lie in host memory, and one look at the list after another took 1.2 to 2.2 us a block.
 struct Mat {
   int64_t offset, ws;                  // in the flat vectors; in the workspace (halves)
-  int m, n;                            // m <= n
-  bool t;                              // the matrix in the vector is n x m
+  int m, n, t;                         // m <= n; t: the matrix in the vector is n x m
   int chunk;                           // entries of one partial sum of squares
+  int first_sum;                       // its first partial sum
+  int first;                           // its first block in this launch
+  int parts;                           // products: parts that the sums of its tiles are cut into, a block each
+  int blocks;                          // in this launch
 };
 struct MuonArgs {
   int count;
-  int first[kGroup + 1];               // first block of each matrix in this launch
-  Mat mat[kGroup];
-  int first_sum[kGroup + 1];           // first partial sum of each
-  int parts[kGroup];                   // products: parts that the sums of each matrix's tiles are cut into, a block each
+  int flip;                            // which of the two X^T holds the current one
   int share[9];                        // products: first block of each XCD's share
-  float *partial;                      // [blocks of a launch][T * T] sums of parts
-  int *arrived;                        // [blocks of a launch] parts of a tile that are there, zero between launches
   int n_arrived;
+  Mat mat[kGroup];
   float *w, *mom;
   const float *g;
   _Float16 *ws;
   double *sums;
+  float *partial;                      // [blocks of a launch][T * T] sums of parts
+  int *arrived;                        // [blocks of a launch] parts of a tile that are there, zero between launches
   float mu, decay, step;               // step: lr rms (times sqrt(max(rows, cols)))
-  bool nesterov;
-  int flip;                            // which of the two X^T holds the current one
+  int nesterov;
 };
 
 __device__ __forceinline__ int padded(int x) { return (x + kTile - 1) / kTile * kTile; }
@@ -69,10 +72,18 @@ __device__ __forceinline__ Buffers buffers(const MuonArgs &p, const Mat &q) {
   _Float16 *w = p.ws + q.ws;
   return {w, w + (p.flip ? 2 : 1) * nx, w + (p.flip ? 1 : 2) * nx, w + 3 * nx, w + 3 * nx + na};
 }
-// The matrix that a block belongs to: a lane looks at one.
-__device__ __forceinline__ int matrix_of(const MuonArgs &p, int block) {
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
+  const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)x, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+// The matrix that block `block` of a launch belongs to.
+__device__ __forceinline__ Mat matrix_of(const MuonArgs &p, int block) {
+  static_assert(kGroup <= 64, "a lane for each");
   const int lane = threadIdx.x & 63;
-  return __popcll(__ballot(lane < p.count && p.first[lane < p.count ? lane : 0] <= block)) - 1;
+  const Mat x = p.mat[lane < kGroup ? lane : 0];
+  const int k = __popcll(__ballot(lane < p.count && x.first <= block)) - 1;
+  auto of = [&](int v) { return __builtin_amdgcn_readlane(v, k); };
+  return {from_lane(x.offset, k), from_lane(x.ws, k), of(x.m), of(x.n), of(x.t), of(x.chunk), of(x.first_sum), of(x.first), of(x.parts), of(x.blocks)};
 }
 // N values split in two halves each: pairs, so that one instruction rounds two.
 template <int N, typename V>
@@ -93,8 +104,8 @@ __device__ __forceinline__ void split(const float *y, V &hi, V &lo) {
 // M = mu M + G, and of each chunk the sum of squares of U
 __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < p.n_arrived; i += gridDim.x * 256) p.arrived[i] = 0;
-  const int k = matrix_of(p, blockIdx.x), part = blockIdx.x - p.first[k];
-  const Mat &q = p.mat[k];
+  const Mat q = matrix_of(p, blockIdx.x);
+  const int part = blockIdx.x - q.first;
   const int64_t size = (int64_t)q.m * q.n, i0 = (int64_t)part * q.chunk, i1 = i0 + q.chunk < size ? i0 + q.chunk : size;
   float *mom = p.mom + q.offset;
   const float *g = p.g + q.offset;
@@ -132,15 +143,15 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
   __shared__ double part_sum[4];
   if ((threadIdx.x & 63) == 0) part_sum[threadIdx.x >> 6] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) p.sums[p.first_sum[k] + part] = part_sum[0] + part_sum[1] + part_sum[2] + part_sum[3];
+  if (threadIdx.x == 0) p.sums[q.first_sum + part] = part_sum[0] + part_sum[1] + part_sum[2] + part_sum[3];
 }
 
 __device__ __forceinline__ int wave_of(int t) { return t >> 6; }
 
 // X = U / (|U| + 1e-7) in both orders, a 64 x 64 tile a block
 __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
-  const int k = matrix_of(p, blockIdx.x), tile = blockIdx.x - p.first[k], t = threadIdx.x, lane = t & 63;
-  const Mat &q = p.mat[k];
+  const Mat q = matrix_of(p, blockIdx.x);
+  const int tile = blockIdx.x - q.first, t = threadIdx.x, lane = t & 63;
   const int mp = padded(q.m), np = padded(q.n), ti = tile / (np / kTile), tj = tile % (np / kTile);
   const Buffers buf = buffers(p, q);
   const int ld = q.t ? q.m : q.n;
@@ -154,8 +165,8 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
     g[u] = in && p.nesterov ? p.g[at] : 0.f;
   }
   double sum = 0.;
-  const int n_sums = p.first_sum[k + 1] - p.first_sum[k];
-  for (int i = lane; i < n_sums; i += 64) sum += p.sums[p.first_sum[k] + i];
+  const int n_sums = (int)(((int64_t)q.m * q.n + q.chunk - 1) / q.chunk);
+  for (int i = lane; i < n_sums; i += 64) sum += p.sums[q.first_sum + i];
   for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
   const float inv = (float)(1. / (sqrt(sum) + 1e-7));
   __shared__ float x[kTile][kTile + 1];
@@ -188,9 +199,11 @@ enum { STEP_GRAM, STEP_POLY, STEP_APPLY, STEP_LAST };
 
 // One product of a step, D[i][j] = sum over k of P[i][k] Q[j][k], both in fragment order along k: the block's tile, of T x T.
 struct Product {
-  int k, ti, tj, mp, np, kbs;          // matrix; tile; padded sizes; fragments along k
+  bool there;
+  int ti, tj, mp, np, kbs;             // tile; padded sizes; fragments along k
   int block, part, parts;              // block of the launch, which part of the tile's sums it adds up
   const _Float16 *P, *Q;
+  Mat q;
   Buffers buf;
 };
 template <int STEP, int T>
@@ -198,14 +211,13 @@ __device__ __forceinline__ Product product_of(const MuonArgs &p) {
   Product d;
   // Blocks are dealt to the eight XCDs in turn; an XCD takes consecutive tiles, whose operands its L2 then holds
   const int xcd = blockIdx.x % 8, block = p.share[xcd] + (int)(blockIdx.x / 8);
-  d.k = -1;
-  if (block >= p.share[xcd + 1]) return d;
-  d.k = matrix_of(p, block);
-  const Mat &q = p.mat[d.k];
-  d.parts = p.parts[d.k];
+  d.there = block < p.share[xcd + 1];
+  d.q = matrix_of(p, block);
+  const Mat &q = d.q;
+  d.parts = q.parts;
   d.block = block;
-  const int tile = (block - p.first[d.k]) / d.parts;
-  d.part = block - p.first[d.k] - tile * d.parts;
+  const int tile = (block - q.first) / d.parts;
+  d.part = block - q.first - tile * d.parts;
   d.mp = padded(q.m);
   d.np = padded(q.n);
   d.buf = buffers(p, q);
@@ -229,47 +241,46 @@ __device__ __forceinline__ Product product_of(const MuonArgs &p) {
   return d;
 }
 
-// What becomes of a wave's 32 x 32 of a product, block (ib, jb). turn: the wave's own 32 x 33 floats of LDS.
+// The last product's entry r of a lane in its matrix of the vector, lanes along that one's rows (of a matrix taken transposed: along i); -1: none.
+__device__ __forceinline__ int64_t weight_at(const Mat &q, int ib, int jb, int r) {
+  const int lane = threadIdx.x & 63, g = lane >> 5, jl = lane & 31;
+  const int i = ib * 32 + (q.t ? jl : acc_row(r, g)), j = jb * 32 + (q.t ? 2 * r + g : jl);
+  return i < q.m && j < q.n ? (q.t ? (int64_t)j * q.m + i : (int64_t)i * q.n + j) : -1;
+}
+__device__ __forceinline__ void old_weights(const MuonArgs &p, const Mat &q, int ib, int jb, float *old) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int64_t at = weight_at(q, ib, jb, r);
+    old[r] = at >= 0 ? p.w[q.offset + at] : 0.f;
+  }
+}
+
+// What becomes of a wave's 32 x 32 of a product, block (ib, jb). turn: the wave's own 32 x 33 floats of LDS; old: the weights there (last product).
 template <int STEP>
-__device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f32x16 &acc, int ib, int jb, float (*turn)[33]) {
-  const Mat &q = p.mat[d.k];
+__device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f32x16 &acc, int ib, int jb, float (*turn)[33], const float *old) {
+  const Mat &q = d.q;
   // register r of a lane: D[i][j] with i = ib 32 + 8 (r / 4) + 4 (lane / 32) + r % 4, j = jb 32 + lane % 32
   const int lane = threadIdx.x & 63, g = lane >> 5, jl = lane & 31;
   if (STEP == STEP_LAST) {
     const float step = p.step * sqrtf((float)q.n) * (kDown * kDown);
-    float *w = p.w + q.offset;
-    if (!q.t) {
-      const int j = jb * 32 + jl;
-      float old[16];
+    float y[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i = ib * 32 + acc_row(r, g);
-        old[r] = i < q.m && j < q.n ? w[(int64_t)i * q.n + j] : 0.f;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i = ib * 32 + acc_row(r, g);
-        if (i < q.m && j < q.n) w[(int64_t)i * q.n + j] = p.decay * old[r] - step * acc[r];
-      }
-    } else {                                               // rows j of the vector's matrix, along i
+    for (int r = 0; r < 16; ++r) y[r] = acc[r];
+    if (q.t) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = acc[r];
       __builtin_amdgcn_wave_barrier();
       __threadfence_block();
-      const int i = ib * 32 + jl;
-      float old[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = jb * 32 + 2 * r + g;
-        old[r] = i < q.m && j < q.n ? w[(int64_t)j * q.m + i] : 0.f;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = jb * 32 + 2 * r + g;
-        if (i < q.m && j < q.n) w[(int64_t)j * q.m + i] = p.decay * old[r] - step * turn[jl][2 * r + g];
-      }
+      for (int r = 0; r < 16; ++r) y[r] = turn[jl][2 * r + g];
       __threadfence_block();
       __builtin_amdgcn_wave_barrier();
+    }
+    float *w = p.w + q.offset;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int64_t at = weight_at(q, ib, jb, r);
+      if (at >= 0) w[at] = p.decay * old[r] - step * y[r];
     }
     return;
   }
@@ -321,34 +332,37 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
   __builtin_amdgcn_wave_barrier();
 }
 
-// Three products of the halves of two factors, 32 x 32 x 16, into NB x NB blocks; an instruction that adds to the sums of the one before it waits for
-// that, so the three of a block stand apart.
 template <int NB>
-__device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *ph, const f16x8 *pl, const f16x8 *qh, const f16x8 *ql) {
+__device__ __forceinline__ void zero(f32x16 (*acc)[NB]) {
 #pragma unroll
   for (int a = 0; a < NB; ++a)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], ql[b], acc[a][b], 0, 0, 0);
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+}
+// One of the three products of the halves of two factors, 32 x 32 x 16, into NB x NB blocks.
+template <int NB>
+__device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *p, const f16x8 *q) {
 #pragma unroll
   for (int a = 0; a < NB; ++a)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[a], qh[b], acc[a][b], 0, 0, 0);
-#pragma unroll
-  for (int a = 0; a < NB; ++a)
-#pragma unroll
-    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[a], qh[b], acc[a][b], 0, 0, 0);
+    for (int b = 0; b < NB; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[a], q[b], acc[a][b], 0, 0, 0);
 }
 
-// A block takes T x T of a product, each of its four waves a quarter. KB fragments along the summed dimension at a time (a stage) go from L2 straight into LDS, where two
-// waves each read them; while a stage is multiplied the STAGES - 1 behind it are on their way.
-template <int STEP, int T, int STAGES, int KB = 2>
+// A block takes T x T of a product, each of its four waves a quarter. 32 of the summed dimension at a time (a stage, two fragments) go from L2 straight into
+// LDS, where two waves each read them; while a stage is multiplied those behind it are on their way. Tiles of 64 x 64, which often are alone on a compute
+// unit, also read the fragments of each product from LDS while the one before is multiplied, across the barrier between two stages too: a lone block's stage
+// 0.25 us, 0.31 without that. (530 clocks, of which the LDS takes 384 to be written and read and the matrix pipes 192.) Of tiles of 128 x 128 two blocks
+// fill in for each other: X X^T of two 2048^2 and two 2048 x 8192 342 us so, 331 without.
+template <int STEP, int T, int STAGES>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) {
   constexpr int NB = T / 64;                               // blocks of 32 of a wave, in each direction
+  constexpr int KB = 2;
   constexpr unsigned kRows = KB * 2048, kFactor = T / 32 * kRows, kStage = 2 * kFactor;   // bytes: T / 32 blocks of rows x KB fragments x (hi, lo) of 1 KB
-  constexpr int kLoads = (int)(kStage / 4096);             // of a wave, 1 KB each: half of one factor's blocks
   extern __shared__ __align__(16) char lds[];
   const Product d = product_of<STEP, T>(p);
-  if (d.k < 0) return;
+  if (!d.there) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wi = wave >> 1, wj = wave & 1;
   const int rows_q = (STEP == STEP_GRAM || STEP == STEP_POLY ? d.mp : d.np) / 32;
@@ -369,41 +383,80 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 #pragma unroll
       for (int k = 0; k < 2 * KB; ++k) lds_direct_load16(src[u] + (int64_t)s * kRows + k * 1024, base + buffer * kStage + u * kRows + k * 1024);
   };
+  float old[16];                                           // (of one block: requested now, needed at the end)
+  if (STEP == STEP_LAST && NB == 1) old_weights(p, d.q, d.ti * 2 + wi, d.tj * 2 + wj, old);
   f32x16 acc[NB][NB];
-#pragma unroll
-  for (int a = 0; a < NB; ++a)
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+  zero<NB>(acc);
+  f32x16 other[2][NB][NB];                                 // NB == 1: sums of their own for two of the three products of a pair of halves,
+  if (NB == 1) {                                           // or each would wait for the one before
+    zero<NB>(other[0]);
+    zero<NB>(other[1]);
+  }
   // this block's part of the sums (kbs is a multiple of four)
   const int per = (d.kbs / KB + d.parts - 1) / d.parts, first = d.part * per, stages = first + per < d.kbs / KB ? per : d.kbs / KB - first;
 #pragma unroll
   for (int u = 0; u < NB; ++u) src[u] += (int64_t)first * kRows;
+  struct Fragments {
+    f16x8 ph[NB], pl[NB], qh[NB], ql[NB];
+  };
+  auto read = [&](Fragments &f, int buffer, int k) {
+    const char *at = lds + buffer * kStage + lane * 16 + k * 2048;
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s)
-    if (s < stages) request(s, s);
-  int buffer = 0;
-  for (int s = 0; s < stages; ++s) {
-    // this wave's part of stage s is there (loads arrive in order), and behind the barrier all of it; and nobody reads the buffer of stage s - 1 any more
-    if (STAGES > 2 && s + STAGES - 2 < stages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * kLoads) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    if (s + STAGES - 1 < stages) request(s + STAGES - 1, buffer == 0 ? STAGES - 1 : buffer - 1);
-    const char *at = lds + buffer * kStage + lane * 16;
-#pragma unroll
-    for (int k = 0; k < KB; ++k) {
-      f16x8 ph[NB], pl[NB], qh[NB], ql[NB];
-#pragma unroll
-      for (int u = 0; u < NB; ++u) {
-        const char *a = at + (wi * NB + u) * kRows + k * 2048, *b = at + kFactor + (wj * NB + u) * kRows + k * 2048;
-        ph[u] = *(const f16x8 *)a; pl[u] = *(const f16x8 *)(a + 1024);
-        qh[u] = *(const f16x8 *)b; ql[u] = *(const f16x8 *)(b + 1024);
-      }
-      add_products<NB>(acc, ph, pl, qh, ql);
+    for (int u = 0; u < NB; ++u) {
+      const char *a = at + (wi * NB + u) * kRows, *b = at + kFactor + (wj * NB + u) * kRows;
+      f.ph[u] = *(const f16x8 *)a; f.pl[u] = *(const f16x8 *)(a + 1024);
+      f.qh[u] = *(const f16x8 *)b; f.ql[u] = *(const f16x8 *)(b + 1024);
     }
-    buffer = buffer + 1 == STAGES ? 0 : buffer + 1;
+  };
+  auto multiply = [&](const Fragments &f) {
+    add_products<NB>(NB == 1 ? other[0] : acc, f.ph, f.ql);
+    add_products<NB>(NB == 1 ? other[1] : acc, f.pl, f.qh);
+    add_products<NB>(acc, f.ph, f.qh);
+  };
+  // A stage is there: this wave's part (loads arrive in order; `behind` stages behind it may be on their way still), and behind the barrier all of it;
+  // and what was read from LDS before is in registers everywhere
+  constexpr int kLoads = (int)(kStage / 4096);             // of a wave and stage
+  auto arrive = [&](bool all, auto behind) {
+    if (all) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(behind)::value * kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+  };
+  Fragments f0, f1;
+  int buffer = 0;
+  if constexpr (NB == 1) {
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+      if (s < stages) request(s, s);
+    arrive(stages < STAGES, std::integral_constant<int, STAGES - 1>());
+    read(f0, 0, 0);
+    for (int s = 0; s < stages; ++s) {
+      read(f1, buffer, 1);
+      multiply(f0);
+      if (s + 1 < stages) {
+        const int next = buffer + 1 == STAGES ? 0 : buffer + 1;
+        arrive(s + STAGES - 1 >= stages, std::integral_constant<int, STAGES - 2>());
+        if (s + STAGES < stages) request(s + STAGES, buffer);
+        read(f0, next, 0);
+        buffer = next;
+      }
+      multiply(f1);
+    }
+  } else {
+    static_assert(NB == 1 || STAGES == 2, "the other half of the LDS");
+    request(0, 0);
+    for (int s = 0; s < stages; ++s) {
+      arrive(true, std::integral_constant<int, 0>());
+      if (s + 1 < stages) request(s + 1, buffer ^ 1);
+      read(f0, buffer, 0);
+      multiply(f0);
+      read(f1, buffer, 1);
+      multiply(f1);
+      buffer ^= 1;
+    }
   }
+  if (NB == 1)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][0][r] += other[0][0][0][r] + other[1][0][0][r];
   if (d.parts > 1) {
     // The part is laid down, past the L2 that other XCDs do not see; the block that comes last adds up all of them in order.
     constexpr int kTileFloats = T * T;
@@ -447,7 +500,10 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int ib = (d.ti * 2 + wi) * NB + a, jb = (d.tj * 2 + wj) * NB + b;
-      if (ib < d.mp / 32 && jb < rows_q) put<STEP>(p, d, acc[a][b], ib, jb, turn);
+      if (ib < d.mp / 32 && jb < rows_q) {
+        if (STEP == STEP_LAST && NB > 1) old_weights(p, d.q, ib, jb, old);
+        put<STEP>(p, d, acc[a][b], ib, jb, turn, old);
+      }
     }
 }
 
@@ -469,7 +525,7 @@ __device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, in
 
 __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArgs p, int steps) {
   extern __shared__ __align__(16) char lds[];
-  const Mat &q = p.mat[blockIdx.x];
+  const Mat q = matrix_of(p, blockIdx.x);
   const int m = q.m, n = q.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, jl = lane & 31;
   const int j = wave * 32 + jl, used = (n + 31) / 32;     // waves that have columns
   _Float16 *X = (_Float16 *)lds, *A = (_Float16 *)(lds + kSmallX), *B = A + 8192;
@@ -674,6 +730,13 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
   }
 }
 
+int64_t put_blocks(Mat &q, int64_t first, int64_t blocks) {
+  q.first = (int)first;
+  q.blocks = (int)blocks;
+  return first + blocks;
+}
+int all_blocks(const MuonArgs &p) { return p.mat[p.count - 1].first + p.mat[p.count - 1].blocks; }
+
 // The blocks of product `step` of all matrices, in p: tiles of 128 x 128 where they fill the chip, else of 64 x 64; a sum that is long beside what each
 // compute unit has to do is cut into parts. Returns the tile's size.
 int plan_product(MuonArgs &p, int step, int n_cu) {
@@ -692,13 +755,12 @@ int plan_product(MuonArgs &p, int step, int n_cu) {
   const int64_t least = std::max<int64_t>(384, work / n_cu);
   int64_t at = 0;
   for (int k = 0; k < p.count; ++k) {
-    p.parts[k] = half && T == 64 ? (int)std::min<int64_t>(16, std::max<int64_t>(1, sum_length(k) / least)) : 1;
-    const int64_t stages = sum_length(k) / 32, per = (stages + p.parts[k] - 1) / p.parts[k];
-    p.parts[k] = (int)((stages + per - 1) / per);          // none is empty
-    p.first[k] = (int)at;
-    at += tiles(k, T) * p.parts[k];
+    p.mat[k].parts = half && T == 64 ? (int)std::min<int64_t>(16, std::max<int64_t>(1, sum_length(k) / least)) : 1;
+    Mat &q = p.mat[k];
+    const int64_t stages = sum_length(k) / 32, per = (stages + q.parts - 1) / q.parts;
+    q.parts = (int)((stages + per - 1) / per);             // none is empty
+    at = put_blocks(q, at, tiles(k, T) * q.parts);
   }
-  p.first[p.count] = (int)at;
   return T;
 }
 
@@ -707,20 +769,20 @@ int plan_product(MuonArgs &p, int step, int n_cu) {
 int deal_blocks(MuonArgs &p, int step) {
   constexpr int kFixed = 256;                              // what a block costs beside its products, as a sum's length
   int64_t work = 0, done = 0;
-  auto length = [&](int k) { return (int64_t)(step == STEP_GRAM ? p.mat[k].n : p.mat[k].m) / p.parts[k] + kFixed; };
-  for (int k = 0; k < p.count; ++k) work += (p.first[k + 1] - p.first[k]) * length(k);
+  auto length = [&](int k) { return (int64_t)(step == STEP_GRAM ? p.mat[k].n : p.mat[k].m) / p.mat[k].parts + kFixed; };
+  for (int k = 0; k < p.count; ++k) work += p.mat[k].blocks * length(k);
   int x = 1, most = 0;
   for (int k = 0; k < p.count; ++k) {
-    const int64_t blocks = p.first[k + 1] - p.first[k], each = length(k);
+    const int64_t blocks = p.mat[k].blocks, each = length(k);
     for (; x < 8; ++x) {                                   // share x ends inside matrix k
       const int64_t n = std::max<int64_t>(0, (work * x / 8 - done + each / 2) / each);
       if (n > blocks) break;
-      p.share[x] = p.first[k] + (int)n;
+      p.share[x] = p.mat[k].first + (int)n;
     }
     done += blocks * each;
   }
   p.share[0] = 0;
-  for (; x <= 8; ++x) p.share[x] = p.first[p.count];
+  for (; x <= 8; ++x) p.share[x] = all_blocks(p);
   for (int s = 0; s < 8; ++s) most = std::max(most, p.share[s + 1] - p.share[s]);
   return most * 8;
 }
@@ -729,10 +791,7 @@ template <int STEP>
 int launch_product(const xrl_ctx *c, MuonArgs &p) {
   const int T = plan_product(p, STEP, op_compute_units(c));
   const dim3 grid((unsigned)deal_blocks(p, STEP)), block(256);
-  // (the last product reads and writes the weights besides: four blocks of half the LDS a compute unit, 555 / 516 us for two 2048^2 and two 2048 x 8192;
-  // X X^T so 331 / 365, the others alike)
-  constexpr int KB = STEP == STEP_LAST ? 1 : 2;
-  if (T == 128) muon_product_kernel<STEP, 128, 2, KB><<<grid, block, 2 * KB * 16 * 1024, op_stream(c)>>>(p);
+  if (T == 128) muon_product_kernel<STEP, 128, 2><<<grid, block, 2 * 32 * 1024, op_stream(c)>>>(p);
   else muon_product_kernel<STEP, 64, 3><<<grid, block, 3 * 16 * 1024, op_stream(c)>>>(p);
   OP_TRY(hipGetLastError());
   return XRL_OK;
@@ -744,16 +803,21 @@ int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
   if (small) {
     static const hipError_t allowed = hipFuncSetAttribute((const void *)muon_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);
     if (allowed != hipSuccess) return fail(XRL_ERR_HIP, "xrl_muon_step: %d bytes of LDS: %s", kSmallLds, hipGetErrorString(allowed));
+    for (int k = 0; k < p.count; ++k) put_blocks(p.mat[k], k, 1);
     muon_small_kernel<<<dim3((unsigned)p.count), dim3(kSmallThreads), kSmallLds, op_stream(c)>>>(p, steps);
     OP_TRY(hipGetLastError());
     return XRL_OK;
   }
-  for (int k = 0; k <= p.count; ++k) p.first[k] = p.first_sum[k];   // (one partial sum a block)
-  muon_momentum_kernel<<<dim3((unsigned)p.first[p.count]), dim3(256), 0, op_stream(c)>>>(p);
-  p.first[0] = 0;
-  for (int k = 0; k < p.count; ++k)
-    p.first[k + 1] = p.first[k] + (p.mat[k].m + kTile - 1) / kTile * ((p.mat[k].n + kTile - 1) / kTile);
-  muon_begin_kernel<<<dim3((unsigned)p.first[p.count]), dim3(256), 0, op_stream(c)>>>(p);
+  int64_t at = 0;
+  for (int k = 0; k < p.count; ++k) {
+    Mat &q = p.mat[k];
+    q.first_sum = (int)at;                                 // (one partial sum a block)
+    at = put_blocks(q, at, ((int64_t)q.m * q.n + q.chunk - 1) / q.chunk);
+  }
+  muon_momentum_kernel<<<dim3((unsigned)all_blocks(p)), dim3(256), 0, op_stream(c)>>>(p);
+  at = 0;
+  for (int k = 0; k < p.count; ++k) at = put_blocks(p.mat[k], at, (int64_t)((p.mat[k].m + kTile - 1) / kTile) * ((p.mat[k].n + kTile - 1) / kTile));
+  muon_begin_kernel<<<dim3((unsigned)all_blocks(p)), dim3(256), 0, op_stream(c)>>>(p);
   OP_TRY(hipGetLastError());
   for (int s = 0; s < steps; ++s) {
     if (int rc = launch_product<STEP_GRAM>(c, p)) return rc;
@@ -826,19 +890,17 @@ int xrl_muon_step(xrl_ctx *c, const xrl_muon_desc *desc, int32_t n_matrices, con
       int64_t halves = 0;
       for (int k = 0; k < p.count; ++k) {
         Mat &q = p.mat[k] = list[i + k];
-        const int64_t size = (int64_t)q.m * q.n;
         q.ws = halves;
         halves += 3 * x_halves(q.m, q.n) + 2 * x_halves(q.m, q.m);
-        p.first_sum[k + 1] = p.first_sum[k] + (int)((size + q.chunk - 1) / q.chunk);
       }
       most = std::max(most, (size_t)halves * 2);
       for (int step : {STEP_GRAM, STEP_POLY}) {
         const int T = plan_product(p, step, op_compute_units(c));
         bool cut = false;
-        for (int k = 0; k < p.count; ++k) cut = cut || p.parts[k] > 1;
+        for (int k = 0; k < p.count; ++k) cut = cut || p.mat[k].parts > 1;
         if (!cut) continue;
-        counters = std::max(counters, (size_t)p.first[p.count]);
-        floats = std::max(floats, (size_t)p.first[p.count] * T * T);
+        counters = std::max(counters, (size_t)all_blocks(p));
+        floats = std::max(floats, (size_t)all_blocks(p) * T * T);
       }
       groups.push_back(p);
     }
