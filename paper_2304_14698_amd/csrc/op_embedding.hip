@@ -72,6 +72,15 @@ int launch_embed(const xrl_ctx *c, EmbedArgs &a) {
 }
 
 // ---- gradient
+// The columns of a thread: N from `at` on, of which the first `skip` are another thread's too and not stored. (The last thread of a row reads back into its
+// neighbour's columns, a thread behind the row all of them, so that every thread's loads are the same: one that is made in a branch of its own is
+// waited for at that branch's end. dim >= N.)
+template <int N>
+struct Columns {
+  int at, skip;
+  __device__ Columns(int c, int dim) : at(c + N <= dim ? c : dim - N), skip(c - at) {}
+};
+
 // Few ids: a block per place t and slab of columns. It ends at once if the id stands before t; else it adds up all places of the id, wave w those of the
 // w-th eighth of the places from t on, and the eight sums in order. One launch and no workspace.
 constexpr int kFewIds = 1024, kFewWaves = 8;
@@ -94,7 +103,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void embed_few_kernel(const FewArgs
   int before = 0;
   for (int i = threadIdx.x; i < t; i += kFewWaves * 64) before |= a.ids[i] == id;
   if (__syncthreads_or(before)) return;
-  const int c = ((int)blockIdx.y * 64 + lane) * VEC, nv = a.dim - c < VEC ? a.dim - c : VEC;
+  const Columns<VEC> c(((int)blockIdx.y * 64 + lane) * VEC, a.dim);
   const int chunks = (a.n - t + 63) / 64, per = (chunks + kFewWaves - 1) / kFewWaves;
   const int i0 = t + w * per * 64, i1 = i0 + per * 64 < a.n ? i0 + per * 64 : a.n;
   float acc[VEC];
@@ -109,12 +118,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void embed_few_kernel(const FewArgs
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
         if (!here) break;
-        const T *p = (const T *)a.dout + (int64_t)(i + __ffsll(here) - 1) * a.dout_stride + c;
+        v[k] = load_piece<T, VEC>((const T *)a.dout + (int64_t)(i + __ffsll(here) - 1) * a.dout_stride + c.at);
         here &= here - 1;
         got = k + 1;
-        if (nv == VEC) v[k] = load_piece<T, VEC>(p);
-        else
-          for (int j = 0; j < VEC; ++j) v[k].v[j] = j < nv ? p[j] : (T)0.f;
       }
 #pragma unroll
       for (int k = 0; k < BATCH; ++k)
@@ -129,13 +135,126 @@ __global__ __launch_bounds__(kFewWaves * 64) void embed_few_kernel(const FewArgs
     for (int j = 0; j < VEC; ++j) part[w - 1][lane][j] = acc[j];
   __syncthreads();
   if (w) return;
-  float *p = a.dtable + (int64_t)id * a.dtable_stride + c;
+  float *p = a.dtable + (int64_t)id * a.dtable_stride + c.at;
 #pragma unroll
   for (int j = 0; j < VEC; ++j) {
 #pragma unroll
     for (int k = 0; k < kFewWaves - 1; ++k) acc[j] += part[k][lane][j];
-    if (j < nv) p[j] += a.scale * acc[j];
+    if (j >= c.skip) p[j] += a.scale * acc[j];
   }
+}
+
+// A small table: no sort. A block takes consecutive places and 64 C columns; each of its four waves adds its quarter of the rows, one after another, into a
+// table of its own in LDS, a lane C columns (so every sum has one order), and the four tables in order are the block's. A second launch adds up the
+// blocks' in order. Ids outside the vocabulary go to a row behind the table. Four rows whose ids differ are added at once, else one waits for the other's
+// 130 clocks through the LDS (its own atomic additions of floats take 12 clocks a lane: 90 us where this takes 12). Two columns a lane up to 24 ids; the
+// more ids the fewer waves the LDS has room for: up to 64 ids and 512 columns one column a lane, beyond the sort. us a call, this / sorted: 77013 x 128 in
+// fp32, 8 ids 16 / 38, 40 18 / 29, 64 23 / 30, 100 26 / 29; 77013 x 1024 in bf16, 8 ids 36 / 60, 24 44 / 55, 40 68 / 55, 100 115 / 55.
+constexpr int kBinIds = 64, kBinWaves = 4, kBinWideIds = 24, kBinDim = 512;
+
+struct BinArgs {
+  const int32_t *ids;
+  const void *dout;
+  float *dtable, *partial;      // partial [blocks][vocab][dim]
+  unsigned *seen;               // [blocks][kBinIds / 32] bits of the ids that a block met
+  int64_t dout_stride, dtable_stride, n;
+  int vocab, dim, per, blocks;  // per: places of a wave, a multiple of 64
+  float scale;
+};
+
+template <typename T, int C>
+__global__ __launch_bounds__(kBinWaves * 64) void embed_bins_kernel(const BinArgs a) {
+  touch_args(a);
+  constexpr int AHEAD = 16;
+  extern __shared__ __align__(16) float bins[];
+  __shared__ unsigned seen[kBinIds / 32];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), table = (a.vocab + 1) * 64 * C;
+  for (int i = threadIdx.x; i < kBinWaves * table; i += kBinWaves * 64) bins[i] = 0.f;
+  if (threadIdx.x < kBinIds / 32) seen[threadIdx.x] = 0;
+  __syncthreads();
+  const Columns<C> c((int)blockIdx.y * 64 * C + lane * C, a.dim);
+  float *mine = bins + w * table + lane;
+  const int64_t r0 = ((int64_t)blockIdx.x * kBinWaves + w) * a.per;
+  for (int64_t r = r0; r < r0 + a.per && r < a.n; r += 64) {
+    int id = r + lane < a.n ? a.ids[r + lane] : -1;
+    if ((unsigned)id >= (unsigned)a.vocab) id = a.vocab;
+    else atomicOr(&seen[id >> 5], 1u << (id & 31));
+    Piece<T, C> v[2][AHEAD];
+    auto request = [&](int h, int q) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int64_t row = r + q + u < a.n ? r + q + u : a.n - 1;      // (behind the end the id is no row's)
+        v[h][u] = load_piece<T, C>((const T *)a.dout + row * a.dout_stride + c.at);
+      }
+    };
+    request(0, 0);
+#pragma unroll
+    for (int q = 0; q < 64; q += AHEAD) {
+      if (r + q >= a.n) break;
+      const int h = q / AHEAD & 1;
+      if (q + AHEAD < 64) request(h ^ 1, q + AHEAD);
+#pragma unroll
+      for (int u = 0; u < AHEAD; u += 4) {
+        int to[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[k] = __builtin_amdgcn_readlane(id, q + u + k) * 64 * C;
+        if (to[0] != to[1] && to[0] != to[2] && to[0] != to[3] && to[1] != to[2] && to[1] != to[3] && to[2] != to[3]) {
+          float x[4][C];                                    // four rows of the table at once
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < C; ++j) x[k][j] = mine[to[k] + j * 64];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < C; ++j) mine[to[k] + j * 64] = x[k][j] + (float)v[h][u + k].v[j];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < C; ++j) mine[to[k] + j * 64] += (float)v[h][u + k].v[j];
+        }
+      }
+    }
+  }
+  __syncthreads();
+  for (int v = w; v < a.vocab; v += kBinWaves) {
+    const float *from = bins + v * 64 * C + lane;
+    float *to = a.partial + ((int64_t)blockIdx.x * a.vocab + v) * a.dim + c.at;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      float sum = from[j * 64];
+#pragma unroll
+      for (int k = 1; k < kBinWaves; ++k) sum += from[k * table + j * 64];
+      if (j >= c.skip) to[j] = sum;
+    }
+  }
+  if (blockIdx.y == 0 && threadIdx.x < kBinIds / 32) a.seen[blockIdx.x * (kBinIds / 32) + threadIdx.x] = seen[threadIdx.x];
+}
+
+// A block per id and 64 columns: sixteen waves a part of the blocks' sums each, and their sums in order.
+__global__ __launch_bounds__(1024) void embed_bins_join_kernel(const BinArgs a) {
+  touch_args(a);
+  __shared__ float part[15][64];
+  const int id = blockIdx.x, lane = threadIdx.x & 63, g = threadIdx.x >> 6, c = (int)blockIdx.y * 64 + lane;
+  bool met = false;
+  for (int b = threadIdx.x; b < a.blocks; b += 1024) met = met || (a.seen[b * (kBinIds / 32) + (id >> 5)] >> (id & 31) & 1);
+  if (!__syncthreads_or(met)) return;
+  const int per = (a.blocks + 15) / 16, b0 = g * per, b1 = b0 + per < a.blocks ? b0 + per : a.blocks;
+  float sum = 0.f;
+  if (c < a.dim)
+    for (int b = b0; b < b1; b += 8) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = b + u < b1 ? a.partial[((int64_t)(b + u) * a.vocab + id) * a.dim + c] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sum += x[u];
+    }
+  if (g) part[g - 1][lane] = sum;
+  __syncthreads();
+  if (g || c >= a.dim) return;
+  for (int k = 0; k < 15; ++k) sum += part[k][lane];
+  a.dtable[(int64_t)id * a.dtable_stride + c] += a.scale * sum;
 }
 
 // More ids: sorted pairs (id, t) by a stable radix sort of up to kDigitBits bits a pass. Ids outside the vocabulary sort behind all others, as
@@ -280,9 +399,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   const int64_t w = (int64_t)blockIdx.x * (256 / a.lanes) + in_block;
   const int64_t i0 = w * kWindow;
   if (i0 >= a.n) return;
-  const int c = ((int)blockIdx.y * a.lanes + lane) * VEC;
-  if (c >= a.dim) return;
-  const int nv = a.dim - c < VEC ? a.dim - c : VEC;     // columns of this thread
+  const Columns<VEC> c(((int)blockIdx.y * a.lanes + lane) * VEC, a.dim);
+  if (c.skip >= VEC) return;
   const unsigned vocab = (unsigned)a.vocab;
   const uint2 *it = a.items + i0;
   // the window's pairs, and the ids around it (behind the last pair: no row's)
@@ -308,11 +426,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
     for (int k = 0; k < BATCH; ++k) {
       const int i = b0 + k;
       if (id[i + 1] >= vocab) continue;
-      const T *p = (const T *)a.dout + (int64_t)at[i] * a.dout_stride + c;
-      if (nv == VEC) v[k] = load_piece<T, VEC, STREAM>(p);
-      else
-        for (int j = 0; j < VEC; ++j) v[k].v[j] = j < nv ? p[j] : (T)0.f;
-      if (id[i + 2] != id[i + 1] && nv == VEC) old[k] = load_piece<float, VEC>(a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c);
+      v[k] = load_piece<T, VEC, STREAM>((const T *)a.dout + (int64_t)at[i] * a.dout_stride + c.at);
+      if (id[i + 2] != id[i + 1]) old[k] = load_piece<float, VEC>(a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c.at);
     }
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
@@ -323,21 +438,17 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
       const bool goes_on = id[i + 2] == id[i + 1];
       if (goes_on && i < kWindow - 1) continue;
       if (head || goes_on) {
-        float *p = a.carry + ((size_t)w * 2 + (head ? 0 : 1)) * a.dim + c;
-        if (nv == VEC) store_piece<float, VEC>(p, acc);
-        else
-          for (int j = 0; j < nv; ++j) p[j] = acc[j];
+        store_piece<float, VEC>(a.carry + ((size_t)w * 2 + (head ? 0 : 1)) * a.dim + c.at, acc);   // (what two threads store is the same)
         if (!head && lane == 0 && blockIdx.y == 0) a.list[atomicAdd(a.listed, 1)] = make_int2((int)w, (int)id[i + 1]);
       } else {
-        float *p = a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c;
-        if (nv == VEC) {
-          float s[VEC];
+        float *p = a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c.at, s[VEC];
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) s[j] = old[k].v[j] + a.scale * acc[j];
-          store_piece<float, VEC, STREAM>(p, s);
-        } else {
-          for (int j = 0; j < nv; ++j) p[j] += a.scale * acc[j];
-        }
+        for (int j = 0; j < VEC; ++j) s[j] = old[k].v[j] + a.scale * acc[j];
+        if (c.skip == 0) store_piece<float, VEC, STREAM>(p, s);
+        else
+#pragma unroll
+          for (int j = 0; j < VEC; ++j)
+            if (j >= c.skip) p[j] = s[j];
       }
       head = false;
 #pragma unroll
@@ -367,48 +478,44 @@ __device__ __forceinline__ Run run_of(const SumArgs &a, int listed, int lane) {
   r.pieces = more + 1;
   return r;
 }
-// Pieces [p0, p1) of a run added up in their order, eight requests at a time: four columns from c on.
-__device__ __forceinline__ void add_pieces(const SumArgs &a, const Run &r, int64_t p0, int64_t p1, int c, int nv, float *sum) {
+// Pieces [p0, p1) of a run added up in their order, eight requests at a time.
+template <int N>
+__device__ __forceinline__ void add_pieces(const SumArgs &a, const Run &r, int64_t p0, int64_t p1, const Columns<N> &c, float *sum) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) sum[j] = 0.f;
-  const float *src = a.carry + (size_t)r.w * 2 * a.dim + c;
+  for (int j = 0; j < N; ++j) sum[j] = 0.f;
+  const float *src = a.carry + (size_t)r.w * 2 * a.dim + c.at;
   for (int64_t k = p0; k < p1; k += 8) {
-    Piece<float, 4> x[8];
+    Piece<float, N> x[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      if (k + u < p1) {
-        const float *p = src + ((size_t)(k + u) * 2 + (k + u == 0)) * a.dim;
-        if (nv == 4) x[u] = load_piece<float, 4>(p);
-        else
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[u].v[j] = j < nv ? p[j] : 0.f;
-      }
+      if (k + u < p1) x[u] = load_piece<float, N>(src + ((size_t)(k + u) * 2 + (k + u == 0)) * a.dim);
 #pragma unroll
     for (int u = 0; u < 8; ++u)
       if (k + u < p1)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] += x[u].v[j];
+        for (int j = 0; j < N; ++j) sum[j] += x[u].v[j];
   }
 }
-__device__ __forceinline__ void add_run(const SumArgs &a, const Run &r, int c, int nv, const float *sum) {
-  float *p = a.dtable + (int64_t)r.id * a.dtable_stride + c;
+template <int N>
+__device__ __forceinline__ void add_run(const SumArgs &a, const Run &r, const Columns<N> &c, const float *sum) {
+  float *p = a.dtable + (int64_t)r.id * a.dtable_stride + c.at;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (j < nv) p[j] += a.scale * sum[j];
+  for (int j = 0; j < N; ++j)
+    if (j >= c.skip) p[j] += a.scale * sum[j];
 }
 
-// The runs that go over windows, 256 columns a block: each wave takes a listed window and adds up the run's pieces if they are few; the runs of many
+// The runs that go over windows, 64 N columns a block: each wave takes a listed window and adds up the run's pieces if they are few; the runs of many
 // pieces are then taken by all waves of the block, a part of the pieces each, and their sums in order. A block for every run leaves most of its waves
 // idle, a wave for every run is long at an id that fills the batch: us of this kernel at 65536 long-tailed ids of 1024 columns, and of the whole
 // call at 131072 times the same id of 128 columns: sixteen waves a run 49 and 113, four 17 and 263, this 19 and 197.
 constexpr int kFewPieces = 32;
+template <int N>
 __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumArgs a) {
   touch_args(a);
-  __shared__ float part[kJoinWaves - 1][256];
+  __shared__ float part[kJoinWaves - 1][64 * N];
   __shared__ int many[kJoinWaves];
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, listed = *a.listed;
-  const int c = (int)blockIdx.y * 256 + lane * 4;
-  const int nv = a.dim - c < 4 ? a.dim - c : 4;
+  const Columns<N> c(((int)blockIdx.y * 64 + lane) * N, a.dim);
   for (int q0 = blockIdx.x; q0 < listed; q0 += gridDim.x * kJoinWaves) {   // neighbours in the list go to different blocks
     bool left = false;
     const int q = q0 + g * (int)gridDim.x;
@@ -416,9 +523,9 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumAr
       const Run r = run_of(a, q, lane);
       left = r.pieces > kFewPieces;
       if (!left) {
-        float sum[4];
-        add_pieces(a, r, 0, r.pieces, c, nv, sum);
-        add_run(a, r, c, nv, sum);
+        float sum[N];
+        add_pieces<N>(a, r, 0, r.pieces, c, sum);
+        add_run<N>(a, r, c, sum);
       }
     }
     if (!__syncthreads_or(left)) continue;
@@ -428,26 +535,46 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumAr
       if (!many[k]) continue;
       const Run r = run_of(a, q0 + k * (int)gridDim.x, lane);
       const int64_t per = (r.pieces + kJoinWaves - 1) / kJoinWaves, p0 = g * per, p1 = p0 + per < r.pieces ? p0 + per : r.pieces;
-      float sum[4];
-      add_pieces(a, r, p0, p1, c, nv, sum);
+      float sum[N];
+      add_pieces<N>(a, r, p0, p1, c, sum);
       if (g)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) part[g - 1][lane * 4 + j] = sum[j];
+        for (int j = 0; j < N; ++j) part[g - 1][lane * N + j] = sum[j];
       __syncthreads();
       if (g == 0) {
         for (int u = 0; u < kJoinWaves - 1; ++u)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sum[j] += part[u][lane * 4 + j];
-        add_run(a, r, c, nv, sum);
+          for (int j = 0; j < N; ++j) sum[j] += part[u][lane * N + j];
+        add_run<N>(a, r, c, sum);
       }
       __syncthreads();
     }
   }
 }
 
-template <typename T>
+template <typename T, int C>
+int launch_embed_bins(xrl_ctx *c, BinArgs &a, const char *who) {
+  const int n_cu = op_compute_units(c), slabs = (a.dim + 64 * C - 1) / (64 * C), lds = kBinWaves * (a.vocab + 1) * 64 * C * 4;
+  static const hipError_t allowed =
+      hipFuncSetAttribute((const void *)embed_bins_kernel<T, C>, hipFuncAttributeMaxDynamicSharedMemorySize, kBinWaves * ((C == 2 ? kBinWideIds : kBinIds) + 1) * 64 * C * 4);
+  if (allowed != hipSuccess) return fail(XRL_ERR_HIP, "%s: %d bytes of LDS: %s", who, lds, hipGetErrorString(allowed));
+  // as many blocks as the LDS lets run at once, of 64 places a wave at least: what they write is then at most half of what they read
+  const int64_t at_once = std::max<int64_t>(1, (int64_t)n_cu * std::min(8, 163840 / (lds + 64)) / slabs);
+  a.per = (int)(std::max<int64_t>(64, (a.n + kBinWaves * at_once - 1) / (kBinWaves * at_once)) + 63) / 64 * 64;
+  a.blocks = (int)((a.n + (int64_t)kBinWaves * a.per - 1) / ((int64_t)kBinWaves * a.per));
+  const size_t o_p = op_align((size_t)a.blocks * (kBinIds / 32) * 4);
+  char *ws = nullptr;
+  if (int rc = op_workspace(c, o_p + (size_t)a.blocks * a.vocab * a.dim * 4, &ws, who)) return rc;
+  a.seen = (unsigned *)ws;
+  a.partial = (float *)(ws + o_p);
+  embed_bins_kernel<T, C><<<dim3((unsigned)a.blocks, (unsigned)slabs), dim3(kBinWaves * 64), lds, op_stream(c)>>>(a);
+  embed_bins_join_kernel<<<dim3((unsigned)a.vocab, (unsigned)((a.dim + 63) / 64)), dim3(1024), 0, op_stream(c)>>>(a);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}
+
+template <typename T, int VEC>
 int launch_embed_few(const xrl_ctx *c, const FewArgs &a) {
-  constexpr int VEC = sizeof(T) == 2 ? 8 : 4;
   embed_few_kernel<T, VEC><<<dim3((unsigned)a.n, (unsigned)((a.dim + 64 * VEC - 1) / (64 * VEC))), dim3(kFewWaves * 64), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
@@ -455,33 +582,34 @@ int launch_embed_few(const xrl_ctx *c, const FewArgs &a) {
 
 // Threads that share a row of the gradient, and pairs of a window.
 void sum_shape(const xrl_ctx *c, int elem, int dim, int64_t n, int *lanes, int *window) {
-  const int vec = 16 / elem, pieces = (dim + vec - 1) / vec;
+  const int vec = dim >= 16 / elem ? 16 / elem : 1, pieces = (dim + vec - 1) / vec;
   *lanes = 1;
   while (*lanes < pieces && *lanes < 256) *lanes *= 2;
   *window = *lanes >= 64 && n / 32 * (*lanes / 64) >= 8 * op_compute_units(c) ? 32 : 16;
 }
 
+template <typename T, int VEC, bool STREAM>
+void launch_sum_kernel(const xrl_ctx *c, const SumArgs &a, dim3 grid) {
+  constexpr int BATCH = 4;
+  if (a.window == 32) embed_sum_kernel<T, VEC, BATCH, true, 32, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else if (a.lanes >= 64) embed_sum_kernel<T, VEC, BATCH, true, 16, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else embed_sum_kernel<T, VEC, BATCH, false, 16, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+}
 template <typename T>
 int launch_embed_sums(const xrl_ctx *c, SumArgs &a) {
-  constexpr int VEC = sizeof(T) == 2 ? 8 : 4, BATCH = 4;
-  const int pieces = (a.dim + VEC - 1) / VEC;
+  constexpr int VEC = 16 / (int)sizeof(T);
   const int64_t windows = (a.n + a.window - 1) / a.window, per = 256 / a.lanes;
+  const int vec = a.dim >= VEC ? VEC : 1, pieces = (a.dim + vec - 1) / vec;
   const dim3 grid((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes));
   // A gradient of more than 64 MB is read, and the table's rows are stored, past the caches: 65536 x 1024 in bf16 117 / 100 us a call; but 77013 x 128 in
   // fp32, 39 MB that the last-level cache may still have, 30 / 33.
   const bool stream = a.n * a.dim * (int64_t)sizeof(T) > (int64_t)64 << 20;
-  if (a.window == 32) {
-    if (stream) embed_sum_kernel<T, VEC, BATCH, true, 32, true><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-    else embed_sum_kernel<T, VEC, BATCH, true, 32, false><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-  } else if (a.lanes >= 64) {
-    if (stream) embed_sum_kernel<T, VEC, BATCH, true, 16, true><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-    else embed_sum_kernel<T, VEC, BATCH, true, 16, false><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-  } else {
-    if (stream) embed_sum_kernel<T, VEC, BATCH, false, 16, true><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-    else embed_sum_kernel<T, VEC, BATCH, false, 16, false><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-  }
-  embed_join_kernel<<<dim3((unsigned)std::min<int64_t>(windows, 2 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256)),
-                      dim3(kJoinWaves * 64), 0, op_stream(c)>>>(a);
+  if (vec == 1) embed_sum_kernel<T, 1, 4, false, 16, false><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else if (stream) launch_sum_kernel<T, VEC, true>(c, a, grid);
+  else launch_sum_kernel<T, VEC, false>(c, a, grid);
+  const dim3 join((unsigned)std::min<int64_t>(windows, 2 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256));
+  if (a.dim >= 4) embed_join_kernel<4><<<join, dim3(kJoinWaves * 64), 0, op_stream(c)>>>(a);
+  else embed_join_kernel<1><<<join, dim3(kJoinWaves * 64), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
@@ -525,7 +653,13 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
     return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
   if (n <= kFewIds) {
     const FewArgs a = {d_ids, d_dout, d_dtable, dout_stride, dtable_stride, (int)n, (int)vocab, (int)dim, scale};
-    return dout_type == XRL_PREC_BF16 ? launch_embed_few<bf16_t>(c, a) : launch_embed_few<float>(c, a);
+    if (dout_type == XRL_PREC_BF16) return dim >= 8 ? launch_embed_few<bf16_t, 8>(c, a) : launch_embed_few<bf16_t, 1>(c, a);
+    return dim >= 4 ? launch_embed_few<float, 4>(c, a) : launch_embed_few<float, 1>(c, a);
+  }
+  if (vocab <= kBinWideIds || (vocab <= kBinIds && dim <= kBinDim)) {
+    BinArgs a = {d_ids, d_dout, d_dtable, nullptr, nullptr, dout_stride, dtable_stride, n, (int)vocab, (int)dim, 0, 0, scale};
+    if (vocab <= kBinWideIds && dim > 1) return dout_type == XRL_PREC_BF16 ? launch_embed_bins<bf16_t, 2>(c, a, who) : launch_embed_bins<float, 2>(c, a, who);
+    return dout_type == XRL_PREC_BF16 ? launch_embed_bins<bf16_t, 1>(c, a, who) : launch_embed_bins<float, 1>(c, a, who);
   }
   int bits = 1;
   while ((vocab >> bits) > 0) ++bits;                   // of the largest key, `vocab`

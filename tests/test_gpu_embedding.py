@@ -195,3 +195,21 @@ def test_nothing_to_do_and_refusals(enc):
         assert lib.xrl_embedding_backward(*args) == xrl.ERR[code]
     torch.cuda.synchronize()
     assert (out == 7).all() and (table == 1).all()
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 3, 23, 24, 25, 40, 63, 64, 65])
+@pytest.mark.parametrize("n,dim,type", [(1025, 1, "fp32"), (1100, 2, "bf16"), (3000, 127, "bf16"), (2500, 128, "fp32"), (40000, 65, "fp32"),
+                                        (9000, 513, "bf16"), (150000, 9, "fp32")])
+def test_gradient_of_small_tables(enc, vocab, n, dim, type):
+    """Tables that fit a wave's LDS, at the sizes where that changes: every id, one id of many, most ids never met, padding."""
+    import torch
+    dt = dict(fp32=torch.float32, bf16=torch.bfloat16)[type]
+    rng = np.random.Generator(np.random.PCG64(vocab * 7 + n))
+    dout = torch.from_numpy(rng.standard_normal((n, dim)).astype(np.float32)).cuda().to(dt)
+    before = torch.from_numpy(rng.standard_normal((vocab, dim)).astype(np.float32)).cuda()
+    for kind in ("even", "one", "pads", "up", "none"):
+        ids = torch.from_numpy(ids_of(rng, n, vocab, kind)).cuda()
+        after = [enc.embedding_backward(dout, ids, before.clone(), scale=0.7) for _ in range(2)]
+        torch.cuda.synchronize()
+        assert torch.equal(after[0], after[1])
+        check_gradient(dout, ids, before, after[0], float(np.float32(0.7)))
