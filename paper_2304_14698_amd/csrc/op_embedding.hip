@@ -82,8 +82,9 @@ struct Columns {
 };
 
 // Few ids: a block per place t and slab of columns. It ends at once if the id stands before t; else it adds up all places of the id, wave w those of the
-// w-th eighth of the places from t on, and the eight sums in order. One launch and no workspace.
-constexpr int kFewIds = 1024, kFewWaves = 8;
+// w-th eighth of the places from t on, and the eight sums in order. One launch and no workspace; the work grows with the square of the ids. us a call, this /
+// sorted: 2048 ids of 50021, 128 columns in fp32 7 / 33, 1024 in bf16 20 / 34, 2048 in fp32 44 / 37 (1024 of these 19 / 35); 2048 times one id 21 / 24, 34 / 25.
+constexpr int kFewIds = 1024, kFewSlabIds = 2048, kFewWaves = 8;   // however many slabs, and of one or two
 
 struct FewArgs {
   const int32_t *ids;
@@ -651,7 +652,8 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   if (!d_ids || !d_dout || !d_dtable) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
   if ((uintptr_t)d_dout % (dout_type == XRL_PREC_BF16 ? 2 : 4) || (uintptr_t)d_dtable % 4 || (uintptr_t)d_ids % 4)
     return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
-  if (n <= kFewIds) {
+  const int64_t slabs = (dim * (dout_type == XRL_PREC_BF16 ? 2 : 4) + 1023) / 1024;
+  if (n <= (slabs <= 2 ? kFewSlabIds : kFewIds)) {
     const FewArgs a = {d_ids, d_dout, d_dtable, dout_stride, dtable_stride, (int)n, (int)vocab, (int)dim, scale};
     if (dout_type == XRL_PREC_BF16) return dim >= 8 ? launch_embed_few<bf16_t, 8>(c, a) : launch_embed_few<bf16_t, 1>(c, a);
     return dim >= 4 ? launch_embed_few<float, 4>(c, a) : launch_embed_few<float, 1>(c, a);
