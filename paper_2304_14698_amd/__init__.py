@@ -289,6 +289,8 @@ class Encoder:
         if w.size != self.n_weights:
             raise ValueError(f"weights has {w.size} entries, the model needs {self.n_weights}")
         self.stream = torch.cuda.current_stream() if stream is None else stream
+        self._raw_stream, self._device = self.stream.cuda_stream, self.stream.device
+        self._types = {torch.float32: 0, torch.bfloat16: 1}
         self.handle = C.c_void_p()
         _check(self.lib.xrl_create(C.byref(model_desc(model)), w.ctypes.data,
                                    C.c_void_p(self.stream.cuda_stream), C.byref(self.handle)))
@@ -392,27 +394,28 @@ class Encoder:
     def _made(self, *specs):
         t = self.torch
         # (the stream's handle: an object of it takes 3 us to make, the call to the library 4)
-        if t._C._cuda_getCurrentRawStream(self.stream.device_index) == self.stream.cuda_stream:
-            return [t.empty(shape, dtype=dtype, device="cuda") for shape, dtype in specs]
+        if t._C._cuda_getCurrentRawStream(self._device.index) == self._raw_stream:
+            return [t.empty(shape, dtype=dtype, device=self._device) for shape, dtype in specs]
         with t.cuda.stream(self.stream):
-            return [t.empty(shape, dtype=dtype, device="cuda") for shape, dtype in specs]
+            return [t.empty(shape, dtype=dtype, device=self._device) for shape, dtype in specs]
 
     def _type(self, x, name):
-        t = self.torch
-        if x.dtype == t.float32:
-            return 0
-        if x.dtype == t.bfloat16:
-            return 1
-        raise ValueError(f"{name}: {x.dtype}, float32 or bfloat16 is needed")
+        kind = self._types.get(x.dtype)
+        if kind is None:
+            raise ValueError(f"{name}: {x.dtype}, float32 or bfloat16 is needed")
+        return kind
 
     @staticmethod
     def _rows(x, name, shape=None):
         """Elements from row to row of a matrix on the GPU whose rows are contiguous."""
-        if not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-            raise ValueError(f"{name}: a matrix on the GPU with contiguous rows is needed")
-        if shape is not None and tuple(x.shape) != tuple(shape):
-            raise ValueError(f"{name}: shape {tuple(x.shape)}, {tuple(shape)} is needed")
-        return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], x.stride(0))
+        if x.dim() != 2 or not x.is_cuda:
+            raise ValueError(f"{name}: a matrix on the GPU is needed")
+        (rows, cols), (stride, step) = x.shape, x.stride()
+        if cols > 1 and step != 1:
+            raise ValueError(f"{name}: contiguous rows are needed")
+        if shape is not None and (rows, cols) != tuple(shape):
+            raise ValueError(f"{name}: shape {(rows, cols)}, {tuple(shape)} is needed")
+        return stride if rows > 1 else max(cols, stride)
 
     @staticmethod
     def _flat(x, name, dtype, n):
@@ -426,14 +429,17 @@ class Encoder:
     def embedding(self, table, ids, scale=1.0, dtype=None, out=None):
         """[n, dim] rows scale * table[ids], zeros for ids outside the table; ids int32, out of `dtype` (the table's)."""
         t = self.torch
-        stride, n = self._rows(table, "table"), ids.numel()
+        stride, (vocab, dim), n = self._rows(table, "table"), table.shape, ids.numel()
         if out is None:
-            out, = self._made(((n, table.shape[1]), dtype or table.dtype))
-        elif dtype is not None and out.dtype != dtype:
-            raise ValueError(f"out: {out.dtype}, {dtype} is asked for")
-        _check(self.lib.xrl_embedding(self.handle, table.data_ptr(), self._type(table, "table"), stride, table.shape[0],
-                                      table.shape[1], self._flat(ids, "ids", t.int32, n), n, scale, out.data_ptr(),
-                                      self._type(out, "out"), self._rows(out, "out", (n, table.shape[1]))))
+            out, = self._made(((n, dim), dtype or table.dtype))
+            ostride = dim
+        else:
+            if dtype is not None and out.dtype != dtype:
+                raise ValueError(f"out: {out.dtype}, {dtype} is asked for")
+            ostride = self._rows(out, "out", (n, dim))
+        _check(self.lib.xrl_embedding(self.handle, table.data_ptr(), self._type(table, "table"), stride, vocab, dim,
+                                      self._flat(ids, "ids", t.int32, n), n, scale, out.data_ptr(), self._type(out, "out"),
+                                      ostride))
         return out
 
     def embedding_backward(self, dout, ids, dtable, scale=1.0):
@@ -507,15 +513,18 @@ class Encoder:
         n = d.n_rows
         if out is None:
             out, = self._made((logits.shape, logits.dtype))
-        if out.dtype != logits.dtype:
+            stride = d.n_cols
+        elif out.dtype != logits.dtype:
             raise ValueError(f"out: {out.dtype}, {logits.dtype} is needed")
-        if row_ptr is not None:
+        elif row_ptr is not None:
             self._flat(out, "out", logits.dtype, d.n_cols)
+            stride = 0
+        else:
+            stride = self._rows(out, "out", logits.shape)
         _check(self.lib.xrl_token_logp_backward(
             self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), self._flat(forward["entropy"], "entropy", f, n),
             self._flat(forward["stats"], "stats", f, 2 * n), self._flat(dlogp, "dlogp", f, n),
-            self._flat(dentropy, "dentropy", f, n), out.data_ptr(),
-            0 if row_ptr is not None else self._rows(out, "out", logits.shape)))
+            self._flat(dentropy, "dentropy", f, n), out.data_ptr(), stride))
         return out
 
     def muon_step(self, weights, grads, momentum, matrices, lr, beta=0.95, nesterov=True, weight_decay=0.0, steps=5,
