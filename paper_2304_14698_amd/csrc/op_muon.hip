@@ -161,8 +161,9 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
     const int a = wave_of(t) + u * 4, b = lane, i = ti * kTile + (q.t ? b : a), j = tj * kTile + (q.t ? a : b);
     const bool in = i < q.m && j < q.n;
     const int64_t at = q.offset + (q.t ? (int64_t)j * ld + i : (int64_t)i * ld + j);
-    m[u] = in ? p.mom[at] : 0.f;
-    g[u] = in && p.nesterov ? p.g[at] : 0.f;
+    m[u] = p.mom[in ? at : q.offset];
+    g[u] = p.g[in ? at : q.offset];
+    if (!in) m[u] = g[u] = 0.f;
   }
   double sum = 0.;
   const int n_sums = (int)(((int64_t)q.m * q.n + q.chunk - 1) / q.chunk);
@@ -251,7 +252,7 @@ __device__ __forceinline__ void old_weights(const MuonArgs &p, const Mat &q, int
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int64_t at = weight_at(q, ib, jb, r);
-    old[r] = at >= 0 ? p.w[q.offset + at] : 0.f;
+    old[r] = p.w[q.offset + (at >= 0 ? at : 0)];
   }
 }
 
@@ -510,10 +511,31 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 // ---- matrices of at most 64 x 512: a whole step of one matrix in one block, nothing but the vectors' entries read and written.
 // Wave w keeps columns 32 w .. 32 w + 31 of X in registers, as the products leave them: x[b][r] is row 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of column
 // 32 w + lane % 32, times 2^12, in fp32. For A = X X^T the waves lay X down in LDS in fragment order (turned round on the way) and share out the four
-// 32 x 32 blocks of A, a quarter of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
-constexpr int kSmallRows = 64, kSmallCols = 512, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
-constexpr int kSmallX = kSmallWaves * 8192, kSmallLds = kSmallX + 2 * 16384;   // X, and the quarters of A after it; A; B
+// 32 x 32 blocks of A, a part of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
+// Bound by latency: 64 x 256 takes about 3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 5 us besides. All of the
+// vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half of the rows behind the other's stores,
+// these were 12 us.
+constexpr int kSmallRows = 64;
+__host__ __device__ constexpr int small_lds(int waves) { return waves * 8192 + 2 * 16384; }   // X, and the parts of A after it; A; B
+constexpr int kTurn = 36;              // floats of a row on its way: 16-byte pieces of 8 rows lie in different banks
 
+// 16 floats of a lane, its own row of 32 columns, in the order of columns kb 16 + 8 (lane / 32) ..: turned round from 32 x 32 of a product
+__device__ __forceinline__ void turn_round(float (*turn)[kTurn], const float *x, int g, int jl, float (*y)[8]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = x[r];
+  __builtin_amdgcn_wave_barrier();
+  __threadfence_block();
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f32x4 v = *(const f32x4 *)&turn[jl][kb * 16 + g * 8 + 4 * u];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[kb][4 * u + e] = v[e];
+    }
+  __threadfence_block();
+  __builtin_amdgcn_wave_barrier();
+}
 // Four rows of one column, as a lane has them in a product, into a fragment-ordered 64 x 64 matrix: rows along the summed dimension.
 __device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, int lane, const float *v) {
   f16x4 hi, lo;
@@ -523,86 +545,85 @@ __device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, in
   *(f16x4 *)(o + 512) = lo;
 }
 
-__global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArgs p, int steps) {
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p, int steps) {
+  constexpr int PARTS = WAVES / 4;                         // of the sums of a block of A
+  constexpr bool EARLY = WAVES == 8;                       // (sixteen waves have 128 registers each)
   extern __shared__ __align__(16) char lds[];
   const Mat q = matrix_of(p, blockIdx.x);
   const int m = q.m, n = q.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, jl = lane & 31;
   const int j = wave * 32 + jl, used = (n + 31) / 32;     // waves that have columns
-  _Float16 *X = (_Float16 *)lds, *A = (_Float16 *)(lds + kSmallX), *B = A + 8192;
-  float *quarters = (float *)lds;
+  _Float16 *X = (_Float16 *)lds, *A = (_Float16 *)(lds + WAVES * 8192), *B = A + 8192;
+  f32x4 *parts = (f32x4 *)lds;
+  float (*turn)[kTurn] = (float (*)[kTurn])(lds + wave * 8192);
   float *w = p.w + q.offset, *mom = p.mom + q.offset;
   const float *grad = p.g + q.offset;
   // entry (b, r) of a lane in the vector: lanes along its rows, which for a matrix that is taken transposed is another order than x's
-  float (*turn)[33] = (float (*)[33])(lds + wave * 8192);
   auto at = [&](int b, int r) {
     const int i = 32 * b + (q.t ? jl : acc_row(r, g)), c = q.t ? wave * 32 + 2 * r + g : j;
     return i < m && c < n ? (q.t ? c * m + i : i * n + c) : -1;
   };
-  // M = mu M + G, U and |U|
-  float x[2][16];
-  double sum = 0.;
+  // M = mu M + G, U and |U|. (Requests for entries that are not there go to the first one: a request in a branch of its own is waited for there.)
+  float x[2][16], old[2][16];
+  {
+    float gi[2][16], mi[2][16];
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    float gi[16], mi[16];
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int k = at(b, r);
-      gi[r] = k >= 0 ? grad[k] : 0.f;
-      mi[r] = k >= 0 ? mom[k] : 0.f;
-    }
+      for (int r = 0; r < 16; ++r) {
+        const int k = at(b, r), from = k >= 0 ? k : 0;
+        gi[b][r] = grad[from];
+        mi[b][r] = mom[from];
+        if (EARLY) old[b][r] = w[from];
+      }
+    double sum = 0.;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int k = at(b, r);
-      const float mr = p.mu * mi[r] + gi[r];
-      if (k >= 0) mom[k] = mr;
-      const float u = p.nesterov ? gi[r] + p.mu * mr : mr;
-      x[b][r] = u;
-      sum += (double)u * (double)u;
-    }
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int k = at(b, r);
+        const float mr = p.mu * mi[b][r] + gi[b][r], u = p.nesterov ? gi[b][r] + p.mu * mr : mr;
+        if (k >= 0) mom[k] = mr;
+        x[b][r] = k >= 0 ? u : 0.f;
+        sum += (double)x[b][r] * (double)x[b][r];
+      }
+    for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
+    double *sums = (double *)lds;
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.;
+    for (int k = 0; k < WAVES; ++k) sum += sums[k];
+    const float inv = (float)(1. / (sqrt(sum) + 1e-7));
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = x[b][r] * inv * kUp;
+    __syncthreads();
   }
-  for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
-  double *sums = (double *)lds;
-  if (lane == 0) sums[wave] = sum;
-  __syncthreads();
-  sum = 0.;
-  for (int k = 0; k < kSmallWaves; ++k) sum += sums[k];
-  const float inv = (float)(1. / (sqrt(sum) + 1e-7));
+  // 32 x 32 between the vector's order of a transposed matrix and x's, in place; the other way round `back`
+  auto reorder = [&](float *v, bool back) {
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+    for (int r = 0; r < 16; ++r) turn[back ? acc_row(r, g) : jl][back ? jl : 2 * r + g] = v[r];
+    __builtin_amdgcn_wave_barrier();
+    __threadfence_block();
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[b][r] = x[b][r] * inv * kUp;
-  __syncthreads();
+    for (int r = 0; r < 16; ++r) v[r] = turn[back ? jl : acc_row(r, g)][back ? 2 * r + g : jl];
+    __threadfence_block();
+    __builtin_amdgcn_wave_barrier();
+  };
   if (q.t)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) turn[jl][2 * r + g] = x[b][r];
-      __builtin_amdgcn_wave_barrier();
-      __threadfence_block();
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[b][r] = turn[acc_row(r, g)][jl];
-      __builtin_amdgcn_wave_barrier();
-      __threadfence_block();
-    }
+    for (int b = 0; b < 2; ++b) reorder(x[b], false);
+  const int ib = wave / (2 * PARTS), jb = wave / PARTS % 2, part = wave % PARTS;   // the block of A, and part of its sums, that the wave takes
   for (int step = 0; step < steps; ++step) {
-    // X in fragment order, rows along the columns: turned round 32 x 32 at a time in the wave's own 8 KB
     if (wave < used) {
       f16x8 hi[2][2], lo[2][2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
+        float y[2][8];
+        turn_round(turn, x[b], g, jl, y);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = x[b][r];
-        __builtin_amdgcn_wave_barrier();
-        __threadfence_block();
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = turn[jl][kb * 16 + g * 8 + e];
-          split<8>(y, hi[b][kb], lo[b][kb]);
-        }
-        __builtin_amdgcn_wave_barrier();
-        __threadfence_block();
+        for (int kb = 0; kb < 2; ++kb) split<8>(y[kb], hi[b][kb], lo[b][kb]);
       }
       // [wave][kb][row block][hi, lo]
 #pragma unroll
@@ -615,12 +636,10 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
         }
     }
     __syncthreads();
-    // A: wave 4 t + s the s-th quarter of the sum of block t
-    const int ib = wave >> 3, jb = (wave >> 2) & 1, quarter = wave & 3;
     f32x16 acc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-    const int kbs = 2 * used, per = (kbs + 3) / 4, k0 = quarter * per, k1 = k0 + per < kbs ? k0 + per : kbs;
+    const int kbs = 2 * used, per = (kbs + PARTS - 1) / PARTS, k0 = part * per, k1 = k0 + per < kbs ? k0 + per : kbs;
     for (int kb = k0; kb < k1; ++kb) {
       const _Float16 *a = X + (kb * 2 + ib) * 1024 + lane * 8, *b = X + (kb * 2 + jb) * 1024 + lane * 8;
       const f16x8 ah = *(const f16x8 *)a, al = *(const f16x8 *)(a + 512), bh = *(const f16x8 *)b, bl = *(const f16x8 *)(b + 512);
@@ -628,18 +647,19 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
       acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc, 0, 0, 0);
       acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
     }
-    __syncthreads();                                       // (the quarters take X's place)
+    __syncthreads();                                       // (the parts take X's place)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) quarters[(wave * 16 + r) * 64 + lane] = acc[r];
+    for (int s = 0; s < 4; ++s) parts[(wave * 4 + s) * 64 + lane] = f32x4{acc[4 * s], acc[4 * s + 1], acc[4 * s + 2], acc[4 * s + 3]};
     __syncthreads();
-    {
-      float v[4];                                          // the same waves: four rows each of the sums of the four quarters
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float *o = quarters + ((wave & ~3) * 16 + quarter * 4 + e) * 64 + lane;
-        v[e] = (((o[0] + o[1024]) + o[2048]) + o[3072]) * kDown;
-      }
-      put_four(A, ib, jb, quarter, lane, v);
+    for (int s = part * 4 / PARTS; s < (part + 1) * 4 / PARTS; ++s) {   // the same waves: some rows each of the sums of all parts
+      f32x4 sum = parts[((wave - part) * 4 + s) * 64 + lane];
+#pragma unroll
+      for (int k = 1; k < PARTS; ++k) sum += parts[((wave - part + k) * 4 + s) * 64 + lane];
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = sum[e] * kDown;
+      put_four(A, ib, jb, s, lane, v);
     }
     __syncthreads();
     if (wave < 4) {                                        // B = a I + b A + c A A, a block a wave
@@ -672,8 +692,7 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
       for (int kb = 0; kb < 4; ++kb) {
         // rows 16 kb .. 16 kb + 15 of the column lie in registers 8 (kb % 2) .. of the lane (rows 0-3 and 8-11) and of its
         // partner in the other half (4-7, 12-15); the operand wants rows 0-7 in the lower half's lane and 8-15 in the upper's
-        typedef unsigned u32x4v __attribute__((ext_vector_type(4)));
-        u32x4v h, l, ph, pl;
+        u32x4 h, l, ph, pl;
         split<8>(x[kb >> 1] + 8 * (kb & 1), h, l);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -701,31 +720,24 @@ __global__ __launch_bounds__(kSmallThreads) void muon_small_kernel(const MuonArg
         for (int r = 0; r < 16; ++r) x[b][r] = acc[r] * kDown;
       }
     }
-    __syncthreads();                                       // (B and the quarters are read no more)
+    __syncthreads();                                       // (B and the parts are read no more)
   }
   const float step = p.step * sqrtf((float)n) * kDown;
+  if (!EARLY)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int k = at(b, r);
+        old[b][r] = w[k >= 0 ? k : 0];
+      }
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    if (q.t) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) turn[acc_row(r, g)][jl] = x[b][r];
-      __builtin_amdgcn_wave_barrier();
-      __threadfence_block();
-#pragma unroll
-      for (int r = 0; r < 16; ++r) x[b][r] = turn[jl][2 * r + g];
-      __builtin_amdgcn_wave_barrier();
-      __threadfence_block();
-    }
-    float old[16];
+    if (q.t) reorder(x[b], true);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int k = at(b, r);
-      old[r] = k >= 0 ? w[k] : 0.f;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int k = at(b, r);
-      if (k >= 0) w[k] = p.decay * old[r] - step * x[b][r];
+      if (k >= 0) w[k] = p.decay * old[b][r] - step * x[b][r];
     }
   }
 }
@@ -797,17 +809,25 @@ int launch_product(const xrl_ctx *c, MuonArgs &p) {
   return XRL_OK;
 }
 
+template <int WAVES>
+int launch_small(const xrl_ctx *c, MuonArgs &p, int steps) {
+  static const hipError_t allowed =
+      hipFuncSetAttribute((const void *)muon_small_kernel<WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, small_lds(WAVES));
+  if (allowed != hipSuccess) return fail(XRL_ERR_HIP, "xrl_muon_step: %d bytes of LDS: %s", small_lds(WAVES), hipGetErrorString(allowed));
+  for (int k = 0; k < p.count; ++k) put_blocks(p.mat[k], k, 1);
+  muon_small_kernel<WAVES><<<dim3((unsigned)p.count), dim3(WAVES * 64), small_lds(WAVES), op_stream(c)>>>(p, steps);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}
+
 int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
-  bool small = true;
-  for (int k = 0; k < p.count; ++k) small = small && p.mat[k].m <= kSmallRows && p.mat[k].n <= kSmallCols;
-  if (small) {
-    static const hipError_t allowed = hipFuncSetAttribute((const void *)muon_small_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kSmallLds);
-    if (allowed != hipSuccess) return fail(XRL_ERR_HIP, "xrl_muon_step: %d bytes of LDS: %s", kSmallLds, hipGetErrorString(allowed));
-    for (int k = 0; k < p.count; ++k) put_blocks(p.mat[k], k, 1);
-    muon_small_kernel<<<dim3((unsigned)p.count), dim3(kSmallThreads), kSmallLds, op_stream(c)>>>(p, steps);
-    OP_TRY(hipGetLastError());
-    return XRL_OK;
+  int rows = 0, cols = 0;
+  for (int k = 0; k < p.count; ++k) {
+    rows = std::max(rows, p.mat[k].m);
+    cols = std::max(cols, p.mat[k].n);
   }
+  if (rows <= kSmallRows && cols <= 256) return launch_small<8>(c, p, steps);
+  if (rows <= kSmallRows && cols <= 512) return launch_small<16>(c, p, steps);
   int64_t at = 0;
   for (int k = 0; k < p.count; ++k) {
     Mat &q = p.mat[k];
