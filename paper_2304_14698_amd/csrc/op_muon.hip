@@ -333,15 +333,6 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
   __builtin_amdgcn_wave_barrier();
 }
 
-template <int NB>
-__device__ __forceinline__ void zero(f32x16 (*acc)[NB]) {
-#pragma unroll
-  for (int a = 0; a < NB; ++a)
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-}
 // One of the three products of the halves of two factors, 32 x 32 x 16, into NB x NB blocks.
 template <int NB>
 __device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *p, const f16x8 *q) {
@@ -387,12 +378,12 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
   float old[16];                                           // (of one block: requested now, needed at the end)
   if (STEP == STEP_LAST && NB == 1) old_weights(p, d.q, d.ti * 2 + wi, d.tj * 2 + wj, old);
   f32x16 acc[NB][NB];
-  zero<NB>(acc);
-  f32x16 other[2][NB][NB];                                 // NB == 1: sums of their own for two of the three products of a pair of halves,
-  if (NB == 1) {                                           // or each would wait for the one before
-    zero<NB>(other[0]);
-    zero<NB>(other[1]);
-  }
+#pragma unroll
+  for (int a = 0; a < NB; ++a)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
   // this block's part of the sums (kbs is a multiple of four)
   const int per = (d.kbs / KB + d.parts - 1) / d.parts, first = d.part * per, stages = first + per < d.kbs / KB ? per : d.kbs / KB - first;
 #pragma unroll
@@ -410,8 +401,8 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     }
   };
   auto multiply = [&](const Fragments &f) {
-    add_products<NB>(NB == 1 ? other[0] : acc, f.ph, f.ql);
-    add_products<NB>(NB == 1 ? other[1] : acc, f.pl, f.qh);
+    add_products<NB>(acc, f.ph, f.ql);
+    add_products<NB>(acc, f.pl, f.qh);
     add_products<NB>(acc, f.ph, f.qh);
   };
   // A stage is there: this wave's part (loads arrive in order; `behind` stages behind it may be on their way still), and behind the barrier all of it;
@@ -455,9 +446,6 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
       buffer ^= 1;
     }
   }
-  if (NB == 1)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[0][0][r] += other[0][0][0][r] + other[1][0][0][r];
   if (d.parts > 1) {
     // The part is laid down, past the L2 that other XCDs do not see; the block that comes last adds up all of them in order.
     constexpr int kTileFloats = T * T;
