@@ -369,7 +369,7 @@ typedef struct xrl_logits_desc {
  *   logp = x[id] - ln sum exp x,  entropy = -sum p ln p,  top_ids / top_logp [n_rows, top_k] = the entries of the largest logits in
  *   falling order, the lowest index first among equals, and their log-probabilities.
  * d_ids [n_rows] (NULL: none is given, and d_logp may be NULL): index inside the row. A negative id is no token: logp 0. An id behind the row's
- * end, or of an entry that may not be chosen: -inf. Alternatives that a row does not have are -1 and -inf. A row with
+ * end, or of an entry that may not be chosen: -inf, and only then (a logp below fp32's lowest value is that value). Alternatives that a row does not have are -1 and -inf. A row with
  * nothing to choose has logp -inf and entropy 0. A NaN or +inf that may be chosen makes the row's logp, entropy and top_logp NaN.
  * d_stats [n_rows, 2] (or NULL): the largest logit and ln sum exp(x - largest), for the backward call. top_k: 0 (the two arrays
  * may be NULL) to 64. Errors: NULL, SHAPE, UNSUPPORTED (type, top_k), VALUE (temperature), OOM, HIP. */
@@ -378,13 +378,13 @@ int xrl_token_logp(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d
 
 /* xrl_token_logp_backward: writes dJ/dlogits (type and layout of the logits, rows dlogits_stride apart; it may be the logits' own
  * memory at their own stride) for dJ/dlogp = d_dlogp [n_rows] and dJ/dentropy = d_dentropy [n_rows] (NULL: zeros), from the logits and what
- * xrl_token_logp wrote of them (d_stats and d_entropy; the same ids, mask and temperature):
+ * xrl_token_logp wrote of them (d_logp if there are ids, d_stats and d_entropy; the same ids, mask and temperature):
  *   dlogits_j = (dlogp ([j = id] - p_j) - dentropy p_j (ln p_j + entropy)) / temperature.
  * Exactly 0 at entries that may not be chosen. A row whose logp is 0 or -inf by the rules above takes nothing from d_dlogp.
  * Errors: as above. */
-int xrl_token_logp_backward(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_entropy,
-                            const float *d_stats, const float *d_dlogp, const float *d_dentropy, void *d_dlogits,
-                            int64_t dlogits_stride);
+int xrl_token_logp_backward(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_logp,
+                            const float *d_entropy, const float *d_stats, const float *d_dlogp, const float *d_dentropy,
+                            void *d_dlogits, int64_t dlogits_stride);
 
 /* A matrix inside a flat vector of weights, row-major (what xrl_weight_tensor says of a tensor with cols > 0). */
 typedef struct xrl_matrix {

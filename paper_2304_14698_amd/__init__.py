@@ -122,7 +122,7 @@ def load_library():
     lib.xrl_embedding.argtypes = [vp, vp, i32, i64, i64, i64, vp, i64, C.c_float, vp, i32, i64]
     lib.xrl_embedding_backward.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, C.c_float, vp, i64]
     lib.xrl_token_logp.argtypes = [vp, C.POINTER(LogitsDesc), vp, i32] + [vp] * 5
-    lib.xrl_token_logp_backward.argtypes = [vp, C.POINTER(LogitsDesc)] + [vp] * 6 + [i64]
+    lib.xrl_token_logp_backward.argtypes = [vp, C.POINTER(LogitsDesc)] + [vp] * 7 + [i64]
     lib.xrl_muon_step.argtypes = [vp, C.POINTER(MuonDesc), i32, vp, i64, vp, vp, vp]
     lib.xrl_last_error.restype = C.c_char_p
     lib.xrl_version.restype = C.c_char_p
@@ -522,7 +522,8 @@ class Encoder:
         else:
             stride = self._rows(out, "out", logits.shape)
         _check(self.lib.xrl_token_logp_backward(
-            self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n), self._flat(forward["entropy"], "entropy", f, n),
+            self.handle, C.byref(d), self._flat(ids, "ids", t.int32, n),
+            self._flat(None if ids is None else forward["logp"], "logp", f, n), self._flat(forward["entropy"], "entropy", f, n),
             self._flat(forward["stats"], "stats", f, 2 * n), self._flat(dlogp, "dlogp", f, n),
             self._flat(dentropy, "dentropy", f, n), out.data_ptr(), stride))
         return out

@@ -9,7 +9,7 @@ using namespace xrl;
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-constexpr float kLowest = -3.402823466e38f;        // a maximum that no entry has reached yet: -inf - kLowest is -inf, not NaN
+constexpr float kLowest = -3.402823466e38f;        // also a maximum that no entry has reached yet: -inf - kLowest is -inf, not NaN
 constexpr int kMaxTop = 64;                        // one alternative a lane
 
 struct LogpArgs {
@@ -122,7 +122,7 @@ __device__ __forceinline__ void finish(const LogpArgs &a, int64_t r, const Given
     }
     if (a.logp) {
       const float v = (given.x - u.m) * a.inv_t - ln_s;
-      a.logp[r] = given.none ? 0.f : any && given.x != -INFINITY ? v : -INFINITY;
+      a.logp[r] = given.none ? 0.f : any && given.x != -INFINITY ? (v < kLowest ? kLowest : v) : -INFINITY;
     }
   }
   if (lane < a.top_k) {
@@ -321,13 +321,9 @@ __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs
   const float m = a.stats[2 * r], ln_s = a.stats[2 * r + 1], H = a.entropy[r];
   const float c = a.inv_t * kLog2e, log2_s = ln_s * kLog2e;
   const bool any = !(m == -INFINITY);
-  const int id0 = a.ids ? a.ids[r] : -1;
-  float g = 0.f;
-  int id = -1;
-  if (id0 >= 0 && id0 < row.len && (!row.mask || row.mask[id0]) && !((float)row.x[id0] == -INFINITY)) {
-    id = id0;
-    g = a.dlogp[r];
-  }
+  // whether the given entry may be chosen: from its log-probability, as in place another block may have written over its logit
+  const int given = a.ids ? a.ids[r] : -1, id = given >= 0 && !(a.logp[r] == -INFINITY) ? given : -1;
+  const float g = id >= 0 ? a.dlogp[r] : 0.f;
   const float h = a.dentropy ? a.dentropy[r] : 0.f;
   const float A = -a.inv_t * (g + h * H), B = -a.inv_t * h * kLn2;
   T *out = (T *)a.dlogits + (a.row_ptr ? row.begin : r * a.dstride);
@@ -444,21 +440,21 @@ int xrl_token_logp(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_i
   return XRL_OK;
 }
 
-int xrl_token_logp_backward(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_entropy,
-                            const float *d_stats, const float *d_dlogp, const float *d_dentropy, void *d_dlogits,
-                            int64_t dlogits_stride) {
+int xrl_token_logp_backward(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_logp,
+                            const float *d_entropy, const float *d_stats, const float *d_dlogp, const float *d_dentropy,
+                            void *d_dlogits, int64_t dlogits_stride) {
   const char *who = "xrl_token_logp_backward";
   LogpArgs a;
   if (int rc = check_logits(c, logits, who, a)) return rc;
   if (a.n_rows == 0 || a.n_cols == 0) return XRL_OK;
-  if (!d_entropy || !d_stats || !d_dlogits || (d_ids && !d_dlogp)) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
+  if (!d_entropy || !d_stats || !d_dlogits || (d_ids && (!d_logp || !d_dlogp))) return fail(XRL_ERR_NULL, "%s: NULL device pointer", who);
   if (!a.row_ptr && dlogits_stride < a.n_cols) return fail(XRL_ERR_SHAPE, "%s: dlogits_stride = %lld", who, (long long)dlogits_stride);
   if (d_dlogits == logits->d_logits && !a.row_ptr && dlogits_stride != a.stride)
     return fail(XRL_ERR_SHAPE, "%s: in place, but at another stride", who);
-  if (((uintptr_t)d_ids | (uintptr_t)d_entropy | (uintptr_t)d_stats | (uintptr_t)d_dlogp | (uintptr_t)d_dentropy) % 4 ||
+  if (((uintptr_t)d_ids | (uintptr_t)d_logp | (uintptr_t)d_entropy | (uintptr_t)d_stats | (uintptr_t)d_dlogp | (uintptr_t)d_dentropy) % 4 ||
       (uintptr_t)d_dlogits % (logits->type == XRL_PREC_BF16 ? 2 : 4))
     return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
-  a.ids = d_ids; a.entropy = (float *)d_entropy; a.stats = (float *)d_stats; a.dlogp = d_dlogp; a.dentropy = d_dentropy;
+  a.ids = d_ids; a.logp = (float *)d_logp; a.entropy = (float *)d_entropy; a.stats = (float *)d_stats; a.dlogp = d_dlogp; a.dentropy = d_dentropy;
   a.dlogits = d_dlogits; a.dstride = dlogits_stride;
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, vec = logits->type == XRL_PREC_BF16 ? 8 : 4;
   const int64_t chunks = std::max<int64_t>(1, (cols + 256 * vec * 2 - 1) / (256 * vec * 2));

@@ -267,6 +267,39 @@ def test_rows_apart_at_any_address_and_many_rows(enc):
     assert (d[:-1] == torch.tensor([-0.5, 0.5], device="cuda")).all() and abs(float(d[-1, 0]) + 0.25) < 1e-6
 
 
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(40, 700), (500, 9001), (700, 50000)])
+def test_in_place_where_the_given_entry_may_not_be_chosen(enc, type, rows, cols):
+    """Many blocks write a row, each over logits that the others need: the same bits as into memory of its own."""
+    import torch
+    dt = dict(fp32=torch.float32, bf16=torch.bfloat16)[type]
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, cols, generator=g, device="cuda").to(dt)
+    ids = torch.randint(0, cols, (rows,), generator=g, device="cuda").int()
+    ids[:8] = torch.tensor([0, cols - 1, cols // 2, 1, cols, -1, 5, 6], device="cuda").int()
+    never = torch.arange(rows, device="cuda") % 4 != 3
+    x[never.nonzero()[:, 0], ids.long().clamp(0, cols - 1)[never]] = -INF
+    dlogp = torch.ones(rows, device="cuda")
+    f = enc.token_logp(x, ids)
+    want = enc.token_logp_backward(x, ids, f, dlogp, -0.5 * dlogp)
+    for _ in range(3):
+        y = x.clone()
+        enc.token_logp_backward(y, ids, f, dlogp, -0.5 * dlogp, out=y)
+        assert torch.equal(y, want)
+
+
+def test_a_logp_below_the_lowest_value_keeps_its_gradient(enc):
+    import torch
+    x = torch.zeros(2, 5, device="cuda")
+    x[:, 1] = torch.finfo(torch.float32).min
+    x[1, 2] = -INF
+    ids = torch.tensor([1, 2], device="cuda", dtype=torch.int32)
+    f = enc.token_logp(x, ids, temperature=0.5)
+    d = enc.token_logp_backward(x, ids, f, torch.ones(2, device="cuda"), temperature=0.5)
+    assert f["logp"].tolist() == [torch.finfo(torch.float32).min, -INF]
+    assert d[0, 1] == 2 and (d[0, [0, 2, 3, 4]] + 0.5).abs().max() < 1e-6 and (d[1] == 0).all()
+
+
 @pytest.mark.parametrize("cols", [40, 2500])
 def test_gradient_against_differences(enc, cols):
     """J = sum of a_r logp_r + b_r entropy_r in 64 bits by the formula, moved by +-e in single logits: the error of the difference is of
