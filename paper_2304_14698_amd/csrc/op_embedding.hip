@@ -32,9 +32,9 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a) {
     for (int c = lane * VEC; c < a.dim; c += a.lanes * VEC) {
       if (c + VEC <= a.dim) {
         Piece<TT, VEC> x[ROWS];
+        if (a.vocab > 0)
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-          if (id[r] >= 0) x[r] = load_piece<TT, VEC>((const TT *)a.table + (int64_t)id[r] * a.table_stride + c);
+          for (int r = 0; r < ROWS; ++r) x[r] = load_piece<TT, VEC>((const TT *)a.table + (int64_t)(id[r] >= 0 ? id[r] : 0) * a.table_stride + c);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
           if (r < rows) {
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const EmbedArgs a) {
 
 // A thread takes 16 bytes of the narrower of the two types. Results that are streamed past the caches are taken two rows a thread, whose ids and
 // pieces are then on their way together. us, four sets of inputs in turn, cached one row / cached two / streamed one / streamed two: 65536 x 768 from
-// fp32 to bf16 49 / 45 / 38 / 34, 65536 x 1024 in bf16 52 / 46 / 33 / 29, 131072 x 512 in fp32 88 / 90 / 86 / 80.
+// fp32 to bf16 49 / 45 / 38 / 33, 65536 x 1024 in bf16 52 / 46 / 33 / 29, 131072 x 512 in fp32 88 / 90 / 86 / 76.
 template <typename TT, typename TO>
 int launch_embed(const xrl_ctx *c, EmbedArgs &a) {
   constexpr int VEC = sizeof(TT) + sizeof(TO) == 8 ? 4 : 8;
@@ -83,8 +83,9 @@ struct Columns {
 
 // Few ids: a block per place t and slab of columns. It ends at once if the id stands before t; else it adds up all places of the id, wave w those of the
 // w-th eighth of the places from t on, and the eight sums in order. One launch and no workspace; the work grows with the square of the ids. us a call, this /
-// sorted: 2048 ids of 50021, 128 columns in fp32 7 / 33, 1024 in bf16 20 / 34, 2048 in fp32 44 / 37 (1024 of these 19 / 35); 2048 times one id 21 / 24, 34 / 25.
-constexpr int kFewIds = 1024, kFewSlabIds = 2048, kFewWaves = 8;   // however many slabs, and of one or two
+// ranked and summed: 2048 long-tailed ids, 128 columns in fp32 6 / 15, 1024 in bf16 17 / 20, 2048 in fp32 40 / 18 (1024 of these 19 / 15, 768 14 / 14, 512
+// 10 / 14); 2048 times one id, 128 columns 21 / 15, 1024 39 / 17.
+constexpr int kFewIds = 768, kFewSlabIds = 2048, kFewWaves = 8;   // however many slabs, and of one or two
 
 struct FewArgs {
   const int32_t *ids;
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void embed_few_kernel(const FewArgs
 // blocks' in order. Ids outside the vocabulary go to a row behind the table. Four rows whose ids differ are added at once, else one waits for the other's
 // 130 clocks through the LDS (its own atomic additions of floats take 12 clocks a lane: 90 us where this takes 12). Two columns a lane up to 24 ids; the
 // more ids the fewer waves the LDS has room for: up to 64 ids and 512 columns one column a lane, beyond the sort. us a call, this / sorted: 77013 x 128 in
-// fp32, 8 ids 16 / 38, 40 18 / 29, 64 23 / 30, 100 26 / 29; 77013 x 1024 in bf16, 8 ids 36 / 60, 24 44 / 55, 40 68 / 55, 100 115 / 55.
+// fp32, 8 ids 16 / 31, 40 18 / 26, 64 22 / 26, 100 26 / 23; 77013 x 1024 in bf16, 8 ids 40 / 54, 24 46 / 49, 40 68 / 47, 100 115 / 47.
 constexpr int kBinIds = 64, kBinWaves = 4, kBinWideIds = 24, kBinDim = 512;
 
 struct BinArgs {
@@ -272,10 +273,30 @@ struct SortArgs {
   int vocab, shift, bits, per_wave;   // per_wave: consecutive items of a wave, a multiple of 64
 };
 
-__device__ __forceinline__ uint2 sort_item(const SortArgs &a, int64_t i) {
-  if (!a.ids) return a.in[i];
-  const int id = a.ids[i];
+__device__ __forceinline__ uint2 sort_item(const SortArgs &a, int id, int64_t i) {
   return make_uint2((unsigned)id < (unsigned)a.vocab ? (unsigned)id : (unsigned)a.vocab, (unsigned)i);
+}
+// Items i, i + step, .. (kAhead of them; the first one for those from `end` on): all are on their way together.
+constexpr int kAhead = 4;
+struct Items {
+  uint2 x[kAhead];
+};
+__device__ __forceinline__ Items sort_items(const SortArgs &a, int64_t i, int step, int64_t end) {
+  Items v;
+  int64_t at[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) at[k] = i + k * step < end ? i + k * step : 0;
+  if (a.ids) {
+    int id[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) id[k] = a.ids[at[k]];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v.x[k] = sort_item(a, id[k], at[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v.x[k] = a.in[at[k]];
+  }
+  return v;
 }
 
 __global__ __launch_bounds__(kSortThreads) void embed_sort_count_kernel(const SortArgs a) {
@@ -287,7 +308,12 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_count_kernel(const So
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * kSortWaves * a.per_wave;
   const int64_t i1 = i0 + (int64_t)kSortWaves * a.per_wave < a.n ? i0 + (int64_t)kSortWaves * a.per_wave : a.n;
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads) atomicAdd(&cnt[(sort_item(a, i).x >> a.shift) & (digits - 1)], 1);
+  for (int64_t i = i0 + threadIdx.x; i < i1; i += kAhead * kSortThreads) {
+    const Items v = sort_items(a, i, kSortThreads, i1);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k * kSortThreads < i1) atomicAdd(&cnt[(v.x[k].x >> a.shift) & (digits - 1)], 1);
+  }
   __syncthreads();
   for (int d = threadIdx.x; d < digits; d += kSortThreads) a.hist[(size_t)blockIdx.x * digits + d] = cnt[d];
 }
@@ -302,8 +328,14 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
   for (int d = t; d < digits; d += kSortThreads) total[d] = before[d] = 0;
   __syncthreads();
   const int64_t w0 = ((int64_t)blockIdx.x * kSortWaves + w) * a.per_wave;
-  for (int k = lane; k < a.per_wave; k += 64)
-    if (w0 + k < a.n) atomicAdd(&off[w][(sort_item(a, w0 + k).x >> a.shift) & (digits - 1)], 1);
+  const int64_t w1 = w0 + a.per_wave < a.n ? w0 + a.per_wave : a.n;
+  const Items first = sort_items(a, w0 + lane, 64, w1);
+  for (int64_t i0 = w0; i0 < w1; i0 += kAhead * 64) {
+    const Items v = i0 == w0 ? first : sort_items(a, i0 + lane, 64, w1);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i0 + k * 64 + lane < w1) atomicAdd(&off[w][(v.x[k].x >> a.shift) & (digits - 1)], 1);
+  }
   // of each digit: the items of all blocks, and those of the blocks before; digits x blocks dealt to the threads, eight requests at a time
   {
     const int d = t & (digits - 1), slices = digits < kSortThreads ? kSortThreads / digits : 1;
@@ -350,34 +382,81 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_scatter_kernel(const 
     }
   }
   __syncthreads();
-  volatile int *mine = off[w];
-  for (int k = 0; k < a.per_wave; k += 64) {
-    const int64_t i = w0 + k + lane;
-    const bool in = i < a.n;
-    const uint2 x = in ? sort_item(a, i) : make_uint2(0, 0);
-    const int d = (int)((x.x >> a.shift) & (unsigned)(digits - 1));
-    unsigned long long same = __ballot(in);
-    for (int b = 0; b < a.bits; ++b) {
-      const unsigned long long m = __ballot((d >> b) & 1);
-      same &= (d >> b) & 1 ? m : ~m;
+  int *mine = off[w];
+  for (int64_t i0 = w0; i0 < w1; i0 += kAhead * 64) {
+    const Items v = i0 == w0 ? first : sort_items(a, i0 + lane, 64, w1);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + k * 64 >= w1) break;
+      const bool in = i0 + k * 64 + lane < w1;
+      const int d = (int)((v.x[k].x >> a.shift) & (unsigned)(digits - 1));
+      unsigned long long same = __ballot(in);
+      for (int b = 0; b < a.bits; ++b) {
+        const unsigned long long m = __ballot((d >> b) & 1);
+        same &= (d >> b) & 1 ? m : ~m;
+      }
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      const int place = mine[d] + rank;
+      __builtin_amdgcn_wave_barrier();
+      if (in && rank == 0) mine[d] = place + __popcll(same);
+      __threadfence_block();
+      __builtin_amdgcn_wave_barrier();
+      if (in) a.out[place] = v.x[k];
     }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    const int place = mine[d] + rank;
-    __builtin_amdgcn_wave_barrier();
-    if (in && rank == 0) mine[d] = place + __popcll(same);
-    __threadfence_block();
-    __builtin_amdgcn_wave_barrier();
-    if (in) a.out[place] = x;
   }
+}
+
+// Up to kRankIds ids: the same pairs in one launch, each place from the count of the pairs before it. A block ranks 32 of them against all ids, which it has in
+// LDS; lane l of a half wave has place t0 + l % 32, and the 32 half waves share out the ids, four at a time. Two instructions an id and place, n^2 of them,
+// against the latency of two launches for each of the sort's passes. us a call, ranked / sorted: two passes, 128 columns in fp32, 3000 ids 16 / 29, 8192 21 / 31,
+// 12288 30 / 32, 1024 in bf16, 8192 28 / 38, 12288 40 / 42; one pass (vocab < 1024), 512 in fp32, 8192 24 / 26, 12288 36 / 30.
+constexpr int kRankIds = 12288, kRankIdsOnePass = 8192, kRankPlaces = 32;
+
+__global__ __launch_bounds__(1024) void embed_rank_kernel(const SortArgs a) {
+  touch_args(a);
+  __shared__ __align__(16) int key[kRankIds];
+  __shared__ int rank[kRankPlaces];
+  const int n = (int)a.n, t0 = blockIdx.x * kRankPlaces, own = threadIdx.x & (kRankPlaces - 1), slot = threadIdx.x / kRankPlaces;
+  const int padded = (n + kRankPlaces - 1) / kRankPlaces * kRankPlaces;
+  for (int i0 = threadIdx.x; i0 < padded; i0 += kAhead * 1024) {
+    const Items v = sort_items(a, i0, 1024, n);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * 1024;
+      if (i < padded) key[i] = i < n ? (int)v.x[k].x : 0x7fffffff;
+    }
+  }
+  if (threadIdx.x < kRankPlaces) rank[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.clear = 0;
+  __syncthreads();
+  const int mine = key[t0 + own];
+  int before = 0;
+  auto count = [&](int from, int to, int bound) {          // chunks of four ids
+#pragma unroll 4
+    for (int k = from + slot; k < to; k += 32) {
+      const int4 x = *(const int4 *)&key[4 * k];
+      before += (x.x < bound) + (x.y < bound) + (x.z < bound) + (x.w < bound);
+    }
+  };
+  count(0, t0 / 4, mine < 0x7fffffff ? mine + 1 : mine);   // equal ids that stand before count, those behind do not
+  count(t0 / 4 + kRankPlaces / 4, padded / 4, mine);
+  const int other = key[t0 + slot];                        // of the block's own places each half wave takes one
+  before += other < mine || (other == mine && slot < own);
+  atomicAdd(&rank[own], before);
+  __syncthreads();
+  if (threadIdx.x < kRankPlaces && t0 + (int)threadIdx.x < n) a.out[rank[threadIdx.x]] = make_uint2((unsigned)mine, (unsigned)(t0 + threadIdx.x));
 }
 
 // Sums over runs of equal ids. A group of `lanes` threads takes a window of consecutive sorted pairs, in their order; a batch's rows, and the rows of the
 // table that its runs are added to, are requested together. A run inside the window is added to its row of the table. The piece of a run that began
 // before goes to carry[window][0], that of one that goes on behind it to carry[window][1]; a window that such a run begins in is listed, and
 // embed_join_kernel adds up the run's pieces.
-// Groups that are whole waves keep their pairs in scalar registers; there a window is of 32 pairs from eight waves a compute unit on, else of 16. us of
-// this kernel and the next, 32 / 16: 65536 long-tailed ids of 1024 columns in bf16 52 + 16 / 53 + 19, 77013 ids of 128 columns in fp32 (no whole waves)
-// 18 + 7 / 11 + 9; whole calls of 8192 and 16384 ids of 1024 columns 56 / 47 and 60 / 55.
+// Groups that are whole waves keep their pairs in scalar registers; there a window is of 32 pairs from eight waves a compute unit on, else of 16. us a call,
+// 32 / 16: 65536 long-tailed ids of 1024 columns in bf16 85 / 95, 77013 of 512 in fp32 75 / 80; of 1024 in bf16 8192 36 / 28, 16384 50 / 46.
+// Bound by memory from some 30000 ids of 1024 columns on (the 65536: 58 us of this kernel for the gradient and two passes over the rows it meets,
+// 263 MB), below by latency. All loads of a batch are on their way together: none stands in a branch that also takes its value apart, which would be waited
+// for there (62 us, and 13 more at 8192 ids). Batches of eight rows but for windows of 16 in bf16, whose registers they would double: us, four / eight, the
+// 65536 88 / 85, 12288 of 128 columns in fp32 31 / 30, 12288 of 1024 in bf16 39 / 41.
 constexpr int kJoinWaves = 8;
 
 struct SumArgs {
@@ -391,30 +470,44 @@ struct SumArgs {
   float scale;
 };
 
-template <typename T, int VEC, int BATCH, bool WHOLE, int kWindow, bool STREAM>
+template <typename T, int VEC, bool WHOLE, int kWindow, bool STREAM>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
   touch_args(a);
+  constexpr int BATCH = kWindow == 32 || sizeof(T) == 4 ? 8 : 4;
   const int lane = threadIdx.x & (a.lanes - 1);
   int in_block = threadIdx.x / a.lanes;
   if (WHOLE) in_block = __builtin_amdgcn_readfirstlane(in_block);   // whole waves: their pairs are in scalar registers
   const int64_t w = (int64_t)blockIdx.x * (256 / a.lanes) + in_block;
   const int64_t i0 = w * kWindow;
   if (i0 >= a.n) return;
-  const Columns<VEC> c(((int)blockIdx.y * a.lanes + lane) * VEC, a.dim);
-  if (c.skip >= VEC) return;
   const unsigned vocab = (unsigned)a.vocab;
-  const uint2 *it = a.items + i0;
-  // the window's pairs, and the ids around it (behind the last pair: no row's)
+  // The window's pairs, and the ids around it (in front of the first pair and behind the last: no row's).
   unsigned id[kWindow + 2];
   int at[kWindow];
-  id[0] = i0 > 0 ? it[-1].x : ~0u;
-  if (WHOLE) id[0] = __builtin_amdgcn_readfirstlane(id[0]);
+  auto pair = [&](int i) {
+    const int64_t k = i0 + i - 1;
+    const bool in = k >= 0 && k < a.n;
+    uint2 x = a.items[in ? k : i0];
+    if (!in) x.x = k < 0 ? ~0u : vocab;
+    return x;
+  };
+  if constexpr (WHOLE) {                                 // one a lane
+    const uint2 x = pair((int)(threadIdx.x & 63) < kWindow + 2 ? (int)(threadIdx.x & 63) : 0);
 #pragma unroll
-  for (int i = 0; i < kWindow + 1; ++i) {
-    const uint2 x = i0 + i < a.n ? it[i] : make_uint2(vocab, 0);
-    id[i + 1] = WHOLE ? __builtin_amdgcn_readfirstlane(x.x) : x.x;
-    if (i < kWindow) at[i] = WHOLE ? __builtin_amdgcn_readfirstlane((int)x.y) : (int)x.y;
+    for (int i = 0; i < kWindow + 2; ++i) {
+      id[i] = __builtin_amdgcn_readlane((int)x.x, i);
+      if (i >= 1 && i <= kWindow) at[i - 1] = __builtin_amdgcn_readlane((int)x.y, i);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWindow + 2; ++i) {
+      const uint2 x = pair(i);
+      id[i] = x.x;
+      if (i >= 1 && i <= kWindow) at[i - 1] = (int)x.y;
+    }
   }
+  const Columns<VEC> c(((int)blockIdx.y * a.lanes + lane) * VEC, a.dim);
+  if (c.skip >= VEC || id[1] >= vocab) return;           // (ids that are no row's stand at the end)
   float acc[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
@@ -426,9 +519,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const SumArgs a) {
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
       const int i = b0 + k;
-      if (id[i + 1] >= vocab) continue;
       v[k] = load_piece<T, VEC, STREAM>((const T *)a.dout + (int64_t)at[i] * a.dout_stride + c.at);
-      if (id[i + 2] != id[i + 1]) old[k] = load_piece<float, VEC>(a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c.at);
+      if (id[i + 2] != id[i + 1] && id[i + 1] < vocab) old[k] = load_piece<float, VEC>(a.dtable + (int64_t)id[i + 1] * a.dtable_stride + c.at);
     }
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
@@ -470,12 +562,16 @@ __device__ __forceinline__ Run run_of(const SumArgs &a, int listed, int lane) {
   r.id = (unsigned)x.y;
   // windows behind w that begin with the id: 64 probes at once, each level 64 times as fine
   const int64_t windows = (a.n + a.window - 1) / a.window;
-  int64_t more = 0;
-  for (int64_t s = (int64_t)1 << 18; s; s >>= 6)
-    if (s == 1 || s < windows) {
-      const int64_t k = r.w + more + (lane + 1) * s;
-      more += s * __popcll(__ballot(k < windows && a.items[k < windows ? k * a.window : 0].x == r.id));
-    }
+  auto follow = [&](int64_t from, int64_t s) {
+    const int64_t k = from + (lane + 1) * s;
+    return s * __popcll(__ballot(k < windows && a.items[k < windows ? k * a.window : 0].x == r.id));
+  };
+  int64_t more = follow(r.w, 1);
+  if (more == 64) {                                       // (few are that long)
+    more = 0;
+    for (int64_t s = (int64_t)1 << 18; s; s >>= 6)
+      if (s == 1 || s < windows) more += follow(r.w + more, s);
+  }
   r.pieces = more + 1;
   return r;
 }
@@ -498,17 +594,19 @@ __device__ __forceinline__ void add_pieces(const SumArgs &a, const Run &r, int64
   }
 }
 template <int N>
-__device__ __forceinline__ void add_run(const SumArgs &a, const Run &r, const Columns<N> &c, const float *sum) {
+__device__ __forceinline__ void add_run(const SumArgs &a, const Run &r, const Columns<N> &c, const Piece<float, N> &old, const float *sum) {
   float *p = a.dtable + (int64_t)r.id * a.dtable_stride + c.at;
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (j >= c.skip) p[j] += a.scale * sum[j];
+    if (j >= c.skip) p[j] = old.v[j] + a.scale * sum[j];
 }
 
 // The runs that go over windows, 64 N columns a block: each wave takes a listed window and adds up the run's pieces if they are few; the runs of many
 // pieces are then taken by all waves of the block, a part of the pieces each, and their sums in order. A block for every run leaves most of its waves
 // idle, a wave for every run is long at an id that fills the batch: us of this kernel at 65536 long-tailed ids of 1024 columns, and of the whole
-// call at 131072 times the same id of 128 columns: sixteen waves a run 49 and 113, four 17 and 263, this 19 and 197.
+// call at 131072 times the same id of 128 columns: sixteen waves a run 49 and 113, four 17 and 263, this 19 and 197; since
+// the row of the table is asked for together with the pieces and the nearest 64 windows are looked at first, 17 and 150 (of which this kernel is 112: one
+// compute unit takes in 4 MB).
 constexpr int kFewPieces = 32;
 template <int N>
 __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumArgs a) {
@@ -524,9 +622,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumAr
       const Run r = run_of(a, q, lane);
       left = r.pieces > kFewPieces;
       if (!left) {
+        const Piece<float, N> old = load_piece<float, N>(a.dtable + (int64_t)r.id * a.dtable_stride + c.at);
         float sum[N];
         add_pieces<N>(a, r, 0, r.pieces, c, sum);
-        add_run<N>(a, r, c, sum);
+        add_run<N>(a, r, c, old, sum);
       }
     }
     if (!__syncthreads_or(left)) continue;
@@ -536,6 +635,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumAr
       if (!many[k]) continue;
       const Run r = run_of(a, q0 + k * (int)gridDim.x, lane);
       const int64_t per = (r.pieces + kJoinWaves - 1) / kJoinWaves, p0 = g * per, p1 = p0 + per < r.pieces ? p0 + per : r.pieces;
+      const Piece<float, N> old = load_piece<float, N>(a.dtable + (int64_t)r.id * a.dtable_stride + c.at);
       float sum[N];
       add_pieces<N>(a, r, p0, p1, c, sum);
       if (g)
@@ -546,7 +646,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(const SumAr
         for (int u = 0; u < kJoinWaves - 1; ++u)
 #pragma unroll
           for (int j = 0; j < N; ++j) sum[j] += part[u][lane * N + j];
-        add_run<N>(a, r, c, sum);
+        add_run<N>(a, r, c, old, sum);
       }
       __syncthreads();
     }
@@ -591,10 +691,9 @@ void sum_shape(const xrl_ctx *c, int elem, int dim, int64_t n, int *lanes, int *
 
 template <typename T, int VEC, bool STREAM>
 void launch_sum_kernel(const xrl_ctx *c, const SumArgs &a, dim3 grid) {
-  constexpr int BATCH = 4;
-  if (a.window == 32) embed_sum_kernel<T, VEC, BATCH, true, 32, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-  else if (a.lanes >= 64) embed_sum_kernel<T, VEC, BATCH, true, 16, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-  else embed_sum_kernel<T, VEC, BATCH, false, 16, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  if (a.window == 32) embed_sum_kernel<T, VEC, true, 32, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else if (a.lanes >= 64) embed_sum_kernel<T, VEC, true, 16, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else embed_sum_kernel<T, VEC, false, 16, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
 }
 template <typename T>
 int launch_embed_sums(const xrl_ctx *c, SumArgs &a) {
@@ -602,10 +701,10 @@ int launch_embed_sums(const xrl_ctx *c, SumArgs &a) {
   const int64_t windows = (a.n + a.window - 1) / a.window, per = 256 / a.lanes;
   const int vec = a.dim >= VEC ? VEC : 1, pieces = (a.dim + vec - 1) / vec;
   const dim3 grid((unsigned)((windows + per - 1) / per), (unsigned)((pieces + a.lanes - 1) / a.lanes));
-  // A gradient of more than 64 MB is read, and the table's rows are stored, past the caches: 65536 x 1024 in bf16 117 / 100 us a call; but 77013 x 128 in
-  // fp32, 39 MB that the last-level cache may still have, 30 / 33.
+  // A gradient of more than 64 MB is read, and the table's rows are stored, past the caches: 65536 x 1024 in bf16 107 / 85 us a call; but 77013 x 128 in
+  // fp32, 39 MB that the last-level cache may still have, 53 / 55.
   const bool stream = a.n * a.dim * (int64_t)sizeof(T) > (int64_t)64 << 20;
-  if (vec == 1) embed_sum_kernel<T, 1, 4, false, 16, false><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  if (vec == 1) embed_sum_kernel<T, 1, false, 16, false><<<grid, dim3(256), 0, op_stream(c)>>>(a);
   else if (stream) launch_sum_kernel<T, VEC, true>(c, a, grid);
   else launch_sum_kernel<T, VEC, false>(c, a, grid);
   const dim3 join((unsigned)std::min<int64_t>(windows, 2 * op_compute_units(c)), (unsigned)((a.dim + 255) / 256));
@@ -680,9 +779,15 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   char *ws = nullptr;
   if (int rc = op_workspace(c, o_c + (size_t)windows * 2 * dim * 4, &ws, who)) return rc;
   uint2 *x = (uint2 *)ws, *y = (uint2 *)(ws + o_b);
+  const bool ranked = n <= (passes > 1 ? kRankIds : kRankIdsOnePass);
   s.hist = (int32_t *)(ws + o_h);
   s.clear = s.hist + hist;                               // the list's length
-  for (int p = 0; p < passes; ++p) {
+  if (ranked) {
+    s.ids = d_ids;
+    s.out = x;
+    embed_rank_kernel<<<dim3((unsigned)((n + kRankPlaces - 1) / kRankPlaces)), dim3(1024), 0, op_stream(c)>>>(s);
+  }
+  for (int p = 0; p < passes && !ranked; ++p) {
     s.ids = p == 0 ? d_ids : nullptr;
     s.in = x; s.out = y; s.shift = p * per_pass;
     embed_sort_count_kernel<<<dim3(blocks), dim3(kSortThreads), 0, op_stream(c)>>>(s);

@@ -213,3 +213,22 @@ def test_gradient_of_small_tables(enc, vocab, n, dim, type):
         torch.cuda.synchronize()
         assert torch.equal(after[0], after[1])
         check_gradient(dout, ids, before, after[0], float(np.float32(0.7)))
+
+
+@pytest.mark.parametrize("kind", ["tail", "one", "pads", "none"])
+@pytest.mark.parametrize("vocab", [70, 1023, 1024, 9001])
+@pytest.mark.parametrize("n,dim,type", [(768, 1100, "fp32"), (769, 1100, "fp32"), (2048, 250, "fp32"), (2049, 250, "fp32"), (8191, 66, "bf16"),
+                                        (8192, 130, "fp32"), (8193, 130, "fp32"), (12288, 513, "bf16"), (12289, 515, "bf16"), (16001, 70, "fp32")])
+def test_gradient_where_its_ways_change(enc, n, dim, type, vocab, kind):
+    """Squares of ids, ranks, one and two passes of the sort; rows apart, from an address that is no multiple of 16."""
+    import torch
+    dt = dict(fp32=torch.float32, bf16=torch.bfloat16)[type]
+    rng = np.random.Generator(np.random.PCG64(vocab + n))
+    g = torch.Generator(device="cuda").manual_seed(n + dim)
+    dout = torch.randn(1 + n * (dim + 3), generator=g, device="cuda").to(dt)[1:].view(n, dim + 3)[:, :dim]
+    before = torch.randn(vocab, dim, generator=g, device="cuda")
+    ids = torch.from_numpy(ids_of(rng, n, vocab, kind)).cuda()
+    after = [enc.embedding_backward(dout, ids, before.clone(), scale=-0.7) for _ in range(2)]
+    torch.cuda.synchronize()
+    assert torch.equal(after[0], after[1])
+    check_gradient(dout, ids, before, after[0], float(np.float32(-0.7)))
