@@ -155,11 +155,34 @@ __device__ __forceinline__ Best merge_best(int lists, int k, int lane, GetX get_
   return out;
 }
 
+// bf16 pieces of 16 bytes that lie 2 bytes behind a multiple of 4 take longer than all others, and every second row of an odd length has nothing else: us,
+// 4096 rows of 32003 61.5, of 32002 55. Such a row's pieces are read from the element before on, five words, and shifted (55.4), which leaves every sum
+// its order wherever the row lies; where each entry stands by itself, in the gradient, a row's pieces begin at the element before its first.
+template <typename T>
+__device__ __forceinline__ int lead_of(const T *p, int len) { return sizeof(T) == 2 && len > 0 ? (int)((uintptr_t)p >> 1 & 1) : 0; }
+
+// VEC elements from such a p. (What is read beside them lies in the same words as the first and the last.)
+template <typename T, int VEC>
+__device__ __forceinline__ Piece<T, VEC> load_odd_piece(const T *p) {
+  Piece<T, VEC> x;
+  if constexpr (sizeof(T) == 2) {
+    unsigned u[VEC / 2 + 1], s[VEC / 2];
+    __builtin_memcpy(u, __builtin_assume_aligned(p - 1, 4), VEC * 2);
+    __builtin_memcpy(u + VEC / 2, __builtin_assume_aligned(p - 1 + VEC, 4), 4);
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) s[i] = __builtin_amdgcn_alignbit(u[i + 1], u[i], 16);
+    __builtin_memcpy(&x, s, sizeof(x));
+  } else {
+    x = load_piece<T, VEC>(p);
+  }
+  return x;
+}
+
 // Columns col .. col + VEC - 1 of the row as fp32, -inf where nothing may be chosen and from c1 on.
 template <typename T, int VEC>
-__device__ __forceinline__ void fetch(const Row<T> &row, int col, int c1, float *x) {
+__device__ __forceinline__ void fetch(const Row<T> &row, bool odd, int col, int c1, float *x) {
   if (col + VEC <= c1) {
-    const Piece<T, VEC> p = load_piece<T, VEC>(row.x + col);
+    const Piece<T, VEC> p = odd ? load_odd_piece<T, VEC>(row.x + col) : load_piece<T, VEC>(row.x + col);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j];
     if (row.mask) {
@@ -210,7 +233,11 @@ __device__ __forceinline__ void take_best(float (*x)[VEC], float *mx, int n_piec
 }
 
 // A team of WAVES waves takes one part of one row, 32 entries a lane at a time: their maximum first, then the two sums against the largest so
-// far, then the best of them.
+// far, then the best of them. One pass: what is read stays in registers for all three.
+// Bound by memory for many long rows: 4096 x 32003 in bf16 55 us, 262 MB at 4.7 TB/s; 8192 x 32000 101, 5.2 TB/s. (All pieces of a step requested before any
+// is waited for, or a step ahead, takes 97 to 140 registers in place of 60, and a third of the waves with them: 50 -> 60 and 70 us.) Bound by latency for few:
+// 8 x 128256 in bf16 with the best eight 13 us in two launches, 8 of them without the best; 32 x 65 7. With the best entries 1000 x 8191 in fp32 under a mask
+// 16.5, 2.5 TB/s: a round of the selection takes 0.4 us, all others wait for it.
 template <typename T, int WAVES, bool TOP>
 __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
   touch_args(a);
@@ -221,6 +248,7 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
   const int part = (int)(job % a.parts);
   if (r >= a.n_rows) return;                              // (a whole wave, and with WAVES > 1 the whole block)
   const Row<T> row = row_of<T>(a, r);
+  const bool odd = __builtin_amdgcn_readfirstlane(lead_of(row.x, row.len)) != 0;
   const float c = a.inv_t * kLog2e;
   // part `part`: columns [c0, c1), whole steps of the team
   const int steps = (row.len + STEP - 1) / STEP, per = (steps + a.parts - 1) / a.parts;
@@ -235,7 +263,7 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
     float x[PIECES][VEC], mx[PIECES];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      if (p < n_pieces) fetch<T, VEC>(row, col + p * STEP, c1, x[p]);
+      if (p < n_pieces) fetch<T, VEC>(row, odd, col + p * STEP, c1, x[p]);
     }
     float m = u.m;
 #pragma unroll
@@ -291,7 +319,7 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
   }
 }
 
-// A wave per row: its parts (at most 64), in order.
+// A wave per row: its parts (at most 64), in order. Latency: 4 to 5 us, of which a launch is 2.7. (The lists in LDS first: 0.5 us more.)
 template <typename T>
 __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
   const int64_t r = blockIdx.x;
@@ -312,6 +340,8 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
 }
 
 // dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
+// Each entry by itself, two pieces a thread. Bound by memory: 2048 x 50021 in bf16 66 us for 205 MB read and written, 6.2 TB/s (some of the logits are
+// still in the last-level cache from the forward call); results of more than the L2s hold are stored past the caches.
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T);
@@ -327,11 +357,11 @@ __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs
   const float h = a.dentropy ? a.dentropy[r] : 0.f;
   const float A = -a.inv_t * (g + h * H), B = -a.inv_t * h * kLn2;
   T *out = (T *)a.dlogits + (a.row_ptr ? row.begin : r * a.dstride);
-  for (int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; col < row.len; col += (int64_t)gridDim.x * 256 * VEC) {
-    const int n = row.len - col < VEC ? (int)(row.len - col) : VEC;
+  for (int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC - lead_of(out, row.len); col < row.len; col += (int64_t)gridDim.x * 256 * VEC) {
+    const bool whole = col >= 0 && col + VEC <= row.len;
     float x[VEC], d[VEC];
     bool ok[VEC];
-    if (n == VEC) {
+    if (whole) {
       const Piece<T, VEC> p = load_piece<T, VEC>(row.x + col);
 #pragma unroll
       for (int j = 0; j < VEC; ++j) x[j] = (float)p.v[j];
@@ -344,10 +374,18 @@ __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs
         for (int j = 0; j < VEC; ++j) ok[j] = true;
       }
     } else {
+      T v[VEC];
+      uint8_t k[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        ok[j] = j < n && (!row.mask || row.mask[col + j]);
-        x[j] = j < n ? (float)row.x[col + j] : 0.f;
+        const int64_t at = col + j < 0 ? 0 : col + j < row.len ? col + j : row.len - 1;
+        v[j] = row.x[at];
+        k[j] = row.mask ? row.mask[at] : 1;
+      }
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        ok[j] = k[j] != 0;
+        x[j] = (float)v[j];
       }
     }
 #pragma unroll
@@ -357,11 +395,11 @@ __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs
       if (col + j == id) v += a.inv_t * g;
       d[j] = ok[j] && any && !(x[j] == -INFINITY) ? v : 0.f;
     }
-    if (n == VEC) store_piece<T, VEC, STREAM>(out + col, d);
+    if (whole) store_piece<T, VEC, STREAM>(out + col, d);
     else
 #pragma unroll
       for (int j = 0; j < VEC; ++j)
-        if (j < n) out[col + j] = (T)d[j];
+        if (col + j >= 0 && col + j < row.len) out[col + j] = (T)d[j];
   }
 }
 
