@@ -156,7 +156,7 @@ __device__ __forceinline__ Best merge_best(int lists, int k, int lane, GetX get_
 }
 
 // bf16 pieces of 16 bytes that lie 2 bytes behind a multiple of 4 take longer than all others, and every second row of an odd length has nothing else: us,
-// 4096 rows of 32003 61.5, of 32002 55. Such a row's pieces are read from the element before on, five words, and shifted (55.4), which leaves every sum
+// 4096 rows of 32003 61.5, of 32002 55. Such a row's pieces are read from the element before on, five words, and shifted (then 55.4), which leaves every sum
 // its order wherever the row lies; where each entry stands by itself, in the gradient, a row's pieces begin at the element before its first.
 template <typename T>
 __device__ __forceinline__ int lead_of(const T *p, int len) { return sizeof(T) == 2 && len > 0 ? (int)((uintptr_t)p >> 1 & 1) : 0; }
@@ -234,14 +234,16 @@ __device__ __forceinline__ void take_best(float (*x)[VEC], float *mx, int n_piec
 
 // A team of WAVES waves takes one part of one row, 32 entries a lane at a time: their maximum first, then the two sums against the largest so
 // far, then the best of them. One pass: what is read stays in registers for all three.
-// Bound by memory for many long rows: 4096 x 32003 in bf16 55 us, 262 MB at 4.7 TB/s; 8192 x 32000 101, 5.2 TB/s. (All pieces of a step requested before any
-// is waited for, or a step ahead, takes 97 to 140 registers in place of 60, and a third of the waves with them: 50 -> 60 and 70 us.) Bound by latency for few:
-// 8 x 128256 in bf16 with the best eight 13 us in two launches, 8 of them without the best; 32 x 65 7. With the best entries 1000 x 8191 in fp32 under a mask
-// 16.5, 2.5 TB/s: a round of the selection takes 0.4 us, all others wait for it.
+// Bound by memory for many long rows: 4096 x 32003 in bf16 54 us, 262 MB at 4.9 TB/s; 4096 x 32000 52; 8192 x 16001 in fp32 91, 5.8 TB/s. Bound by latency for
+// few: 8 x 128256 in bf16 with the best eight 12.5 us in two launches, 8 of them without the best; 32 x 65 7. With the best entries 1000 x 8191 in fp32 under
+// a mask 16, 2.5 TB/s: a round of the selection takes 0.4 us, and all else of the wave waits for it.
+// Four pieces of a lane are requested together where they lie inside the row for the whole wave; each by itself was 1 to 6 % slower in long rows, 20000 x 1024
+// in fp32 39 us with the best four for 31. More of them, or a step ahead, take 97 to 140 registers in place of 64, and the waves that hide it: 50 -> 60 and
+// 70 us. The bounds keep eight waves a SIMD without the best entries (65536 x 200 in bf16 31.4 us with seven, 29.8) and five with them.
 template <typename T, int WAVES, bool TOP>
-__global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
+__global__ __launch_bounds__(256, TOP ? 5 : 8) void token_logp_kernel(const LogpArgs a) {
   touch_args(a);
-  constexpr int VEC = 16 / (int)sizeof(T), PIECES = 32 / VEC, TEAM = WAVES * 64, TEAMS = 256 / TEAM, STEP = TEAM * VEC;
+  constexpr int VEC = 16 / (int)sizeof(T), PIECES = 32 / VEC, TEAM = WAVES * 64, TEAMS = 256 / TEAM, STEP = TEAM * VEC, GROUP = 4;
   const int t = threadIdx.x % TEAM, lane = threadIdx.x & 63, wave = t >> 6;
   const int64_t job = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM;
   const int64_t r = a.row0 + job / a.parts;
@@ -262,8 +264,33 @@ __global__ __launch_bounds__(256) void token_logp_kernel(const LogpArgs a) {
     const int col = w + lane * VEC, left = (c1 - w + STEP - 1) / STEP, n_pieces = left < PIECES ? left : PIECES;
     float x[PIECES][VEC], mx[PIECES];
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      if (p < n_pieces) fetch<T, VEC>(row, odd, col + p * STEP, c1, x[p]);
+    for (int p = 0; p < PIECES; p += GROUP) {
+      if (w + (p + GROUP - 1) * STEP + 64 * VEC <= c1) {      // all of the group inside, for all lanes
+        Piece<T, VEC> v[GROUP];
+        if (odd)
+#pragma unroll
+          for (int k = 0; k < GROUP; ++k) v[k] = load_odd_piece<T, VEC>(row.x + col + (p + k) * STEP);
+        else
+#pragma unroll
+          for (int k = 0; k < GROUP; ++k) v[k] = load_piece<T, VEC>(row.x + col + (p + k) * STEP);
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k)
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) x[p + k][j] = (float)v[k].v[j];
+        if (row.mask) {
+          Piece<uint8_t, VEC> m[GROUP];
+#pragma unroll
+          for (int k = 0; k < GROUP; ++k) m[k] = load_piece<uint8_t, VEC>(row.mask + col + (p + k) * STEP);
+#pragma unroll
+          for (int k = 0; k < GROUP; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) x[p + k][j] = m[k].v[j] ? x[p + k][j] : -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k)
+          if (p + k < n_pieces) fetch<T, VEC>(row, odd, col + (p + k) * STEP, c1, x[p + k]);
+      }
     }
     float m = u.m;
 #pragma unroll
