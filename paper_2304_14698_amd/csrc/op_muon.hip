@@ -110,18 +110,17 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
   float *mom = p.mom + q.offset;
   const float *g = p.g + q.offset;
   double sum = 0.;
-  for (int64_t i = i0 + threadIdx.x * 4; i < i1; i += 4 * 256 * 4) {
-    Piece<float, 4> gi[4], mi[4];
+  for (int64_t b = i0; b < i1; b += 4096) {
+    const int64_t i = b + threadIdx.x * 4;
+    if (b + 4096 <= i1) {                                  // (no load in a branch of its own: eight are on their way together)
+      Piece<float, 4> gi[4], mi[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * 1024 + 4 <= i1) {
+      for (int u = 0; u < 4; ++u) {
         gi[u] = load_piece<float, 4>(g + i + u * 1024);
         mi[u] = load_piece<float, 4>(mom + i + u * 1024);
       }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t at = i + u * 1024;
-      if (at + 4 <= i1) {
+      for (int u = 0; u < 4; ++u) {
         float m[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -129,10 +128,21 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
           const float x = p.nesterov ? gi[u].v[e] + p.mu * m[e] : m[e];
           sum += (double)x * (double)x;
         }
-        store_piece<float, 4>(mom + at, m);
-      } else {
-        for (int64_t k = at; k < i1; ++k) {
-          const float m = p.mu * mom[k] + g[k], x = p.nesterov ? g[k] + p.mu * m : m;
+        store_piece<float, 4>(mom + i + u * 1024, m);
+      }
+    } else {
+      float gk[16], mk[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const int64_t k = b + u * 256 + threadIdx.x, at = k < i1 ? k : i0;
+        gk[u] = g[at];
+        mk[u] = mom[at];
+      }
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const int64_t k = b + u * 256 + threadIdx.x;
+        if (k < i1) {
+          const float m = p.mu * mk[u] + gk[u], x = p.nesterov ? gk[u] + p.mu * m : m;
           mom[k] = m;
           sum += (double)x * (double)x;
         }
