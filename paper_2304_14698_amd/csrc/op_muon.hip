@@ -2,7 +2,7 @@
 //
 // Per matrix, as m x n with m <= n (transposed if it has more rows than columns), X = U / |U|_F and `steps` times
 //   A = X X^T,  B = a I + b A + c A A,  X = B X,
-// the quintic a X + (b A + c A A) X. All matrices share the launches: 2 + 3 steps in all.
+// the quintic a X + (b A + c A A) X. All matrices share the launches: 2 + 3 steps in all; where every matrix is at most 64 x 512 one launch does all of it.
 //
 // Numbers. The products run on the fp16 matrix cores, which are sixteen times as fast as the fp32 ones, on entries x 2^12 split in two halves
 // of 11 bits, hi = fp16(x 2^12) and lo = fp16(x 2^12 - hi), with fp32 sums: hi hi + hi lo + lo hi leaves out 2^-22 of an entry. Entries cannot overflow:
@@ -101,7 +101,7 @@ __device__ __forceinline__ void split(const float *y, V &hi, V &lo) {
   __builtin_memcpy(&lo, l, sizeof(lo));
 }
 
-// M = mu M + G, and of each chunk the sum of squares of U
+// M = mu M + G, and of each chunk the sum of squares of U. Bound by memory: 42 million entries 81 us, 503 MB at 6.2 TB/s.
 __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < p.n_arrived; i += gridDim.x * 256) p.arrived[i] = 0;
   const Mat q = matrix_of(p, blockIdx.x);
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const MuonArgs p) {
 
 __device__ __forceinline__ int wave_of(int t) { return t >> 6; }
 
-// X = U / (|U| + 1e-7) in both orders, a 64 x 64 tile a block
+// X = U / (|U| + 1e-7) in both orders, a 64 x 64 tile a block, turned round in LDS. Bound by memory: 42 million entries 143 us, 671 MB at 4.7 TB/s.
 __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
   const Mat q = matrix_of(p, blockIdx.x);
   const int tile = blockIdx.x - q.first, t = threadIdx.x, lane = t & 63;
@@ -356,7 +356,9 @@ __device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *p, 
 // LDS, where two waves each read them; while a stage is multiplied those behind it are on their way. Tiles of 64 x 64, which often are alone on a compute
 // unit, also read the fragments of each product from LDS while the one before is multiplied, across the barrier between two stages too: a lone block's stage
 // 0.25 us, 0.31 without that. (530 clocks, of which the LDS takes 384 to be written and read and the matrix pipes 192.) Of tiles of 128 x 128 two blocks
-// fill in for each other: X X^T of two 2048^2 and two 2048 x 8192 342 us so, 331 without.
+// fill in for each other: X X^T of two 2048^2 and two 2048 x 8192 342 us so, 331 without. Of these four matrices B X takes 500 us, 515 GF of fp16 products at
+// 1.03 PFLOP/s, bound by the matrix cores; A A 142 and X X^T 330, 0.77 and 0.83: 544 tiles on 512 places, whose last ones have the chip to themselves. Of
+// smaller matrices a product is bound by the latency of its launch, the first stage and the last: 6 to 12 us for those of a 256-wide agent.
 template <int STEP, int T, int STAGES>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) {
   constexpr int NB = T / 64;                               // blocks of 32 of a wave, in each direction
@@ -510,7 +512,8 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 // Wave w keeps columns 32 w .. 32 w + 31 of X in registers, as the products leave them: x[b][r] is row 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of column
 // 32 w + lane % 32, times 2^12, in fp32. For A = X X^T the waves lay X down in LDS in fragment order (turned round on the way) and share out the four
 // 32 x 32 blocks of A, a part of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
-// Bound by latency: 64 x 256 takes about 3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 5 us besides. All of the
+// Bound by latency: 64 x 256 takes 4.3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 10 us a call besides, five steps
+// 31 us (64 x 64 22, 64 x 512 49). All of the
 // vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half of the rows behind the other's stores,
 // these were 12 us.
 constexpr int kSmallRows = 64;
@@ -760,8 +763,8 @@ int plan_product(MuonArgs &p, int step, int n_cu) {
   for (int k = 0; k < p.count; ++k) wide += tiles(k, 128);
   const int T = wide >= n_cu ? 128 : 64;
   for (int k = 0; k < p.count; ++k) work += tiles(k, T) * sum_length(k);
-  // What cutting costs, laying down and adding up, is 2 to 4 us; 64 of a sum take a lone block of 64 x 64 0.8 us. One step of a 1 x 2342 matrix
-  // 31 / 19 us, of 2859 x 89 37 / 22. (Tiles of 128 x 128 are cut nowhere: X X^T of 2048 x 8192, three parts, 336 / 392.)
+  // What cutting costs, laying down and adding up, is 2 to 4 us; 64 of a sum take a lone block of 64 x 64 0.8 us. A call of one step
+  // of a 1 x 2342 matrix 36 / 26 us, of 2859 x 89 44 / 30. (Tiles of 128 x 128 are cut nowhere: X X^T of 2048 x 8192, three parts, 336 / 392.)
   const int64_t least = std::max<int64_t>(384, work / n_cu);
   int64_t at = 0;
   for (int k = 0; k < p.count; ++k) {
