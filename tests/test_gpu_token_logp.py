@@ -389,3 +389,22 @@ def test_nothing_to_do_and_refusals(enc):
     assert ei.value.code == xrl.ERR["SHAPE"]
     lib = xrl.load_library()
     assert lib.xrl_token_logp(enc.handle, None, None, 0, None, None, None, None, None) == xrl.ERR["NULL"]
+
+
+def test_shapes_of_what_is_made_and_a_forward_without_log_probabilities(enc):
+    import torch
+    import paper_2304_14698_amd as xrl
+    x = torch.randn(2, 3, 4, device="cuda")                  # ragged logits are taken flat, whatever their shape
+    ptr = torch.tensor([0, 10, 24], dtype=torch.int32, device="cuda")
+    ids = torch.tensor([9, 0], dtype=torch.int32, device="cuda")
+    f = enc.token_logp(x, ids, row_ptr=ptr, top_k=3)
+    one = torch.ones(2, device="cuda")
+    d = enc.token_logp_backward(x, ids, f, one, row_ptr=ptr)
+    assert d.shape == x.shape and d.is_contiguous() and f["stats"].shape == (2, 2) and f["top_ids"].shape == (2, 3)
+    assert torch.equal(d.flatten(), enc.token_logp_backward(x.flatten(), ids, f, one, row_ptr=ptr))
+    f = enc.token_logp(x, None, row_ptr=ptr)
+    assert "logp" not in f
+    assert enc.token_logp_backward(x, None, f, None, one, row_ptr=ptr).shape == x.shape
+    with pytest.raises(xrl.XrlError) as ei:
+        enc.token_logp_backward(x, ids, f, one, row_ptr=ptr)
+    assert ei.value.code == xrl.ERR["NULL"]
