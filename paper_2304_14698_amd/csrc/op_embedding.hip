@@ -148,10 +148,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void embed_few_kernel(const FewArgs
 
 // A small table: no sort. A block takes consecutive places and 64 C columns; each of its four waves adds its quarter of the rows, one after another, into a
 // table of its own in LDS, a lane C columns (so every sum has one order), and the four tables in order are the block's. A second launch adds up the
-// blocks' in order. Ids outside the vocabulary go to a row behind the table. Four rows whose ids differ are added at once, else one waits for the other's
-// 130 clocks through the LDS (its own atomic additions of floats take 12 clocks a lane: 90 us where this takes 12). Two columns a lane up to 24 ids; the
+// blocks' in order. Ids outside the vocabulary go to a row behind the table. Four rows are added at once, or each would wait for the one before, 130
+// clocks through the LDS; of equal ids among them one takes the other's sum in registers (16.7 us where waiting for those alone takes 18.1; the LDS's own atomic
+// additions of floats, 12 clocks a lane, take 90). Two columns a lane up to 24 ids; the
 // more ids the fewer waves the LDS has room for: up to 64 ids and 512 columns one column a lane, beyond the sort. us a call, this / sorted: 77013 x 128 in
-// fp32, 8 ids 16 / 31, 40 18 / 26, 64 22 / 26, 100 26 / 23; 77013 x 1024 in bf16, 8 ids 40 / 54, 24 46 / 49, 40 68 / 47, 100 115 / 47.
+// fp32, 8 ids 14 / 31, 40 17 / 26, 64 20 / 26, 100 26 / 23; 77013 x 1024 in bf16, 8 ids 38 / 54, 24 43 / 49, 40 68 / 47, 100 115 / 47.
 constexpr int kBinIds = 64, kBinWaves = 4, kBinWideIds = 24, kBinDim = 512;
 
 struct BinArgs {
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(kBinWaves * 64) void embed_bins_kernel(const BinArg
   extern __shared__ __align__(16) float bins[];
   __shared__ unsigned seen[kBinIds / 32];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), table = (a.vocab + 1) * 64 * C;
-  for (int i = threadIdx.x; i < kBinWaves * table; i += kBinWaves * 64) bins[i] = 0.f;
+  for (int i = threadIdx.x; i < kBinWaves * table / 4; i += kBinWaves * 64) ((f32x4 *)bins)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (threadIdx.x < kBinIds / 32) seen[threadIdx.x] = 0;
   __syncthreads();
   const Columns<C> c((int)blockIdx.y * 64 * C + lane * C, a.dim);
@@ -200,22 +201,24 @@ __global__ __launch_bounds__(kBinWaves * 64) void embed_bins_kernel(const BinArg
         int to[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) to[k] = __builtin_amdgcn_readlane(id, q + u + k) * 64 * C;
-        if (to[0] != to[1] && to[0] != to[2] && to[0] != to[3] && to[1] != to[2] && to[1] != to[3] && to[2] != to[3]) {
-          float x[4][C];                                    // four rows of the table at once
+        float x[4][C];                                      // four rows of the table at once
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int j = 0; j < C; ++j) x[k][j] = mine[to[k] + j * 64];
+          for (int j = 0; j < C; ++j) x[k][j] = mine[to[k] + j * 64];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int j = 0; j < C; ++j) mine[to[k] + j * 64] = x[k][j] + (float)v[h][u + k].v[j];
-        } else {
+          for (int j = 0; j < C; ++j) {
+            float old = x[k][j];                            // of an id that came before among the four: the sum so far
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+            for (int l = 0; l < k; ++l) old = to[l] == to[k] ? x[l][j] : old;
+            x[k][j] = old + (float)v[h][u + k].v[j];
+          }
 #pragma unroll
-            for (int j = 0; j < C; ++j) mine[to[k] + j * 64] += (float)v[h][u + k].v[j];
-        }
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int j = 0; j < C; ++j) mine[to[k] + j * 64] = x[k][j];
       }
     }
   }
