@@ -761,6 +761,7 @@ int plan_product(MuonArgs &p, int step, int n_cu) {
   };
   int64_t wide = 0, work = 0;
   for (int k = 0; k < p.count; ++k) wide += tiles(k, 128);
+  // us a call, all products in tiles of 64 / of 128: four 2048^2 2756 / 2404, one 776 / 751 (each as it fits 718), 1500^2 393 / 555, 1024^2 184 / 390
   const int T = wide >= n_cu ? 128 : 64;
   for (int k = 0; k < p.count; ++k) work += tiles(k, T) * sum_length(k);
   // What cutting costs, laying down and adding up, is 2 to 4 us; 64 of a sum take a lone block of 64 x 64 0.8 us. A call of one step
@@ -778,7 +779,8 @@ int plan_product(MuonArgs &p, int step, int n_cu) {
 }
 
 // An XCD's share of the blocks is an eighth of the work, in the order of the matrices: a small matrix is one XCD's in all products of a step, a large
-// one is cut into few pieces. Returns the blocks of the launch.
+// one is cut into few pieces. us a call so / dealt to the XCDs in turn: eight matrices of 256 x 256 and 256 x 512 119 / 123, two 2048^2 and two 2048 x 8192
+// 4937 / 5126. Returns the blocks of the launch.
 int deal_blocks(MuonArgs &p, int step) {
   constexpr int kFixed = 256;                              // what a block costs beside its products, as a sum's length
   int64_t work = 0, done = 0;
@@ -827,6 +829,8 @@ int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
     rows = std::max(rows, p.mat[k].m);
     cols = std::max(cols, p.mat[k].n);
   }
+  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 23 / 28, 64 x 256 65 / 32 / 36, ten of 64 x 128
+  // 63 / 26 / 31; 64 x 512 75 / - / 50
   if (rows <= kSmallRows && cols <= 256) return launch_small<8>(c, p, steps);
   if (rows <= kSmallRows && cols <= 512) return launch_small<16>(c, p, steps);
   int64_t at = 0;

@@ -367,8 +367,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
 }
 
 // dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
-// Each entry by itself, two pieces a thread. Bound by memory: 2048 x 50021 in bf16 66 us for 205 MB read and written, 6.2 TB/s (some of the logits are
-// still in the last-level cache from the forward call); results of more than the L2s hold are stored past the caches.
+// Each entry by itself, two pieces a thread or four. Bound by memory: 2048 x 50021 in bf16 78 us for 205 MB read and written, 5.3 TB/s; results of more than the L2s hold are stored past the caches.
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T);
@@ -482,16 +481,20 @@ int xrl_token_logp(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_i
   if (((uintptr_t)d_ids | (uintptr_t)d_logp | (uintptr_t)d_entropy | (uintptr_t)d_stats | (uintptr_t)d_top_ids | (uintptr_t)d_top_logp) % 4)
     return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
   a.ids = d_ids; a.top_k = top_k; a.logp = d_logp; a.entropy = d_entropy; a.stats = d_stats; a.top_ids = d_top_ids; a.top_logp = d_top_logp;
-  // A wave a row up to 1024 columns (on average, where they are ragged), else a block a row. Few long rows are cut into parts, at most 64, which a second
-  // launch joins: of 2048 columns and a wave each where such parts do not fill the chip by themselves, else of a block each.
+  // A wave a row where that is one step of 2048 columns (on average, where they are ragged), or up to four where there are rows for six waves a compute unit (two
+  // in fp32 without the best entries); else a block a row. us, block / wave: 10000 x 2000 in bf16 18.8 / 14.3, in fp32 20.5 / 17.5; 500 x 4000 in fp32 with the best
+  // four 8.1 / 10.8, 2000 16.4 / 13.4; 1000 x 8000 in bf16 with the best eight 16 / 22, 4000 44 / 33; 8000 x 8000 31.5 / 29.8, in fp32 48.6 / 51.3.
+  // Few rows of more columns than a block's step of 8192, without the best entries than five of these, are cut into parts, at most 64, which a second launch joins:
+  // of 2048 columns and a wave each where such parts do not fill the chip by themselves, else of a block each. us, uncut / cut: best eight of 8 x 8000 in fp32
+  // 10.5 / 12.4, of 16000 15.2 / 12.3, of 8 x 128256 in bf16 39 / 12.5 (parts of a block 14.7); without them 64 x 30000 in fp32 7.3 / 9.2, 64 x 50021 in bf16 10.2 / 8.4,
+  // 16 x 128256 in fp32 20 / 8.6.
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, n_cu = op_compute_units(c), fine = (cols + 2047) / 2048;
-  bool wave_rows = cols <= 1024;
+  const bool bf16 = logits->type == XRL_PREC_BF16;
+  bool wave_rows = cols <= 2048 || (a.n_rows > 6 * n_cu && cols <= (top_k || bf16 ? 8192 : 4096));
   a.parts = 1;
-  if (!wave_rows && fine <= 64 && fine * a.n_rows <= 8 * n_cu) {
-    wave_rows = true;
-    a.parts = (int)fine;
-  } else if (!wave_rows) {
-    a.parts = (int)std::max<int64_t>(1, std::min<int64_t>({4 * n_cu / a.n_rows, cols / 2048, 64}));
+  if (cols > (top_k ? 8192 : 40960)) {
+    wave_rows = fine <= 64 && fine * a.n_rows <= 8 * n_cu;
+    a.parts = wave_rows ? (int)fine : (int)std::max<int64_t>(1, std::min<int64_t>({4 * n_cu / a.n_rows, cols / 2048, 64}));
   }
   if (a.parts > 1) {
     const size_t jobs = (size_t)a.n_rows * a.parts, o_t = op_align(jobs * 12), o_i = o_t + op_align(jobs * top_k * 4);
@@ -499,7 +502,7 @@ int xrl_token_logp(xrl_ctx *c, const xrl_logits_desc *logits, const int32_t *d_i
     if (int rc = op_workspace(c, o_i + jobs * top_k * 4, &ws, who)) return rc;
     a.part_sums = (float *)ws; a.part_top = (float *)(ws + o_t); a.part_ids = (int32_t *)(ws + o_i);
   }
-  if (logits->type == XRL_PREC_BF16) top_k ? launch_logp<bf16_t, true>(c, a, wave_rows) : launch_logp<bf16_t, false>(c, a, wave_rows);
+  if (bf16) top_k ? launch_logp<bf16_t, true>(c, a, wave_rows) : launch_logp<bf16_t, false>(c, a, wave_rows);
   else top_k ? launch_logp<float, true>(c, a, wave_rows) : launch_logp<float, false>(c, a, wave_rows);
   OP_TRY(hipGetLastError());
   return XRL_OK;
@@ -522,7 +525,8 @@ int xrl_token_logp_backward(xrl_ctx *c, const xrl_logits_desc *logits, const int
   a.ids = d_ids; a.logp = (float *)d_logp; a.entropy = (float *)d_entropy; a.stats = (float *)d_stats; a.dlogp = d_dlogp; a.dentropy = d_dentropy;
   a.dlogits = d_dlogits; a.dstride = dlogits_stride;
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, vec = logits->type == XRL_PREC_BF16 ? 8 : 4;
-  const int64_t chunks = std::max<int64_t>(1, (cols + 256 * vec * 2 - 1) / (256 * vec * 2));
+  // Pieces of a thread: us, two / four, 2048 x 50021 in bf16 84 / 78, 4096 x 32000 103 / 95 (eight: 85, 99); 8192 x 16001 in fp32 184 / 198.
+  const int64_t per = 256 * vec * (vec == 8 ? 4 : 2), chunks = std::max<int64_t>(1, (cols + per - 1) / per);
   const bool stream = streams(a.n_cols * (a.row_ptr ? 1 : a.n_rows) * (logits->type == XRL_PREC_BF16 ? 2 : 4));
   for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMaxBlocks) {
     const int64_t rows = std::min(a.n_rows - a.row0, kMaxBlocks);

@@ -200,3 +200,34 @@ def test_rows_of_few_and_of_many_parts():
         best = x.float().sort(dim=1, descending=True, stable=True)
         assert torch.equal(f["top_ids"].long(), best[1][:, :3]), (rows, cols)
     enc.close()
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,k", [(1700, 2049, 0), (1700, 4097, 0), (1700, 8191, 2), (1700, 8193, 2), (1400, 4000, 2), (3, 8192, 5), (3, 8193, 5),
+                                         (3, 40960, 0), (3, 40961, 0), (400, 41000, 0), (5, 200000, 0), (5, 131073, 5)])
+def test_rows_where_their_ways_change(type, rows, cols, k):
+    """Waves of several steps, blocks uncut and cut, with their gradient: against 64 bits."""
+    import torch
+    enc = encoder()
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn(rows, cols, generator=g, device="cuda").to(dict(fp32=torch.float32, bf16=torch.bfloat16)[type])
+    ids = torch.randint(0, cols, (rows,), generator=g, device="cuda").int()
+    f = enc.token_logp(x, ids, top_k=k)
+    dlogp = torch.ones(rows, device="cuda")
+    d = enc.token_logp_backward(x, ids, f, dlogp)
+    torch.cuda.synchronize()
+    u, at = 2.0 ** -24, ids.long()[:, None]
+    D = (3 * (cols / 64 + 8) + 64 + 4 * math.log2(cols)) * u
+    for r in range(0, rows, 200):                        # a part of the rows at a time: they are held in 64 bits
+        s = slice(r, r + 200)
+        lp = torch.log_softmax(x[s].double(), 1)
+        assert (f["logp"][s].double() - lp.gather(1, at[s])[:, 0]).abs().max() <= D + 6 * u * 40
+        H = -(lp.exp() * lp).sum(1)
+        assert (f["entropy"][s].double() - H).abs().max() <= D * (1 + 2 * (math.log(cols) + 12)) + 8 * u * 24
+        if k:
+            assert torch.equal(f["top_ids"][s].long(), x[s].float().sort(dim=1, descending=True, stable=True)[1][:, :k])
+        want = -lp.exp()
+        want.scatter_add_(1, at[s], torch.ones_like(at[s], dtype=torch.float64))
+        bound = want.abs() * (2 * D + (24 + 8 * lp.abs()) * u + (2.0 ** -8 if type == "bf16" else 0)) + 16 * u * (want > 0) + 1e-38
+        assert ((d[s].double() - want).abs() <= bound).all()
+    enc.close()
