@@ -370,17 +370,20 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
 // Each entry by itself, two pieces a thread or four. Bound by memory: 2048 x 50021 in bf16 78 us for 205 MB read and written, 5.3 TB/s; results of more than the L2s hold are stored past the caches.
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs a) {
+  touch_args(a);
   constexpr int VEC = 16 / (int)sizeof(T);
   const int64_t r = a.row0 + blockIdx.y + (int64_t)blockIdx.z * 32768;
   if (r >= a.n_rows) return;
   const Row<T> row = row_of<T>(a, r);
+  // what the row has, all requested together: what is not given is read from the entropy and not looked at
+  const int id0 = (a.ids ? a.ids : (const int32_t *)a.entropy)[r];
+  const float logp = (a.ids ? a.logp : a.entropy)[r], g0 = (a.ids ? a.dlogp : a.entropy)[r], h0 = (a.dentropy ? a.dentropy : a.entropy)[r];
   const float m = a.stats[2 * r], ln_s = a.stats[2 * r + 1], H = a.entropy[r];
   const float c = a.inv_t * kLog2e, log2_s = ln_s * kLog2e;
   const bool any = !(m == -INFINITY);
   // whether the given entry may be chosen: from its log-probability, as in place another block may have written over its logit
-  const int given = a.ids ? a.ids[r] : -1, id = given >= 0 && !(a.logp[r] == -INFINITY) ? given : -1;
-  const float g = id >= 0 ? a.dlogp[r] : 0.f;
-  const float h = a.dentropy ? a.dentropy[r] : 0.f;
+  const int id = a.ids && id0 >= 0 && !(logp == -INFINITY) ? id0 : -1;
+  const float g = id >= 0 ? g0 : 0.f, h = a.dentropy ? h0 : 0.f;
   const float A = -a.inv_t * (g + h * H), B = -a.inv_t * h * kLn2;
   T *out = (T *)a.dlogits + (a.row_ptr ? row.begin : r * a.dstride);
   for (int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC - lead_of(out, row.len); col < row.len; col += (int64_t)gridDim.x * 256 * VEC) {
