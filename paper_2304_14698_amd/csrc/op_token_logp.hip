@@ -367,12 +367,14 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
 }
 
 // dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
-// Each entry by itself, two pieces a thread or four. Bound by memory: 2048 x 50021 in bf16 78 us for 205 MB read and written, 5.3 TB/s; results of more than the L2s hold are stored past the caches.
-template <typename T, bool STREAM>
+// Each entry by itself; a row has a wave, or blocks of two pieces a thread or four. Bound by memory: 2048 x 50021 in bf16 78 us for 205 MB read and written, 5.3 TB/s; results of more than the L2s hold are stored past the caches.
+template <typename T, bool STREAM, int WAVES>
 __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs a) {
   touch_args(a);
   constexpr int VEC = 16 / (int)sizeof(T);
-  const int64_t r = a.row0 + blockIdx.y + (int64_t)blockIdx.z * 32768;
+  constexpr int TEAM = WAVES * 64;
+  const int t = threadIdx.x % TEAM;
+  const int64_t r = a.row0 + (blockIdx.y + (int64_t)blockIdx.z * 32768) * (4 / WAVES) + __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM);
   if (r >= a.n_rows) return;
   const Row<T> row = row_of<T>(a, r);
   // what the row has, all requested together: what is not given is read from the entropy and not looked at
@@ -386,7 +388,7 @@ __global__ __launch_bounds__(256) void token_logp_backward_kernel(const LogpArgs
   const float g = id >= 0 ? g0 : 0.f, h = a.dentropy ? h0 : 0.f;
   const float A = -a.inv_t * (g + h * H), B = -a.inv_t * h * kLn2;
   T *out = (T *)a.dlogits + (a.row_ptr ? row.begin : r * a.dstride);
-  for (int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC - lead_of(out, row.len); col < row.len; col += (int64_t)gridDim.x * 256 * VEC) {
+  for (int64_t col = ((int64_t)blockIdx.x * TEAM + t) * VEC - lead_of(out, row.len); col < row.len; col += (int64_t)gridDim.x * TEAM * VEC) {
     const bool whole = col >= 0 && col + VEC <= row.len;
     float x[VEC], d[VEC];
     bool ok[VEC];
@@ -464,9 +466,10 @@ void launch_logp(const xrl_ctx *c, LogpArgs &a, bool wave_rows) {
   if (a.parts > 1) token_logp_join_kernel<T><<<dim3((unsigned)a.n_rows), dim3(64), 0, op_stream(c)>>>(a);
 }
 
-template <typename T, bool STREAM>
-void launch_backward(const xrl_ctx *c, const LogpArgs &a, dim3 grid) {
-  token_logp_backward_kernel<T, STREAM><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+template <typename T>
+void launch_backward(const xrl_ctx *c, const LogpArgs &a, dim3 grid, bool stream, bool wave_rows) {
+  if (wave_rows) stream ? token_logp_backward_kernel<T, true, 1><<<grid, dim3(256), 0, op_stream(c)>>>(a) : token_logp_backward_kernel<T, false, 1><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+  else stream ? token_logp_backward_kernel<T, true, 4><<<grid, dim3(256), 0, op_stream(c)>>>(a) : token_logp_backward_kernel<T, false, 4><<<grid, dim3(256), 0, op_stream(c)>>>(a);
 }
 
 }  // namespace
@@ -529,13 +532,16 @@ int xrl_token_logp_backward(xrl_ctx *c, const xrl_logits_desc *logits, const int
   a.dlogits = d_dlogits; a.dstride = dlogits_stride;
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols, vec = logits->type == XRL_PREC_BF16 ? 8 : 4;
   // Pieces of a thread: us, two / four, 2048 x 50021 in bf16 84 / 78, 4096 x 32000 103 / 95 (eight: 85, 99); 8192 x 16001 in fp32 184 / 198.
-  const int64_t per = 256 * vec * (vec == 8 ? 4 : 2), chunks = std::max<int64_t>(1, (cols + per - 1) / per);
-  const bool stream = streams(a.n_cols * (a.row_ptr ? 1 : a.n_rows) * (logits->type == XRL_PREC_BF16 ? 2 : 4));
+  const int64_t per = 256 * vec * (vec == 8 ? 4 : 2);
+  // Rows of up to 4 KB have a wave each: us, block / wave, 20000 rows, 200 in bf16 15.7 / 10.3, 1000 22 / 15.4, 1000 in fp32 28.3 / 27.3; 10000 x 2000 in bf16 17.5 /
+  // 16.8, in fp32 24.6 / 26.4.
+  const bool wave_rows = cols <= 256 * vec;
+  const int64_t chunks = wave_rows ? 1 : (cols + per - 1) / per, team_rows = wave_rows ? 4 : 1;
+  const bool stream = streams(a.n_cols * (a.row_ptr ? 1 : a.n_rows) * (16 / vec));
   for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMaxBlocks) {
-    const int64_t rows = std::min(a.n_rows - a.row0, kMaxBlocks);
-    const dim3 grid((unsigned)chunks, (unsigned)std::min<int64_t>(rows, 32768), (unsigned)((rows + 32767) / 32768));
-    if (logits->type == XRL_PREC_BF16) stream ? launch_backward<bf16_t, true>(c, a, grid) : launch_backward<bf16_t, false>(c, a, grid);
-    else stream ? launch_backward<float, true>(c, a, grid) : launch_backward<float, false>(c, a, grid);
+    const int64_t teams = (std::min(a.n_rows - a.row0, kMaxBlocks) + team_rows - 1) / team_rows;
+    const dim3 grid((unsigned)chunks, (unsigned)std::min<int64_t>(teams, 32768), (unsigned)((teams + 32767) / 32768));
+    logits->type == XRL_PREC_BF16 ? launch_backward<bf16_t>(c, a, grid, stream, wave_rows) : launch_backward<float>(c, a, grid, stream, wave_rows);
   }
   OP_TRY(hipGetLastError());
   return XRL_OK;

@@ -231,3 +231,29 @@ def test_rows_where_their_ways_change(type, rows, cols, k):
         bound = want.abs() * (2 * D + (24 + 8 * lp.abs()) * u + (2.0 ** -8 if type == "bf16" else 0)) + 16 * u * (want > 0) + 1e-38
         assert ((d[s].double() - want).abs() <= bound).all()
     enc.close()
+
+
+@pytest.mark.parametrize("type,cols", [("fp32", 1023), ("fp32", 1024), ("fp32", 1025), ("bf16", 2047), ("bf16", 2048), ("bf16", 2049), ("bf16", 131)])
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 1001])
+def test_gradient_of_rows_by_waves_and_by_blocks(rows, type, cols):
+    """The last rows of a block of four, in place and into rows apart: as in float64."""
+    import torch
+    enc = encoder()
+    g = torch.Generator(device="cuda").manual_seed(cols + rows)
+    x = torch.randn(rows, cols, generator=g, device="cuda").to(dict(fp32=torch.float32, bf16=torch.bfloat16)[type])
+    ids = torch.randint(0, cols, (rows,), generator=g, device="cuda").int()
+    f, dlogp = enc.token_logp(x, ids), torch.ones(rows, device="cuda")
+    wide = torch.full((rows, cols + 3), 7.0, device="cuda").to(x.dtype)
+    enc.token_logp_backward(x, ids, f, dlogp, out=wide[:, :cols])
+    y = x.clone()
+    enc.token_logp_backward(y, ids, f, dlogp, out=y)
+    torch.cuda.synchronize()
+    assert torch.equal(y, wide[:, :cols]) and (wide[:, cols:] == 7).all()
+    lp, at = torch.log_softmax(x.double(), 1), ids.long()[:, None]
+    want = -lp.exp()
+    want.scatter_add_(1, at, torch.ones_like(at, dtype=torch.float64))
+    u = 2.0 ** -24
+    D = (3 * (cols / 64 + 8) + 64 + 4 * math.log2(cols)) * u
+    bound = want.abs() * (2 * D + (24 + 8 * lp.abs()) * u + (2.0 ** -8 if type == "bf16" else 0)) + 16 * u * (want > 0) + 1e-38
+    assert ((y.double() - want).abs() <= bound).all()
+    enc.close()
