@@ -104,10 +104,18 @@ struct Given {
   bool none;
   float x;
 };
+__device__ __forceinline__ int given_id(const LogpArgs &a, int64_t r) { return (a.ids ? a.ids : (const int32_t *)a.entropy)[r]; }   // (not looked at without ids)
 template <typename T>
-__device__ __forceinline__ Given given_entry(const LogpArgs &a, int64_t r, const Row<T> &row) {
-  const int id = a.ids ? a.ids[r] : -1;
-  return {id < 0, id >= 0 && id < row.len && (!row.mask || row.mask[id]) ? (float)row.x[id] : -INFINITY};
+__device__ __forceinline__ Given given_entry(const LogpArgs &a, int id, const Row<T> &row) {
+  id = a.ids ? id : -1;
+  T x = (T)0.f;
+  uint8_t ok = 1;
+  const bool in = id >= 0 && id < row.len;
+  if (row.len > 0) {
+    x = row.x[in ? id : 0];
+    if (row.mask) ok = row.mask[in ? id : 0];
+  }
+  return {id < 0, in && ok ? (float)x : -INFINITY};
 }
 
 // The row's results from its sums (the same in all lanes), its given logit (lane 0) and its best entries.
@@ -256,7 +264,7 @@ __global__ __launch_bounds__(256, TOP ? 5 : 8) void token_logp_kernel(const Logp
   const int steps = (row.len + STEP - 1) / STEP, per = (steps + a.parts - 1) / a.parts;
   const int64_t b0 = (int64_t)part * per * STEP, b1 = b0 + (int64_t)per * STEP;
   const int c0 = (int)(b0 < row.len ? b0 : row.len), c1 = (int)(b1 < row.len ? b1 : row.len);
-  const Given given = a.parts == 1 && lane == 0 ? given_entry<T>(a, r, row) : Given{true, 0.f};
+  const int id = given_id(a, r);                          // (needed at the end)
   Sums u = {kLowest, 0.f, 0.f};
   Best best = {-INFINITY, kNone};
   float bar = -INFINITY;
@@ -333,7 +341,7 @@ __global__ __launch_bounds__(256, TOP ? 5 : 8) void token_logp_kernel(const Logp
       best = merge_best(WAVES, a.top_k, lane, [&](int l, int i) { return bx[l][i]; }, [&](int l, int i) { return bi[l][i]; });
   }
   if (a.parts == 1) {
-    finish(a, r, given, u, best, lane);
+    finish(a, r, given_entry<T>(a, id, row), u, best, lane);
     return;
   }
   if (lane == 0) {
@@ -353,7 +361,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
   const int lane = threadIdx.x;
   touch_args(a);
   const Row<T> row = row_of<T>(a, r);
-  const Given given = lane == 0 ? given_entry<T>(a, r, row) : Given{true, 0.f};
+  const int id = given_id(a, r);
   const int64_t job = r * a.parts + lane;
   const bool in = lane < a.parts;
   const float *p = a.part_sums + (in ? job : 0) * 3;
@@ -363,7 +371,7 @@ __global__ __launch_bounds__(64) void token_logp_join_kernel(const LogpArgs a) {
   if (a.top_k)
     best = merge_best(a.parts, a.top_k, lane, [&](int l, int i) { return a.part_top[(r * a.parts + l) * a.top_k + i]; },
                       [&](int l, int i) { return a.part_ids[(r * a.parts + l) * a.top_k + i]; });
-  finish(a, r, given, u, best, lane);
+  finish(a, r, given_entry<T>(a, id, row), u, best, lane);
 }
 
 // dlogits_j = (1 / temperature) (g [j = id] - p_j (g + h (ln p_j + H))): with q = log2 p_j, p_j (A + B q)
