@@ -380,7 +380,9 @@ int xrl_token_logp(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d
  * memory at their own stride) for dJ/dlogp = d_dlogp [n_rows] and dJ/dentropy = d_dentropy [n_rows] (NULL: zeros), from the logits and what
  * xrl_token_logp wrote of them (d_logp if there are ids, d_stats and d_entropy; the same ids, mask and temperature):
  *   dlogits_j = (dlogp ([j = id] - p_j) - dentropy p_j (ln p_j + entropy)) / temperature.
- * Exactly 0 at entries that may not be chosen. A row whose logp is 0 or -inf by the rules above takes nothing from d_dlogp.
+ * Exactly 0 at entries that may not be chosen, and at entries of ragged logits that no row covers (in front of the first row, behind the last,
+ * all of them where there is no row); what lies between dense rows is not written. Rows must not overlap: of an entry of several ragged rows (a d_row_ptr that
+ * falls) one row's gradient is left. A row whose logp is 0 or -inf by the rules above takes nothing from d_dlogp.
  * Errors: as above. */
 int xrl_token_logp_backward(xrl_ctx *ctx, const xrl_logits_desc *logits, const int32_t *d_ids, const float *d_logp,
                             const float *d_entropy, const float *d_stats, const float *d_dlogp, const float *d_dentropy,

@@ -514,8 +514,8 @@ class Encoder:
 
     def token_logp_backward(self, logits, ids, forward, dlogp, dentropy=None, mask=None, row_ptr=None, temperature=1.0,
                             out=None):
-        """dJ/dlogits, like the logits, from `forward` (what token_logp gave), dJ/dlogp and dJ/dentropy [n]; out may be the
-        logits' own memory. See xrl_token_logp_backward."""
+        """dJ/dlogits, like the logits, from `forward` (what token_logp gave), dJ/dlogp and dJ/dentropy [n]: all of it, zeros at
+        flat logits that no row covers; out may be the logits' own memory. See xrl_token_logp_backward."""
         t, f = self.torch, self.torch.float32
         d = self._logits(logits, mask, row_ptr, temperature)
         n = d.n_rows
