@@ -512,10 +512,10 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 // Wave w keeps columns 32 w .. 32 w + 31 of X in registers, as the products leave them: x[b][r] is row 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of column
 // 32 w + lane % 32, times 2^12, in fp32. For A = X X^T the waves lay X down in LDS in fragment order (turned round on the way) and share out the four
 // 32 x 32 blocks of A, a part of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
-// Bound by latency: 64 x 256 takes 4.3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 10 us a call besides, five steps
-// 31 us (64 x 64 22, 64 x 512 49). All of the
-// vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half of the rows behind the other's stores,
-// these were 12 us.
+// Bound by latency: 64 x 256 takes 4.3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 7 us a call besides, five steps
+// 28 us (64 x 64 20, 64 x 512 44). All of the vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half
+// of the rows behind the other's stores, this was 2 us more. Sixteen waves have 128 registers each and do it so: with all at the start, and with the entries'
+// indices kept for the end, they spilled 116 bytes a lane, and 64 x 512 took 49 us.
 constexpr int kSmallRows = 64;
 __host__ __device__ constexpr int small_lds(int waves) { return waves * 8192 + 2 * 16384; }   // X, and the parts of A after it; A; B
 constexpr int kTurn = 36;              // floats of a row on its way: 16-byte pieces of 8 rows lie in different banks
@@ -549,7 +549,8 @@ __device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, in
 template <int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p, int steps) {
   constexpr int PARTS = WAVES / 4;                         // of the sums of a block of A
-  constexpr bool EARLY = WAVES == 8;                       // (sixteen waves have 128 registers each)
+  constexpr bool EARLY = WAVES == 8;                       // (the weights requested at the start, and all rows at once)
+  constexpr int AT_ONCE = EARLY ? 2 : 1;
   extern __shared__ __align__(16) char lds[];
   const Mat q = matrix_of(p, blockIdx.x);
   const int m = q.m, n = q.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, jl = lane & 31;
@@ -560,34 +561,40 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
   float *w = p.w + q.offset, *mom = p.mom + q.offset;
   const float *grad = p.g + q.offset;
   // entry (b, r) of a lane in the vector: lanes along its rows, which for a matrix that is taken transposed is another order than x's
+  // (Sums of products with what depends on the matrix alone: a choice between the two orders at each entry makes branches.)
+  const int of_b = q.t ? 32 : 32 * n, of_r = q.t ? 2 * m : n, of_q = 8 * (q.t ? m : n), row_b = q.t ? 0 : 32, row_r = q.t ? 2 : 1, col_b = q.t ? 32 : 0;
+  int first = q.t ? (wave * 32 + g) * m + jl : 4 * g * n + j, rows = q.t ? n - wave * 32 - g : m - 4 * g, cols = q.t ? m - jl : n - j;
   auto at = [&](int b, int r) {
-    const int i = 32 * b + (q.t ? jl : acc_row(r, g)), c = q.t ? wave * 32 + 2 * r + g : j;
-    return i < m && c < n ? (q.t ? c * m + i : i * n + c) : -1;
+    const bool in = (b * row_b + (r & 3) * row_r + 8 * (r >> 2) < rows) & (b * col_b < cols);
+    return in ? first + b * of_b + (r & 3) * of_r + (r >> 2) * of_q : -1;
   };
   // M = mu M + G, U and |U|. (Requests for entries that are not there go to the first one: a request in a branch of its own is waited for there.)
   float x[2][16], old[2][16];
   {
     float gi[2][16], mi[2][16];
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int k = at(b, r), from = k >= 0 ? k : 0;
-        gi[b][r] = grad[from];
-        mi[b][r] = mom[from];
-        if (EARLY) old[b][r] = w[from];
-      }
     double sum = 0.;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b0 = 0; b0 < 2; b0 += AT_ONCE) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int k = at(b, r);
-        const float mr = p.mu * mi[b][r] + gi[b][r], u = p.nesterov ? gi[b][r] + p.mu * mr : mr;
-        if (k >= 0) mom[k] = mr;
-        x[b][r] = k >= 0 ? u : 0.f;
-        sum += (double)x[b][r] * (double)x[b][r];
-      }
+      for (int b = b0; b < b0 + AT_ONCE; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int k = at(b, r), from = k >= 0 ? k : 0;
+          gi[b][r] = grad[from];
+          mi[b][r] = mom[from];
+          if (EARLY) old[b][r] = w[from];
+        }
+#pragma unroll
+      for (int b = b0; b < b0 + AT_ONCE; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int k = at(b, r);
+          const float mr = p.mu * mi[b][r] + gi[b][r], u = p.nesterov ? gi[b][r] + p.mu * mr : mr;
+          if (k >= 0) mom[k] = mr;
+          x[b][r] = k >= 0 ? u : 0.f;
+          sum += (double)x[b][r] * (double)x[b][r];
+        }
+    }
     for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
     double *sums = (double *)lds;
     if (lane == 0) sums[wave] = sum;
@@ -724,7 +731,8 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
     __syncthreads();                                       // (B and the parts are read no more)
   }
   const float step = p.step * sqrtf((float)n) * kDown;
-  if (!EARLY)
+  if (!EARLY) {
+    asm volatile("" : "+v"(first), "+v"(rows), "+v"(cols));   // (indices made anew, not kept in registers since the start)
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -732,6 +740,7 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
         const int k = at(b, r);
         old[b][r] = w[k >= 0 ? k : 0];
       }
+  }
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     if (q.t) reorder(x[b], true);
@@ -829,8 +838,8 @@ int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
     rows = std::max(rows, p.mat[k].m);
     cols = std::max(cols, p.mat[k].n);
   }
-  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 23 / 28, 64 x 256 65 / 32 / 36, ten of 64 x 128
-  // 63 / 26 / 31; 64 x 512 75 / - / 50
+  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 20 / 28, 64 x 256 65 / 28 / 36, ten of 64 x 128
+  // 63 / 26 / 31; 64 x 512 75 / - / 44
   if (rows <= kSmallRows && cols <= 256) return launch_small<8>(c, p, steps);
   if (rows <= kSmallRows && cols <= 512) return launch_small<16>(c, p, steps);
   int64_t at = 0;
