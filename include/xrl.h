@@ -405,8 +405,8 @@ typedef struct xrl_muon_desc {
  *   M = momentum M + G;  U = nesterov ? G + momentum M : M;  X = U / (|U|_F + 1e-7), transposed if it has more rows than columns;
  *   `steps` times: A = X X^T, X = 3.4445 X + (-4.7750 A + 2.0315 A A) X;
  *   W = (1 - lr weight_decay) W - lr rms sqrt(max(rows, cols)) X.
- * The products run on the matrix cores on entries split in two halves of 11 bits each (22 bits of each factor count), with fp32 sums. |U|
- * is summed in 64 bits. The vectors have n_weights entries each and must not overlap. A NaN or infinity in a matrix's gradient
+ * The products run on the matrix cores on entries split in two halves of 11 bits each, with fp32 sums: of each factor 22 bits count (fp32 has 24), of
+ * entries of X, A and the polynomial below 2^-26 what lies above 2^-48. |U| is summed in 64 bits. The vectors have n_weights entries each and must not overlap. A NaN or infinity in a matrix's gradient
  * makes that matrix NaN, no other. Errors: NULL, SHAPE (a matrix outside the vector, overlapping ones), VALUE (not finite, negative
  * lr, ...), UNSUPPORTED (more than 32768 rows or columns), OOM, HIP. */
 int xrl_muon_step(xrl_ctx *ctx, const xrl_muon_desc *desc, int32_t n_matrices, const xrl_matrix *matrices, int64_t n_weights,

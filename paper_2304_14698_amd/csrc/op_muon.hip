@@ -5,9 +5,12 @@
 // the quintic a X + (b A + c A A) X. All matrices share the launches: 2 + 3 steps in all; where every matrix is at most 64 x 512 one launch does all of it.
 //
 // Numbers. The products run on the fp16 matrix cores, which are sixteen times as fast as the fp32 ones, on entries x 2^12 split in two halves
-// of 11 bits, hi = fp16(x 2^12) and lo = fp16(x 2^12 - hi), with fp32 sums: hi hi + hi lo + lo hi leaves out 2^-22 of an entry. Entries cannot overflow:
-// singular values of X lie in [0, 1.21] in every step (the quintic's largest value on [0, 1.21] is 1.21), so entries of X, A and B are at most 1.21, 1.47
-// and 3.45, and 3.45 2^12 < 65504. An entry from 2^-26 down loses bits of lo to the smallest fp16, 2^-36 of the matrix's scale.
+// of 11 bits, hi = fp16(x 2^12) and lo = fp16((x 2^12 - hi) 2^11), with fp32 sums of their own for hi hi and for hi lo + lo hi, which is added 2^-11 times. That
+// leaves out 2^-22 of an entry, fp32 2^-24. Entries cannot overflow: singular values of X lie in [0, 1.21] in every step (the quintic's largest value on
+// [0, 1.21] is 1.21), so entries of X, A and B are at most 1.21, 1.47 and 3.45, and 3.45 2^12 < 65504; lo is at most 2^12 times the entry, too. An entry keeps
+// its 22 bits down to 2^-26; below, hi and lo together are off by at most 2^-48 (by a subnormal fp16's half, 2^-25, over 2^11 and 2^12). Without the 2^11 lo
+// would be subnormal from entries of 2^-15 on, as rows of small size have: of 256 x 512 with row sizes from 1 to 1e-6 the worst row was off by 3e-4 of
+// itself so, and is by 4e-6, 6e-6 with fp32 products (from 1 to 1e-8 1.5e-5 and 6e-6).
 //
 // Layout. Operands lie in fragment order: 32 rows by 16 of the summed dimension, first hi, then lo, each 64 lanes by 16 bytes, as one matrix
 // instruction takes them. Both X (rows m) and X^T (rows n) are kept.
@@ -28,6 +31,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;
+constexpr float kLowUp = 2048.f, kLowDown = 1.f / 2048.f;   // of the lower halves besides
 constexpr int kGroup = 32;             // matrices of one launch: their list is a kernel argument
 constexpr int kTile = 64;              // sizes are padded to multiples of this
 constexpr int kMaxSums = 1024;         // partial sums of squares of a matrix
@@ -95,7 +99,7 @@ __device__ __forceinline__ void split(const float *y, V &hi, V &lo) {
   for (int e = 0; e < N / 2; ++e) {
     const f32x2 x = {y[2 * e], y[2 * e + 1]};
     h[e] = __builtin_convertvector(x, f16x2);
-    l[e] = __builtin_convertvector(x - __builtin_convertvector(h[e], f32x2), f16x2);
+    l[e] = __builtin_convertvector((x - __builtin_convertvector(h[e], f32x2)) * kLowUp, f16x2);
   }
   __builtin_memcpy(&hi, h, sizeof(hi));
   __builtin_memcpy(&lo, l, sizeof(lo));
@@ -306,7 +310,7 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float diag = ib == jb && 8 * s + 4 * g + e == jl ? kNsA * kUp : 0.f;
-        v[4 * s + e] = kNsC * v[4 * s + e] + (kNsB * ((float)h[e] + (float)l[e]) + diag);
+        v[4 * s + e] = kNsC * v[4 * s + e] + (kNsB * ((float)h[e] + kLowDown * (float)l[e]) + diag);
       }
     }
   }
@@ -389,13 +393,13 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
   };
   float old[16];                                           // (of one block: requested now, needed at the end)
   if (STEP == STEP_LAST && NB == 1) old_weights(p, d.q, d.ti * 2 + wi, d.tj * 2 + wj, old);
-  f32x16 acc[NB][NB];
+  f32x16 acc[NB][NB], low[NB][NB];                         // sums of hi hi; of hi lo + lo hi
 #pragma unroll
   for (int a = 0; a < NB; ++a)
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+      for (int r = 0; r < 16; ++r) acc[a][b][r] = low[a][b][r] = 0.f;
   // this block's part of the sums (kbs is a multiple of four)
   const int per = (d.kbs / KB + d.parts - 1) / d.parts, first = d.part * per, stages = first + per < d.kbs / KB ? per : d.kbs / KB - first;
 #pragma unroll
@@ -413,9 +417,9 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     }
   };
   auto multiply = [&](const Fragments &f) {
-    add_products<NB>(acc, f.ph, f.ql);
-    add_products<NB>(acc, f.pl, f.qh);
+    add_products<NB>(low, f.ph, f.ql);
     add_products<NB>(acc, f.ph, f.qh);
+    add_products<NB>(low, f.pl, f.qh);
   };
   // A stage is there: this wave's part (loads arrive in order; `behind` stages behind it may be on their way still), and behind the barrier all of it;
   // and what was read from LDS before is in registers everywhere
@@ -458,6 +462,12 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
       buffer ^= 1;
     }
   }
+#pragma unroll
+  for (int a = 0; a < NB; ++a)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[a][b][r] += kLowDown * low[a][b][r];
   if (d.parts > 1) {
     // The part is laid down, past the L2 that other XCDs do not see; the block that comes last adds up all of them in order.
     constexpr int kTileFloats = T * T;
@@ -512,8 +522,8 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 // Wave w keeps columns 32 w .. 32 w + 31 of X in registers, as the products leave them: x[b][r] is row 32 b + 8 (r / 4) + 4 (lane / 32) + r % 4 of column
 // 32 w + lane % 32, times 2^12, in fp32. For A = X X^T the waves lay X down in LDS in fragment order (turned round on the way) and share out the four
 // 32 x 32 blocks of A, a part of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
-// Bound by latency: 64 x 256 takes 4.3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 7 us a call besides, five steps
-// 28 us (64 x 64 20, 64 x 512 44). All of the vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half
+// Bound by latency: 64 x 256 takes 4.3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 8 us a call besides, five steps
+// 29 us (64 x 64 21, 64 x 512 46). All of the vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half
 // of the rows behind the other's stores, this was 2 us more. Sixteen waves have 128 registers each and do it so: with all at the start, and with the entries'
 // indices kept for the end, they spilled 116 bytes a lane, and 64 x 512 took 49 us.
 constexpr int kSmallRows = 64;
@@ -544,6 +554,17 @@ __device__ __forceinline__ void put_four(_Float16 *to, int ib, int jb, int s, in
   _Float16 *o = to + (jb * 4 + ib * 2 + (s >> 1)) * 1024 + ((lane & 31) + 32 * (s & 1)) * 8 + 4 * (lane >> 5);
   *(f16x4 *)o = hi;
   *(f16x4 *)(o + 512) = lo;
+}
+
+// The three products of the halves of two factors, 32 x 32 x 16: hi hi to acc, hi lo + lo hi to low; and their sum, in acc.
+__device__ __forceinline__ void add_halves(f32x16 &acc, f32x16 &low, const f16x8 &ah, const f16x8 &al, const f16x8 &bh, const f16x8 &bl) {
+  low = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, low, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
+  low = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, low, 0, 0, 0);
+}
+__device__ __forceinline__ void join_halves(f32x16 &acc, const f32x16 &low) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] += kLowDown * low[r];
 }
 
 template <int WAVES>
@@ -644,17 +665,13 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
         }
     }
     __syncthreads();
-    f32x16 acc;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+    f32x16 acc = {}, low = {};
     const int kbs = 2 * used, per = (kbs + PARTS - 1) / PARTS, k0 = part * per, k1 = k0 + per < kbs ? k0 + per : kbs;
     for (int kb = k0; kb < k1; ++kb) {
       const _Float16 *a = X + (kb * 2 + ib) * 1024 + lane * 8, *b = X + (kb * 2 + jb) * 1024 + lane * 8;
-      const f16x8 ah = *(const f16x8 *)a, al = *(const f16x8 *)(a + 512), bh = *(const f16x8 *)b, bl = *(const f16x8 *)(b + 512);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
+      add_halves(acc, low, *(const f16x8 *)a, *(const f16x8 *)(a + 512), *(const f16x8 *)b, *(const f16x8 *)(b + 512));
     }
+    join_halves(acc, low);
     __syncthreads();                                       // (the parts take X's place)
 #pragma unroll
     for (int s = 0; s < 4; ++s) parts[(wave * 4 + s) * 64 + lane] = f32x4{acc[4 * s], acc[4 * s + 1], acc[4 * s + 2], acc[4 * s + 3]};
@@ -672,16 +689,14 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
     __syncthreads();
     if (wave < 4) {                                        // B = a I + b A + c A A, a block a wave
       const int bi = wave >> 1, bj = wave & 1;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+      f32x16 low = {};
+      acc = f32x16{};
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
         const _Float16 *a = A + (bi * 4 + kb) * 1024 + lane * 8, *b = A + (bj * 4 + kb) * 1024 + lane * 8;
-        const f16x8 ah = *(const f16x8 *)a, al = *(const f16x8 *)(a + 512), bh = *(const f16x8 *)b, bl = *(const f16x8 *)(b + 512);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
+        add_halves(acc, low, *(const f16x8 *)a, *(const f16x8 *)(a + 512), *(const f16x8 *)b, *(const f16x8 *)(b + 512));
       }
+      join_halves(acc, low);
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const _Float16 *o = A + (bj * 4 + bi * 2 + (s >> 1)) * 1024 + (jl + 32 * (s & 1)) * 8 + 4 * g;
@@ -689,7 +704,7 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          v[e] = kNsC * (acc[4 * s + e] * kDown) + (kNsB * ((float)h[e] + (float)l[e]) + (bi == bj && 8 * s + 4 * g + e == jl ? kNsA * kUp : 0.f));
+          v[e] = kNsC * (acc[4 * s + e] * kDown) + (kNsB * ((float)h[e] + kLowDown * (float)l[e]) + (bi == bj && 8 * s + 4 * g + e == jl ? kNsA * kUp : 0.f));
         put_four(B, bi, bj, s, lane, v);
       }
     }
@@ -714,16 +729,14 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
       }
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+        f32x16 low = {};
+        acc = f32x16{};
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
           const _Float16 *o = B + (b * 4 + kb) * 1024 + lane * 8;
-          const f16x8 bh = *(const f16x8 *)o, bl = *(const f16x8 *)(o + 512);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh, xl[kb], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(bl, xh[kb], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(bh, xh[kb], acc, 0, 0, 0);
+          add_halves(acc, low, *(const f16x8 *)o, *(const f16x8 *)(o + 512), xh[kb], xl[kb]);
         }
+        join_halves(acc, low);
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[b][r] = acc[r] * kDown;
       }
@@ -838,8 +851,8 @@ int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
     rows = std::max(rows, p.mat[k].m);
     cols = std::max(cols, p.mat[k].n);
   }
-  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 20 / 28, 64 x 256 65 / 28 / 36, ten of 64 x 128
-  // 63 / 26 / 31; 64 x 512 75 / - / 44
+  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 21 / 28, 64 x 256 65 / 29 / 36, ten of 64 x 128
+  // 63 / 26 / 31; 64 x 512 75 / - / 46
   if (rows <= kSmallRows && cols <= 256) return launch_small<8>(c, p, steps);
   if (rows <= kSmallRows && cols <= 512) return launch_small<16>(c, p, steps);
   int64_t at = 0;
