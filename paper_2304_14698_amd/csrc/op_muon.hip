@@ -428,6 +428,7 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     if (all) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(behind)::value * kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");                          // no read of the stage is moved in front of the barrier
   };
   Fragments f0, f1;
   int buffer = 0;
