@@ -369,7 +369,8 @@ typedef struct xrl_logits_desc {
  *   logp = x[id] - ln sum exp x,  entropy = -sum p ln p,  top_ids / top_logp [n_rows, top_k] = the entries of the largest logits in
  *   falling order, the lowest index first among equals, and their log-probabilities.
  * d_ids [n_rows] (NULL: none is given, and d_logp may be NULL): index inside the row. A negative id is no token: logp 0. An id behind the row's
- * end, or of an entry that may not be chosen: -inf, and only then (a logp below fp32's lowest value is that value). Alternatives that a row does not have are -1 and -inf. A row with
+ * end, or of an entry that may not be chosen: -inf, and only then (a logp below fp32's lowest value is that value). Alternatives that a row does not have are -1 and -inf; one that it has
+ * (an index, not -1) has a top_logp of -inf, too, where that lies below fp32's lowest value. A row with
  * nothing to choose has logp -inf and entropy 0. A NaN or +inf that may be chosen makes the row's logp, entropy and top_logp NaN.
  * d_stats [n_rows, 2] (or NULL): the largest logit and ln sum exp(x - largest), for the backward call. top_k: 0 (the two arrays
  * may be NULL) to 64. Errors: NULL, SHAPE, UNSUPPORTED (type, top_k), VALUE (temperature), OOM, HIP. */
