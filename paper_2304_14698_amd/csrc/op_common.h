@@ -30,9 +30,6 @@ inline size_t op_align(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
 inline bool op_type_ok(int32_t type) { return type == XRL_PREC_FP32 || type == XRL_PREC_BF16; }
 
-// Whether rows of `stride` elements of `elem` bytes from p on all begin at multiples of 16 bytes.
-inline bool rows_aligned(const void *p, int64_t stride, int elem) { return ((uintptr_t)p | (uintptr_t)(stride * elem)) % 16 == 0; }
-
 // N elements from p, which may lie at any multiple of the element's size. STREAM: what is read for the last time, 16-byte pieces that leave no copy in
 // the caches.
 template <typename T, int N>
