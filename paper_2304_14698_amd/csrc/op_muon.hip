@@ -469,7 +469,7 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][b][r] += kLowDown * low[a][b][r];
-  if (d.parts > 1) {
+  if (T == 64 && (STEP == STEP_GRAM || STEP == STEP_POLY) && d.parts > 1) {   // (no other sums are cut)
     // The part is laid down, past the L2 that other XCDs do not see; the block that comes last adds up all of them in order.
     constexpr int kTileFloats = T * T;
     const int64_t mine = (int64_t)wave * NB * NB * 1024 + lane;
