@@ -183,12 +183,12 @@ __global__ __launch_bounds__(256) void muon_begin_kernel(const MuonArgs p) {
   const int n_sums = (int)(((int64_t)q.m * q.n + q.chunk - 1) / q.chunk);
   for (int i = lane; i < n_sums; i += 64) sum += p.sums[q.first_sum + i];
   for (int s = 32; s; s /= 2) sum += __shfl_xor(sum, s);
-  const float inv = (float)(1. / (sqrt(sum) + 1e-7));
+  const float scale = (float)(kUp / (sqrt(sum) + 1e-7));   // (of a norm from 2^126 on 1 / |U| alone would be subnormal)
   __shared__ float x[kTile][kTile + 1];
 #pragma unroll
   for (int u = 0; u < kTile * kTile / 256; ++u) {
     const int a = wave_of(t) + u * 4, b = lane;
-    x[q.t ? b : a][q.t ? a : b] = (p.nesterov ? g[u] + p.mu * m[u] : m[u]) * inv * kUp;
+    x[q.t ? b : a][q.t ? a : b] = (p.nesterov ? g[u] + p.mu * m[u] : m[u]) * scale;
   }
   __syncthreads();
   for (int s = t; s < 512; s += 256) {
@@ -623,11 +623,11 @@ __global__ __launch_bounds__(WAVES * 64) void muon_small_kernel(const MuonArgs p
     __syncthreads();
     sum = 0.;
     for (int k = 0; k < WAVES; ++k) sum += sums[k];
-    const float inv = (float)(1. / (sqrt(sum) + 1e-7));
+    const float scale = (float)(kUp / (sqrt(sum) + 1e-7));
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[b][r] = x[b][r] * inv * kUp;
+      for (int r = 0; r < 16; ++r) x[b][r] *= scale;
     __syncthreads();
   }
   // 32 x 32 between the vector's order of a transposed matrix and x's, in place; the other way round `back`
