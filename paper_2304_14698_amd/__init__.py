@@ -464,6 +464,8 @@ class Encoder:
 
     def _logits(self, logits, mask, row_ptr, temperature):
         t = self.torch
+        if mask is not None and mask.dtype == t.bool:
+            mask = mask.view(t.uint8)                # the same bytes
         if row_ptr is not None:
             n, total = row_ptr.numel() - 1, logits.numel()
             if n < 0:
@@ -474,7 +476,7 @@ class Encoder:
         stride, mstride = self._rows(logits, "logits"), 0
         if mask is not None:
             if mask.dtype != t.uint8:
-                raise ValueError(f"mask: {mask.dtype}, uint8 is needed")
+                raise ValueError(f"mask: {mask.dtype}, uint8 or bool is needed")
             if mask.dim() == 1:
                 self._flat(mask, "mask", t.uint8, logits.shape[1])
             else:
@@ -485,7 +487,7 @@ class Encoder:
     def token_logp(self, logits, ids=None, mask=None, row_ptr=None, top_k=0, temperature=1.0, out=None):
         """Of every row of logits [n, cols] -- or, with row_ptr [n + 1] int32, of every range of flat logits --: dict(logp, entropy
         [n], stats [n, 2] for the backward call, and with top_k: top_ids, top_logp [n, top_k]). ids int32 (None: no logp), mask
-        uint8 like the logits or, dense, one row for all; out: a dict that an earlier call of these sizes gave, written again. See
+        uint8 or bool like the logits or, dense, one row for all; out: a dict that an earlier call of these sizes gave, written again. See
         xrl_token_logp."""
         t = self.torch
         d = self._logits(logits, mask, row_ptr, temperature)
