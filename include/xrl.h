@@ -345,8 +345,8 @@ int xrl_embedding(xrl_ctx *ctx, const void *d_table, int32_t table_type, int64_t
                   const int32_t *d_ids, int64_t n, float scale, void *d_out, int32_t out_type, int64_t out_stride);
 
 /* xrl_embedding_backward: dtable[v, :] += scale * sum of dout[t, :] over the t with ids[t] = v, added up in fp32 in a fixed order; ids
- * outside [0, vocab) add nothing, and rows that no id names are neither read nor written. d_dout [n, dim] of dout_type, d_dtable
- * [vocab, dim] fp32. Errors: NULL, SHAPE, UNSUPPORTED (type; n from 2^27 or vocab from 2^30 on), OOM, HIP. */
+ * outside [0, vocab) add nothing, and rows that no id names are neither read nor written. d_dout [n, dim] of dout_type (dout_stride 0:
+ * one row for all t), d_dtable [vocab, dim] fp32. Errors: NULL, SHAPE, UNSUPPORTED (type; n from 2^27 or vocab from 2^30 on), OOM, HIP. */
 int xrl_embedding_backward(xrl_ctx *ctx, const void *d_dout, int32_t dout_type, int64_t dout_stride, const int32_t *d_ids,
                            int64_t n, int64_t vocab, int64_t dim, float scale, float *d_dtable, int64_t dtable_stride);
 

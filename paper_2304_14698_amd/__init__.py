@@ -451,7 +451,7 @@ class Encoder:
         return out
 
     def embedding_backward(self, dout, ids, dtable, scale=1.0):
-        """dtable[v] += scale * sum of the rows of dout whose id is v (dtable float32); returns dtable."""
+        """dtable[v] += scale * sum of the rows of dout whose id is v (dtable float32, dout's one row may be expanded); returns dtable."""
         t = self.torch
         n, dim = dout.shape[0], dtable.shape[1]
         stride, tstride = self._rows(dout, "dout", (n, dim)), self._rows(dtable, "dtable")

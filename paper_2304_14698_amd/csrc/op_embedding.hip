@@ -745,7 +745,7 @@ int xrl_embedding_backward(xrl_ctx *c, const void *d_dout, int32_t dout_type, in
   const char *who = "xrl_embedding_backward";
   if (!c) return fail(XRL_ERR_NULL, "%s: ctx is NULL", who);
   if (!op_type_ok(dout_type)) return fail(XRL_ERR_UNSUPPORTED, "%s: type %d", who, dout_type);
-  if (n < 0 || vocab < 0 || dim < 0 || dout_stride < dim || dtable_stride < dim)
+  if (n < 0 || vocab < 0 || dim < 0 || (dout_stride < dim && dout_stride != 0) || dtable_stride < dim)   // (0: one row for all, as a broadcast's gradient has)
     return fail(XRL_ERR_SHAPE, "%s: n = %lld, vocab = %lld, dim = %lld, strides %lld and %lld", who, (long long)n, (long long)vocab,
                 (long long)dim, (long long)dout_stride, (long long)dtable_stride);
   if (n >= 1 << 27 || vocab >= 1 << 30 || dim > (1 << 20))
