@@ -543,7 +543,10 @@ class Encoder:
         """One step of momentum with orthogonalised updates, in place, on the matrices of flat float32 vectors (see
         xrl_muon_step): matrices = [(offset, rows, cols)], a list or an int64 array (see weight_matrices)."""
         f, n = self.torch.float32, weights.numel()
-        m = np.ascontiguousarray(matrices, dtype=np.int64).reshape(-1, 3)
+        m = np.asarray(matrices)
+        if m.size and (m.ndim != 2 or m.shape[1] != 3 or m.dtype.kind not in "iu"):
+            raise ValueError(f"matrices: shape {m.shape} of {m.dtype}, [count, 3] of integers is needed")
+        m = np.ascontiguousarray(m, dtype=np.int64).reshape(-1, 3)
         d = MuonDesc(lr, beta, weight_decay, rms, int(nesterov), steps)
         _check(self.lib.xrl_muon_step(self.handle, C.byref(d), m.shape[0], m.ctypes.data, n,
                                       self._flat(weights, "weights", f, n), self._flat(grads, "grads", f, n),
