@@ -33,6 +33,8 @@ constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;
 constexpr float kLowUp = 2048.f, kLowDown = 1.f / 2048.f;   // of the lower halves besides
 constexpr int kGroup = 32;             // matrices of one launch: their list is a kernel argument
+constexpr int64_t kGroupHalves = (int64_t)1 << 30;   // operands of a group that has more than one: 2 GB, several times what fills the chip (two 2048^2 and two
+                                                    // 2048 x 8192 are 0.5); a model of thirty-two 16384^2 would need 172 GB for them at once
 constexpr int kTile = 64;              // sizes are padded to multiples of this
 constexpr int kMaxSums = 1024;         // partial sums of squares of a matrix
 
@@ -932,14 +934,17 @@ int xrl_muon_step(xrl_ctx *c, const xrl_muon_desc *desc, int32_t n_matrices, con
   std::vector<MuonArgs> groups;
   size_t most = 0, floats = 0, counters = 0;
   try {
-    for (size_t i = 0; i < list.size(); i += kGroup) {
+    for (size_t i = 0; i < list.size();) {
       MuonArgs p = {};
-      p.count = (int)std::min<size_t>(kGroup, list.size() - i);
       int64_t halves = 0;
-      for (int k = 0; k < p.count; ++k) {
-        Mat &q = p.mat[k] = list[i + k];
+      while (p.count < kGroup && i < list.size()) {
+        Mat q = list[i];
+        const int64_t more = 3 * x_halves(q.m, q.n) + 2 * x_halves(q.m, q.m);
+        if (p.count > 0 && halves + more > kGroupHalves) break;
         q.ws = halves;
-        halves += 3 * x_halves(q.m, q.n) + 2 * x_halves(q.m, q.m);
+        halves += more;
+        p.mat[p.count++] = q;
+        ++i;
       }
       most = std::max(most, (size_t)halves * 2);
       for (int step : {STEP_GRAM, STEP_POLY}) {
