@@ -258,17 +258,30 @@ __device__ __forceinline__ Product product_of(const MuonArgs &p) {
   return d;
 }
 
-// The last product's entry r of a lane in its matrix of the vector, lanes along that one's rows (of a matrix taken transposed: along i); -1: none.
-__device__ __forceinline__ int64_t weight_at(const Mat &q, int ib, int jb, int r) {
-  const int lane = threadIdx.x & 63, g = lane >> 5, jl = lane & 31;
-  const int i = ib * 32 + (q.t ? jl : acc_row(r, g)), j = jb * 32 + (q.t ? 2 * r + g : jl);
-  return i < q.m && j < q.n ? (q.t ? (int64_t)j * q.m + i : (int64_t)i * q.n + j) : -1;
-}
+// The last product's entries of a lane in its matrix of the vector, lanes along that one's rows (of a matrix taken transposed: along i); -1: none.
+// (Sums of products with what depends on the block alone: a choice between the two orders at each entry makes branches. A matrix has at most 2^30 entries.)
+struct Entries {
+  int first, of_r, of_q, row_r, left;
+  bool in;
+  __device__ Entries(const Mat &q, int ib, int jb) {
+    const int lane = threadIdx.x & 63, g = lane >> 5, jl = lane & 31;
+    const int row = q.t ? jb * 32 + g : ib * 32 + 4 * g, col = (q.t ? ib : jb) * 32 + jl, rows = q.t ? q.n : q.m, cols = q.t ? q.m : q.n;
+    first = row * cols + col;
+    row_r = q.t ? 2 : 1;                                   // register r: 2 r rows on, or 8 (r / 4) + r % 4
+    of_r = row_r * cols;
+    of_q = 8 * cols;
+    left = rows - row;
+    in = col < cols;
+  }
+  __device__ int at(int r) const { return (in & ((r & 3) * row_r + 8 * (r >> 2) < left)) ? first + (r & 3) * of_r + (r >> 2) * of_q : -1; }
+};
 __device__ __forceinline__ void old_weights(const MuonArgs &p, const Mat &q, int ib, int jb, float *old) {
+  const Entries e(q, ib, jb);
+  const float *w = p.w + q.offset;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const int64_t at = weight_at(q, ib, jb, r);
-    old[r] = p.w[q.offset + (at >= 0 ? at : 0)];
+    const int at = e.at(r);
+    old[r] = w[at >= 0 ? at : 0];
   }
 }
 
@@ -294,9 +307,10 @@ __device__ __forceinline__ void put(const MuonArgs &p, const Product &d, const f
       __builtin_amdgcn_wave_barrier();
     }
     float *w = p.w + q.offset;
+    const Entries e(q, ib, jb);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int64_t at = weight_at(q, ib, jb, r);
+      const int at = e.at(r);
       if (at >= 0) w[at] = p.decay * old[r] - step * y[r];
     }
     return;
