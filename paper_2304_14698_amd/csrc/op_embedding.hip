@@ -608,7 +608,7 @@ __device__ __forceinline__ void add_run(const SumArgs &a, const Run &r, const Co
 // pieces are then taken by all waves of the block, a part of the pieces each, and their sums in order. A block for every run leaves most of its waves
 // idle, a wave for every run is long at an id that fills the batch: us of this kernel at 65536 long-tailed ids of 1024 columns, and of the whole
 // call at 131072 times the same id of 128 columns: sixteen waves a run 49 and 113, four 17 and 263, this 19 and 197; since
-// the row of the table is asked for together with the pieces and the nearest 64 windows are looked at first, 17 and 150 (of which this kernel is 112: one
+// the row of the table is asked for together with the pieces and the nearest 64 windows are looked at first, 14 and 150 (of which this kernel is 112: one
 // compute unit takes in 4 MB).
 constexpr int kFewPieces = 32;
 template <int N>

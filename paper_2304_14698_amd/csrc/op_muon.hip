@@ -376,8 +376,9 @@ __device__ __forceinline__ void add_products(f32x16 (*acc)[NB], const f16x8 *p, 
 // LDS, where two waves each read them; while a stage is multiplied those behind it are on their way. Tiles of 64 x 64, which often are alone on a compute
 // unit, also read the fragments of each product from LDS while the one before is multiplied, across the barrier between two stages too: a lone block's stage
 // 0.25 us, 0.31 without that. (530 clocks, of which the LDS takes 384 to be written and read and the matrix pipes 192.) Of tiles of 128 x 128 two blocks
-// fill in for each other: X X^T of two 2048^2 and two 2048 x 8192 342 us so, 331 without. Of these four matrices B X takes 500 us, 515 GF of fp16 products at
-// 1.03 PFLOP/s, bound by the matrix cores; A A 142 and X X^T 330, 0.77 and 0.83: 544 tiles on 512 places, whose last ones have the chip to themselves. Of
+// fill in for each other: X X^T of two 2048^2 and two 2048 x 8192 342 us so, 331 without. Of these four matrices B X takes 500 us (520 on a machine at
+// 1.76 GHz), 515 GF of fp16 products at 1.03 PFLOP/s, bound by the matrix cores; A A 142 and X X^T 330, 0.77 and 0.83: 544 tiles on 512 places, whose last ones
+// have the chip to themselves. Of
 // smaller matrices a product is bound by the latency of its launch, the first stage and the last: 6 to 12 us for those of a 256-wide agent.
 template <int STEP, int T, int STAGES>
 __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) {
@@ -540,7 +541,7 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(const MuonArgs p) 
 // 32 w + lane % 32, times 2^12, in fp32. For A = X X^T the waves lay X down in LDS in fragment order (turned round on the way) and share out the four
 // 32 x 32 blocks of A, a part of the summed columns each; for B X a wave's own columns become its operand by exchanges between the two halves of the wave.
 // Bound by latency: 64 x 256 takes 4.3 us a step (turning, X X^T, joining its parts, B, B X with a barrier behind each) and 8 us a call besides, five steps
-// 29 us (64 x 64 21, 64 x 512 46). All of the vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half
+// 29 us (64 x 64 21, 64 x 512 47). All of the vectors' entries are requested at the start; with the weights requested at the end, and the requests of each half
 // of the rows behind the other's stores, this was 2 us more. Sixteen waves have 128 registers each and do it so: with all at the start, and with the entries'
 // indices kept for the end, they spilled 116 bytes a lane, and 64 x 512 took 49 us.
 constexpr int kSmallRows = 64;
@@ -868,8 +869,8 @@ int run_group(xrl_ctx *c, MuonArgs &p, int steps) {
     rows = std::max(rows, p.mat[k].m);
     cols = std::max(cols, p.mat[k].n);
   }
-  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 21 / 28, 64 x 256 65 / 29 / 36, ten of 64 x 128
-  // 63 / 26 / 31; 64 x 512 75 / - / 46
+  // us a call of five steps, in launches of their own / a block each of eight waves / of sixteen: 64 x 64 54 / 21 / 26, 64 x 256 65 / 29 / 34, ten of 64 x 128
+  // 62 / 24 / 28; 64 x 512 74 / - / 47
   if (rows <= kSmallRows && cols <= 256) return launch_small<8>(c, p, steps);
   if (rows <= kSmallRows && cols <= 512) return launch_small<16>(c, p, steps);
   int64_t at = 0;
