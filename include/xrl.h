@@ -413,6 +413,39 @@ typedef struct xrl_muon_desc {
 int xrl_muon_step(xrl_ctx *ctx, const xrl_muon_desc *desc, int32_t n_matrices, const xrl_matrix *matrices, int64_t n_weights,
                   float *d_weights, const float *d_grads, float *d_momentum);
 
+/* ---- operators over histories ----------------------------------------------------------------
+ * What a policy needs that reads a history (the rules applied so far, tokens) in order: attention with its positions, for an update over whole packed
+ * histories and for a rollout that adds to a cache. Stream, workspace, types, alignment and errors as above. A tensor [n, heads, dim] is given by its address and
+ * strides; dim is contiguous. What is only read may overlap (strides of 0), what is written may not. */
+typedef struct xrl_heads {
+  void *d_data;
+  int64_t stride, head_stride;   /* elements from one row to the next, and from one head to the next */
+} xrl_heads;
+
+/* Packed sequences: sequence s has rows [d_q_ptr[s], d_q_ptr[s + 1]) of the queries and [d_k_ptr[s], d_k_ptr[s + 1]) of keys and values (the same array where they are
+ * the same rows). The arrays must not fall; what they say outside the tensors counts as not there. Query head h reads the key head h / (q_heads / kv_heads). */
+typedef struct xrl_attention_desc {
+  int64_t n_seqs, n_q, n_k;      /* sequences; rows of the tensors of queries, and of keys and values */
+  const int32_t *d_q_ptr, *d_k_ptr;   /* [n_seqs + 1]                                                 */
+  int32_t q_heads, kv_heads, dim;
+  int32_t type;
+  int32_t causal;                /* not 0: row i of a sequence of n rows and m keys sees keys 0 .. i + m - n, else all m */
+  float scale;                   /* > 0, usually dim^-1/2                                             */
+} xrl_attention_desc;
+
+/* xrl_attention: per sequence and head, with s_ij = scale q_i . k_j over the keys that row i sees,
+ *   lse_i = ln sum_j exp s_ij,  out_i = sum_j exp(s_ij - lse_i) v_j.
+ * q, out [n_q, q_heads, dim], k, v [n_k, kv_heads, dim], d_lse [n_q, q_heads] fp32. Sums and exponentials in fp32; in bf16 the exponentials are rounded to it as factors of v.
+ * A row that sees no key, or keys of score -inf alone, has out 0 and lse -inf. Rows of no sequence are left as they were. A NaN or infinity in a key or value reaches the rows that see it, as NaN or
+ * infinity, and no others. Errors: NULL, SHAPE, VALUE (scale), UNSUPPORTED (type, dim above 128, strides above 2^23), HIP. */
+int xrl_attention(xrl_ctx *ctx, const xrl_attention_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out, float *d_lse);
+
+/* xrl_attention_backward: from the inputs, xrl_attention's results and dout = dJ/dout the gradients dq, dk, dv, of the inputs' shapes and type, written (not added to).
+ * The gradients of a key head are sums over the query heads that share it, in a fixed order. Rows of no sequence are left as they were; keys that no row sees get 0.
+ * Errors: as above, OOM. */
+int xrl_attention_backward(xrl_ctx *ctx, const xrl_attention_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out,
+                           const float *d_lse, const xrl_heads *dout, const xrl_heads *dq, const xrl_heads *dk, const xrl_heads *dv);
+
 /* ---- building blocks exposed for measurement and per-step checks ----------------------------
  * xrl_segment_sum: out[i, :] = sum of values[r, :] over rows r in [d_ptr[i], d_ptr[i+1]) -- the
  * receiver-side aggregation of Section 3.4's first two equations on receiver-ordered rows, and

@@ -70,6 +70,16 @@ class MuonDesc(C.Structure):
                 ("nesterov", C.c_int32), ("steps", C.c_int32)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("d_data", C.c_void_p), ("stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [("n_seqs", C.c_int64), ("n_q", C.c_int64), ("n_k", C.c_int64), ("d_q_ptr", C.c_void_p), ("d_k_ptr", C.c_void_p),
+                ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("type", C.c_int32), ("causal", C.c_int32),
+                ("scale", C.c_float)]
+
+
 EXPORTS = ["xrl_weight_count", "xrl_weight_tensor_count", "xrl_weight_tensor", "xrl_pack_state", "xrl_pack_state_edits",
            "xrl_batch_dims", "xrl_batch_level", "xrl_batch_host_view", "xrl_batch_free", "xrl_create",
            "xrl_set_weights", "xrl_destroy", "xrl_batch_upload", "xrl_encode", "xrl_policy_value",
@@ -77,7 +87,8 @@ EXPORTS = ["xrl_weight_count", "xrl_weight_tensor_count", "xrl_weight_tensor", "
            "xrl_policy_value_backward", "xrl_encode_backward", "xrl_ppo_objective", "xrl_segment_sum",
            "xrl_get_activation", "xrl_set_timing", "xrl_read_timing", "xrl_measure_peaks",
            "xrl_edge_features_from_shapes", "xrl_weight_gradient", "xrl_mlp_backward", "xrl_embedding",
-           "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_muon_step", "xrl_last_error", "xrl_version"]
+           "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_muon_step",
+           "xrl_attention", "xrl_attention_backward", "xrl_last_error", "xrl_version"]
 
 
 def load_library():
@@ -124,6 +135,9 @@ def load_library():
     lib.xrl_token_logp.argtypes = [vp, C.POINTER(LogitsDesc), vp, i32] + [vp] * 5
     lib.xrl_token_logp_backward.argtypes = [vp, C.POINTER(LogitsDesc)] + [vp] * 7 + [i64]
     lib.xrl_muon_step.argtypes = [vp, C.POINTER(MuonDesc), i32, vp, i64, vp, vp, vp]
+    hp = C.POINTER(Heads)
+    lib.xrl_attention.argtypes = [vp, C.POINTER(AttentionDesc)] + [hp] * 4 + [vp]
+    lib.xrl_attention_backward.argtypes = [vp, C.POINTER(AttentionDesc)] + [hp] * 4 + [vp] + [hp] * 4
     lib.xrl_last_error.restype = C.c_char_p
     lib.xrl_version.restype = C.c_char_p
     _lib = lib
@@ -551,6 +565,74 @@ class Encoder:
         _check(self.lib.xrl_muon_step(self.handle, C.byref(d), m.shape[0], m.ctypes.data, n,
                                       self._flat(weights, "weights", f, n), self._flat(grads, "grads", f, n),
                                       self._flat(momentum, "momentum", f, n)))
+
+    # ---- operators over histories (see xrl.h)
+
+    def _heads(self, x, name, shape=None, type=None):
+        """A tensor [n, heads, dim] on the context's GPU, dim contiguous, as the library takes it."""
+        if x.dim() != 3 or x.device != self._device:
+            raise ValueError(f"{name}: a tensor [n, heads, dim] on {self._device} is needed")
+        if shape is not None and x.shape != shape:
+            raise ValueError(f"{name}: shape {tuple(x.shape)}, {tuple(shape)} is needed")
+        if type is not None and x.dtype != type:
+            raise ValueError(f"{name}: {x.dtype}, {type} is needed")
+        stride, head_stride, step = x.stride()
+        if step != 1 and x.shape[2] > 1:
+            raise ValueError(f"{name}: heads of contiguous columns are needed")
+        return Heads(x.data_ptr(), stride, head_stride)
+
+    def _here(self, x, name, dtype, n):
+        """As _flat, on the context's GPU."""
+        if x is not None and x.device != self._device:
+            raise ValueError(f"{name}: a tensor on {self._device} is needed")
+        return self._flat(x, name, dtype, n)
+
+    def _attention(self, q, k, v, q_ptr, k_ptr, causal, scale):
+        t = self.torch
+        hq = self._heads(q, "q")
+        n, heads, dim = q.shape
+        hk = self._heads(k, "k", type=q.dtype)
+        m, kv = k.shape[:2]
+        if k.shape[2] != dim or kv < 1 or heads % kv:
+            raise ValueError(f"k: shape {tuple(k.shape)} with q of {tuple(q.shape)}")
+        hv = self._heads(v, "v", k.shape, q.dtype)
+        if q_ptr.numel() < 1:
+            raise ValueError("q_ptr: at least one element is needed")
+        if k_ptr is None and m != n:
+            raise ValueError(f"k: {m} rows with q of {n}, and no k_ptr")
+        seqs = q_ptr.numel() - 1
+        at = self._here(q_ptr, "q_ptr", t.int32, seqs + 1)
+        d = AttentionDesc(seqs, n, m, at, at if k_ptr is None else self._here(k_ptr, "k_ptr", t.int32, seqs + 1), heads, kv, dim,
+                          self._type(q, "q"), int(causal), dim ** -0.5 if scale is None else scale)
+        return d, hq, hk, hv
+
+    def attention(self, q, k, v, q_ptr, k_ptr=None, causal=True, scale=None, out=None):
+        """Attention over packed sequences: q [n, heads, dim], k and v [m, kv heads, dim], q_ptr and k_ptr (None: the same) [sequences + 1] int32.
+        dict(out like q, lse [n, heads] for the backward call); out: a dict that an earlier call of these sizes gave, written again. See
+        xrl_attention."""
+        f = self.torch.float32
+        d, hq, hk, hv = self._attention(q, k, v, q_ptr, k_ptr, causal, scale)
+        if out is None:
+            o, lse = self._made((q.shape, q.dtype), (q.shape[:2], f))
+            out = dict(out=o, lse=lse)
+        ho = self._heads(out["out"], "out", q.shape, q.dtype)
+        _check(self.lib.xrl_attention(self.handle, C.byref(d), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho),
+                                      self._here(out["lse"], "lse", f, q.shape[0] * q.shape[1])))
+        return out
+
+    def attention_backward(self, q, k, v, q_ptr, forward, dout, k_ptr=None, causal=True, scale=None, out=None):
+        """(dq, dk, dv), like q, k and v, from `forward` (what attention gave) and dout = dJ/dout; out: three tensors to write them to. See
+        xrl_attention_backward."""
+        d, hq, hk, hv = self._attention(q, k, v, q_ptr, k_ptr, causal, scale)
+        if out is None:
+            out = self._made((q.shape, q.dtype), (k.shape, k.dtype), (v.shape, v.dtype))
+        dq, dk, dv = out
+        _check(self.lib.xrl_attention_backward(
+            self.handle, C.byref(d), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(self._heads(forward["out"], "out", q.shape, q.dtype)),
+            self._here(forward["lse"], "lse", self.torch.float32, q.shape[0] * q.shape[1]),
+            C.byref(self._heads(dout, "dout", q.shape, q.dtype)), C.byref(self._heads(dq, "dq", q.shape, q.dtype)),
+            C.byref(self._heads(dk, "dk", k.shape, k.dtype)), C.byref(self._heads(dv, "dv", v.shape, v.dtype))))
+        return dq, dk, dv
 
     def get_activation(self, batch, what, rnd=0):
         shape = {"a0": (batch.N, self.model["d_edge"]), "pool": (batch.G, self.H)}.get(what, (batch.N, self.H))

@@ -1,0 +1,174 @@
+// Attention over packed sequences.
+//
+// Per sequence and head, s_ij = scale q_i . k_j over the keys j that row i sees, p = softmax of a row, o_i = sum_j p_ij v_j. Scores are computed in tiles of
+// 32 x 32 on the matrix cores and never stored: a row's maximum and sum run along. An accumulator tile has one query a lane and keys in its registers, so maxima and sums are taken over
+// a lane's own registers, and these are the other operand of the second product as they lie (Tile::across reads the values in the same order).
+#include "attn_packed.hip.h"
+
+#include <type_traits>
+
+namespace {
+
+// One block: BM = 32 WAVES rows of one sequence and one head, KT keys at a time, two tiles of K and V each.
+template <typename T, int DP, int WAVES, int KT>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 : 2) void attention_kernel(const AttnArgs a) {
+  using L = Tile<T, DP>;
+  using vec = typename L::vec;
+  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB;
+  __shared__ __attribute__((aligned(16))) char lds[4 * BYTES];
+  touch_args(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
+  Place at;
+  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, lane, at)) return;
+  const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
+  const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
+  if (i0 < 0) return;
+  const int len_k = __builtin_amdgcn_readfirstlane(ks.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len);
+  const int kv = at.head / (a.q_heads / a.kv_heads);
+  // keys that rows i0 .. i0 + BM - 1 see, and that this wave's rows see, all of them and any
+  auto keys_of = [&](int i) { const int e = a.causal ? i + 1 + off : len_k; return e < 0 ? 0 : e < len_k ? e : len_k; };
+  const int last = (i0 + BM < qs.len ? i0 + BM : qs.len) - 1, w0 = i0 + 32 * wave, w1 = w0 + 31 < last ? w0 + 31 : last;
+  const int keys = __builtin_amdgcn_readfirstlane(keys_of(last)), tiles = (keys + KT - 1) / KT;
+  const int all_see = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w0) : 0), any_sees = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w1) : 0);
+  const int i = w0 + l32, mine = keys_of(i);        // keys that the lane's row sees
+  const bool there = i < qs.len;
+  vec q[L::SLABS];
+  load_row<T, DP>(q, head_at<T>(a.q, qs.begin + (there ? i : 0), at.head), there, a.dim_in, g);
+  const T *k = head_at<T>(a.k, ks.begin, kv), *v = head_at<T>(a.v, ks.begin, kv);
+  const unsigned base = lds_address(lds);
+  const float c = a.scale * kLog2e;
+  f32x16 o[L::BLOCKS];
+  float mc, l;
+  auto pass = [&](auto safe) {
+    constexpr bool SAFE = decltype(safe)::value;
+    mc = kLowest;
+    l = 0.f;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db) o[db] = zero_acc();
+    if (tiles > 0) {
+      stage_tile<T, DP, KT, WAVES>(k, keys, a.k.stride, a.dim_in, base, wave, lane);
+      stage_tile<T, DP, KT, WAVES>(v, keys, a.v.stride, a.dim_in, base + 2 * BYTES, wave, lane);
+    }
+    for (int t = 0; t < tiles; ++t) {
+      const unsigned kt = base + (t & 1) * BYTES, vt = kt + 2 * BYTES;
+      wait_direct_loads();
+      __syncthreads();                              // tile t is there, and t - 1 is read
+      if (t + 1 < tiles) {
+        const int64_t j = (int64_t)(t + 1) * KT;
+        stage_tile<T, DP, KT, WAVES>(k + j * a.k.stride, keys - (int)j, a.k.stride, a.dim_in, base + ((t + 1) & 1) * BYTES, wave, lane);
+        stage_tile<T, DP, KT, WAVES>(v + j * a.v.stride, keys - (int)j, a.v.stride, a.dim_in, base + ((t + 1) & 1) * BYTES + 2 * BYTES, wave, lane);
+      }
+      const int j0 = t * KT;
+      if (j0 >= any_sees) continue;
+      f32x16 s[KT / 32];
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb) {
+        s[kb] = zero_acc();
+#pragma unroll
+        for (int x = 0; x < L::SLABS; ++x) Operand<T>::mma(L::along(kt, 32 * kb, x, lane), q[x], s[kb]);
+      }
+      const bool whole = j0 + KT <= all_see;
+      if (!whole) {
+#pragma unroll
+        for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = sees(j0 + 32 * kb + acc_row(r, g), mine) ? s[kb][r] : -INFINITY;
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+      mx = half_max(mx) * c;
+      // The reference of the exponentials follows the maximum only where that has grown by 2^8: until then sums and results are up to 2^8 times as large, and nothing is
+      // multiplied. Each row by its own maximum: what shares its wave changes none of its bits.
+      const bool grown = mx > mc + 8.f;
+      if (__ballot(grown)) {
+        const float m = grown ? mx : mc, f = __builtin_amdgcn_exp2f(mc - m);
+        mc = m;
+        l *= f;
+#pragma unroll
+        for (int db = 0; db < L::BLOCKS; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[db][r] *= f;
+      }
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c, -mc));
+          l += s[kb][r];
+        }
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+        for (int x = 0; x < 32 / L::STEP; ++x) {
+          const vec p = acc_operand<T>(s[kb], x);
+          if (SAFE && !whole) {
+            vec seen;
+#pragma unroll
+            for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(j0 + 32 * kb + acc_row(x * L::V + n, g), mine) ? 1.f : 0.f);
+#pragma unroll
+            for (int db = 0; db < L::BLOCKS; ++db) mma_seen<T>(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, seen, o[db]);
+          } else {
+#pragma unroll
+            for (int db = 0; db < L::BLOCKS; ++db) Operand<T>::mma(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, o[db]);
+          }
+        }
+    }
+  };
+  pass(std::false_type());
+  // What stands in a key or value that a row does not see may have reached it through a product with 0. Where results are not finite, a second time with such
+  // places kept apart.
+  if (a.causal) {
+    bool fine = true;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(o[db]);
+    if (__syncthreads_or(!fine)) pass(std::true_type());
+  }
+  l = half_sum(l);
+  const bool any = !(l == 0.f);
+  store_row<T, DP>(head_at<T>(a.out, qs.begin + i, at.head), there, a.dim, a.quads, o, any ? 1.f / l : 0.f, g);
+  if (there && g == 0) a.lse[(qs.begin + i) * a.q_heads + at.head] = any ? mc * kLn2 + logf(l) : -INFINITY;
+}
+
+template <typename T, int DP>
+void launch(const xrl_ctx *c, AttnArgs &a) {
+  constexpr int KT = sizeof(T) == 2 ? 64 : 32;
+  if (a.n_q <= 64 * a.seqs) launch_tiles(c, a, attention_kernel<T, DP, 1, 32>, a.n_q, a.q_heads, 32, 64);
+  else launch_tiles(c, a, attention_kernel<T, DP, 4, KT>, a.n_q, a.q_heads, 128, 256);
+}
+template <typename T>
+void launch_dim(const xrl_ctx *c, AttnArgs &a) {
+  a.dim <= 32 ? launch<T, 32>(c, a) : a.dim <= 64 ? launch<T, 64>(c, a) : launch<T, 128>(c, a);
+}
+
+}  // namespace
+
+extern "C" int xrl_attention(xrl_ctx *c, const xrl_attention_desc *d, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out, float *d_lse) {
+  const char *who = "xrl_attention";
+  AttnArgs a;
+  if (int rc = check_attention(c, d, who, a)) return rc;
+  const int es = d->type == XRL_PREC_BF16 ? 2 : 4;
+  if (int rc = check_heads(q, d->n_q, d->q_heads, d->dim, es, "q", who, a.q)) return rc;
+  if (int rc = check_heads(k, d->n_k, d->kv_heads, d->dim, es, "k", who, a.k)) return rc;
+  if (int rc = check_heads(v, d->n_k, d->kv_heads, d->dim, es, "v", who, a.v)) return rc;
+  if (int rc = check_heads(out, d->n_q, d->q_heads, d->dim, es, "out", who, a.out, &a.quads)) return rc;
+  if (d->n_q > 0 && !d_lse) return fail(XRL_ERR_NULL, "%s: d_lse is NULL", who);
+  if ((uintptr_t)d_lse % 4) return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
+  if (d->n_q == 0 || d->n_seqs == 0) return XRL_OK;
+  a.lse = d_lse;
+  Inputs in(d->type, d->dim);
+  in.add(a.q, d->n_q, d->q_heads);
+  in.add(a.k, d->n_k, d->kv_heads);
+  in.add(a.v, d->n_k, d->kv_heads);
+  if (in.count) {
+    char *ws = nullptr;
+    if (int rc = op_workspace(c, in.bytes, &ws, who)) return rc;
+    in.copy(c, ws);
+  }
+  a.dim_in = in.dim_in;
+  d->type == XRL_PREC_BF16 ? launch_dim<bf16_t>(c, a) : launch_dim<float>(c, a);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}

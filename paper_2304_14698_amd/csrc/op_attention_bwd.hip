@@ -1,0 +1,296 @@
+// Gradients of attention over packed sequences.
+//
+// With p from the forward pass's lse and D_i = dout_i . out_i: ds_ij = p_ij (dout_i . v_j - D_i), dq_i = scale sum_j ds_ij k_j, dk_j = scale sum_i ds_ij q_i, dv_j = sum_i p_ij dout_i. Two kernels, each
+// of which computes the scores anew: one has a query a lane and sums over keys, the other a key a lane and sums over queries. That is seven products where one kernel
+// would do with five, but no sum is shared by blocks: no float atomics, the same bits from run to run.
+#include "attn_packed.hip.h"
+
+#include <type_traits>
+
+namespace {
+
+// dq, and of every row what the keys' gradients need besides: lse log2(e) and do . o. Rows and tiles as in the forward kernel.
+template <typename T, int DP, int WAVES, int KT>
+__global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnArgs a) {
+  using L = Tile<T, DP>;
+  using vec = typename L::vec;
+  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB;
+  __shared__ __attribute__((aligned(16))) char lds[4 * BYTES];
+  touch_args(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
+  Place at;
+  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, lane, at)) return;
+  const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
+  const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
+  if (i0 < 0) return;
+  const int len_k = __builtin_amdgcn_readfirstlane(ks.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len);
+  const int kv = at.head / (a.q_heads / a.kv_heads);
+  auto keys_of = [&](int i) { const int e = a.causal ? i + 1 + off : len_k; return e < 0 ? 0 : e < len_k ? e : len_k; };
+  const int last = (i0 + BM < qs.len ? i0 + BM : qs.len) - 1, w0 = i0 + 32 * wave, w1 = w0 + 31 < last ? w0 + 31 : last;
+  const int keys = __builtin_amdgcn_readfirstlane(keys_of(last)), tiles = (keys + KT - 1) / KT;
+  const int all_see = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w0) : 0), any_sees = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w1) : 0);
+  const int i = w0 + l32, mine = keys_of(i);
+  const bool there = i < qs.len;
+  const int64_t row = qs.begin + (there ? i : 0);
+  vec q[L::SLABS], dout[L::SLABS];
+  float delta = 0.f;
+  {
+    load_row<T, DP>(q, head_at<T>(a.out, row, at.head), there, a.dim_in, g);
+    load_row<T, DP>(dout, head_at<T>(a.dout, row, at.head), there, a.dim_in, g);
+#pragma unroll
+    for (int x = 0; x < L::SLABS; ++x)
+#pragma unroll
+      for (int j = 0; j < L::V; ++j) delta = fmaf((float)q[x][j], (float)dout[x][j], delta);
+    delta = half_sum(delta);
+  }
+  load_row<T, DP>(q, head_at<T>(a.q, row, at.head), there, a.dim_in, g);
+  // (a row without keys, or with scores of -inf alone: every exponential below is 0)
+  const float lse = a.lse[row * a.q_heads + at.head], lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  if (there && g == 0) {
+    a.stat_lse[at.head * a.n_q + row] = lse2;
+    a.stat_delta[at.head * a.n_q + row] = delta;
+  }
+  const T *k = head_at<T>(a.k, ks.begin, kv), *v = head_at<T>(a.v, ks.begin, kv);
+  const unsigned base = lds_address(lds);
+  const float c = a.scale * kLog2e;
+  f32x16 dq[L::BLOCKS];
+  auto pass = [&](auto safe) {
+    constexpr bool SAFE = decltype(safe)::value;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db) dq[db] = zero_acc();
+    if (tiles > 0) {
+      stage_tile<T, DP, KT, WAVES>(k, keys, a.k.stride, a.dim_in, base, wave, lane);
+      stage_tile<T, DP, KT, WAVES>(v, keys, a.v.stride, a.dim_in, base + 2 * BYTES, wave, lane);
+    }
+    for (int t = 0; t < tiles; ++t) {
+      const unsigned kt = base + (t & 1) * BYTES, vt = kt + 2 * BYTES;
+      wait_direct_loads();
+      __syncthreads();
+      if (t + 1 < tiles) {
+        const int64_t j = (int64_t)(t + 1) * KT;
+        stage_tile<T, DP, KT, WAVES>(k + j * a.k.stride, keys - (int)j, a.k.stride, a.dim_in, base + ((t + 1) & 1) * BYTES, wave, lane);
+        stage_tile<T, DP, KT, WAVES>(v + j * a.v.stride, keys - (int)j, a.v.stride, a.dim_in, base + ((t + 1) & 1) * BYTES + 2 * BYTES, wave, lane);
+      }
+      const int j0 = t * KT;
+      if (j0 >= any_sees) continue;
+      const bool whole = j0 + KT <= all_see;
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb) {
+        f32x16 s = zero_acc(), dp = zero_acc();
+#pragma unroll
+        for (int x = 0; x < L::SLABS; ++x) {
+          Operand<T>::mma(L::along(kt, 32 * kb, x, lane), q[x], s);
+          Operand<T>::mma(L::along(vt, 32 * kb, x, lane), dout[x], dp);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - delta);
+        if (!whole) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = sees(j0 + 32 * kb + acc_row(r, g), mine) ? s[r] : 0.f;
+        }
+#pragma unroll
+        for (int x = 0; x < 32 / L::STEP; ++x) {
+          const vec ds = acc_operand<T>(s, x);
+          if (SAFE && !whole) {
+            vec seen;
+#pragma unroll
+            for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(j0 + 32 * kb + acc_row(x * L::V + n, g), mine) ? 1.f : 0.f);
+#pragma unroll
+            for (int db = 0; db < L::BLOCKS; ++db) mma_seen<T>(L::across(kt, 32 * kb + x * L::STEP, db, lane), ds, seen, dq[db]);
+          } else {
+#pragma unroll
+            for (int db = 0; db < L::BLOCKS; ++db) Operand<T>::mma(L::across(kt, 32 * kb + x * L::STEP, db, lane), ds, dq[db]);
+          }
+        }
+      }
+    }
+  };
+  pass(std::false_type());
+  if (a.causal) {
+    bool fine = true;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(dq[db]);
+    if (__syncthreads_or(!fine)) pass(std::true_type());
+  }
+  store_row<T, DP>(head_at<T>(a.dq, row, at.head), there, a.dim, a.quads, dq, a.scale, g);
+}
+
+// n floats from p on into LDS, past the registers, zeros behind them (n at most 64; wave-uniform).
+__device__ __forceinline__ void stage_floats(const float *p, int n, unsigned lds, int lane) {
+  const u32x4 rows = rows_descriptor(p, n > 0 ? n * 4u : 0u);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(lane * 4), "s"(rows), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+#pragma clang diagnostic pop
+}
+
+// dk and dv: one block has 32 WAVES keys of one sequence and one head of keys, a key a lane, and goes over the queries that see them, 32 rows at a time, of all
+// heads that share the keys, in order: no sum is taken by two blocks.
+template <typename T, int DP, int WAVES, bool DK, bool DV>
+__global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const AttnArgs a) {
+  using L = Tile<T, DP>;
+  using vec = typename L::vec;
+  constexpr int BM = 32 * WAVES, QT = 32, BYTES = QT * L::RB;
+  __shared__ __attribute__((aligned(16))) char lds[4 * BYTES + 4 * 256];
+  touch_args(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
+  Place at;
+  if (!place_of(a, a.k_ptr, a.n_k, a.kv_heads, BM, lane, at)) return;
+  const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
+  const int j0 = __builtin_amdgcn_readfirstlane(at.tile < (ks.len + BM - 1) / BM ? at.tile * BM : -1);
+  if (j0 < 0) return;
+  const int len_q = __builtin_amdgcn_readfirstlane(qs.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len), group = a.q_heads / a.kv_heads;
+  const int j = j0 + 32 * wave + l32;
+  const bool there = j < ks.len;
+  // the first row that sees a key
+  auto first_of = [&](int j) { const int i = a.causal ? j - off : 0; return i < 0 ? 0 : i < len_q ? i : len_q; };
+  const int w0 = j0 + 32 * wave, w1 = w0 + 31;
+  const int begin = __builtin_amdgcn_readfirstlane(first_of(j0)) / QT * QT;
+  const int any_sees = __builtin_amdgcn_readfirstlane(first_of(w0)), all_see = __builtin_amdgcn_readfirstlane(first_of(w1)), mine = first_of(j);
+  const int per_head = (len_q - begin + QT - 1) / QT, tiles = per_head * group;
+  vec k[L::SLABS], v[L::SLABS];
+  load_row<T, DP>(k, head_at<T>(a.k, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
+  if (DK) load_row<T, DP>(v, head_at<T>(a.v, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
+  const unsigned base = lds_address(lds), stats = base + 4 * BYTES;
+  const float c = a.scale * kLog2e;
+  auto stage = [&](int t) {
+    const int head = at.head * group + t / per_head, i = begin + t % per_head * QT, b = t & 1;
+    const int64_t row = qs.begin + i;
+    stage_tile<T, DP, QT, WAVES>(head_at<T>(a.q, row, head), len_q - i, a.q.stride, a.dim_in, base + b * BYTES, wave, lane);
+    stage_tile<T, DP, QT, WAVES>(head_at<T>(a.dout, row, head), len_q - i, a.dout.stride, a.dim_in, base + (2 + b) * BYTES, wave, lane);
+    const int n = len_q - i < QT ? len_q - i : QT;
+    if (wave == 0) stage_floats(a.stat_lse + head * a.n_q + row, n, stats + b * 512, lane);
+    if (DK && wave == WAVES - 1) stage_floats(a.stat_delta + head * a.n_q + row, n, stats + b * 512 + 256, lane);
+  };
+  f32x16 dk[L::BLOCKS], dv[L::BLOCKS];
+  auto pass = [&](auto safe) {
+    constexpr bool SAFE = decltype(safe)::value;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db) {
+      dk[db] = zero_acc();
+      dv[db] = zero_acc();
+    }
+    if (tiles > 0) stage(0);
+    for (int t = 0; t < tiles; ++t) {
+      const unsigned qt = base + (t & 1) * BYTES, dt = qt + 2 * BYTES, st = stats + (t & 1) * 512;
+      wait_direct_loads();
+      __syncthreads();
+      if (t + 1 < tiles) stage(t + 1);
+      const int i0 = begin + t % per_head * QT;
+      if (i0 + QT <= any_sees) continue;
+      const bool whole = i0 >= all_see && i0 + QT <= len_q;
+      f32x16 s = zero_acc(), dp = zero_acc();
+#pragma unroll
+      for (int x = 0; x < L::SLABS; ++x) {
+        Operand<T>::mma(L::along(qt, 0, x, lane), k[x], s);
+        if (DK) Operand<T>::mma(L::along(dt, 0, x, lane), v[x], dp);
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const f32x4 lse2 = *lds_at<const f32x4>(st + (8 * n + 4 * g) * 4), delta = *lds_at<const f32x4>(st + 256 + (8 * n + 4 * g) * 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * n + r], c, -lse2[r]));
+          s[4 * n + r] = p;
+          if (DK) dp[4 * n + r] = p * (dp[4 * n + r] - delta[r]);
+        }
+      }
+      auto counts = [&](int r) { const int i = i0 + acc_row(r, g); return i >= mine && i < len_q; };
+      if (!whole) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = counts(r) ? s[r] : 0.f;
+          if (DK) dp[r] = counts(r) ? dp[r] : 0.f;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 32 / L::STEP; ++x) {
+        const vec p = acc_operand<T>(s, x), ds = acc_operand<T>(dp, x);
+        if (SAFE && !whole) {
+          vec seen;
+#pragma unroll
+          for (int n = 0; n < L::V; ++n) seen[n] = (T)(counts(x * L::V + n) ? 1.f : 0.f);
+#pragma unroll
+          for (int db = 0; db < L::BLOCKS; ++db) {
+            if (DV) mma_seen<T>(L::across(dt, x * L::STEP, db, lane), p, seen, dv[db]);
+            if (DK) mma_seen<T>(L::across(qt, x * L::STEP, db, lane), ds, seen, dk[db]);
+          }
+        } else {
+#pragma unroll
+          for (int db = 0; db < L::BLOCKS; ++db) {
+            if (DV) Operand<T>::mma(L::across(dt, x * L::STEP, db, lane), p, dv[db]);
+            if (DK) Operand<T>::mma(L::across(qt, x * L::STEP, db, lane), ds, dk[db]);
+          }
+        }
+      }
+    }
+  };
+  pass(std::false_type());
+  if (a.causal) {
+    bool fine = true;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db) fine = fine && (!DK || all_finite(dk[db])) && (!DV || all_finite(dv[db]));
+    if (__syncthreads_or(!fine)) pass(std::true_type());
+  }
+  if (DK) store_row<T, DP>(head_at<T>(a.dk, ks.begin + j, at.head), there, a.dim, a.quads, dk, a.scale, g);
+  if (DV) store_row<T, DP>(head_at<T>(a.dv, ks.begin + j, at.head), there, a.dim, a.quads, dv, 1.f, g);
+}
+
+template <typename T, int DP>
+void launch(const xrl_ctx *c, AttnArgs &a) {
+  if (a.n_q <= 64 * a.seqs) launch_tiles(c, a, attention_dq_kernel<T, DP, 1, 32>, a.n_q, a.q_heads, 32, 64);
+  else launch_tiles(c, a, attention_dq_kernel<T, DP, 4, 32>, a.n_q, a.q_heads, 128, 256);
+  // One launch for both where both sums fit in the registers with their operands, else one for each, which computes the scores once more.
+  constexpr bool BOTH = DP * sizeof(T) <= 256;
+  if constexpr (!BOTH) {
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, true, false>, a.n_k, a.kv_heads, 128, 256);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, false, true>, a.n_k, a.kv_heads, 128, 256);
+  } else if (a.n_k <= 64 * a.seqs) {
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 1, true, true>, a.n_k, a.kv_heads, 32, 64);
+  } else {
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, true, true>, a.n_k, a.kv_heads, 128, 256);
+  }
+}
+template <typename T>
+void launch_dim(const xrl_ctx *c, AttnArgs &a) {
+  a.dim <= 32 ? launch<T, 32>(c, a) : a.dim <= 64 ? launch<T, 64>(c, a) : launch<T, 128>(c, a);
+}
+
+}  // namespace
+
+extern "C" int xrl_attention_backward(xrl_ctx *c, const xrl_attention_desc *d, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out,
+                                      const float *d_lse, const xrl_heads *dout, const xrl_heads *dq, const xrl_heads *dk, const xrl_heads *dv) {
+  const char *who = "xrl_attention_backward";
+  AttnArgs a;
+  if (int rc = check_attention(c, d, who, a)) return rc;
+  const int es = d->type == XRL_PREC_BF16 ? 2 : 4;
+  if (int rc = check_heads(q, d->n_q, d->q_heads, d->dim, es, "q", who, a.q)) return rc;
+  if (int rc = check_heads(k, d->n_k, d->kv_heads, d->dim, es, "k", who, a.k)) return rc;
+  if (int rc = check_heads(v, d->n_k, d->kv_heads, d->dim, es, "v", who, a.v)) return rc;
+  if (int rc = check_heads(out, d->n_q, d->q_heads, d->dim, es, "out", who, a.out)) return rc;
+  if (int rc = check_heads(dout, d->n_q, d->q_heads, d->dim, es, "dout", who, a.dout)) return rc;
+  if (int rc = check_heads(dq, d->n_q, d->q_heads, d->dim, es, "dq", who, a.dq, &a.quads)) return rc;
+  if (int rc = check_heads(dk, d->n_k, d->kv_heads, d->dim, es, "dk", who, a.dk, &a.quads)) return rc;
+  if (int rc = check_heads(dv, d->n_k, d->kv_heads, d->dim, es, "dv", who, a.dv, &a.quads)) return rc;
+  if (d->n_q > 0 && !d_lse) return fail(XRL_ERR_NULL, "%s: d_lse is NULL", who);
+  if ((uintptr_t)d_lse % 4) return fail(XRL_ERR_SHAPE, "%s: a pointer that is no multiple of its elements' size", who);
+  if (d->n_seqs == 0 || (d->n_q == 0 && d->n_k == 0)) return XRL_OK;
+  a.lse = (float *)d_lse;
+  Inputs in(d->type, d->dim);
+  const size_t one = op_align((size_t)d->n_q * d->q_heads * 4 + 4);
+  in.bytes = 2 * one;
+  in.add(a.q, d->n_q, d->q_heads);
+  in.add(a.k, d->n_k, d->kv_heads);
+  in.add(a.v, d->n_k, d->kv_heads);
+  in.add(a.out, d->n_q, d->q_heads);
+  in.add(a.dout, d->n_q, d->q_heads);
+  char *ws = nullptr;
+  if (int rc = op_workspace(c, in.bytes, &ws, who)) return rc;
+  in.copy(c, ws);
+  a.dim_in = in.dim_in;
+  a.stat_lse = (float *)ws;
+  a.stat_delta = (float *)(ws + one);
+  d->type == XRL_PREC_BF16 ? launch_dim<bf16_t>(c, a) : launch_dim<float>(c, a);
+  OP_TRY(hipGetLastError());
+  return XRL_OK;
+}
