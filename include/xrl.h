@@ -422,6 +422,37 @@ typedef struct xrl_heads {
   int64_t stride, head_stride;   /* elements from one row to the next, and from one head to the next */
 } xrl_heads;
 
+/* xrl_head_rotary: per row x of dim columns of q [n, q_heads, dim] and of k [n, kv_heads, dim], in one pass: with the tensor's weight w [dim] fp32 the norm
+ *   y = x w / sqrt(mean x^2 + eps)  (NULL: y = x),
+ * then its first `rotary` columns turned in pairs j by the angle a = positions[row] freqs[j], z1 = y1 cos a - y2 sin a, z2 = y1 sin a + y2 cos a; pair j is columns
+ * j and j + rotary / 2, or (interleaved) 2 j and 2 j + 1. Columns behind them keep y. The angle is taken in 64 bits, the rest in fp32, rounded once. The results may
+ * lie in the inputs' own memory at their own strides. Either tensor may have no heads (then NULL). Errors: NULL, SHAPE, VALUE (eps), UNSUPPORTED (type, dim above
+ * 256), HIP. */
+typedef struct xrl_rotary_desc {
+  int64_t n;
+  int32_t q_heads, kv_heads, dim, rotary;   /* rotary: even, 0 to dim                                 */
+  int32_t type, interleaved;
+  float eps;
+  const int32_t *d_positions;    /* [n], any int32                                                    */
+  const float *d_freqs;          /* [rotary / 2]                                                      */
+  const float *d_q_weight, *d_k_weight;   /* [dim], or NULL                                           */
+} xrl_rotary_desc;
+int xrl_head_rotary(xrl_ctx *ctx, const xrl_rotary_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *q_out, const xrl_heads *k_out);
+
+/* xrl_head_rotary_backward: from the inputs (not read, and may be NULL, where there is no weight) and the gradients to the results, dq_out and dk_out, the gradients dq and dk,
+ * written (they may lie in dq_out's and dk_out's own memory), and d_dq_weight, d_dk_weight [dim] fp32, added to in a fixed order (NULL: not wanted).
+ * Errors: as above, OOM. */
+int xrl_head_rotary_backward(xrl_ctx *ctx, const xrl_rotary_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *dq_out, const xrl_heads *dk_out,
+                             const xrl_heads *dq, const xrl_heads *dk, float *d_dq_weight, float *d_dk_weight);
+
+/* xrl_rotary_freqs: freqs[j] = base^(-2 j / rotary), j < rotary / 2, scaled for contexts `factor` times as long as those a policy was trained on: divided by factor, but
+ * (length > 0) only where a pair makes few turns over `length` positions: with t = length f / 2 pi turns, f stays as it is from `fast` turns on, is divided up to
+ * `slow`, and in proportion between. Host arrays. Errors: NULL, SHAPE, VALUE. */
+typedef struct xrl_rotary_scaling {
+  double base, factor, length, slow, fast;
+} xrl_rotary_scaling;
+int xrl_rotary_freqs(int32_t rotary, const xrl_rotary_scaling *scaling, float *freqs);
+
 /* Packed sequences: sequence s has rows [d_q_ptr[s], d_q_ptr[s + 1]) of the queries and [d_k_ptr[s], d_k_ptr[s + 1]) of keys and values (the same array where they are
  * the same rows). The arrays must not fall; what they say outside the tensors counts as not there. Query head h reads the key head h / (q_heads / kv_heads). */
 typedef struct xrl_attention_desc {

@@ -74,6 +74,16 @@ class Heads(C.Structure):
     _fields_ = [("d_data", C.c_void_p), ("stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
+class RotaryDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("rotary", C.c_int32),
+                ("type", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float), ("d_positions", C.c_void_p),
+                ("d_freqs", C.c_void_p), ("d_q_weight", C.c_void_p), ("d_k_weight", C.c_void_p)]
+
+
+class RotaryScaling(C.Structure):
+    _fields_ = [(k, C.c_double) for k in ("base", "factor", "length", "slow", "fast")]
+
+
 class AttentionDesc(C.Structure):
     _fields_ = [("n_seqs", C.c_int64), ("n_q", C.c_int64), ("n_k", C.c_int64), ("d_q_ptr", C.c_void_p), ("d_k_ptr", C.c_void_p),
                 ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("type", C.c_int32), ("causal", C.c_int32),
@@ -88,7 +98,7 @@ EXPORTS = ["xrl_weight_count", "xrl_weight_tensor_count", "xrl_weight_tensor", "
            "xrl_get_activation", "xrl_set_timing", "xrl_read_timing", "xrl_measure_peaks",
            "xrl_edge_features_from_shapes", "xrl_weight_gradient", "xrl_mlp_backward", "xrl_embedding",
            "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_muon_step",
-           "xrl_attention", "xrl_attention_backward", "xrl_last_error", "xrl_version"]
+           "xrl_head_rotary", "xrl_head_rotary_backward", "xrl_rotary_freqs", "xrl_attention", "xrl_attention_backward", "xrl_last_error", "xrl_version"]
 
 
 def load_library():
@@ -136,6 +146,9 @@ def load_library():
     lib.xrl_token_logp_backward.argtypes = [vp, C.POINTER(LogitsDesc)] + [vp] * 7 + [i64]
     lib.xrl_muon_step.argtypes = [vp, C.POINTER(MuonDesc), i32, vp, i64, vp, vp, vp]
     hp = C.POINTER(Heads)
+    lib.xrl_head_rotary.argtypes = [vp, C.POINTER(RotaryDesc)] + [hp] * 4
+    lib.xrl_head_rotary_backward.argtypes = [vp, C.POINTER(RotaryDesc)] + [hp] * 6 + [vp] * 2
+    lib.xrl_rotary_freqs.argtypes = [i32, C.POINTER(RotaryScaling), vp]
     lib.xrl_attention.argtypes = [vp, C.POINTER(AttentionDesc)] + [hp] * 4 + [vp]
     lib.xrl_attention_backward.argtypes = [vp, C.POINTER(AttentionDesc)] + [hp] * 4 + [vp] + [hp] * 4
     lib.xrl_last_error.restype = C.c_char_p
@@ -285,6 +298,13 @@ def edge_features_from_shapes(shapes, M=4096.0):
     _check(lib.xrl_edge_features_from_shapes(ptr.ctypes.data, dims.ctypes.data if dims.size else None,
                                              len(shapes), C.c_double(M), out.ctypes.data))
     return out
+
+
+def rotary_freqs(rotary, base=10000.0, factor=1.0, length=0.0, slow=1.0, fast=32.0):
+    """[rotary / 2] float32 frequencies of the pairs that head_rotary turns, scaled for contexts `factor` times as long (see xrl_rotary_freqs)."""
+    f = np.empty(max(rotary, 0) // 2, np.float32)
+    _check(load_library().xrl_rotary_freqs(rotary, C.byref(RotaryScaling(base, factor, length, slow, fast)), f.ctypes.data))
+    return f
 
 
 class Encoder:
@@ -586,6 +606,57 @@ class Encoder:
         if x is not None and x.device != self._device:
             raise ValueError(f"{name}: a tensor on {self._device} is needed")
         return self._flat(x, name, dtype, n)
+
+    def _rotary(self, q, k, positions, freqs, q_weight, k_weight, eps, interleaved):
+        t = self.torch
+        hq = self._heads(q, "q")
+        n, heads, dim = q.shape
+        hk, kv = None, 0
+        if k is not None:
+            hk, kv = self._heads(k, "k", type=q.dtype), k.shape[1]
+            if k.shape[0] != n or k.shape[2] != dim:
+                raise ValueError(f"k: shape {tuple(k.shape)} with q of {tuple(q.shape)}")
+        pairs = freqs.numel()
+        f = t.float32
+        return RotaryDesc(n, heads, kv, dim, 2 * pairs, self._type(q, "q"), int(interleaved), eps, self._here(positions, "positions", t.int32, n),
+                          self._here(freqs, "freqs", f, pairs), self._here(q_weight, "q_weight", f, dim),
+                          self._here(k_weight, "k_weight", f, dim)), hq, hk
+
+    @staticmethod
+    def _maybe(h):
+        return None if h is None else C.byref(h)
+
+    def head_rotary(self, q, k, positions, freqs, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, out=None):
+        """(q', k'): the norm per head where there is a weight [dim] float32, then the first 2 len(freqs) columns turned in pairs by positions * freqs; q
+        [n, heads, dim], k [n, kv heads, dim] or None, positions [n] int32, freqs float32 (see rotary_freqs); out: two tensors to write
+        to, the inputs themselves among others. See xrl_head_rotary."""
+        d, hq, hk = self._rotary(q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
+        if out is None:
+            out = self._made((q.shape, q.dtype), *([] if k is None else [(k.shape, k.dtype)]))
+            if k is None:
+                out.append(None)
+        oq, ok = out
+        _check(self.lib.xrl_head_rotary(self.handle, C.byref(d), C.byref(hq), self._maybe(hk), C.byref(self._heads(oq, "out", q.shape, q.dtype)),
+                                        None if k is None else C.byref(self._heads(ok, "out", k.shape, q.dtype))))
+        return oq, ok
+
+    def head_rotary_backward(self, q, k, positions, freqs, dq_out, dk_out, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
+                             eps=1e-6, interleaved=False, out=None):
+        """(dq, dk) from the inputs and the gradients to the results; dq_weight, dk_weight [dim] float32 are added to; out: two tensors to write
+        to, dq_out and dk_out among others. See xrl_head_rotary_backward."""
+        d, hq, hk = self._rotary(q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
+        if out is None:
+            out = self._made((q.shape, q.dtype), *([] if k is None else [(k.shape, k.dtype)]))
+            if k is None:
+                out.append(None)
+        oq, ok = out
+        f, dim = self.torch.float32, q.shape[2]
+        gk, wk = (None, None) if k is None else (self._heads(dk_out, "dk_out", k.shape, q.dtype), self._heads(ok, "out", k.shape, q.dtype))
+        _check(self.lib.xrl_head_rotary_backward(
+            self.handle, C.byref(d), C.byref(hq), self._maybe(hk), C.byref(self._heads(dq_out, "dq_out", q.shape, q.dtype)), self._maybe(gk),
+            C.byref(self._heads(oq, "out", q.shape, q.dtype)), self._maybe(wk),
+            self._here(dq_weight, "dq_weight", f, dim), self._here(dk_weight, "dk_weight", f, dim)))
+        return oq, ok
 
     def _attention(self, q, k, v, q_ptr, k_ptr, causal, scale):
         t = self.torch
