@@ -389,6 +389,19 @@ int xrl_token_logp_backward(xrl_ctx *ctx, const xrl_logits_desc *logits, const i
                             const float *d_entropy, const float *d_stats, const float *d_dlogp, const float *d_dentropy,
                             void *d_dlogits, int64_t dlogits_stride);
 
+/* xrl_token_sample: draws one entry of every row by a given random number d_uniforms [n_rows] in [0, 1). Over the entries that may be chosen, with x the logits over the
+ * temperature and w = exp(x - largest x): in the order of falling logits, the lowest index first among equals, the first top_k (0: all); of these the ones in front of
+ * which less than top_p of their weight lies (1: all); of these the ones with w >= min_p. The first of them by index up to whose end more than d_uniforms[row] of their weight
+ * lies is drawn: d_ids [n_rows] its index inside the row, d_logp [n_rows] its log-probability among all entries that may be chosen, as xrl_token_logp gives it for
+ * the same temperature. Weights and their sums are exact to some 2^-45 of the largest weight (rows of 2^17 entries; 2^-51 up to 2^11). A random number outside [0, 1) counts as
+ * the nearest inside (NaN: 0). A row with nothing to choose: -1 and -inf; one with a NaN or +inf that may be chosen: -1 and NaN.
+ * Errors: NULL, SHAPE, UNSUPPORTED (type), VALUE (temperature; top_k < 0, top_p outside (0, 1], min_p outside [0, 1]), HIP. */
+typedef struct xrl_sample_desc {
+  int32_t top_k;
+  float top_p, min_p;
+} xrl_sample_desc;
+int xrl_token_sample(xrl_ctx *ctx, const xrl_logits_desc *logits, const xrl_sample_desc *how, const float *d_uniforms, int32_t *d_ids, float *d_logp);
+
 /* A matrix inside a flat vector of weights, row-major (what xrl_weight_tensor says of a tensor with cols > 0). */
 typedef struct xrl_matrix {
   int64_t offset, rows, cols;

@@ -65,6 +65,10 @@ class LogitsDesc(C.Structure):
                 ("temperature", C.c_float)]
 
 
+class SampleDesc(C.Structure):
+    _fields_ = [("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
+
+
 class MuonDesc(C.Structure):
     _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("rms", C.c_float),
                 ("nesterov", C.c_int32), ("steps", C.c_int32)]
@@ -97,7 +101,7 @@ EXPORTS = ["xrl_weight_count", "xrl_weight_tensor_count", "xrl_weight_tensor", "
            "xrl_policy_value_backward", "xrl_encode_backward", "xrl_ppo_objective", "xrl_segment_sum",
            "xrl_get_activation", "xrl_set_timing", "xrl_read_timing", "xrl_measure_peaks",
            "xrl_edge_features_from_shapes", "xrl_weight_gradient", "xrl_mlp_backward", "xrl_embedding",
-           "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_muon_step",
+           "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_token_sample", "xrl_muon_step",
            "xrl_head_rotary", "xrl_head_rotary_backward", "xrl_rotary_freqs", "xrl_attention", "xrl_attention_backward", "xrl_last_error", "xrl_version"]
 
 
@@ -144,6 +148,7 @@ def load_library():
     lib.xrl_embedding_backward.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, C.c_float, vp, i64]
     lib.xrl_token_logp.argtypes = [vp, C.POINTER(LogitsDesc), vp, i32] + [vp] * 5
     lib.xrl_token_logp_backward.argtypes = [vp, C.POINTER(LogitsDesc)] + [vp] * 7 + [i64]
+    lib.xrl_token_sample.argtypes = [vp, C.POINTER(LogitsDesc), C.POINTER(SampleDesc)] + [vp] * 3
     lib.xrl_muon_step.argtypes = [vp, C.POINTER(MuonDesc), i32, vp, i64, vp, vp, vp]
     hp = C.POINTER(Heads)
     lib.xrl_head_rotary.argtypes = [vp, C.POINTER(RotaryDesc)] + [hp] * 4
@@ -570,6 +575,19 @@ class Encoder:
             self._flat(None if ids is None else forward.get("logp"), "logp", f, n), self._flat(forward["entropy"], "entropy", f, n),
             self._flat(forward["stats"], "stats", f, 2 * n), self._flat(dlogp, "dlogp", f, n),
             self._flat(dentropy, "dentropy", f, n), out.data_ptr(), stride))
+        return out
+
+    def token_sample(self, logits, uniforms, mask=None, row_ptr=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None):
+        """One entry drawn of every row of logits (rows, mask and row_ptr as in token_logp) by uniforms [n] float32: dict(ids [n] int32, logp [n], as
+        token_logp gives it); out: a dict that an earlier call of these sizes gave, written again. See xrl_token_sample."""
+        t = self.torch
+        d = self._logits(logits, mask, row_ptr, temperature)
+        n, f = d.n_rows, t.float32
+        if out is None:
+            ids, logp = self._made(((n,), t.int32), ((n,), f))
+            out = dict(ids=ids, logp=logp)
+        _check(self.lib.xrl_token_sample(self.handle, C.byref(d), C.byref(SampleDesc(top_k, top_p, min_p)), self._flat(uniforms, "uniforms", f, n),
+                                         self._flat(out["ids"], "ids", t.int32, n), self._flat(out["logp"], "logp", f, n)))
         return out
 
     def muon_step(self, weights, grads, momentum, matrices, lr, beta=0.95, nesterov=True, weight_decay=0.0, steps=5,
