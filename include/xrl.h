@@ -490,6 +490,29 @@ int xrl_attention(xrl_ctx *ctx, const xrl_attention_desc *desc, const xrl_heads 
 int xrl_attention_backward(xrl_ctx *ctx, const xrl_attention_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out,
                            const float *d_lse, const xrl_heads *dout, const xrl_heads *dq, const xrl_heads *dk, const xrl_heads *dv);
 
+/* A paged cache of keys and values: k_cache and v_cache [n_pages, page, kv_heads, dim] in any order of strides (dim contiguous). Row s of d_table [n_seqs, table_cols] names sequence s's
+ * pages: its token j lies in slot j % page of page d_table[s][j / page]. d_lengths [n_seqs]: the sequence's tokens, the new ones among them; sequence s has rows
+ * [d_q_ptr[s], d_q_ptr[s + 1]) of the new tokens, its last ones. Sequences may share pages. A token behind the table's columns or on a page outside [0, n_pages) counts as not there. */
+typedef struct xrl_pages {
+  void *d_data;
+  int64_t page_stride, stride, head_stride;   /* elements from a page, slot, head to the next         */
+} xrl_pages;
+typedef struct xrl_cache_desc {
+  int64_t n_seqs, n_q, n_pages, table_stride;   /* sequences, new tokens, pages, elements from one row of the table to the next */
+  const int32_t *d_q_ptr, *d_lengths, *d_table;
+  int32_t table_cols, page;
+  int32_t q_heads, kv_heads, dim, type;
+} xrl_cache_desc;
+
+/* xrl_cache_write: the new tokens' keys and values, k and v [n_q, kv_heads, dim], to their places in the cache (q_heads is not looked at beyond its checks). Nothing else is written; two new
+ * tokens must not have one place. Errors: NULL, SHAPE, UNSUPPORTED (type, dim above 128), HIP. */
+int xrl_cache_write(xrl_ctx *ctx, const xrl_cache_desc *desc, const xrl_heads *k, const xrl_heads *v, const xrl_pages *k_cache, const xrl_pages *v_cache);
+
+/* xrl_cache_attention: attention of the new tokens, q and out [n_q, q_heads, dim], over the tokens of their sequences up to themselves, as xrl_attention (causal, with the same rounding and the
+ * same rules for rows that see nothing, for rows of no sequence, and for what is not finite), the cache holding the new tokens already. A sequence's keys are split over
+ * blocks; the parts are joined in order. Errors: as above, VALUE (scale), OOM. */
+int xrl_cache_attention(xrl_ctx *ctx, const xrl_cache_desc *desc, float scale, const xrl_heads *q, const xrl_pages *k_cache, const xrl_pages *v_cache, const xrl_heads *out);
+
 /* ---- building blocks exposed for measurement and per-step checks ----------------------------
  * xrl_segment_sum: out[i, :] = sum of values[r, :] over rows r in [d_ptr[i], d_ptr[i+1]) -- the
  * receiver-side aggregation of Section 3.4's first two equations on receiver-ordered rows, and

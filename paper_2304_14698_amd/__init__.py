@@ -88,6 +88,16 @@ class RotaryScaling(C.Structure):
     _fields_ = [(k, C.c_double) for k in ("base", "factor", "length", "slow", "fast")]
 
 
+class Pages(C.Structure):
+    _fields_ = [("d_data", C.c_void_p), ("page_stride", C.c_int64), ("stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [("n_seqs", C.c_int64), ("n_q", C.c_int64), ("n_pages", C.c_int64), ("table_stride", C.c_int64), ("d_q_ptr", C.c_void_p),
+                ("d_lengths", C.c_void_p), ("d_table", C.c_void_p), ("table_cols", C.c_int32), ("page", C.c_int32), ("q_heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("dim", C.c_int32), ("type", C.c_int32)]
+
+
 class AttentionDesc(C.Structure):
     _fields_ = [("n_seqs", C.c_int64), ("n_q", C.c_int64), ("n_k", C.c_int64), ("d_q_ptr", C.c_void_p), ("d_k_ptr", C.c_void_p),
                 ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("type", C.c_int32), ("causal", C.c_int32),
@@ -102,7 +112,8 @@ EXPORTS = ["xrl_weight_count", "xrl_weight_tensor_count", "xrl_weight_tensor", "
            "xrl_get_activation", "xrl_set_timing", "xrl_read_timing", "xrl_measure_peaks",
            "xrl_edge_features_from_shapes", "xrl_weight_gradient", "xrl_mlp_backward", "xrl_embedding",
            "xrl_embedding_backward", "xrl_token_logp", "xrl_token_logp_backward", "xrl_token_sample", "xrl_muon_step",
-           "xrl_head_rotary", "xrl_head_rotary_backward", "xrl_rotary_freqs", "xrl_attention", "xrl_attention_backward", "xrl_last_error", "xrl_version"]
+           "xrl_head_rotary", "xrl_head_rotary_backward", "xrl_rotary_freqs", "xrl_attention", "xrl_attention_backward",
+           "xrl_cache_write", "xrl_cache_attention", "xrl_last_error", "xrl_version"]
 
 
 def load_library():
@@ -156,6 +167,8 @@ def load_library():
     lib.xrl_rotary_freqs.argtypes = [i32, C.POINTER(RotaryScaling), vp]
     lib.xrl_attention.argtypes = [vp, C.POINTER(AttentionDesc)] + [hp] * 4 + [vp]
     lib.xrl_attention_backward.argtypes = [vp, C.POINTER(AttentionDesc)] + [hp] * 4 + [vp] + [hp] * 4
+    lib.xrl_cache_write.argtypes = [vp, C.POINTER(CacheDesc)] + [hp] * 2 + [C.POINTER(Pages)] * 2
+    lib.xrl_cache_attention.argtypes = [vp, C.POINTER(CacheDesc), C.c_float, hp] + [C.POINTER(Pages)] * 2 + [hp]
     lib.xrl_last_error.restype = C.c_char_p
     lib.xrl_version.restype = C.c_char_p
     _lib = lib
@@ -722,6 +735,48 @@ class Encoder:
             C.byref(self._heads(dout, "dout", q.shape, q.dtype)), C.byref(self._heads(dq, "dq", q.shape, q.dtype)),
             C.byref(self._heads(dk, "dk", k.shape, k.dtype)), C.byref(self._heads(dv, "dv", v.shape, v.dtype))))
         return dq, dk, dv
+
+    def _cache(self, n, heads, q_ptr, k_cache, v_cache, table, lengths, type):
+        t = self.torch
+        for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            if x.dim() != 4 or x.device != self._device or x.dtype != type or x.shape != k_cache.shape:
+                raise ValueError(f"{name}: a tensor [pages, page, kv heads, dim] of {type} on {self._device} is needed, both of one shape")
+            if x.stride(3) != 1 and x.shape[3] > 1:
+                raise ValueError(f"{name}: heads of contiguous columns are needed")
+        pages, page, kv, dim = k_cache.shape
+        if q_ptr.numel() < 1 or table.dim() != 2 or table.device != self._device or table.dtype != t.int32 or table.shape[0] != q_ptr.numel() - 1:
+            raise ValueError("table: a matrix of int32 on the GPU with a row for each sequence of q_ptr is needed")
+        if table.stride(1) != 1 and table.shape[1] > 1:
+            raise ValueError("table: contiguous rows are needed")
+        seqs, cols = table.shape
+        d = CacheDesc(seqs, n, pages, max(cols, table.stride(0)), self._here(q_ptr, "q_ptr", t.int32, seqs + 1),
+                      self._here(lengths, "lengths", t.int32, seqs), table.data_ptr(), cols, page, heads or kv, kv, dim, self._type(k_cache, "k_cache"))
+        return d, *(Pages(x.data_ptr(), *x.stride()[:3]) for x in (k_cache, v_cache))
+
+    def cache_write(self, k, v, q_ptr, k_cache, v_cache, table, lengths):
+        """The new tokens' keys and values [n, kv heads, dim] into the cache [pages, page, kv heads, dim]; q_ptr [sequences + 1], lengths
+        [sequences] (with the new tokens) and table [sequences, columns] int32. See xrl_cache_write."""
+        hk = self._heads(k, "k")
+        d, pk, pv = self._cache(k.shape[0], 0, q_ptr, k_cache, v_cache, table, lengths, k.dtype)
+        shape = (k.shape[0], *k_cache.shape[2:])
+        if tuple(k.shape) != shape:
+            raise ValueError(f"k: shape {tuple(k.shape)}, {shape} is needed")
+        _check(self.lib.xrl_cache_write(self.handle, C.byref(d), C.byref(hk), C.byref(self._heads(v, "v", k.shape, k.dtype)), C.byref(pk),
+                                        C.byref(pv)))
+
+    def cache_attention(self, q, q_ptr, k_cache, v_cache, table, lengths, scale=None, out=None):
+        """Attention of the new tokens q [n, heads, dim] over their sequences' tokens in the cache, themselves among them; the arguments as in
+        cache_write. See xrl_cache_attention."""
+        hq = self._heads(q, "q")
+        n, heads, dim = q.shape
+        d, pk, pv = self._cache(n, heads, q_ptr, k_cache, v_cache, table, lengths, q.dtype)
+        if dim != d.dim or heads < 1 or heads % max(d.kv_heads, 1):
+            raise ValueError(f"q: shape {tuple(q.shape)} with a cache of {tuple(k_cache.shape)}")
+        if out is None:
+            out, = self._made((q.shape, q.dtype))
+        _check(self.lib.xrl_cache_attention(self.handle, C.byref(d), dim ** -0.5 if scale is None else scale, C.byref(hq), C.byref(pk), C.byref(pv),
+                                            C.byref(self._heads(out, "out", q.shape, q.dtype))))
+        return out
 
     def get_activation(self, batch, what, rnd=0):
         shape = {"a0": (batch.N, self.model["d_edge"]), "pool": (batch.G, self.H)}.get(what, (batch.N, self.H))

@@ -173,6 +173,7 @@ __device__ __forceinline__ void mma_seen(Vec<T> a, const Vec<T> &b, const Vec<T>
     odd[j] = (T)(fine ? 0.f : 1.f);
     a[j] = fine ? a[j] : (T)0.f;
   }
+  __builtin_amdgcn_sched_barrier(0);                  // (one at a time: this way is taken where something is not finite, and its registers count for all calls)
   f32x16 n = zero_acc();
   Operand<T>::mma(odd, seen, n);
   Operand<T>::mma(a, b, acc);
@@ -185,6 +186,70 @@ __device__ __forceinline__ bool all_finite(const f32x16 &a) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) z = fmaf(a[i], 0.f, z);
   return z == 0.f;
+}
+
+// One step of a softmax that runs along: KT keys and values in tiles, q the fragments of 32 queries, one a lane. o += sum over the keys n of 2^(s_n c - mc) v_n, l their sum in
+// this lane's half of the keys, mc the reference of the exponentials. `whole`: every query of the wave sees all keys, else those for which sees(n). SAFE: what stands in keys
+// and values that are not seen reaches nothing.
+template <typename T, int DP, int KT, bool SAFE, typename Sees>
+__device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> *q, float c, bool whole, Sees sees, f32x16 (&o)[DP / 32], float &mc, float &l, int lane) {
+  using L = Tile<T, DP>;
+  using vec = Vec<T>;
+  const int g = lane >> 5;
+  f32x16 s[KT / 32];
+#pragma unroll
+  for (int kb = 0; kb < KT / 32; ++kb) {
+    s[kb] = zero_acc();
+#pragma unroll
+    for (int x = 0; x < L::SLABS; ++x) Operand<T>::mma(L::along(kt, 32 * kb, x, lane), q[x], s[kb]);
+  }
+  if (!whole) {
+#pragma unroll
+    for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = sees(32 * kb + acc_row(r, g)) ? s[kb][r] : -INFINITY;
+  }
+  float mx = s[0][0];
+#pragma unroll
+  for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+  mx = half_max(mx) * c;
+  // The reference of the exponentials follows the maximum only where that has grown by 2^8: until then sums and results are up to 2^8 times as large, and nothing is
+  // multiplied. Each row by its own maximum: what shares its wave changes none of its bits.
+  const bool grown = mx > mc + 8.f;
+  if (__ballot(grown)) {
+    const float m = grown ? mx : mc, f = __builtin_amdgcn_exp2f(mc - m);
+    mc = m;
+    l *= f;
+#pragma unroll
+    for (int db = 0; db < L::BLOCKS; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] *= f;
+  }
+#pragma unroll
+  for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c, -mc));
+      l += s[kb][r];
+    }
+#pragma unroll
+  for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+    for (int x = 0; x < 32 / L::STEP; ++x) {
+      const vec p = acc_operand<T>(s[kb], x);
+      if (SAFE && !whole) {
+        vec seen;
+#pragma unroll
+        for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(32 * kb + acc_row(x * L::V + n, g)) ? 1.f : 0.f);
+#pragma unroll
+        for (int db = 0; db < L::BLOCKS; ++db) mma_seen<T>(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, seen, o[db]);
+      } else {
+#pragma unroll
+        for (int db = 0; db < L::BLOCKS; ++db) Operand<T>::mma(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, o[db]);
+      }
+    }
 }
 
 // Packed sequences. Tiles of BM rows are counted so that sequence s has the numbers from ptr[s] / BM + s on: no two sequences share one, the last few of a
@@ -200,6 +265,19 @@ __device__ __forceinline__ int64_t end_at(const int32_t *ptr, int64_t s, int64_t
 __device__ __forceinline__ Span span_of(const int32_t *ptr, int64_t s, int64_t n) {
   const int64_t b = end_at(ptr, s, n), e = end_at(ptr, s + 1, n);
   return {b, e > b ? (int)(e - b) : 0};
+}
+// The sequence of a row, or -1.
+__device__ __forceinline__ int64_t sequence_of_row(const int32_t *ptr, int64_t seqs, int64_t n, int64_t row, int lane) {
+  int64_t lo = 0, hi = seqs;
+  do {
+    const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
+    const unsigned long long b = __ballot(p < hi && end_at(ptr, p < hi ? p : lo, n) <= row);
+    const int c = ~b ? __builtin_ctzll(~b) : 64;
+    if (c == 0) return -1;
+    lo += (c - 1) * step;
+    hi = lo + step < hi ? lo + step : hi;
+  } while (hi - lo > 1);
+  return row < end_at(ptr, lo + 1, n) ? lo : -1;
 }
 // The sequence that tile number u belongs to, or -1; 64 of them are looked at at once.
 __device__ __forceinline__ int64_t sequence_of(const int32_t *ptr, int64_t seqs, int64_t n, int bm, int64_t u, int lane) {

@@ -60,61 +60,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
       }
       const int j0 = t * KT;
       if (j0 >= any_sees) continue;
-      f32x16 s[KT / 32];
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb) {
-        s[kb] = zero_acc();
-#pragma unroll
-        for (int x = 0; x < L::SLABS; ++x) Operand<T>::mma(L::along(kt, 32 * kb, x, lane), q[x], s[kb]);
-      }
-      const bool whole = j0 + KT <= all_see;
-      if (!whole) {
-#pragma unroll
-        for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[kb][r] = sees(j0 + 32 * kb + acc_row(r, g), mine) ? s[kb][r] : -INFINITY;
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-      mx = half_max(mx) * c;
-      // The reference of the exponentials follows the maximum only where that has grown by 2^8: until then sums and results are up to 2^8 times as large, and nothing is
-      // multiplied. Each row by its own maximum: what shares its wave changes none of its bits.
-      const bool grown = mx > mc + 8.f;
-      if (__ballot(grown)) {
-        const float m = grown ? mx : mc, f = __builtin_amdgcn_exp2f(mc - m);
-        mc = m;
-        l *= f;
-#pragma unroll
-        for (int db = 0; db < L::BLOCKS; ++db)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[db][r] *= f;
-      }
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c, -mc));
-          l += s[kb][r];
-        }
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-        for (int x = 0; x < 32 / L::STEP; ++x) {
-          const vec p = acc_operand<T>(s[kb], x);
-          if (SAFE && !whole) {
-            vec seen;
-#pragma unroll
-            for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(j0 + 32 * kb + acc_row(x * L::V + n, g), mine) ? 1.f : 0.f);
-#pragma unroll
-            for (int db = 0; db < L::BLOCKS; ++db) mma_seen<T>(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, seen, o[db]);
-          } else {
-#pragma unroll
-            for (int db = 0; db < L::BLOCKS; ++db) Operand<T>::mma(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, o[db]);
-          }
-        }
+      add_tile<T, DP, KT, SAFE>(kt, vt, q, c, j0 + KT <= all_see, [&](int n) { return j0 + n < mine; }, o, mc, l, lane);
     }
   };
   pass(std::false_type());
