@@ -25,28 +25,28 @@ struct SampleArgs {
   const float *uniforms;
   int32_t *ids;
   float *logp;
+  // rows in parts whose groups of entries were looked at before (token_sample_groups_kernel); parts 0: not
+  int parts;
+  float *group_max;             // [rows][parts][256]
+  float *part_stats;            // [rows][parts][2]: the largest logit, and the sum of exponentials relative to it
 };
 
-constexpr int kBins = 2048, kList = 1024;         // of a histogram; entries that are ranked against each other
+constexpr int kBins = 2048, kList = 1024, kListBins = 1024;         // of a histogram; entries that are ranked against each other
+constexpr int kPart = 8192, kGroups = 256;          // entries of a part, and its groups: what one thread has of it
 constexpr float kBinsATurn = 64.f;                 // bins for a factor e in weight: 32 of these, the last bin has all below
 
 // 2^t, t <= 0, in 64 bits: the integer part by the exponent, the rest in [-1/2, 1/2] by Taylor's sum of thirteen terms, whose rest is below 2^-52. Below 2^-100: of no weight.
+constexpr double kExp2[13] = {2.5678435993488206e-11, 4.4455382718708116e-10, 7.054911620801123e-09, 1.01780860092397e-07, 1.321548679014431e-06, 1.5252733804059841e-05, 0.0001540353039338161, 0.0013333558146428443, 0.009618129107628477, 0.05550410866482158, 0.24022650695910072, 0.6931471805599453, 1.0};   // ln(2)^k / k!, k = 12 .. 0
 __device__ __forceinline__ double exp2_64(double t) {
   t = t > -100.0 ? t : -100.0;
   const double n = rint(t), f = t - n;
-  double p = 2.5678435993488206e-11;               // ln(2)^12 / 12!
-  p = fma(p, f, 4.4455382718708116e-10);
-  p = fma(p, f, 7.054911620801123e-09);
-  p = fma(p, f, 1.01780860092397e-07);
-  p = fma(p, f, 1.321548679014431e-06);
-  p = fma(p, f, 1.5252733804059841e-05);
-  p = fma(p, f, 0.0001540353039338161);
-  p = fma(p, f, 0.0013333558146428443);
-  p = fma(p, f, 0.009618129107628477);
-  p = fma(p, f, 0.05550410866482158);
-  p = fma(p, f, 0.24022650695910072);
-  p = fma(p, f, 0.6931471805599453);
-  p = fma(p, f, 1.0);
+  double p = kExp2[0];
+#pragma unroll
+  for (int i = 1; i < 13; ++i) {
+    double k = kExp2[i];
+    asm("" : "+s"(k));                             // (in scalar registers: as a literal each takes a move more)
+    p = fma(p, f, k);
+  }
   return __longlong_as_double(__double_as_longlong(p) + ((long long)(int)n << 52));
 }
 
@@ -54,11 +54,6 @@ __device__ __forceinline__ double exp2_64(double t) {
 __device__ __forceinline__ unsigned key_of(float x) {
   const unsigned u = __float_as_uint(x + 0.f);
   return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
-}
-
-// Between two entries' exponentials: eight of them side by side take registers that waves to hide the memory's latency need.
-__device__ __forceinline__ void apart(int j) {
-  if (j & 1) __builtin_amdgcn_sched_barrier(0);
 }
 
 struct RowScale {
@@ -71,6 +66,10 @@ __device__ __forceinline__ double weight_of(const RowScale &s, float x) { return
 // w as a multiple of 2^-S: in the sum with 2^52 the last place is 1.
 __device__ __forceinline__ unsigned long long whole_of(const RowScale &s, double w) {
   return (unsigned long long)__double_as_longlong(fma(w, s.one, 4503599627370496.0)) & 0xfffffffffffffull;
+}
+__device__ __forceinline__ RowScale scale_of(const SampleArgs &a, float m, int len) {
+  const int bits = 32 - __clz(len - 1);
+  return {m, a.c, __longlong_as_double((long long)(1023 + 51 - (bits > 11 ? bits - 11 : 0)) << 52), a.inv_t * kBinsATurn};
 }
 // Falls as x rises, so a bin is an interval of keys.
 __device__ __forceinline__ int bin_of(const RowScale &s, float x) { return (int)fminf((s.m - x) * s.bins, (float)(kBins - 1)); }
@@ -100,7 +99,10 @@ template <int WAVES>
 struct Shared {
   u64 mass[kBins];
   unsigned count[kBins];
+  u64 list_mass[kListBins];     // bins over the list
+  unsigned list_count[kListBins];
   Entry list[kList];
+  int members[64], few;
   u64 sums[WAVES];
   float floats[WAVES];
   unsigned lows[WAVES], highs[WAVES];
@@ -119,29 +121,69 @@ struct Cut {
 };
 __device__ __forceinline__ bool inside(const Cut &c, unsigned key, int id) { return key > c.key || (key == c.key && id <= c.id); }
 
-// A wave's share of the row: columns [begin, end) in steps of 64 VEC; f(col, x) for the lane's piece of each.
+// A wave's share of the row: columns [begin, end) in steps of 64 VEC; f(col, x) for the lane's piece of each. Two steps' loads are on their way while one is worked on: each by
+// itself is a round trip to memory of a microsecond or two. The steps' registers move up, and the body stands once: with bodies for four steps side by side the kernel had
+// 270 KB of code, of which the instruction cache holds 64 (2048 x 32003 with min-p 580 us for 284 without the list below).
 template <typename T, typename F>
 __device__ __forceinline__ void for_pieces(const Row<T> &row, bool odd, int begin, int end, int lane, F f) {
-  constexpr int VEC = 16 / (int)sizeof(T);
-  for (int w = begin; w < end; w += 64 * VEC) {
+  constexpr int VEC = 16 / (int)sizeof(T), STEP = 64 * VEC, AHEAD = 2;
+  Piece<T, VEC> v[AHEAD + 1];
+  Piece<uint8_t, VEC> k[AHEAD + 1];
+  auto request = [&](int w, int at) {
+    if (w + STEP > end) return;
+    const T *p = row.x + w + lane * VEC;
+    v[at] = odd ? load_odd_piece<T, VEC>(p) : load_piece<T, VEC>(p);
+    if (row.mask) k[at] = load_piece<uint8_t, VEC>(row.mask + w + lane * VEC);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) request(begin + i * STEP, i);
+#pragma unroll 1
+  for (int w = begin; w < end; w += STEP) {
+    request(w + AHEAD * STEP, AHEAD);
     float x[VEC];
-    fetch<T, VEC>(row, odd, w + lane * VEC, end, x);
+    if (w + STEP <= end) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[j] = row.mask && !k[0].v[j] ? -INFINITY : (float)v[0].v[j];
+    } else {
+      fetch<T, VEC>(row, odd, w + lane * VEC, end, x);
+    }
     f(w + lane * VEC, x);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      v[i] = v[i + 1];
+      k[i] = k[i + 1];
+    }
+  }
+}
+// f(j, x[j]) for the entries of a piece, two bodies for all of them.
+template <int VEC, typename F>
+__device__ __forceinline__ void for_entries(const float *x, F f) {
+  float y[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) y[j] = x[j];
+#pragma unroll 1
+  for (int j = 0; j < VEC; j += 2) {
+    f(j, y[0]);
+    f(j + 1, y[1]);
+#pragma unroll
+    for (int i = 0; i + 2 < VEC; ++i) y[i] = y[i + 2];
   }
 }
 
 // One block a row.
+constexpr u64 kBelow = 1ull << 63;                 // beside a listed entry's weight: below min-p
 template <typename T, int WAVES>
 struct Sampler {
   static constexpr int VEC = 16 / (int)sizeof(T), STEP = 64 * VEC;
   const SampleArgs &a;
   const Row<T> &row;
   Shared<WAVES> &sh;
-  bool odd;
+  bool odd, masses;             // masses: weights are needed, not counts alone
   int lane, wave, begin, end;   // columns of this wave
   RowScale s;
+  bool spoiled;                 // bins over keys have taken the first histogram's place
 
-  // Σ of one value a wave, over the waves in front of this one and over all.
+  // The sum of one value a wave, over the waves in front of this one and over all.
   __device__ __forceinline__ u64 over_waves(u64 mine, u64 &all) {
     __syncthreads();
     if (lane == 0) sh.sums[wave] = mine;
@@ -157,52 +199,54 @@ struct Sampler {
   }
 
   // The bin in which the sum of what lies in front (counts or weights of larger entries) passes `limit`: sh.bin, and sh.before what lies in front of it.
-  __device__ __forceinline__ void find_bin(bool by_mass, u64 limit) {
-    if (wave == 0) {
-      constexpr int EACH = kBins / 64;
-      u64 mine = 0;
-#pragma unroll 4
-      for (int i = 0; i < EACH; ++i) mine += by_mass ? sh.mass[lane * EACH + i] : sh.count[lane * EACH + i];
-      const u64 upto = wave_scan64(mine, lane);
-      const int at = __ffsll(__ballot(upto >= limit)) - 1;
-      if (lane == (at < 0 ? 63 : at)) {
-        u64 before = upto - mine;
-        int b = lane * EACH;
-#pragma unroll 1
-        for (; b < lane * EACH + EACH - 1; ++b) {
-          const u64 one = by_mass ? sh.mass[b] : sh.count[b];
-          if (before + one >= limit) break;
-          before += one;
-        }
-        sh.bin = b;
-        sh.before = before;
+  template <int BINS>
+  __device__ __forceinline__ void find_bin(const unsigned (&counts)[BINS], const u64 (&masses_)[BINS], bool by_mass, u64 limit) {
+    constexpr int EACH = BINS / (WAVES * 64);
+    u64 v[EACH], mine = 0, all;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      v[i] = by_mass ? masses_[threadIdx.x * EACH + i] : counts[threadIdx.x * EACH + i];
+      mine += v[i];
+    }
+    const u64 scan = wave_scan64(mine, lane), upto = over_waves(__shfl(scan, 63), all) + scan;
+    if (upto >= limit && upto - mine < limit) {
+      u64 before = upto - mine;
+      int at = 0;
+#pragma unroll
+      for (int i = 0; i < EACH - 1; ++i) {
+        const bool on = at == i && before + v[i] < limit;
+        before += on ? v[i] : 0;
+        at += on ? 1 : 0;
       }
-      if (lane == 63) sh.all = upto;
+      sh.bin = threadIdx.x * EACH + at;
+      sh.before = before;
     }
     __syncthreads();
   }
 
-  __device__ __forceinline__ void clear_bins(bool by_mass) {
-    for (int i = threadIdx.x; i < kBins; i += WAVES * 64) {
-      sh.count[i] = 0;
-      if (by_mass) sh.mass[i] = 0;
+  template <int BINS>
+  __device__ __forceinline__ void clear_bins(unsigned (&counts)[BINS], u64 (&masses_)[BINS]) {
+    for (int i = threadIdx.x; i < BINS; i += WAVES * 64) {
+      counts[i] = 0;
+      masses_[i] = 0;
     }
-    if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
+  }
+  // The sum of the bins' weights in front of `bin`.
+  __device__ __forceinline__ u64 mass_before(const u64 *masses_, int bin) {
+    u64 t = 0, all;
+    for (int i = threadIdx.x; i < bin; i += WAVES * 64) t += masses_[i];
+    over_waves(wave_sum64(t), all);
+    return all;
   }
 
   // The cut at which the entries in front of it (by_mass: their weights) are fewer than `limit`, from the bins of the first histogram. sh.upto: the weight of all that
   // is kept.
   __device__ __forceinline__ Cut cut_at(bool by_mass, u64 limit) {
-    find_bin(by_mass, limit);
+    find_bin(sh.count, sh.mass, by_mass, limit);
     const int bin = sh.bin;
-    u64 before = sh.before, mass_before = before;
-    if (!by_mass) {                                    // (the weights in front as well: top-p takes its share of them)
-      u64 t = 0, all;
-      for (int i = threadIdx.x; i < bin; i += WAVES * 64) t += sh.mass[i];
-      over_waves(wave_sum64(t), all);
-      mass_before = all;
-    }
+    u64 before = sh.before, in_front = before;
+    if (!by_mass && masses) in_front = mass_before(sh.mass, bin);   // (the weights in front as well: top-p takes its share of them)
     // its entries, and the range of their keys
     unsigned lo = 0xffffffffu, hi = 0;
     int n = 0;
@@ -210,16 +254,14 @@ struct Sampler {
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
     for_pieces<T>(row, odd, begin, end, lane, [&](int col, const float *x) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        if (x[j] == -INFINITY || bin_of(s, x[j]) != bin) continue;
-        const unsigned key = key_of(x[j]);
+      for_entries<VEC>(x, [&](int j, float xj) {
+        if (xj == -INFINITY || bin_of(s, xj) != bin) return;
+        const unsigned key = key_of(xj);
         lo = min(lo, key);
         hi = max(hi, key);
         const int at = atomicAdd(&sh.n, 1);
-        if (at < kList) sh.list[at] = {whole_of(s, weight_of(s, x[j])), key, col + j};
-        apart(j);
-      }
+        if (at < kList) sh.list[at] = {whole_of(s, weight_of(s, xj)), key, col + j};
+      });
     });
     __syncthreads();
     n = sh.n;
@@ -227,27 +269,23 @@ struct Sampler {
       // too many: bins over their keys
       lo = block_min(lo);
       hi = ~block_min(~hi);
-      if (lo == hi) return cut_of_equal(by_mass, limit, before, mass_before, lo);
+      if (lo == hi) return cut_of_equal(by_mass, limit, before, in_front, lo);
       int shift = 0;
       while ((hi - lo) >> shift >= kBins) ++shift;
-      clear_bins(true);
+      clear_bins(sh.count, sh.mass);
+      spoiled = true;
       for_pieces<T>(row, odd, begin, end, lane, [&](int, const float *x) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const unsigned key = key_of(x[j]);
-          if (x[j] == -INFINITY || key < lo || key > hi) continue;
-          atomicAdd(&sh.count[(hi - key) >> shift], 1u);
-          atomicAdd(&sh.mass[(hi - key) >> shift], whole_of(s, weight_of(s, x[j])));
-          apart(j);
-        }
+        for_entries<VEC>(x, [&](int j, float xj) {
+          const unsigned key = key_of(xj);
+          if (xj == -INFINITY || key < lo || key > hi) return;
+          if (!by_mass) atomicAdd(&sh.count[(hi - key) >> shift], 1u);
+          if (masses) atomicAdd(&sh.mass[(hi - key) >> shift], whole_of(s, weight_of(s, xj)));
+        });
       });
       __syncthreads();
-      find_bin(by_mass, limit - before);
+      find_bin(sh.count, sh.mass, by_mass, limit - before);
       const int b = sh.bin;
-      u64 t = 0, all;
-      for (int i = threadIdx.x; i < b; i += WAVES * 64) t += sh.mass[i];
-      over_waves(wave_sum64(t), all);
-      mass_before += all;
+      if (masses) in_front += mass_before(sh.mass, b);
       before += sh.before;
       const unsigned top = hi - ((unsigned)b << shift), span = (1u << shift) - 1;
       const unsigned range_lo = top - lo > span ? top - span : lo, range_hi = top;
@@ -257,41 +295,218 @@ struct Sampler {
       lo = 0xffffffffu;
       hi = 0;
       for_pieces<T>(row, odd, begin, end, lane, [&](int col, const float *x) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const unsigned key = key_of(x[j]);
-          if (x[j] == -INFINITY || key < range_lo || key > range_hi) continue;
+        for_entries<VEC>(x, [&](int j, float xj) {
+          const unsigned key = key_of(xj);
+          if (xj == -INFINITY || key < range_lo || key > range_hi) return;
           lo = min(lo, key);
           hi = max(hi, key);
           const int at = atomicAdd(&sh.n, 1);
-          if (at < kList) sh.list[at] = {whole_of(s, weight_of(s, x[j])), key, col + j};
-          apart(j);
-        apart(j);
-        }
+          if (at < kList) sh.list[at] = {whole_of(s, weight_of(s, xj)), key, col + j};
+        });
       });
       __syncthreads();
       n = sh.n;
     }
-    // every entry against all others: what lies in front of it
-    for (int i = threadIdx.x; i < n; i += WAVES * 64) {
-      const Entry e = sh.list[i];
-      u64 count = 0, mass = 0;
-#pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const Entry o = sh.list[k];
-        const bool front = o.key > e.key || (o.key == e.key && o.id < e.id);
-        count += front ? 1 : 0;
-        mass += front ? o.w : 0;
+    in_front += select(n, by_mass, false, limit - before, [](int) { return true; });
+    if (threadIdx.x == 0) sh.upto = in_front;
+    __syncthreads();
+    return {sh.key, sh.id};
+  }
+
+  // One more entry of the list, if there is room: sh.n counts all.
+  __device__ __forceinline__ void push(float x, int id, double w) {
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < kList) sh.list[at] = {whole_of(s, w) | (w >= a.min_p ? 0 : kBelow), key_of(x), id};
+  }
+
+  // Of those of the list's n entries that count(i), in the order of the cuts (by_index: of their indices), the one at which the sum of counts (by_mass: weights) reaches `limit`: its key and
+  // index to sh.key and sh.id; returned: the weight up to it and with it. By bins over the entries' places in that order, a range narrower by the number of bins each time until a
+  // few are left, which are ranked against each other. (Ranking all against all took 230 us for 200 to 700 entries.)
+  template <typename Counts>
+  __device__ __forceinline__ u64 select(int n, bool by_mass, bool by_index, u64 limit, Counts counts) {
+    constexpr int EACH = kList / (WAVES * 64);
+    Entry e[EACH];
+    u64 place[EACH];
+    bool in[EACH];
+    unsigned least = 0xffffffffu, most = 0;
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+      const int i = threadIdx.x + q * WAVES * 64;
+      in[q] = i < n && counts(i);
+      e[q] = in[q] ? sh.list[i] : Entry{0, 0, 0};
+      e[q].w &= ~kBelow;
+      const unsigned first = by_index ? (unsigned)e[q].id : ~e[q].key;
+      place[q] = by_index ? first : (u64)first << 32 | (unsigned)e[q].id;
+      if (!in[q]) continue;
+      least = min(least, first);
+      most = max(most, first);
+    }
+    least = block_min(least);
+    most = ~block_min(~most);
+    u64 lo = by_index ? least : (u64)least << 32, hi = by_index ? most : (u64)most << 32 | 0xffffffffu, before = 0, mass = 0;
+    for (int step = 0; step < 7; ++step) {            // (64 bits by ten each time)
+      const int bits = 64 - __clzll((long long)(hi - lo)), shift = bits > 10 ? bits - 10 : 0;
+      clear_bins(sh.list_count, sh.list_mass);
+#pragma unroll
+      for (int q = 0; q < EACH; ++q) {
+        if (!in[q] || place[q] < lo || place[q] > hi) continue;
+        atomicAdd(&sh.list_count[(place[q] - lo) >> shift], 1u);
+        atomicAdd(&sh.list_mass[(place[q] - lo) >> shift], e[q].w);
       }
-      const u64 from = before + (by_mass ? mass : count), to = from + (by_mass ? e.w : 1);
-      if (from < limit && limit <= to) {
-        sh.key = e.key;
-        sh.id = e.id;
-        sh.upto = mass_before + mass + e.w;
+      if (threadIdx.x == 0) sh.few = 0;
+      __syncthreads();
+      find_bin(sh.list_count, sh.list_mass, by_mass, limit - before);
+      const int bin = sh.bin;
+      mass += mass_before(sh.list_mass, bin);
+      before += sh.before;
+      lo += (u64)bin << shift;
+      hi = min(hi, lo + (((u64)1 << shift) - 1));
+      if (sh.list_count[bin] <= 64) break;
+      __syncthreads();
+    }
+#pragma unroll
+    for (int q = 0; q < EACH; ++q)
+      if (in[q] && place[q] >= lo && place[q] <= hi) sh.members[atomicAdd(&sh.few, 1)] = threadIdx.x + q * WAVES * 64;
+    __syncthreads();
+    const int m = sh.few;
+    if ((int)threadIdx.x < m) {
+      const Entry f = sh.list[sh.members[threadIdx.x]];
+      u64 from = before, front = 0;
+      for (int k = 0; k < m; ++k) {
+        const Entry o = sh.list[sh.members[k]];
+        const bool ahead = by_index ? o.id < f.id : o.key > f.key || (o.key == f.key && o.id < f.id);
+        front += ahead ? o.w & ~kBelow : 0;
+        from += !by_mass && ahead ? 1 : 0;
+      }
+      from += by_mass ? front : 0;
+      const u64 own = by_mass ? f.w & ~kBelow : 1;
+      if (from < limit && limit <= from + own) {
+        sh.key = f.key;
+        sh.id = f.id;
+        sh.upto = mass + front + (f.w & ~kBelow);
       }
     }
     __syncthreads();
-    return {sh.key, sh.id};
+    const u64 upto = sh.upto;
+    __syncthreads();
+    return upto;
+  }
+
+  // The list's n entries are the row's n first in the order of the cuts, and all that can be kept are among them. sum: of all weights that may be chosen (without top-k, top-p
+  // takes its share of `whole`).
+  __device__ __forceinline__ void draw_from_list(int64_t r, float u, bool by_k, bool by_p, u64 whole, float sum) {
+    constexpr int EACH = kList / (WAVES * 64);
+    const int n = sh.n;
+    Cut cut = {0, 0x7fffffff};
+    auto all_of = [](int) { return true; };
+    const bool cut_k = by_k && n > a.top_k;
+    u64 kept = 0, all;
+    auto kept_weight = [&](int i) {
+      const Entry e = sh.list[i];
+      return inside(cut, e.key, e.id) ? e.w : 0;
+    };
+    if (cut_k) {
+      whole = select(n, false, false, a.top_k, all_of);
+      cut = {sh.key, sh.id};
+    } else if (by_k && by_p) {
+#pragma unroll
+      for (int q = 0; q < EACH; ++q) kept += (int)threadIdx.x + q * WAVES * 64 < n ? sh.list[threadIdx.x + q * WAVES * 64].w & ~kBelow : 0;
+      over_waves(wave_sum64(kept), whole);
+    }
+    if (by_p) {
+      const double part = ceil(a.top_p * (double)whole);
+      const u64 limit = part < 1.0 ? 1 : (u64)part;
+      // (by min-p alone the list may end in front of top-p's cut)
+      kept = 0;
+#pragma unroll
+      for (int q = 0; q < EACH; ++q) kept += (int)threadIdx.x + q * WAVES * 64 < n ? kept_weight(threadIdx.x + q * WAVES * 64) & ~kBelow : 0;
+      over_waves(wave_sum64(kept), all);
+      __syncthreads();
+      if (limit <= all) {
+        select(n, true, false, limit, all_of);
+        cut = {sh.key, sh.id};
+      }
+    }
+    kept = 0;
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+      const u64 w = (int)threadIdx.x + q * WAVES * 64 < n ? kept_weight(threadIdx.x + q * WAVES * 64) : kBelow;
+      kept += w & kBelow ? 0 : w;
+    }
+    over_waves(wave_sum64(kept), all);
+    __syncthreads();
+    select(n, true, true, target_of(u, all) + 1, [&](int i) {
+      const u64 w = kept_weight(i);
+      return w != 0 && !(w & kBelow);
+    });
+    if (threadIdx.x == 0) {
+      a.ids[r] = sh.id;
+      a.logp[r] = log_share(__uint_as_float(sh.key >> 31 ? sh.key ^ 0x80000000u : ~sh.key), sum);
+    }
+  }
+  // From the largest logits of the row's groups: the entries of those groups that can hold one which is kept (of the first top_k, or not below min-p), as a list. false: they are
+  // more than the list takes.
+  __device__ __forceinline__ bool draw_from_groups(int64_t r, float u, const float *tops, float sum) {
+    constexpr int PIECES = kPart / (kGroups * VEC);
+    const bool by_k = a.top_k > 0;
+    const int groups = a.parts * kGroups;
+    unsigned *chosen = (unsigned *)sh.mass;            // [kList]
+    clear_bins(sh.count, sh.mass);
+    if (threadIdx.x == 0) {
+      sh.n = 0;
+      sh.few = 0;
+      sh.bin = kBins - 1;
+    }
+    int bin = kBins - 1;
+    if (by_k) {
+      for (int i = threadIdx.x; i < groups; i += WAVES * 64)
+        if (tops[i] > -INFINITY) atomicAdd(&sh.count[bin_of(s, tops[i])], 1u);
+      __syncthreads();
+      find_bin(sh.count, sh.mass, false, a.top_k);
+      bin = sh.bin;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < groups; i += WAVES * 64) {
+      if (tops[i] == -INFINITY || bin_of(s, tops[i]) > bin || (!by_k && !(weight_of(s, tops[i]) >= a.min_p))) continue;
+      const int at = atomicAdd(&sh.few, 1);
+      if (at < kList) chosen[at] = i;
+    }
+    __syncthreads();
+    const int n = sh.few;
+    if (n > kList) return false;
+    for (int i = threadIdx.x; i < n * PIECES; i += WAVES * 64) {
+      const int g = chosen[i / PIECES], col = g / kGroups * kPart + (i % PIECES * kGroups + g % kGroups) * VEC;
+      float x[VEC];
+      fetch<T, VEC>(row, odd, col, row.len, x);
+      for_entries<VEC>(x, [&](int j, float xj) {
+        if (xj == -INFINITY || bin_of(s, xj) > bin) return;
+        const double w = weight_of(s, xj);
+        if (by_k || w >= a.min_p) push(xj, col + j, w);
+      });
+    }
+    __syncthreads();
+    if (sh.n > kList) return false;
+    draw_from_list(r, u, by_k, a.top_p < 1.0, 0, sum);
+    return true;
+  }
+  static __device__ __forceinline__ u64 target_of(float u, u64 all) {
+    const double want = u > 0.f ? floor((double)u * (double)all) : 0.0;
+    return want < (double)all && (u64)want < all ? (u64)want : all - 1;
+  }
+  __device__ __forceinline__ float log_share(float x, float sum) const {
+    const float v = (x - s.m) * a.inv_t - logf(sum);
+    return v < kLowest ? kLowest : v;
+  }
+  // The sum of one float a wave.
+  __device__ __forceinline__ float block_sum(float x) {
+    x = wave_sum(x);
+    __syncthreads();
+    if (lane == 0) sh.floats[wave] = x;
+    __syncthreads();
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) t += sh.floats[w];
+    return t;
   }
 
   __device__ __forceinline__ unsigned block_min(unsigned x) {
@@ -306,7 +521,7 @@ struct Sampler {
   }
 
   // All entries of the bin are equal: the first so many of them, by index.
-  __device__ __forceinline__ Cut cut_of_equal(bool by_mass, u64 limit, u64 before, u64 mass_before, unsigned key) {
+  __device__ __forceinline__ Cut cut_of_equal(bool by_mass, u64 limit, u64 before, u64 in_front, unsigned key) {
     const unsigned bits = key >> 31 ? key ^ 0x80000000u : ~key;
     const u64 w = whole_of(s, weight_of(s, __uint_as_float(bits)));
     const u64 left = limit - before, m = by_mass ? (left + w - 1) / w : left;      // (w > 0: the limit lies inside the bin)
@@ -340,15 +555,71 @@ struct Sampler {
     }
     if (threadIdx.x == 0) {
       sh.key = key;
-      sh.upto = mass_before + m * w;
+      sh.upto = in_front + m * w;
     }
     __syncthreads();
     return {sh.key, sh.id};
   }
 };
 
+// One block a part of a row: every thread's largest logit, and the part's sum of exponentials. Memory-bound; it spares the kernel behind it all entries but those of the groups
+// that can hold one which is kept.
+template <typename T>
+__global__ __launch_bounds__(256) void token_sample_groups_kernel(const SampleArgs a) {
+  touch_args(a);
+  constexpr int VEC = 16 / (int)sizeof(T), PIECES = kPart / (kGroups * VEC);
+  __shared__ float tops[4], sums[4];
+  const int64_t job = a.row0 * a.parts + blockIdx.x, r = job / a.parts;
+  const int part = (int)(job % a.parts), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Row<T> row = row_of<T>(a, r);
+  const bool odd = __builtin_amdgcn_readfirstlane(lead_of(row.x, row.len)) != 0;
+  const int first = part * kPart + threadIdx.x * VEC, end = part * kPart + kPart < row.len ? part * kPart + kPart : row.len;
+  float x[PIECES][VEC], m = -INFINITY;
+  bool odd_one = false;
+  if (end == part * kPart + kPart && !row.mask) {
+    Piece<T, VEC> v[PIECES];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const T *at = row.x + first + p * kGroups * VEC;
+      v[p] = odd ? load_odd_piece<T, VEC>(at) : load_piece<T, VEC>(at);
+    }
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) x[p][j] = (float)v[p].v[j];
+  } else {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) fetch<T, VEC>(row, odd, first + p * kGroups * VEC, end, x[p]);
+  }
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      m = fmaxf(m, x[p][j]);
+      odd_one = odd_one | !(x[p][j] < INFINITY);
+    }
+  a.group_max[job * kGroups + threadIdx.x] = m;
+  m = wave_max(m);
+  if (lane == 0) tops[wave] = m;
+  odd_one = __syncthreads_or(odd_one);
+  m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  const float c = a.inv_t * kLog2e, from = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum += __builtin_amdgcn_exp2f((x[p][j] - from) * c);
+  sum = wave_sum(sum);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.part_stats[2 * job] = m;
+    a.part_stats[2 * job + 1] = odd_one ? __builtin_nanf("") : sums[0] + sums[1] + sums[2] + sums[3];
+  }
+}
+
 template <typename T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void token_sample_kernel(const SampleArgs a) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_kernel(const SampleArgs a) {
   touch_args(a);
   using S = Sampler<T, WAVES>;
   constexpr int VEC = S::VEC, STEP = S::STEP;
@@ -359,7 +630,24 @@ __global__ __launch_bounds__(WAVES * 64) void token_sample_kernel(const SampleAr
   const float u = a.uniforms[r];
   const int steps = (row.len + STEP - 1) / STEP, per = (steps + WAVES - 1) / WAVES;
   const int64_t b0 = (int64_t)wave * per * STEP, b1 = b0 + (int64_t)per * STEP;
-  S t = {a, row, sh, __builtin_amdgcn_readfirstlane(lead_of(row.x, row.len)) != 0, lane, wave, (int)(b0 < row.len ? b0 : row.len), (int)(b1 < row.len ? b1 : row.len), {}};
+  S t = {a, row, sh, __builtin_amdgcn_readfirstlane(lead_of(row.x, row.len)) != 0, a.top_p < 1.0, lane, wave, (int)(b0 < row.len ? b0 : row.len), (int)(b1 < row.len ? b1 : row.len), {}, false};
+  const float c = a.inv_t * kLog2e;
+  if (a.parts) {
+    const float *stats = a.part_stats + 2 * r * a.parts, *tops = a.group_max + r * a.parts * kGroups;
+    float m = -INFINITY, sum = 0.f;
+    for (int i = 0; i < a.parts; ++i) m = fmaxf(m, stats[2 * i]);
+    for (int i = 0; i < a.parts; ++i) sum += __builtin_amdgcn_exp2f((stats[2 * i] - (m == -INFINITY ? 0.f : m)) * c) * stats[2 * i + 1];
+    if (!(sum == sum) || m == -INFINITY) {             // (no number, or +inf: a sum that is none)
+      if (threadIdx.x == 0) {
+        a.ids[r] = -1;
+        a.logp[r] = sum == sum ? -INFINITY : __builtin_nanf("");
+      }
+      return;
+    }
+    t.s = scale_of(a, m, row.len);
+    if (t.draw_from_groups(r, u, tops, sum)) return;
+    __syncthreads();
+  }
   // the largest logit; what is no number or +inf makes itself known
   float m = -INFINITY;
   bool odd_one = false;
@@ -370,6 +658,7 @@ __global__ __launch_bounds__(WAVES * 64) void token_sample_kernel(const SampleAr
       odd_one = odd_one | !(x[j] < INFINITY);
     }
   });
+  const float mine = m;
   m = wave_max(m);
   if (lane == 0) sh.floats[wave] = m;
   odd_one = __syncthreads_or(odd_one);
@@ -382,94 +671,115 @@ __global__ __launch_bounds__(WAVES * 64) void token_sample_kernel(const SampleAr
     }
     return;
   }
-  const int bits = 32 - __clz(row.len - 1);
-  t.s = {m, a.c, __longlong_as_double((long long)(1023 + 51 - (bits > 11 ? bits - 11 : 0)) << 52), a.inv_t * kBinsATurn};
+  t.s = scale_of(a, m, row.len);
   const RowScale s = t.s;
   Cut cut = {0, 0x7fffffff};
   const bool by_k = a.top_k > 0 && a.top_k < row.len, by_p = a.top_p < 1.0;
-  if (by_k || by_p) {
-    t.clear_bins(true);
+  u64 whole = 0;                                       // by_p: the weight of all entries that may be chosen
+  // Few entries can be kept: a list of them. Of the first top_k, what the threads' largest logits tell: so many entries are at least in the bins up to the one that holds
+  // the top_k-th of these.
+  const bool few = by_k && a.top_k <= WAVES * 16;
+  if (few || a.min_p > 0.0) {
+    int bin = kBins - 1;
+    t.clear_bins(sh.count, sh.mass);
+    if (threadIdx.x == 0) sh.n = 0;
+    if (few) {
+      if (mine > -INFINITY) atomicAdd(&sh.count[bin_of(s, mine)], 1u);
+      if (threadIdx.x == 0) sh.bin = kBins - 1;
+      __syncthreads();
+      t.find_bin(sh.count, sh.mass, false, a.top_k);                      // (where fewer threads have an entry the last bin stays)
+      bin = sh.bin;
+    }
+    __syncthreads();
+    float sum = 0.f;
+    u64 mass = 0;
+    for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int col, const float *x) {
+      for_entries<VEC>(x, [&](int j, float xj) {
+        if (few || !by_p) sum += __builtin_amdgcn_exp2f((xj - m) * c);
+        if (few) {
+          if (xj != -INFINITY && bin_of(s, xj) <= bin) t.push(xj, col + j, weight_of(s, xj));
+        } else {
+          const double w = weight_of(s, xj);
+          if (by_p) mass += xj != -INFINITY ? whole_of(s, w) : 0;
+          if (xj != -INFINITY && w >= a.min_p) t.push(xj, col + j, w);
+        }
+      });
+    });
+    sum = t.block_sum(sum);                            // (its barriers: the list is there)
+    if (!few && by_p) {
+      t.over_waves(wave_sum64(mass), whole);
+      sum = (float)((double)whole / s.one);
+    }
+    // (by min-p alone the first top_k have to be there for top-p to take its share of them)
+    if (sh.n <= kList && (few || !(by_k && by_p) || sh.n >= a.top_k)) {
+      t.draw_from_list(r, u, by_k, by_p, whole, sum);
+      return;
+    }
+    __syncthreads();
+    whole = 0;
+  }
+  auto histogram = [&](bool counts) {
+    t.clear_bins(sh.count, sh.mass);
     for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int, const float *x) {
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        if (x[j] == -INFINITY) continue;
-        const int b = bin_of(s, x[j]);
-        if (by_k) atomicAdd(&sh.count[b], 1u);
-        atomicAdd(&sh.mass[b], whole_of(s, weight_of(s, x[j])));
-        apart(j);
-      }
+      for_entries<VEC>(x, [&](int j, float xj) {
+        if (xj == -INFINITY) return;
+        const int b = bin_of(s, xj);
+        if (counts) atomicAdd(&sh.count[b], 1u);
+        if (by_p) atomicAdd(&sh.mass[b], whole_of(s, weight_of(s, xj)));
+      });
     });
     __syncthreads();
-    u64 whole = 0;
+  };
+  if (by_k || by_p) {
+    histogram(by_k);
+    if (by_p) whole = t.mass_before(sh.mass, kBins);
+    u64 share = whole;                                 // what top-p takes its part of
     if (by_k) {
       u64 n = 0, all;
       for (int i = threadIdx.x; i < kBins; i += WAVES * 64) n += sh.count[i];
       t.over_waves(wave_sum64(n), all);
       if ((u64)a.top_k < all) {
-        // (bins over keys may take the histogram's place, which top-p needs after it)
         cut = t.cut_at(false, a.top_k);
-        whole = sh.upto;
+        share = sh.upto;
+        __syncthreads();
+        if (by_p && t.spoiled) histogram(false);
       }
     }
     if (by_p) {
-      if (by_k && whole > 0) {
-        __syncthreads();
-        t.clear_bins(true);
-        for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int, const float *x) {
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            if (x[j] != -INFINITY) atomicAdd(&sh.mass[bin_of(s, x[j])], whole_of(s, weight_of(s, x[j])));
-            apart(j);
-          }
-        });
-        __syncthreads();
-      } else {
-        u64 n = 0;
-        for (int i = threadIdx.x; i < kBins; i += WAVES * 64) n += sh.mass[i];
-        t.over_waves(wave_sum64(n), whole);
-      }
-      const u64 limit = (u64)ceil(a.top_p * (double)whole);
+      const u64 limit = (u64)ceil(a.top_p * (double)share);
       cut = t.cut_at(true, limit < 1 ? 1 : limit);
     }
   }
   // sums of what is kept, of the waves' shares and, for the log-probability, of all
   u64 kept = 0;
   float sum = 0.f;
-  const float c = a.inv_t * kLog2e;
   auto weight = [&](int col, const float *x) {
     u64 k = 0;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      if (x[j] == -INFINITY || !inside(cut, key_of(x[j]), col + j)) continue;
-      const double w = weight_of(s, x[j]);
+    for_entries<VEC>(x, [&](int j, float xj) {
+      if (xj == -INFINITY || !inside(cut, key_of(xj), col + j)) return;
+      const double w = weight_of(s, xj);
       if (w >= a.min_p) k += whole_of(s, w);
-      apart(j);
-    }
+    });
     return k;
   };
   for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int col, const float *x) {
     kept += weight(col, x);
+    if (!by_p)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) sum += __builtin_amdgcn_exp2f((x[j] - m) * c);
+      for (int j = 0; j < VEC; ++j) sum += __builtin_amdgcn_exp2f((x[j] - m) * c);
   });
   kept = wave_sum64(kept);
   u64 all;
   u64 before = t.over_waves(kept, all);
-  sum = wave_sum(sum);
-  __syncthreads();
-  if (lane == 0) sh.floats[wave] = sum;
+  sum = by_p ? (float)((double)whole / s.one) : t.block_sum(sum);
   // the drawn entry is the first whose sum passes `target`
-  const double want = u > 0.f ? floor((double)u * (double)all) : 0.0;
-  const u64 target = want < (double)all && (u64)want < all ? (u64)want : all - 1;
+  const u64 target = S::target_of(u, all);
   if (before <= target && target < before + kept) {    // in this wave's columns
     sh.bin = t.begin;
     sh.n = t.end;
     sh.before = before;
   }
   __syncthreads();
-  sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) sum += sh.floats[w];
   // those columns shared out once more
   {
     const int first = sh.bin, last = sh.n, n = (last - first + STEP - 1) / STEP, each = (n + WAVES - 1) / WAVES;
@@ -494,26 +804,27 @@ __global__ __launch_bounds__(WAVES * 64) void token_sample_kernel(const SampleAr
     u64 at = before + scan - mine;
     if (!(at <= target && target < at + mine)) return;
     bool found = false;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      if (found || x[j] == -INFINITY || !inside(cut, key_of(x[j]), col + j)) continue;
-      const double w = weight_of(s, x[j]);
+    for_entries<VEC>(x, [&](int j, float xj) {
+      if (found || xj == -INFINITY || !inside(cut, key_of(xj), col + j)) return;
+      const double w = weight_of(s, xj);
       if (w >= a.min_p) at += whole_of(s, w);
-      if (at <= target) continue;
+      if (at <= target) return;
       found = true;
       a.ids[r] = col + j;
-      const float v = (x[j] - m) * a.inv_t - logf(sum);
-      a.logp[r] = v < kLowest ? kLowest : v;
-    }
+      a.logp[r] = t.log_share(xj, sum);
+    });
   });
 }
 
 template <typename T>
-void launch(const xrl_ctx *c, SampleArgs &a, bool small) {
-  for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMaxBlocks) {
-    const dim3 grid((unsigned)std::min(a.n_rows - a.row0, kMaxBlocks));
-    if (small) token_sample_kernel<T, 4><<<grid, dim3(256), 0, op_stream(c)>>>(a);
-    else token_sample_kernel<T, 8><<<grid, dim3(512), 0, op_stream(c)>>>(a);
+void launch(const xrl_ctx *c, SampleArgs &a, int waves) {
+  const int64_t most = kMaxBlocks / std::max(1, a.parts);
+  for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += most) {
+    const dim3 grid((unsigned)std::min(a.n_rows - a.row0, most));
+    if (a.parts) token_sample_groups_kernel<T><<<dim3((unsigned)(grid.x * a.parts)), dim3(256), 0, op_stream(c)>>>(a);
+    if (waves == 4) token_sample_kernel<T, 4><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+    else if (waves == 8) token_sample_kernel<T, 8><<<grid, dim3(512), 0, op_stream(c)>>>(a);
+    else token_sample_kernel<T, 16><<<grid, dim3(1024), 0, op_stream(c)>>>(a);
   }
 }
 
@@ -533,8 +844,18 @@ extern "C" int xrl_token_sample(xrl_ctx *c, const xrl_logits_desc *logits, const
   a.top_k = how->top_k; a.top_p = how->top_p; a.min_p = how->min_p;
   a.uniforms = d_uniforms; a.ids = d_ids; a.logp = d_logp;
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols;
-  const bool small = cols <= 4096;
-  logits->type == XRL_PREC_BF16 ? launch<bf16_t>(c, a, small) : launch<float>(c, a, small);
+  const int waves = cols <= 4096 ? 4 : a.n_rows > op_compute_units(c) ? 8 : 16;
+  // Long rows of which few entries can be kept: by groups.
+  const int64_t parts = (cols + kPart - 1) / kPart;
+  if (!a.row_ptr && cols > kPart && (a.top_k > 0 ? a.top_k * 16 <= parts * kGroups : a.top_p == 1.0 && a.min_p > 0.0) && parts <= 1024) {
+    const size_t tops = op_align((size_t)a.n_rows * parts * kGroups * 4);
+    char *ws = nullptr;
+    if (int rc = op_workspace(c, tops + (size_t)a.n_rows * parts * 8, &ws, who)) return rc;
+    a.parts = (int)parts;
+    a.group_max = (float *)ws;
+    a.part_stats = (float *)(ws + tops);
+  }
+  logits->type == XRL_PREC_BF16 ? launch<bf16_t>(c, a, waves) : launch<float>(c, a, waves);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
