@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 using namespace xrl;
 
@@ -77,37 +78,95 @@ __device__ __forceinline__ void angle_of(int position, float freq, float &c, flo
   sincospif(2.f * (float)t, &s, &c);
 }
 
-// The V columns of a row from e on, and of the other halves of their pairs, as floats; zeros behind dim.
+// V columns of a row as they lie: 16 bytes, or one element.
 template <typename T, int V>
-__device__ __forceinline__ void load_pair(const RotaryArgs &a, const T *row, int e, bool there, float *x, float *o) {
+struct Raw;
+template <>
+struct Raw<float, 4> { typedef u32x4 type; };
+template <>
+struct Raw<bf16_t, 8> { typedef u32x4 type; };
+template <>
+struct Raw<float, 1> { typedef float type; };
+template <>
+struct Raw<bf16_t, 1> { typedef bf16_t type; };
+template <typename T, int V>
+__device__ __forceinline__ float column_of(const typename Raw<T, V>::type &r, int j) {
+  if constexpr (V == 1) return (float)r;
+  else if constexpr (sizeof(T) == 4) return __uint_as_float(r[j]);
+  else return __uint_as_float(j & 1 ? r[j >> 1] & 0xffff0000u : r[j >> 1] << 16);
+}
+// Columns e on of the row, and of the other halves of their pairs: of its first ones where e lies behind dim (what is not there counts as 0 later). No
+// load depends on a condition, so that those of several rows go out together.
+template <typename T, int V>
+struct Two {
+  typename Raw<T, V>::type x, o;
+};
+template <typename T, int V>
+__device__ __forceinline__ typename Raw<T, V>::type load_columns(const T *row, int e, int dim) {
+  return *(const typename Raw<T, V>::type *)(row + (e < dim ? e : 0));
+}
+template <typename T, int V>
+__device__ __forceinline__ Two<T, V> load_pair(const RotaryArgs &a, const T *row, int e) {
+  Two<T, V> c;
+  c.x = load_columns<T, V>(row, e, a.dim);
+  if (V > 1 && a.interleaved) c.o = c.x;
+  else c.o = load_columns<T, V>(row, pair_of(a, e).other, a.dim);
+  return c;
+}
+// Columns behind the pairs have no other half: 0.
+template <typename T, int V>
+__device__ __forceinline__ void alone(Two<T, V> &c, bool paired) {
   if constexpr (V > 1) {
-    Piece<T, V> p, q;
 #pragma unroll
-    for (int j = 0; j < V; ++j) p.v[j] = q.v[j] = (T)0.f;
-    const int other = pair_of(a, e).other;
-    if (there) p = load_piece<T, V>((const T *)__builtin_assume_aligned(row + e, 16));
-    if (a.interleaved) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) q.v[j] = p.v[j ^ 1];
-    } else {
-      q = p;
-      if (there && other != e) q = load_piece<T, V>((const T *)__builtin_assume_aligned(row + other, 16));
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      x[j] = (float)p.v[j];
-      o[j] = (float)q.v[j];
-    }
+    for (int i = 0; i < 4; ++i) c.o[i] = paired ? c.o[i] : 0u;
   } else {
-    x[0] = there ? (float)row[e] : 0.f;
-    o[0] = there ? (float)row[pair_of(a, e).other] : 0.f;
+    c.o = paired ? c.o : (T)0.f;
   }
 }
 template <typename T, int V>
+__device__ __forceinline__ float own_of(const Two<T, V> &c, int j) { return column_of<T, V>(c.x, j); }
+template <typename T, int V>
+__device__ __forceinline__ float other_of(const RotaryArgs &a, const Two<T, V> &c, int j) {
+  if constexpr (V > 1) return a.interleaved ? column_of<T, V>(c.o, j ^ 1) : column_of<T, V>(c.o, j);
+  else return column_of<T, V>(c.o, j);
+}
+template <typename T, int V, bool STREAM>
 __device__ __forceinline__ void store_columns(T *row, int e, bool there, const float *z) {
   if (!there) return;
-  if constexpr (V > 1) store_piece<T, V>((T *)__builtin_assume_aligned(row + e, 16), z);
+  if constexpr (V > 1) store_piece<T, V, STREAM>((T *)__builtin_assume_aligned(row + e, 16), z);
   else row[e] = (T)z[0];
+}
+
+// Cosines and sines of the lane's columns at a position: of column e, z_e = y_e c + y_other s. Behind the pairs 1 and 0.
+template <int V, int PIECES, int LANES>
+__device__ __forceinline__ void turns_of(const RotaryArgs &a, const Columns<V, LANES> &col, int position, float back, float (&c)[PIECES][V], float (&s)[PIECES][V]) {
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      c[p][j] = 1.f;
+      s[p][j] = 0.f;
+    }
+    if (col.at(p, 0) >= a.rotary) continue;
+    if (V > 1 && a.interleaved) {
+#pragma unroll
+      for (int j = 0; j < V; j += 2) {
+        float x, y;
+        angle_of(position, a.freqs[col.at(p, j) >> 1], x, y);
+        c[p][j] = c[p][V > 1 ? j + 1 : 0] = x;
+        s[p][j] = -back * y;
+        s[p][V > 1 ? j + 1 : 0] = back * y;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const Pair r = pair_of(a, col.at(p, j));
+        float y;
+        angle_of(position, a.freqs[r.index], c[p][j], y);
+        s[p][j] = back * r.sign * y;
+      }
+    }
+  }
 }
 
 // A job's token, first head and number of heads.
@@ -121,145 +180,156 @@ __device__ __forceinline__ Job job_of(const RotaryArgs &a, int64_t job) {
   return {t, h0, a.heads - h0 < a.per_job ? a.heads - h0 : a.per_job};
 }
 
-template <typename T, int V, int PIECES, int LANES>
+// Rows of a wave at once: their loads are requested together.
+template <int V>
+constexpr int kRowsAtOnce = V > 1 ? 4 : 1;
+
+template <typename T, int V, int PIECES, int LANES, bool STREAM>
 __global__ __launch_bounds__(256) void head_rotary_kernel(const RotaryArgs a) {
   touch_args(a);
-  constexpr int GROUPS = 64 / LANES;
+  constexpr int GROUPS = 64 / LANES, U = kRowsAtOnce<V>;
   const int64_t job = a.job0 + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (job >= a.jobs) return;
   const Job w = job_of(a, job);
   const int lane = threadIdx.x & 63, group = lane / LANES;
   const Columns<V, LANES> col = {lane % LANES * V};
-  float c[PIECES][V], s[PIECES][V], weight[2][PIECES][V], other[2][PIECES][V];
-  const int position = a.rotary ? a.positions[w.t] : 0;
-#pragma unroll
-  for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int e = col.at(p, j);
-      const Pair r = pair_of(a, e);
-      c[p][j] = 1.f;
-      s[p][j] = 0.f;
-      if (r.index >= 0) {
-        float sine;
-        angle_of(position, a.freqs[r.index], c[p][j], sine);
-        s[p][j] = r.sign * sine;
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const bool has = a.weight[k] && e < a.dim;
-        weight[k][p][j] = has ? a.weight[k][e] : 1.f;
-        other[k][p][j] = has ? a.weight[k][r.other] : 1.f;
-      }
-    }
+  float c[PIECES][V], s[PIECES][V];
+  turns_of<V, PIECES, LANES>(a, col, a.rotary ? a.positions[w.t] : 0, 1.f, c, s);
   const float mean = 1.f / (float)a.dim;
-  for (int i = 0; i < w.count; i += GROUPS) {
-    const int h = w.h0 + i + group, k = h < a.q_heads ? 0 : 1, head = k ? h - a.q_heads : h;
-    const bool row_there = i + group < w.count;
-    const T *x = (const T *)a.x[k].p + w.t * a.x[k].stride + (row_there ? head : 0) * a.x[k].head_stride;
-    T *z = (T *)a.z[k].p + w.t * a.z[k].stride + (row_there ? head : 0) * a.z[k].head_stride;
-    float y[PIECES][V], o[PIECES][V], sum = 0.f;
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    // the job's heads of q, then of k
+    const int lo = k ? max(w.h0, a.q_heads) - a.q_heads : w.h0, hi = k ? w.h0 + w.count - a.q_heads : min(w.h0 + w.count, a.q_heads);
+    if (lo >= hi) continue;
+    const bool norm = a.weight[k] != nullptr;
+    float wc[PIECES][V], ws[PIECES][V];                // z_e = r (x_e w_e c + x_other w_other s)
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-      load_pair<T, V>(a, x, col.at(p, 0), row_there && col.at(p, 0) < a.dim, y[p], o[p]);
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum = fmaf(y[p][j], y[p][j], sum);
-    }
-    const float r = a.weight[k] ? rsqrtf(group_sum<LANES>(sum) * mean + a.eps) : 1.f;
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
+    for (int p = 0; p < PIECES; ++p)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float y1 = y[p][j] * r * (k ? weight[1][p][j] : weight[0][p][j]), y2 = o[p][j] * r * (k ? other[1][p][j] : other[0][p][j]);
-        y[p][j] = s[p][j] == 0.f && c[p][j] == 1.f ? y1 : fmaf(y1, c[p][j], y2 * s[p][j]);
+        const int e = col.at(p, j) < a.dim ? col.at(p, j) : 0;
+        wc[p][j] = norm ? a.weight[k][e] * c[p][j] : c[p][j];
+        ws[p][j] = norm ? a.weight[k][pair_of(a, e).other] * s[p][j] : s[p][j];
       }
-      store_columns<T, V>(z, col.at(p, 0), row_there && col.at(p, 0) < a.dim, y[p]);
+    const T *x = (const T *)a.x[k].p + w.t * a.x[k].stride;
+    T *z = (T *)a.z[k].p + w.t * a.z[k].stride;
+    for (int h0 = lo; h0 < hi; h0 += U * GROUPS) {
+      Two<T, V> v[U][PIECES];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = h0 + i * GROUPS + group;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) v[i][p] = load_pair<T, V>(a, x + (h < hi ? h : lo) * a.x[k].head_stride, col.at(p, 0));
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = h0 + i * GROUPS + group;
+        float sum = 0.f, r = 1.f;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) alone<T, V>(v[i][p], col.at(p, 0) < a.rotary);
+        if (norm) {
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p) {
+            float t = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) t = fmaf(own_of(v[i][p], j), own_of(v[i][p], j), t);
+            sum += col.at(p, 0) < a.dim ? t : 0.f;
+          }
+          r = rsqrtf(group_sum<LANES>(sum) * mean + a.eps);
+        }
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+          float y[V];
+#pragma unroll
+          for (int j = 0; j < V; ++j) y[j] = r * fmaf(own_of(v[i][p], j), wc[p][j], other_of(a, v[i][p], j) * ws[p][j]);
+          store_columns<T, V, STREAM>(z + (h < hi ? h : lo) * a.z[k].head_stride, col.at(p, 0), h < hi && col.at(p, 0) < a.dim, y);
+        }
+      }
     }
   }
 }
 
 // Jobs in turn by a fixed number of blocks, each of which leaves one sum of the weights' gradients.
-template <typename T, int V, int PIECES, int LANES>
+template <typename T, int V, int PIECES, int LANES, bool STREAM>
 __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryArgs a) {
   touch_args(a);
-  constexpr int GROUPS = 64 / LANES;
+  constexpr int GROUPS = 64 / LANES, U = V > 1 ? 2 : 1;
   __shared__ float sums[4][2][LANES * PIECES * V];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane / LANES;
   const Columns<V, LANES> col = {lane % LANES * V};
-  float weight[2][PIECES][V], dw[2][PIECES][V];
+  float dw[2][PIECES][V];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        weight[k][p][j] = a.weight[k] && col.at(p, j) < a.dim ? a.weight[k][col.at(p, j)] : 1.f;
-        dw[k][p][j] = 0.f;
-      }
+    for (int j = 0; j < V; ++j) dw[0][p][j] = dw[1][p][j] = 0.f;
   const float mean = 1.f / (float)a.dim;
   for (int64_t job = (int64_t)blockIdx.x * 4 + wave; job < a.jobs; job += (int64_t)gridDim.x * 4) {
     const Job w = job_of(a, job);
-    const int position = a.rotary ? a.positions[w.t] : 0;
     float c[PIECES][V], s[PIECES][V];
+    turns_of<V, PIECES, LANES>(a, col, a.rotary ? a.positions[w.t] : 0, -1.f, c, s);
+    auto heads = [&](auto tensor) {
+      constexpr int k = decltype(tensor)::value;
+      const int lo = k ? max(w.h0, a.q_heads) - a.q_heads : w.h0, hi = k ? w.h0 + w.count - a.q_heads : min(w.h0 + w.count, a.q_heads);
+      if (lo >= hi) return;
+      const bool norm = a.weight[k] != nullptr;
+      float weight[PIECES][V];
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p)
+      for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const Pair r = pair_of(a, col.at(p, j));
-        c[p][j] = 1.f;
-        s[p][j] = 0.f;
-        if (r.index >= 0) {
-          float sine;
-          angle_of(position, a.freqs[r.index], c[p][j], sine);
-          s[p][j] = -r.sign * sine;                   // back
-        }
-      }
-    for (int i = 0; i < w.count; i += GROUPS) {
-      const int h = w.h0 + i + group, k = h < a.q_heads ? 0 : 1, head = k ? h - a.q_heads : h;
-      const bool row_there = i + group < w.count, norm = a.weight[k] != nullptr;
-      const int hh = row_there ? head : 0;
-      const T *x = norm ? (const T *)a.x[k].p + w.t * a.x[k].stride + hh * a.x[k].head_stride : nullptr;
-      const T *dz = (const T *)a.dz[k].p + w.t * a.dz[k].stride + hh * a.dz[k].head_stride;
-      T *dx = (T *)a.dx[k].p + w.t * a.dx[k].stride + hh * a.dx[k].head_stride;
-      float g[PIECES][V], y[PIECES][V], sum = 0.f, dot = 0.f;
+        for (int j = 0; j < V; ++j) weight[p][j] = norm && col.at(p, j) < a.dim ? a.weight[k][col.at(p, j)] : 1.f;
+      const T *x = (const T *)a.x[k].p + w.t * a.x[k].stride, *dz = (const T *)a.dz[k].p + w.t * a.dz[k].stride;
+      T *dx = (T *)a.dx[k].p + w.t * a.dx[k].stride;
+      for (int h0 = lo; h0 < hi; h0 += U * GROUPS) {
+        Two<T, V> v[U][PIECES];
+        typename Raw<T, V>::type xs[U][PIECES];
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const int e = col.at(p, 0);
-        const bool there = row_there && e < a.dim;
-        float o[V];
-        load_pair<T, V>(a, dz, e, there, g[p], o);
+        for (int i = 0; i < U; ++i) {
+          const int h = h0 + i * GROUPS + group, hh = h < hi ? h : lo;
 #pragma unroll
-        for (int j = 0; j < V; ++j) g[p][j] = s[p][j] == 0.f && c[p][j] == 1.f ? g[p][j] : fmaf(g[p][j], c[p][j], o[j] * s[p][j]);
-#pragma unroll
-        for (int j = 0; j < V; ++j) y[p][j] = 0.f;
-        if (norm && there) {
-          if constexpr (V > 1) {
-            const Piece<T, V> q = load_piece<T, V>((const T *)__builtin_assume_aligned(x + e, 16));
-#pragma unroll
-            for (int j = 0; j < V; ++j) y[p][j] = (float)q.v[j];
-          } else {
-            y[p][0] = (float)x[e];
+          for (int p = 0; p < PIECES; ++p) {
+            const int e = col.at(p, 0);
+            v[i][p] = load_pair<T, V>(a, dz + hh * a.dz[k].head_stride, e);
+            xs[i][p] = norm ? load_columns<T, V>(x + hh * a.x[k].head_stride, e, a.dim) : v[i][p].x;
           }
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          sum = fmaf(y[p][j], y[p][j], sum);
-          dot = fmaf(g[p][j] * (k ? weight[1][p][j] : weight[0][p][j]), y[p][j], dot);
+        for (int i = 0; i < U; ++i) {
+          const int h = h0 + i * GROUPS + group;
+          float g[PIECES][V], sum = 0.f, dot = 0.f, r = 1.f, along = 0.f;
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p) {
+            alone<T, V>(v[i][p], col.at(p, 0) < a.rotary);
+            float t = 0.f, d = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              const float y = column_of<T, V>(xs[i][p], j);
+              g[p][j] = fmaf(own_of(v[i][p], j), c[p][j], other_of(a, v[i][p], j) * s[p][j]);
+              t = fmaf(y, y, t);
+              d = fmaf(g[p][j] * weight[p][j], y, d);
+            }
+            sum += col.at(p, 0) < a.dim ? t : 0.f;
+            dot += col.at(p, 0) < a.dim ? d : 0.f;
+          }
+          if (norm) {
+            r = rsqrtf(group_sum<LANES>(sum) * mean + a.eps);
+            along = group_sum<LANES>(dot) * mean * r * r * r;
+            const float counts = h < hi ? r : 0.f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+              for (int j = 0; j < V; ++j) {
+                const float y = column_of<T, V>(xs[i][p], j);
+                dw[k][p][j] = fmaf(g[p][j] * y, counts, dw[k][p][j]);
+                g[p][j] = fmaf(-y, along, r * g[p][j] * weight[p][j]);
+              }
+          }
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p) store_columns<T, V, STREAM>(dx + (h < hi ? h : lo) * a.dx[k].head_stride, col.at(p, 0), h < hi && col.at(p, 0) < a.dim, g[p]);
         }
       }
-      const float r = norm ? rsqrtf(group_sum<LANES>(sum) * mean + a.eps) : 1.f, along = norm ? group_sum<LANES>(dot) * mean * r * r : 0.f;
-#pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float d = norm ? g[p][j] * y[p][j] * r : 0.f;
-          dw[0][p][j] += k ? 0.f : d;
-          dw[1][p][j] += k ? d : 0.f;
-          g[p][j] = norm ? r * (g[p][j] * (k ? weight[1][p][j] : weight[0][p][j]) - y[p][j] * along) : g[p][j];
-        }
-        store_columns<T, V>(dx, col.at(p, 0), row_there && col.at(p, 0) < a.dim, g[p]);
-      }
-    }
+    };
+    heads(std::integral_constant<int, 0>());
+    heads(std::integral_constant<int, 1>());
   }
   if (!a.partial) return;
   // of the wave's groups, then of the block's waves, in order
@@ -281,18 +351,19 @@ __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryA
   }
 }
 
-// A block of 256 for 16 columns: sixteen sums of every sixteenth block's, then one of these.
-__global__ __launch_bounds__(256) void head_rotary_weights_kernel(const RotaryArgs a) {
-  __shared__ float sums[16][17];
+// A block of 1024 for 16 columns: 64 sums of every 64th block's, then one of these. (With 16 sums of 2048 blocks' 40 us, a chain of loads.)
+__global__ __launch_bounds__(1024) void head_rotary_weights_kernel(const RotaryArgs a) {
+  __shared__ float sums[64][17];
   const int i = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
   float t = 0.f;
   if (i < 2 * a.dim)
-    for (int b = part; b < a.partials; b += 16) t += a.partial[(int64_t)b * 2 * a.dim + i];
+#pragma unroll 8
+    for (int b = part; b < a.partials; b += 64) t += a.partial[(int64_t)b * 2 * a.dim + i];
   sums[part][threadIdx.x & 15] = t;
   __syncthreads();
   if (part || i >= 2 * a.dim) return;
 #pragma unroll
-  for (int p = 1; p < 16; ++p) t += sums[p][threadIdx.x];
+  for (int p = 1; p < 64; ++p) t += sums[p][threadIdx.x];
   float *to = a.dweight[i / a.dim];
   if (to) to[i % a.dim] += t;
 }
@@ -346,14 +417,18 @@ void share_out(const xrl_ctx *c, RotaryArgs &a, int groups) {
   a.jobs = a.n * a.jobs_a_token;
 }
 
-template <typename T, int V, int PIECES, int LANES>
+template <typename T, int V, int PIECES, int LANES, bool STREAM>
 void launch(const xrl_ctx *c, RotaryArgs &a, bool backward) {
   if (backward) {
-    head_rotary_backward_kernel<T, V, PIECES, LANES><<<dim3((unsigned)a.partials), dim3(256), 0, op_stream(c)>>>(a);
+    head_rotary_backward_kernel<T, V, PIECES, LANES, STREAM><<<dim3((unsigned)a.partials), dim3(256), 0, op_stream(c)>>>(a);
     return;
   }
   for (a.job0 = 0; a.job0 < a.jobs; a.job0 += 4 * kMaxBlocks)
-    head_rotary_kernel<T, V, PIECES, LANES><<<dim3((unsigned)((std::min(a.jobs - a.job0, 4 * kMaxBlocks) + 3) / 4)), dim3(256), 0, op_stream(c)>>>(a);
+    head_rotary_kernel<T, V, PIECES, LANES, STREAM><<<dim3((unsigned)((std::min(a.jobs - a.job0, 4 * kMaxBlocks) + 3) / 4)), dim3(256), 0, op_stream(c)>>>(a);
+}
+template <typename T, int V, int LANES>
+void launch_whole(const xrl_ctx *c, RotaryArgs &a, bool backward) {
+  streams(a.n * a.heads * a.dim * (int)sizeof(T)) ? launch<T, V, 1, LANES, true>(c, a, backward) : launch<T, V, 1, LANES, false>(c, a, backward);
 }
 
 // A row in as many lanes as have 16 bytes of it each, at least eight; rows at odd places, or pairs that such pieces would cut, element by element.
@@ -366,11 +441,11 @@ int lanes_of(const RotaryArgs &a, int v, bool aligned) {
 template <typename T>
 void launch_lanes(const xrl_ctx *c, RotaryArgs &a, bool aligned, int lanes, bool backward) {
   constexpr int V = 16 / (int)sizeof(T);
-  if (!aligned) launch<T, 1, 4, 64>(c, a, backward);
-  else if (lanes == 8) launch<T, V, 1, 8>(c, a, backward);
-  else if (lanes == 16) launch<T, V, 1, 16>(c, a, backward);
-  else if (lanes == 32 || V * 32 >= 256) launch<T, V, 1, 32>(c, a, backward);
-  else if constexpr (V * 32 < 256) launch<T, V, 1, 64>(c, a, backward);
+  if (!aligned) launch<T, 1, 4, 64, false>(c, a, backward);
+  else if (lanes == 8) launch_whole<T, V, 8>(c, a, backward);
+  else if (lanes == 16) launch_whole<T, V, 16>(c, a, backward);
+  else if (lanes == 32 || V * 32 >= 256) launch_whole<T, V, 32>(c, a, backward);
+  else if constexpr (V * 32 < 256) launch_whole<T, V, 64>(c, a, backward);
 }
 
 }  // namespace
@@ -433,14 +508,14 @@ int xrl_head_rotary_backward(xrl_ctx *c, const xrl_rotary_desc *d, const xrl_hea
   a.dweight[1] = d->d_k_weight ? d_dk_weight : nullptr;
   const int lanes = lanes_of(a, v, aligned);
   share_out(c, a, 64 / lanes);
-  a.partials = (int)std::min<int64_t>((a.jobs + 3) / 4, 8 * (int64_t)op_compute_units(c));
+  a.partials = (int)std::min<int64_t>((a.jobs + 3) / 4, 4 * (int64_t)op_compute_units(c));
   if (a.dweight[0] || a.dweight[1]) {
     char *ws = nullptr;
     if (int rc = op_workspace(c, (size_t)a.partials * 2 * a.dim * 4, &ws, who)) return rc;
     a.partial = (float *)ws;
   }
   es == 2 ? launch_lanes<bf16_t>(c, a, aligned, lanes, true) : launch_lanes<float>(c, a, aligned, lanes, true);
-  if (a.partial) head_rotary_weights_kernel<<<dim3((unsigned)((2 * a.dim + 15) / 16)), dim3(256), 0, op_stream(c)>>>(a);
+  if (a.partial) head_rotary_weights_kernel<<<dim3((unsigned)((2 * a.dim + 15) / 16)), dim3(1024), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
