@@ -4,7 +4,8 @@
 // gradient to z rotated back: dw += g x r, dx = r (g w - x r^2 mean(g w x)).
 //
 // Bound by memory. A row lies in the lanes of one wave, 16 bytes a lane, so its mean is a few lane moves; the other half of a pair comes from the lane's own piece, or from the
-// cache line that a neighbour has just read. A wave keeps its token while it goes over heads: cosines and sines, of an angle in 64 bits, are computed once a token.
+// cache line that a neighbour has just read. A block has up to eight tokens, computes their
+// cosines and sines, of angles in 64 bits, once, while its first rows are on their way, and goes over all their heads with the next rows' loads ahead.
 #include "op_common.h"
 
 #include <algorithm>
@@ -15,20 +16,22 @@ using namespace xrl;
 
 namespace {
 
+constexpr int kTokens = 8, kPairs = 128;           // rows of a block, and pairs of a head, at most
+
 struct Heads {
   const void *p;
   int64_t stride, head_stride;
 };
 
 struct RotaryArgs {
-  int64_t n, jobs, job0;        // rows; jobs of a token and some of its heads, and the first one of this launch
+  int64_t n, block0;            // rows; first block of this launch
   int q_heads, heads, dim, rotary, interleaved;   // heads: of q and k
-  int per_job, jobs_a_token;    // heads of one job
+  int tokens;                   // rows of a block
   float eps;
   const int32_t *positions;
   const float *freqs, *weight[2];
   Heads x[2], z[2], dz[2], dx[2];   // q, k
-  float *partial;               // [jobs' blocks][2][dim]: sums of the weights' gradients
+  float *partial;               // [blocks][2][dim]: sums of the weights' gradients
   float *dweight[2];
   int partials;
 };
@@ -137,93 +140,104 @@ __device__ __forceinline__ void store_columns(T *row, int e, bool there, const f
   else row[e] = (T)z[0];
 }
 
-// Cosines and sines of the lane's columns at a position: of column e, z_e = y_e c + y_other s. Behind the pairs 1 and 0.
-template <int V, int PIECES, int LANES>
-__device__ __forceinline__ void turns_of(const RotaryArgs &a, const Columns<V, LANES> &col, int position, float back, float (&c)[PIECES][V], float (&s)[PIECES][V]) {
-#pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
+// Cosines and sines of a block's tokens, every pair's once: [token][pair].
+struct Turns {
+  float c[kTokens * kPairs], s[kTokens * kPairs];
+};
+__device__ __forceinline__ void make_turns(const RotaryArgs &a, Turns &t, int64_t t0, int tokens, float back) {
+  const int pairs = a.rotary >> 1;
+  for (int i = threadIdx.x; i < tokens * pairs; i += 256) {
+    const int token = i / pairs, pair = i % pairs;
+    float c, s;
+    angle_of(a.positions[t0 + token], a.freqs[pair], c, s);
+    t.c[token * kPairs + pair] = c;
+    t.s[token * kPairs + pair] = back * s;
+  }
+  __syncthreads();
+}
+// Of the lane's V columns from e on: z_e = y_e c + y_other s. Behind the pairs 1 and 0.
+template <int V>
+__device__ __forceinline__ void turn_of(const RotaryArgs &a, const Turns &t, int token, int e, float (&c)[V], float (&s)[V]) {
+  if (e >= a.rotary) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      c[p][j] = 1.f;
-      s[p][j] = 0.f;
+      c[j] = 1.f;
+      s[j] = 0.f;
     }
-    if (col.at(p, 0) >= a.rotary) continue;
-    if (V > 1 && a.interleaved) {
+    return;
+  }
+  if (V > 1 && a.interleaved) {
+    const float *tc = t.c + token * kPairs + (e >> 1), *ts = t.s + token * kPairs + (e >> 1);
 #pragma unroll
-      for (int j = 0; j < V; j += 2) {
-        float x, y;
-        angle_of(position, a.freqs[col.at(p, j) >> 1], x, y);
-        c[p][j] = c[p][V > 1 ? j + 1 : 0] = x;
-        s[p][j] = -back * y;
-        s[p][V > 1 ? j + 1 : 0] = back * y;
-      }
-    } else {
+    for (int j = 0; j < V; ++j) {
+      c[j] = tc[j >> 1];
+      s[j] = j & 1 ? ts[j >> 1] : -ts[j >> 1];
+    }
+  } else {
+    const Pair r = pair_of(a, e);
+    const float *tc = t.c + token * kPairs + r.index, *ts = t.s + token * kPairs + r.index;
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const Pair r = pair_of(a, col.at(p, j));
-        float y;
-        angle_of(position, a.freqs[r.index], c[p][j], y);
-        s[p][j] = back * r.sign * y;
-      }
+    for (int j = 0; j < V; ++j) {
+      c[j] = tc[j];
+      s[j] = r.sign * ts[j];
     }
   }
 }
 
-// A job's token, first head and number of heads.
-struct Job {
-  int64_t t;
-  int h0, count;
+// A block's rows of one tensor: token by token, head by head. A group of LANES lanes has every so many-th of them, U at a time.
+struct RowAt {
+  int token, head;
 };
-__device__ __forceinline__ Job job_of(const RotaryArgs &a, int64_t job) {
-  const int64_t t = job / a.jobs_a_token;
-  const int h0 = (int)(job % a.jobs_a_token) * a.per_job;
-  return {t, h0, a.heads - h0 < a.per_job ? a.heads - h0 : a.per_job};
+__device__ __forceinline__ RowAt row_at(unsigned i, unsigned rows, unsigned heads) {
+  i = i < rows ? i : 0;
+  const unsigned t = i / heads;
+  return {(int)t, (int)(i - t * heads)};
 }
 
-// Rows of a wave at once: their loads are requested together.
-template <int V>
-constexpr int kRowsAtOnce = V > 1 ? 4 : 1;
-
+// us, 16384 rows of 32 + 8 heads of 128 in bf16, half of each rotated: 83, 4.05 TB/s read and written (one row at a time 86, four 88, with results that stay in the caches 107, without
+// the next rows' loads ahead 110).
 template <typename T, int V, int PIECES, int LANES, bool STREAM>
 __global__ __launch_bounds__(256) void head_rotary_kernel(const RotaryArgs a) {
   touch_args(a);
-  constexpr int GROUPS = 64 / LANES, U = kRowsAtOnce<V>;
-  const int64_t job = a.job0 + (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (job >= a.jobs) return;
-  const Job w = job_of(a, job);
-  const int lane = threadIdx.x & 63, group = lane / LANES;
-  const Columns<V, LANES> col = {lane % LANES * V};
-  float c[PIECES][V], s[PIECES][V];
-  turns_of<V, PIECES, LANES>(a, col, a.rotary ? a.positions[w.t] : 0, 1.f, c, s);
+  constexpr int GROUPS = 256 / LANES, U = V > 1 ? 2 : 1;
+  __shared__ Turns turns;
+  const int64_t t0 = (a.block0 + blockIdx.x) * a.tokens;
+  const int tokens = (int)(a.n - t0 < a.tokens ? a.n - t0 : a.tokens), group = threadIdx.x / LANES;
+  const Columns<V, LANES> col = {(int)threadIdx.x % LANES * V};
   const float mean = 1.f / (float)a.dim;
 #pragma unroll 1
   for (int k = 0; k < 2; ++k) {
-    // the job's heads of q, then of k
-    const int lo = k ? max(w.h0, a.q_heads) - a.q_heads : w.h0, hi = k ? w.h0 + w.count - a.q_heads : min(w.h0 + w.count, a.q_heads);
-    if (lo >= hi) continue;
+    const int heads = k ? a.heads - a.q_heads : a.q_heads, rows = tokens * heads;
+    const T *x = (const T *)a.x[k].p + t0 * a.x[k].stride;
+    T *z = (T *)a.z[k].p + t0 * a.z[k].stride;
+    Two<T, V> v[U][PIECES], next[U][PIECES];
+    auto load = [&](int first, Two<T, V> (&to)[U][PIECES]) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const RowAt at = row_at(first + i * GROUPS + group, rows, heads);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) to[i][p] = load_pair<T, V>(a, x + at.token * a.x[k].stride + at.head * a.x[k].head_stride, col.at(p, 0));
+      }
+    };
+    if (rows > 0) load(0, v);                          // (on their way while the angles are computed)
+    if (k == 0) make_turns(a, turns, t0, tokens, 1.f);
+    if (rows == 0) continue;
     const bool norm = a.weight[k] != nullptr;
-    float wc[PIECES][V], ws[PIECES][V];                // z_e = r (x_e w_e c + x_other w_other s)
+    float weight[PIECES][V], other[PIECES][V];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const int e = col.at(p, j) < a.dim ? col.at(p, j) : 0;
-        wc[p][j] = norm ? a.weight[k][e] * c[p][j] : c[p][j];
-        ws[p][j] = norm ? a.weight[k][pair_of(a, e).other] * s[p][j] : s[p][j];
+        weight[p][j] = norm ? a.weight[k][e] : 1.f;
+        other[p][j] = norm ? a.weight[k][pair_of(a, e).other] : 1.f;
       }
-    const T *x = (const T *)a.x[k].p + w.t * a.x[k].stride;
-    T *z = (T *)a.z[k].p + w.t * a.z[k].stride;
-    for (int h0 = lo; h0 < hi; h0 += U * GROUPS) {
-      Two<T, V> v[U][PIECES];
+    for (int first = 0; first < rows; first += U * GROUPS) {
+      if (first + U * GROUPS < rows) load(first + U * GROUPS, next);
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const int h = h0 + i * GROUPS + group;
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) v[i][p] = load_pair<T, V>(a, x + (h < hi ? h : lo) * a.x[k].head_stride, col.at(p, 0));
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int h = h0 + i * GROUPS + group;
+        const int n = first + i * GROUPS + group;
+        const RowAt at = row_at(n, rows, heads);
         float sum = 0.f, r = 1.f;
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) alone<T, V>(v[i][p], col.at(p, 0) < a.rotary);
@@ -239,71 +253,82 @@ __global__ __launch_bounds__(256) void head_rotary_kernel(const RotaryArgs a) {
         }
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-          float y[V];
+          float c[V], s[V], y[V];
+          turn_of<V>(a, turns, at.token, col.at(p, 0), c, s);
 #pragma unroll
-          for (int j = 0; j < V; ++j) y[j] = r * fmaf(own_of(v[i][p], j), wc[p][j], other_of(a, v[i][p], j) * ws[p][j]);
-          store_columns<T, V, STREAM>(z + (h < hi ? h : lo) * a.z[k].head_stride, col.at(p, 0), h < hi && col.at(p, 0) < a.dim, y);
+          for (int j = 0; j < V; ++j) y[j] = r * fmaf(own_of(v[i][p], j) * weight[p][j], c[j], other_of(a, v[i][p], j) * other[p][j] * s[j]);
+          store_columns<T, V, STREAM>(z + at.token * a.z[k].stride + at.head * a.z[k].head_stride, col.at(p, 0), n < rows && col.at(p, 0) < a.dim, y);
         }
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) v[i][p] = next[i][p];
       }
     }
   }
 }
 
-// Jobs in turn by a fixed number of blocks, each of which leaves one sum of the weights' gradients.
+// Tokens in turn by a fixed number of blocks, each of which leaves one sum of the weights' gradients. The same rows: 121 us, 4.2 TB/s (two rows at a time 158: 149 registers for 110).
 template <typename T, int V, int PIECES, int LANES, bool STREAM>
 __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryArgs a) {
   touch_args(a);
-  constexpr int GROUPS = 64 / LANES, U = V > 1 ? 2 : 1;
+  constexpr int GROUPS = 256 / LANES, IN_WAVE = 64 / LANES, U = 1;
+  __shared__ Turns turns;
   __shared__ float sums[4][2][LANES * PIECES * V];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = lane / LANES;
-  const Columns<V, LANES> col = {lane % LANES * V};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, group = threadIdx.x / LANES;
+  const Columns<V, LANES> col = {(int)threadIdx.x % LANES * V};
   float dw[2][PIECES][V];
 #pragma unroll
   for (int p = 0; p < PIECES; ++p)
 #pragma unroll
     for (int j = 0; j < V; ++j) dw[0][p][j] = dw[1][p][j] = 0.f;
   const float mean = 1.f / (float)a.dim;
-  for (int64_t job = (int64_t)blockIdx.x * 4 + wave; job < a.jobs; job += (int64_t)gridDim.x * 4) {
-    const Job w = job_of(a, job);
-    float c[PIECES][V], s[PIECES][V];
-    turns_of<V, PIECES, LANES>(a, col, a.rotary ? a.positions[w.t] : 0, -1.f, c, s);
-    auto heads = [&](auto tensor) {
-      constexpr int k = decltype(tensor)::value;
-      const int lo = k ? max(w.h0, a.q_heads) - a.q_heads : w.h0, hi = k ? w.h0 + w.count - a.q_heads : min(w.h0 + w.count, a.q_heads);
-      if (lo >= hi) return;
+  for (int64_t t0 = (int64_t)blockIdx.x * a.tokens; t0 < a.n; t0 += (int64_t)gridDim.x * a.tokens) {
+    const int tokens = (int)(a.n - t0 < a.tokens ? a.n - t0 : a.tokens);
+    auto tensor = [&](auto which) {
+      constexpr int k = decltype(which)::value;
+      const int heads = k ? a.heads - a.q_heads : a.q_heads, rows = tokens * heads;
       const bool norm = a.weight[k] != nullptr;
+      const T *x = (const T *)a.x[k].p + t0 * a.x[k].stride, *dz = (const T *)a.dz[k].p + t0 * a.dz[k].stride;
+      T *dx = (T *)a.dx[k].p + t0 * a.dx[k].stride;
+      Two<T, V> v[U][PIECES], next[U][PIECES];
+      typename Raw<T, V>::type xs[U][PIECES], next_xs[U][PIECES];
+      auto load = [&](int first, Two<T, V> (&to)[U][PIECES], typename Raw<T, V>::type (&to_xs)[U][PIECES]) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const RowAt at = row_at(first + i * GROUPS + group, rows, heads);
+#pragma unroll
+          for (int p = 0; p < PIECES; ++p) {
+            to[i][p] = load_pair<T, V>(a, dz + at.token * a.dz[k].stride + at.head * a.dz[k].head_stride, col.at(p, 0));
+            to_xs[i][p] = norm ? load_columns<T, V>(x + at.token * a.x[k].stride + at.head * a.x[k].head_stride, col.at(p, 0), a.dim) : to[i][p].x;
+          }
+        }
+      };
+      if (rows > 0) load(0, v, xs);
+      if (k == 0) {
+        __syncthreads();                               // (the tokens before are done)
+        make_turns(a, turns, t0, tokens, -1.f);
+      }
+      if (rows == 0) return;
       float weight[PIECES][V];
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-        for (int j = 0; j < V; ++j) weight[p][j] = norm && col.at(p, j) < a.dim ? a.weight[k][col.at(p, j)] : 1.f;
-      const T *x = (const T *)a.x[k].p + w.t * a.x[k].stride, *dz = (const T *)a.dz[k].p + w.t * a.dz[k].stride;
-      T *dx = (T *)a.dx[k].p + w.t * a.dx[k].stride;
-      for (int h0 = lo; h0 < hi; h0 += U * GROUPS) {
-        Two<T, V> v[U][PIECES];
-        typename Raw<T, V>::type xs[U][PIECES];
+        for (int j = 0; j < V; ++j) weight[p][j] = norm ? a.weight[k][col.at(p, j) < a.dim ? col.at(p, j) : 0] : 1.f;
+      for (int first = 0; first < rows; first += U * GROUPS) {
+        if (first + U * GROUPS < rows) load(first + U * GROUPS, next, next_xs);
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-          const int h = h0 + i * GROUPS + group, hh = h < hi ? h : lo;
-#pragma unroll
-          for (int p = 0; p < PIECES; ++p) {
-            const int e = col.at(p, 0);
-            v[i][p] = load_pair<T, V>(a, dz + hh * a.dz[k].head_stride, e);
-            xs[i][p] = norm ? load_columns<T, V>(x + hh * a.x[k].head_stride, e, a.dim) : v[i][p].x;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int h = h0 + i * GROUPS + group;
+          const int n = first + i * GROUPS + group;
+          const RowAt at = row_at(n, rows, heads);
           float g[PIECES][V], sum = 0.f, dot = 0.f, r = 1.f, along = 0.f;
 #pragma unroll
           for (int p = 0; p < PIECES; ++p) {
             alone<T, V>(v[i][p], col.at(p, 0) < a.rotary);
-            float t = 0.f, d = 0.f;
+            float c[V], s[V], t = 0.f, d = 0.f;
+            turn_of<V>(a, turns, at.token, col.at(p, 0), c, s);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
               const float y = column_of<T, V>(xs[i][p], j);
-              g[p][j] = fmaf(own_of(v[i][p], j), c[p][j], other_of(a, v[i][p], j) * s[p][j]);
+              g[p][j] = fmaf(own_of(v[i][p], j), c[j], other_of(a, v[i][p], j) * s[j]);
               t = fmaf(y, y, t);
               d = fmaf(g[p][j] * weight[p][j], y, d);
             }
@@ -313,7 +338,7 @@ __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryA
           if (norm) {
             r = rsqrtf(group_sum<LANES>(sum) * mean + a.eps);
             along = group_sum<LANES>(dot) * mean * r * r * r;
-            const float counts = h < hi ? r : 0.f;
+            const float counts = n < rows ? r : 0.f;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p)
 #pragma unroll
@@ -324,12 +349,16 @@ __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryA
               }
           }
 #pragma unroll
-          for (int p = 0; p < PIECES; ++p) store_columns<T, V, STREAM>(dx + (h < hi ? h : lo) * a.dx[k].head_stride, col.at(p, 0), h < hi && col.at(p, 0) < a.dim, g[p]);
+          for (int p = 0; p < PIECES; ++p) {
+            store_columns<T, V, STREAM>(dx + at.token * a.dx[k].stride + at.head * a.dx[k].head_stride, col.at(p, 0), n < rows && col.at(p, 0) < a.dim, g[p]);
+            v[i][p] = next[i][p];
+            xs[i][p] = next_xs[i][p];
+          }
         }
       }
     };
-    heads(std::integral_constant<int, 0>());
-    heads(std::integral_constant<int, 1>());
+    tensor(std::integral_constant<int, 0>());
+    tensor(std::integral_constant<int, 1>());
   }
   if (!a.partial) return;
   // of the wave's groups, then of the block's waves, in order
@@ -341,8 +370,8 @@ __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryA
       for (int j = 0; j < V; ++j) {
         float t = dw[k][p][j], u = t;
 #pragma unroll
-        for (int m = 1; m < GROUPS; ++m) u += __shfl(t, (lane + m * LANES) & 63);
-        if (group == 0) sums[wave][k][col.at(p, j)] = u;
+        for (int m = 1; m < IN_WAVE; ++m) u += __shfl(t, (lane + m * LANES) & 63);
+        if (lane < LANES) sums[wave][k][col.at(p, j)] = u;
       }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.dim; i += 256) {
@@ -408,14 +437,8 @@ int check_rotary(const xrl_ctx *c, const xrl_rotary_desc *d, const char *who, Ro
   return XRL_OK;
 }
 
-// Heads of a job: all of a token where there are tokens for eight waves a SIMD, else so many that the chip is full, or one round of a wave's.
-void share_out(const xrl_ctx *c, RotaryArgs &a, int groups) {
-  const int64_t waves = 32 * (int64_t)op_compute_units(c);
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>((waves + a.n - 1) / a.n, (a.heads + groups - 1) / groups));
-  a.per_job = (int)((a.heads + parts - 1) / parts + groups - 1) / groups * groups;
-  a.jobs_a_token = (a.heads + a.per_job - 1) / a.per_job;
-  a.jobs = a.n * a.jobs_a_token;
-}
+// Rows of a block: as many as leave four blocks for every compute unit, at most eight.
+int rows_of_block(const xrl_ctx *c, int64_t n) { return (int)std::min<int64_t>(std::max<int64_t>(1, n / (4 * op_compute_units(c))), kTokens); }
 
 template <typename T, int V, int PIECES, int LANES, bool STREAM>
 void launch(const xrl_ctx *c, RotaryArgs &a, bool backward) {
@@ -423,8 +446,9 @@ void launch(const xrl_ctx *c, RotaryArgs &a, bool backward) {
     head_rotary_backward_kernel<T, V, PIECES, LANES, STREAM><<<dim3((unsigned)a.partials), dim3(256), 0, op_stream(c)>>>(a);
     return;
   }
-  for (a.job0 = 0; a.job0 < a.jobs; a.job0 += 4 * kMaxBlocks)
-    head_rotary_kernel<T, V, PIECES, LANES, STREAM><<<dim3((unsigned)((std::min(a.jobs - a.job0, 4 * kMaxBlocks) + 3) / 4)), dim3(256), 0, op_stream(c)>>>(a);
+  const int64_t blocks = (a.n + a.tokens - 1) / a.tokens;
+  for (a.block0 = 0; a.block0 < blocks; a.block0 += kMaxBlocks)
+    head_rotary_kernel<T, V, PIECES, LANES, STREAM><<<dim3((unsigned)std::min(blocks - a.block0, kMaxBlocks)), dim3(256), 0, op_stream(c)>>>(a);
 }
 template <typename T, int V, int LANES>
 void launch_whole(const xrl_ctx *c, RotaryArgs &a, bool backward) {
@@ -483,7 +507,7 @@ int xrl_head_rotary(xrl_ctx *c, const xrl_rotary_desc *d, const xrl_heads *q, co
   if (int rc = check_rows(k_out, a.n, d->kv_heads, a.dim, es, true, "k_out", who, a.z[1], aligned)) return rc;
   if (a.n == 0 || a.heads == 0) return XRL_OK;
   const int lanes = lanes_of(a, v, aligned);
-  share_out(c, a, 64 / lanes);
+  a.tokens = rows_of_block(c, a.n);
   es == 2 ? launch_lanes<bf16_t>(c, a, aligned, lanes, false) : launch_lanes<float>(c, a, aligned, lanes, false);
   OP_TRY(hipGetLastError());
   return XRL_OK;
@@ -507,8 +531,8 @@ int xrl_head_rotary_backward(xrl_ctx *c, const xrl_rotary_desc *d, const xrl_hea
   a.dweight[0] = d->d_q_weight ? d_dq_weight : nullptr;
   a.dweight[1] = d->d_k_weight ? d_dk_weight : nullptr;
   const int lanes = lanes_of(a, v, aligned);
-  share_out(c, a, 64 / lanes);
-  a.partials = (int)std::min<int64_t>((a.jobs + 3) / 4, 4 * (int64_t)op_compute_units(c));
+  a.tokens = rows_of_block(c, a.n);
+  a.partials = (int)std::min<int64_t>((a.n + a.tokens - 1) / a.tokens, 4 * (int64_t)op_compute_units(c));
   if (a.dweight[0] || a.dweight[1]) {
     char *ws = nullptr;
     if (int rc = op_workspace(c, (size_t)a.partials * 2 * a.dim * 4, &ws, who)) return rc;
