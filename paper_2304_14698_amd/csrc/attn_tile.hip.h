@@ -123,16 +123,16 @@ __device__ __forceinline__ void load_row(Vec<T> *x, const T *p, bool there, int 
   }
 }
 
-// An accumulator tile whose columns are rows of the result (lane l % 32: the row at p, registers: its columns), times f. `quads`: four columns may be stored
-// together.
-template <typename T, int DP>
-__device__ __forceinline__ void store_row(T *p, bool there, int dim, bool quads, const f32x16 (&acc)[DP / 32], float f, int g) {
+// Accumulator tiles whose columns are rows of the result (lane l % 32: the row at p, registers: NB blocks of 32 of its columns from block db0 on), times f. `quads`: four
+// columns may be stored together.
+template <typename T, int NB>
+__device__ __forceinline__ void store_row(T *p, bool there, int dim, bool quads, const f32x16 (&acc)[NB], float f, int g, int db0 = 0) {
   if (!there) return;
 #pragma unroll
-  for (int db = 0; db < DP / 32; ++db)
+  for (int db = 0; db < NB; ++db)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const int d = 32 * db + 8 * q + 4 * g;
+      const int d = 32 * (db0 + db) + 8 * q + 4 * g;
       const float v[4] = {acc[db][4 * q] * f, acc[db][4 * q + 1] * f, acc[db][4 * q + 2] * f, acc[db][4 * q + 3] * f};
       if (quads) {
         if (d < dim) store4<T>(p + d, v);
@@ -161,6 +161,9 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// What stands in a key or value that a row does not see may reach it through a product with 0. Where results of the ordinary way are not finite, a kernel goes over its keys again with
+// such places kept apart (SAFE), 32 columns of the result at a time: that takes few registers, which would otherwise count for every call.
+//
 // acc += a b where b is 0 at places that do not count: what a holds there reaches nothing, an infinity or NaN neither. `seen` has 1 at the places of b that
 // count; an a that is not finite makes NaN of the results that see it.
 template <typename T>
@@ -173,7 +176,6 @@ __device__ __forceinline__ void mma_seen(Vec<T> a, const Vec<T> &b, const Vec<T>
     odd[j] = (T)(fine ? 0.f : 1.f);
     a[j] = fine ? a[j] : (T)0.f;
   }
-  __builtin_amdgcn_sched_barrier(0);                  // (one at a time: this way is taken where something is not finite, and its registers count for all calls)
   f32x16 n = zero_acc();
   Operand<T>::mma(odd, seen, n);
   Operand<T>::mma(a, b, acc);
@@ -189,10 +191,11 @@ __device__ __forceinline__ bool all_finite(const f32x16 &a) {
 }
 
 // One step of a softmax that runs along: KT keys and values in tiles, q the fragments of 32 queries, one a lane. o += sum over the keys n of 2^(s_n c - mc) v_n, l their sum in
-// this lane's half of the keys, mc the reference of the exponentials. `whole`: every query of the wave sees all keys, else those for which sees(n). SAFE: what stands in keys
-// and values that are not seen reaches nothing.
-template <typename T, int DP, int KT, bool SAFE, typename Sees>
-__device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> *q, float c, bool whole, Sees sees, f32x16 (&o)[DP / 32], float &mc, float &l, int lane) {
+// this lane's half of the keys, mc the reference of the exponentials. `whole`: every query of the wave sees all keys, else key
+// n + 4 (lane / 32) where sees(n): n is a constant at each place. NB blocks of
+// 32 of v's columns, from block db0 on. SAFE: what stands in keys and values that are not seen reaches nothing.
+template <typename T, int DP, int KT, bool SAFE, int NB, typename Sees>
+__device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> *q, float c, bool whole, Sees sees, f32x16 (&o)[NB], float &mc, float &l, int lane, int db0 = 0) {
   using L = Tile<T, DP>;
   using vec = Vec<T>;
   const int g = lane >> 5;
@@ -207,7 +210,7 @@ __device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> 
 #pragma unroll
     for (int kb = 0; kb < KT / 32; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[kb][r] = sees(32 * kb + acc_row(r, g)) ? s[kb][r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) s[kb][r] = sees(32 * kb + acc_row(r, 0)) ? s[kb][r] : -INFINITY;
   }
   float mx = s[0][0];
 #pragma unroll
@@ -223,7 +226,7 @@ __device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> 
     mc = m;
     l *= f;
 #pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db)
+    for (int db = 0; db < NB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[db][r] *= f;
   }
@@ -242,12 +245,12 @@ __device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> 
       if (SAFE && !whole) {
         vec seen;
 #pragma unroll
-        for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(32 * kb + acc_row(x * L::V + n, g)) ? 1.f : 0.f);
+        for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(32 * kb + acc_row(x * L::V + n, 0)) ? 1.f : 0.f);
 #pragma unroll
-        for (int db = 0; db < L::BLOCKS; ++db) mma_seen<T>(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, seen, o[db]);
+        for (int db = 0; db < NB; ++db) mma_seen<T>(L::across(vt, 32 * kb + x * L::STEP, db0 + db, lane), p, seen, o[db]);
       } else {
 #pragma unroll
-        for (int db = 0; db < L::BLOCKS; ++db) Operand<T>::mma(L::across(vt, 32 * kb + x * L::STEP, db, lane), p, o[db]);
+        for (int db = 0; db < NB; ++db) Operand<T>::mma(L::across(vt, 32 * kb + x * L::STEP, db0 + db, lane), p, o[db]);
       }
     }
 }

@@ -37,14 +37,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
   const T *k = head_at<T>(a.k, ks.begin, kv), *v = head_at<T>(a.v, ks.begin, kv);
   const unsigned base = lds_address(lds);
   const float c = a.scale * kLog2e;
-  f32x16 o[L::BLOCKS];
   float mc, l;
-  auto pass = [&](auto safe) {
+  auto pass = [&](auto safe, auto &o, int db0) {
     constexpr bool SAFE = decltype(safe)::value;
     mc = kLowest;
     l = 0.f;
-#pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db) o[db] = zero_acc();
+    for (auto &x : o) x = zero_acc();
     if (tiles > 0) {
       stage_tile<T, DP, KT, WAVES>(k, keys, a.k.stride, a.dim_in, base, wave, lane);
       stage_tile<T, DP, KT, WAVES>(v, keys, a.v.stride, a.dim_in, base + 2 * BYTES, wave, lane);
@@ -60,22 +58,25 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
       }
       const int j0 = t * KT;
       if (j0 >= any_sees) continue;
-      add_tile<T, DP, KT, SAFE>(kt, vt, q, c, j0 + KT <= all_see, [&](int n) { return j0 + n < mine; }, o, mc, l, lane);
+      add_tile<T, DP, KT, SAFE>(kt, vt, q, c, j0 + KT <= all_see, [&](int n) { return n < mine - j0 - 4 * g; }, o, mc, l, lane, db0);
     }
+    l = half_sum(l);
+    store_row<T>(head_at<T>(a.out, qs.begin + i, at.head), there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, g, db0);
   };
-  pass(std::false_type());
-  // What stands in a key or value that a row does not see may have reached it through a product with 0. Where results are not finite, a second time with such
-  // places kept apart.
-  if (a.causal) {
-    bool fine = true;
+  f32x16 o[L::BLOCKS];
+  pass(std::false_type(), o, 0);
+  if (there && g == 0) a.lse[(qs.begin + i) * a.q_heads + at.head] = l == 0.f ? -INFINITY : mc * kLn2 + logf(l);
+  if (!a.causal) return;
+  bool fine = true;
 #pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(o[db]);
-    if (__syncthreads_or(!fine)) pass(std::true_type());
+  for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(o[db]);
+  if (!__syncthreads_or(!fine)) return;
+#pragma unroll 1
+  for (int db = 0; db < L::BLOCKS; ++db) {
+    __syncthreads();                                // (the last tiles are read)
+    f32x16 one[1];
+    pass(std::true_type(), one, db);
   }
-  l = half_sum(l);
-  const bool any = !(l == 0.f);
-  store_row<T, DP>(head_at<T>(a.out, qs.begin + i, at.head), there, a.dim, a.quads, o, any ? 1.f / l : 0.f, g);
-  if (there && g == 0) a.lse[(qs.begin + i) * a.q_heads + at.head] = any ? mc * kLn2 + logf(l) : -INFINITY;
 }
 
 template <typename T, int DP>

@@ -53,11 +53,10 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
   const T *k = head_at<T>(a.k, ks.begin, kv), *v = head_at<T>(a.v, ks.begin, kv);
   const unsigned base = lds_address(lds);
   const float c = a.scale * kLog2e;
-  f32x16 dq[L::BLOCKS];
-  auto pass = [&](auto safe) {
+  auto pass = [&](auto safe, auto &dq, int db0) {
     constexpr bool SAFE = decltype(safe)::value;
-#pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db) dq[db] = zero_acc();
+    constexpr int NB = sizeof(dq) / sizeof(f32x16);
+    for (auto &x : dq) x = zero_acc();
     if (tiles > 0) {
       stage_tile<T, DP, KT, WAVES>(k, keys, a.k.stride, a.dim_in, base, wave, lane);
       stage_tile<T, DP, KT, WAVES>(v, keys, a.v.stride, a.dim_in, base + 2 * BYTES, wave, lane);
@@ -96,23 +95,29 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
 #pragma unroll
             for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(j0 + 32 * kb + acc_row(x * L::V + n, g), mine) ? 1.f : 0.f);
 #pragma unroll
-            for (int db = 0; db < L::BLOCKS; ++db) mma_seen<T>(L::across(kt, 32 * kb + x * L::STEP, db, lane), ds, seen, dq[db]);
+            for (int db = 0; db < NB; ++db) mma_seen<T>(L::across(kt, 32 * kb + x * L::STEP, db0 + db, lane), ds, seen, dq[db]);
           } else {
 #pragma unroll
-            for (int db = 0; db < L::BLOCKS; ++db) Operand<T>::mma(L::across(kt, 32 * kb + x * L::STEP, db, lane), ds, dq[db]);
+            for (int db = 0; db < NB; ++db) Operand<T>::mma(L::across(kt, 32 * kb + x * L::STEP, db0 + db, lane), ds, dq[db]);
           }
         }
       }
     }
+    store_row<T>(head_at<T>(a.dq, row, at.head), there, a.dim, a.quads, dq, a.scale, g, db0);
   };
-  pass(std::false_type());
-  if (a.causal) {
-    bool fine = true;
+  f32x16 dq[L::BLOCKS];
+  pass(std::false_type(), dq, 0);
+  if (!a.causal) return;
+  bool fine = true;
 #pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(dq[db]);
-    if (__syncthreads_or(!fine)) pass(std::true_type());
+  for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(dq[db]);
+  if (!__syncthreads_or(!fine)) return;
+#pragma unroll 1
+  for (int db = 0; db < L::BLOCKS; ++db) {
+    __syncthreads();
+    f32x16 one[1];
+    pass(std::true_type(), one, db);
   }
-  store_row<T, DP>(head_at<T>(a.dq, row, at.head), there, a.dim, a.quads, dq, a.scale, g);
 }
 
 // n floats from p on into LDS, past the registers, zeros behind them (n at most 64; wave-uniform).
@@ -162,14 +167,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Attn
     if (wave == 0) stage_floats(a.stat_lse + head * a.n_q + row, n, stats + b * 512, lane);
     if (DK && wave == WAVES - 1) stage_floats(a.stat_delta + head * a.n_q + row, n, stats + b * 512 + 256, lane);
   };
-  f32x16 dk[L::BLOCKS], dv[L::BLOCKS];
-  auto pass = [&](auto safe) {
+  auto pass = [&](auto safe, auto &dk, auto &dv, int db0) {
     constexpr bool SAFE = decltype(safe)::value;
-#pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db) {
-      dk[db] = zero_acc();
-      dv[db] = zero_acc();
-    }
+    constexpr int NB = sizeof(dk) / sizeof(f32x16);
+    for (auto &x : dk) x = zero_acc();
+    for (auto &x : dv) x = zero_acc();
     if (tiles > 0) stage(0);
     for (int t = 0; t < tiles; ++t) {
       const unsigned qt = base + (t & 1) * BYTES, dt = qt + 2 * BYTES, st = stats + (t & 1) * 512;
@@ -211,29 +213,35 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Attn
 #pragma unroll
           for (int n = 0; n < L::V; ++n) seen[n] = (T)(counts(x * L::V + n) ? 1.f : 0.f);
 #pragma unroll
-          for (int db = 0; db < L::BLOCKS; ++db) {
-            if (DV) mma_seen<T>(L::across(dt, x * L::STEP, db, lane), p, seen, dv[db]);
-            if (DK) mma_seen<T>(L::across(qt, x * L::STEP, db, lane), ds, seen, dk[db]);
+          for (int db = 0; db < NB; ++db) {
+            if (DV) mma_seen<T>(L::across(dt, x * L::STEP, db0 + db, lane), p, seen, dv[db]);
+            if (DK) mma_seen<T>(L::across(qt, x * L::STEP, db0 + db, lane), ds, seen, dk[db]);
           }
         } else {
 #pragma unroll
-          for (int db = 0; db < L::BLOCKS; ++db) {
-            if (DV) Operand<T>::mma(L::across(dt, x * L::STEP, db, lane), p, dv[db]);
-            if (DK) Operand<T>::mma(L::across(qt, x * L::STEP, db, lane), ds, dk[db]);
+          for (int db = 0; db < NB; ++db) {
+            if (DV) Operand<T>::mma(L::across(dt, x * L::STEP, db0 + db, lane), p, dv[db]);
+            if (DK) Operand<T>::mma(L::across(qt, x * L::STEP, db0 + db, lane), ds, dk[db]);
           }
         }
       }
     }
+    if (DK) store_row<T>(head_at<T>(a.dk, ks.begin + j, at.head), there, a.dim, a.quads, dk, a.scale, g, db0);
+    if (DV) store_row<T>(head_at<T>(a.dv, ks.begin + j, at.head), there, a.dim, a.quads, dv, 1.f, g, db0);
   };
-  pass(std::false_type());
-  if (a.causal) {
-    bool fine = true;
+  f32x16 dk[L::BLOCKS], dv[L::BLOCKS];
+  pass(std::false_type(), dk, dv, 0);
+  if (!a.causal) return;
+  bool fine = true;
 #pragma unroll
-    for (int db = 0; db < L::BLOCKS; ++db) fine = fine && (!DK || all_finite(dk[db])) && (!DV || all_finite(dv[db]));
-    if (__syncthreads_or(!fine)) pass(std::true_type());
+  for (int db = 0; db < L::BLOCKS; ++db) fine = fine && (!DK || all_finite(dk[db])) && (!DV || all_finite(dv[db]));
+  if (!__syncthreads_or(!fine)) return;
+#pragma unroll 1
+  for (int db = 0; db < L::BLOCKS; ++db) {
+    __syncthreads();
+    f32x16 one[1], two[1];
+    pass(std::true_type(), one, two, db);
   }
-  if (DK) store_row<T, DP>(head_at<T>(a.dk, ks.begin + j, at.head), there, a.dim, a.quads, dk, a.scale, g);
-  if (DV) store_row<T, DP>(head_at<T>(a.dv, ks.begin + j, at.head), there, a.dim, a.quads, dv, 1.f, g);
 }
 
 template <typename T, int DP>

@@ -118,10 +118,14 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheArgs a) {
   }
 }
 
-// KT rows of the cache into a tile: lane n % KT of the wave has key n's place in `at` (a place that is there for every key). WHOLE: in pieces of 16 bytes past the registers,
-// there behind wait_direct_loads() and a barrier; else element by element.
+// Where a tile's keys and values lie: elements from the heads' own base on. A wave's table, written by one lane a key and read by the lanes that fetch the rows.
+struct Places {
+  int64_t k, v;
+};
+
+// KT rows of both caches into two tiles. WHOLE: in pieces of 16 bytes past the registers, there behind wait_direct_loads() and a barrier; else element by element.
 template <typename T, int DP, int KT, int WAVES, bool WHOLE>
-__device__ __forceinline__ void stage_pages(const Pages &c, const Slot &at, int head, int dim, unsigned tile, int wave, int lane) {
+__device__ __forceinline__ void stage_pages(const T *k, const T *v, unsigned places, int dim, unsigned kt, unsigned vt, int wave, int lane) {
   using L = Tile<T, DP>;
   constexpr int N = KT * L::RB / 1024, EACH = (N + WAVES - 1) / WAVES;
 #pragma unroll
@@ -129,18 +133,23 @@ __device__ __forceinline__ void stage_pages(const Pages &c, const Slot &at, int 
     const int n = wave + i * WAVES;
     if (N % WAVES && n >= N) break;
     const int e = n * 64 + lane, row = e / L::CPR, piece = (e % L::CPR) ^ L::swizzle(row);
-    const T *p = page_row<T>(c, __shfl(at.page, row), __shfl(at.slot, row), head);
+    typedef int64_t i64x2 __attribute__((ext_vector_type(2)));
+    const i64x2 at = *lds_at<const i64x2>(places + row * 16);
     if constexpr (WHOLE) {
       // (pieces behind dim: any that is there; q has zeros for them, and results there are not stored)
-      lds_direct_load16(p + (piece * L::V < dim ? piece * L::V : 0), __builtin_amdgcn_readfirstlane(tile + n * 1024));
+      const int d = piece * L::V < dim ? piece * L::V : 0;
+      lds_direct_load16(k + at[0] + d, __builtin_amdgcn_readfirstlane(kt + n * 1024));
+      lds_direct_load16(v + at[1] + d, __builtin_amdgcn_readfirstlane(vt + n * 1024));
     } else {
-      typename L::vec x;
+      typename L::vec x, y;
 #pragma unroll
       for (int j = 0; j < L::V; ++j) {
         const int d = piece * L::V + j;
-        x[j] = d < dim ? p[d < dim ? d : 0] : (T)0.f;
+        x[j] = d < dim ? k[at[0] + d] : (T)0.f;
+        y[j] = d < dim ? v[at[1] + d] : (T)0.f;
       }
-      *lds_at<typename L::vec>(tile + (unsigned)(e * 16)) = x;
+      *lds_at<typename L::vec>(kt + (unsigned)(e * 16)) = x;
+      *lds_at<typename L::vec>(vt + (unsigned)(e * 16)) = y;
     }
   }
 }
@@ -167,7 +176,7 @@ struct CacheWalk {
   using L = Tile<T, DP>;
   static constexpr int BM = 32 * WAVES, BYTES = KT * L::RB;
   const CacheArgs &a;
-  unsigned base;
+  unsigned base, places;        // tiles; the wave's table of places, KT of them
   int lane, wave;
 
   // Tiles [t0, t1) of the unit (s, block of columns, head of keys); slot: where a part of it goes, -1: all of it is here.
@@ -193,30 +202,36 @@ struct CacheWalk {
     vec q[L::SLABS];
     load_query<T, DP, WHOLE>(q, (const T *)a.q.p + row * a.q.stride + head * a.q.head_stride, there, a.dim, g);
     const float c = a.scale * kLog2e;
+    const T *kb = (const T *)a.kc.p + kv * a.kc.head_stride, *vb = (const T *)a.vc.p + kv * a.vc.head_stride;
     // Keys that are not there stand for the sequence's first one, or for the cache's first row: their scores do not count.
-    const Slot first = slot_of(a, s, 0);
-    auto place = [&](int t, unsigned long long &valid) {
+    Slot first = slot_of(a, s, 0);
+    if (first.page < 0) first = {0, 0};
+    auto look_up = [&](int t) {                       // (a load that the next step waits for)
       const int j = t * KT + lane % KT;
-      Slot at = j < keys ? slot_of(a, s, j) : Slot{-1, 0};
-      valid = __ballot(at.page >= 0);
-      if (at.page < 0) at = first.page >= 0 ? first : Slot{0, 0};
-      return at;
+      return j < keys ? slot_of(a, s, j) : Slot{-1, 0};
     };
-    f32x16 o[L::BLOCKS];
-    float mc, l;
-    auto pass = [&](auto safe) {
+    auto write_places = [&](Slot at) {                // which of the tile's keys are there
+      const unsigned long long valid = __ballot(at.page >= 0);
+      if (at.page < 0) at = first;
+      wave_lds_fence();
+      if (lane < KT) {
+        typedef int64_t i64x2 __attribute__((ext_vector_type(2)));
+        *lds_at<i64x2>(places + lane * 16) =
+            i64x2{(int64_t)at.page * a.kc.page_stride + (int64_t)at.slot * a.kc.stride, (int64_t)at.page * a.vc.page_stride + (int64_t)at.slot * a.vc.stride};
+      }
+      wave_lds_fence();
+      return valid;
+    };
+    auto pass = [&](auto safe, auto &o, int db0) {
       constexpr bool SAFE = decltype(safe)::value;
-      mc = kLowest;
-      l = 0.f;
-#pragma unroll
-      for (int db = 0; db < L::BLOCKS; ++db) o[db] = zero_acc();
-      unsigned long long valid = 0, next_valid = 0;
-      Slot at = {0, 0}, next = {0, 0};
+      float mc = kLowest, l = 0.f;
+      for (auto &x : o) x = zero_acc();
+      unsigned long long valid = 0;
+      Slot next = {-1, 0};
       if (t0 < stop) {
-        at = place(t0, valid);
-        stage_pages<T, DP, KT, WAVES, WHOLE>(a.kc, at, kv, a.dim, base, wave, lane);
-        stage_pages<T, DP, KT, WAVES, WHOLE>(a.vc, at, kv, a.dim, base + 2 * BYTES, wave, lane);
-        next = place(t0 + 1, next_valid);
+        valid = write_places(look_up(t0));
+        stage_pages<T, DP, KT, WAVES, WHOLE>(kb, vb, places, a.dim, base, base + 2 * BYTES, wave, lane);
+        next = look_up(t0 + 1);
       }
       for (int t = t0; t < stop; ++t) {
         const unsigned b = (unsigned)((t - t0) & 1) * BYTES, kt = base + b, vt = kt + 2 * BYTES;
@@ -224,45 +239,53 @@ struct CacheWalk {
         __syncthreads();
         const unsigned long long now = valid;
         if (t + 1 < stop) {
-          valid = next_valid;
-          stage_pages<T, DP, KT, WAVES, WHOLE>(a.kc, next, kv, a.dim, base + (BYTES - b), wave, lane);
-          stage_pages<T, DP, KT, WAVES, WHOLE>(a.vc, next, kv, a.dim, base + (BYTES - b) + 2 * BYTES, wave, lane);
-          next = place(t + 2, next_valid);
+          valid = write_places(next);
+          stage_pages<T, DP, KT, WAVES, WHOLE>(kb, vb, places, a.dim, base + (BYTES - b), base + (BYTES - b) + 2 * BYTES, wave, lane);
+          next = look_up(t + 2);
         }
         const int j0 = t * KT;
         if (j0 >= any_sees) continue;
         const bool whole = j0 + KT <= all_see && now == ~0ull;
-        add_tile<T, DP, KT, SAFE>(kt, vt, q, c, whole, [&](int n) { return j0 + n < mine && (now >> n & 1); }, o, mc, l, lane);
+        // the keys that the lane's column sees, a bit each
+        const int left = mine - j0;
+        const unsigned long long below = left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull, seen = (now & below) >> (4 * g);
+        add_tile<T, DP, KT, SAFE>(kt, vt, q, c, whole, [&](int n) { return (seen >> n & 1) != 0; }, o, mc, l, lane, db0);
       }
-      __syncthreads();                                // (the next unit's first tiles go where the last ones are read)
+      __syncthreads();                                // (the next tiles go where the last ones are read)
+      l = half_sum(l);
+      if (slot < 0) {
+        store_row<T>((T *)a.out.p + row * a.out.stride + head * a.out.head_stride, there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, g, db0);
+      } else {
+        const int64_t at = slot * BM + 32 * wave + l32;
+        store_row<float>(a.part + at * DP, there, DP, true, o, 1.f, g, db0);
+        if (there && g == 0) {
+          a.part_sums[2 * at] = mc;
+          a.part_sums[2 * at + 1] = l;
+        }
+      }
     };
-    pass(std::false_type());
+    f32x16 o[L::BLOCKS];
+    pass(std::false_type(), o, 0);
     bool fine = true;
 #pragma unroll
     for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(o[db]);
-    if (WAVES == 1 ? __ballot(!fine) != 0 : __syncthreads_or(!fine)) pass(std::true_type());
-    l = half_sum(l);
-    if (slot < 0) {
-      store_row<T, DP>((T *)a.out.p + row * a.out.stride + head * a.out.head_stride, there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, g);
-    } else {
-      const int64_t at = slot * BM + 32 * wave + l32;
-      store_row<float, DP>(a.part + at * DP, there, DP, true, o, 1.f, g);
-      if (there && g == 0) {
-        a.part_sums[2 * at] = mc;
-        a.part_sums[2 * at + 1] = l;
-      }
+    if (WAVES == 1 ? __ballot(!fine) == 0 : !__syncthreads_or(!fine)) return;
+#pragma unroll 1
+    for (int db = 0; db < L::BLOCKS; ++db) {
+      f32x16 one[1];
+      pass(std::true_type(), one, db);
     }
   }
 };
 
 // A piece of the line each, all of it by a fixed number of blocks.
 template <typename T, int DP, int WAVES, int KT, bool WHOLE>
-__global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 ? 1 : 2) void cache_attention_kernel(const CacheArgs a) {
+__global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 || (WAVES == 1 && DP * sizeof(T) == 256) ? 1 : 2) void cache_attention_kernel(const CacheArgs a) {
   using W = CacheWalk<T, DP, WAVES, KT, WHOLE>;
-  __shared__ __attribute__((aligned(16))) char lds[4 * W::BYTES];
+  __shared__ __attribute__((aligned(16))) char lds[4 * W::BYTES + WAVES * KT * 16];
   touch_args(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const W walk = {a, lds_address(lds), lane, wave};
+  const W walk = {a, lds_address(lds), lds_address(lds) + 4 * W::BYTES + wave * KT * 16, lane, wave};
   auto weight = [&](int64_t s) {
     if (s >= a.seqs) return (int64_t)0;
     const Seq q = seq_of<W::BM, KT>(a, s);
@@ -315,12 +338,12 @@ __global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 ? 1 : 2) void cach
 
 // Where units are short: a whole one a block.
 template <typename T, int DP, int WAVES, int KT, bool WHOLE>
-__global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 ? 1 : 2) void cache_attention_short_kernel(const CacheArgs a) {
+__global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 || (WAVES == 1 && DP * sizeof(T) == 256) ? 1 : 2) void cache_attention_short_kernel(const CacheArgs a) {
   using W = CacheWalk<T, DP, WAVES, KT, WHOLE>;
-  __shared__ __attribute__((aligned(16))) char lds[4 * W::BYTES];
+  __shared__ __attribute__((aligned(16))) char lds[4 * W::BYTES + WAVES * KT * 16];
   touch_args(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const W walk = {a, lds_address(lds), lane, wave};
+  const W walk = {a, lds_address(lds), lds_address(lds) + 4 * W::BYTES + wave * KT * 16, lane, wave};
   const int64_t b = a.block0 + blockIdx.x, u = b / a.kv_heads;
   // (numbers of a sequence's blocks of columns: from ptr group / BM + sequences on, as in the packed kernels)
   int64_t lo = 0, hi = a.seqs;
@@ -352,16 +375,34 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a) {
   for (int e = threadIdx.x; e < columns * (DP / 4); e += 256) {
     const int col = e / (DP / 4), d = e % (DP / 4) * 4;
     if (d >= a.dim) continue;
-    float m = kLowest;
-    for (int i = 0; i <= s.follow; ++i) m = fmaxf(m, a.part_sums[2 * (at(i) + col)]);
-    float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i <= s.follow; ++i) {
-      const int64_t p = at(i) + col;
-      const float f = __builtin_amdgcn_exp2f(a.part_sums[2 * p] - m);
-      const f32x4 x = *(const f32x4 *)(a.part + p * DP + d);
-      l = fmaf(f, a.part_sums[2 * p + 1], l);
+    // (eight parts' loads together: each by itself is a round trip to memory)
+    float m = kLowest, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 <= s.follow; i0 += 8) {
+      float pm[8], pl[8];
+      f32x4 x[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = fmaf(f, x[k], v[k]);
+      for (int i = 0; i < 8; ++i) {
+        const int64_t p = at(i0 + i <= s.follow ? i0 + i : s.follow) + col;
+        pm[i] = a.part_sums[2 * p];
+        pl[i] = a.part_sums[2 * p + 1];
+        x[i] = *(const f32x4 *)(a.part + p * DP + d);
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, pm[i]);
+      const float old = __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      l *= old;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] *= old;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i0 + i > s.follow) continue;
+        const float f = __builtin_amdgcn_exp2f(pm[i] - m);
+        l = fmaf(f, pl[i], l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = fmaf(f, x[i][k], v[k]);
+      }
     }
     const float f = l == 0.f ? 0.f : 1.f / l;
     const int token = (s.block * BM + col) / a.group, head = s.kv * a.group + (s.block * BM + col) % a.group;
@@ -435,7 +476,7 @@ int check_pages(const xrl_pages *x, const CacheArgs &a, int es, bool written, co
 
 template <typename T, int DP, int WAVES, bool WHOLE>
 int launch(xrl_ctx *c, CacheArgs &a, const char *who) {
-  constexpr int KT = WAVES == 1 || sizeof(T) == 4 ? 32 : 64, BM = 32 * WAVES, LDS = 4 * KT * DP * (int)sizeof(T);
+  constexpr int KT = WAVES == 1 || sizeof(T) == 4 ? 32 : 64, BM = 32 * WAVES, LDS = 4 * KT * DP * (int)sizeof(T) + WAVES * KT * 16 + 256;
   const int64_t most = ((int64_t)a.table_cols * a.page + KT - 1) / KT;
   if (most <= 4) {
     a.blocks = (a.n_q * a.group / BM + a.seqs) * a.kv_heads;
