@@ -29,20 +29,25 @@ struct AttnArgs {
   float *stat_lse, *stat_delta;                     // [q_heads, n_q]: lse log2(e) and do . o
 };
 
+// Tiles in LDS at a time: the next one's loads run while one is worked on. A wave by itself, for short sequences, has one: it seldom has a second tile, and twice as many such waves
+// fit on a compute unit.
+template <int WAVES>
+constexpr int kBuffers = WAVES == 1 ? 1 : 2;
+
 template <typename T>
 __device__ __forceinline__ T *head_at(const Heads &x, int64_t row, int head) { return (T *)x.p + row * x.stride + head * x.head_stride; }
 
 // Block -> tile of rows and head. Blocks are dealt to the eight XCDs in turn: the heads of one row tile follow each other, those that share keys at a distance of kv_heads,
-// so that with eight of these (or a multiple) an XCD's L2 holds the keys of its own heads alone. The last tiles of a sequence, the longest under a causal
-// mask, come first.
+// so that with eight of these (or a multiple) an XCD's L2 holds the keys of its own heads alone. Under a causal mask a sequence's last queries and its first
+// keys have the most work: these tiles come first.
 struct Place {
   int64_t seq;
   int head, tile;
 };
-__device__ __forceinline__ bool place_of(const AttnArgs &a, const int32_t *ptr, int64_t n, int heads, int bm, int lane, Place &o) {
+__device__ __forceinline__ bool place_of(const AttnArgs &a, const int32_t *ptr, int64_t n, int heads, int bm, bool last_first, int lane, Place &o) {
   const int64_t b = a.block0 + blockIdx.x;
   const int h = (int)(b % heads);
-  const int64_t u = a.blocks / heads - 1 - b / heads;
+  const int64_t u = last_first ? a.blocks / heads - 1 - b / heads : b / heads;
   const int group = heads / a.kv_heads;
   o.head = h % a.kv_heads * group + h / a.kv_heads;
   o.seq = sequence_of(ptr, a.seqs, n, bm, u, lane);

@@ -9,17 +9,17 @@
 
 namespace {
 
-// One block: BM = 32 WAVES rows of one sequence and one head, KT keys at a time, two tiles of K and V each.
+// One block: BM = 32 WAVES rows of one sequence and one head, KT keys at a time.
 template <typename T, int DP, int WAVES, int KT>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 : 2) void attention_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
   using vec = typename L::vec;
-  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB;
-  __shared__ __attribute__((aligned(16))) char lds[4 * BYTES];
+  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB, BUFS = kBuffers<WAVES>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFS * BYTES];
   touch_args(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
   Place at;
-  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, lane, at)) return;
+  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, true, lane, at)) return;
   const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
   const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
   if (i0 < 0) return;
@@ -43,19 +43,22 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
     mc = kLowest;
     l = 0.f;
     for (auto &x : o) x = zero_acc();
-    if (tiles > 0) {
-      stage_tile<T, DP, KT, WAVES>(k, keys, a.k.stride, a.dim_in, base, wave, lane);
-      stage_tile<T, DP, KT, WAVES>(v, keys, a.v.stride, a.dim_in, base + 2 * BYTES, wave, lane);
-    }
+    auto stage = [&](int t) {
+      const int64_t j = (int64_t)t * KT;
+      const unsigned to = base + t % BUFS * BYTES;
+      stage_tile<T, DP, KT, WAVES>(k + j * a.k.stride, keys - (int)j, a.k.stride, a.dim_in, to, wave, lane);
+      stage_tile<T, DP, KT, WAVES>(v + j * a.v.stride, keys - (int)j, a.v.stride, a.dim_in, to + BUFS * BYTES, wave, lane);
+    };
+    if (tiles > 0) stage(0);
     for (int t = 0; t < tiles; ++t) {
-      const unsigned kt = base + (t & 1) * BYTES, vt = kt + 2 * BYTES;
+      const unsigned kt = base + t % BUFS * BYTES, vt = kt + BUFS * BYTES;
+      if (BUFS == 1 && t > 0) {
+        __syncthreads();
+        stage(t);
+      }
       wait_direct_loads();
       __syncthreads();                              // tile t is there, and t - 1 is read
-      if (t + 1 < tiles) {
-        const int64_t j = (int64_t)(t + 1) * KT;
-        stage_tile<T, DP, KT, WAVES>(k + j * a.k.stride, keys - (int)j, a.k.stride, a.dim_in, base + ((t + 1) & 1) * BYTES, wave, lane);
-        stage_tile<T, DP, KT, WAVES>(v + j * a.v.stride, keys - (int)j, a.v.stride, a.dim_in, base + ((t + 1) & 1) * BYTES + 2 * BYTES, wave, lane);
-      }
+      if (BUFS == 2 && t + 1 < tiles) stage(t + 1);
       const int j0 = t * KT;
       if (j0 >= any_sees) continue;
       add_tile<T, DP, KT, SAFE>(kt, vt, q, c, j0 + KT <= all_see, [&](int n) { return n < mine - j0 - 4 * g; }, o, mc, l, lane, db0);

@@ -14,12 +14,12 @@ template <typename T, int DP, int WAVES, int KT>
 __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
   using vec = typename L::vec;
-  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB;
-  __shared__ __attribute__((aligned(16))) char lds[4 * BYTES];
+  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB, BUFS = kBuffers<WAVES>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUFS * BYTES];
   touch_args(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
   Place at;
-  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, lane, at)) return;
+  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, true, lane, at)) return;
   const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
   const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
   if (i0 < 0) return;
@@ -57,19 +57,22 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
     constexpr bool SAFE = decltype(safe)::value;
     constexpr int NB = sizeof(dq) / sizeof(f32x16);
     for (auto &x : dq) x = zero_acc();
-    if (tiles > 0) {
-      stage_tile<T, DP, KT, WAVES>(k, keys, a.k.stride, a.dim_in, base, wave, lane);
-      stage_tile<T, DP, KT, WAVES>(v, keys, a.v.stride, a.dim_in, base + 2 * BYTES, wave, lane);
-    }
+    auto stage = [&](int t) {
+      const int64_t j = (int64_t)t * KT;
+      const unsigned to = base + t % BUFS * BYTES;
+      stage_tile<T, DP, KT, WAVES>(k + j * a.k.stride, keys - (int)j, a.k.stride, a.dim_in, to, wave, lane);
+      stage_tile<T, DP, KT, WAVES>(v + j * a.v.stride, keys - (int)j, a.v.stride, a.dim_in, to + BUFS * BYTES, wave, lane);
+    };
+    if (tiles > 0) stage(0);
     for (int t = 0; t < tiles; ++t) {
-      const unsigned kt = base + (t & 1) * BYTES, vt = kt + 2 * BYTES;
-      wait_direct_loads();
-      __syncthreads();
-      if (t + 1 < tiles) {
-        const int64_t j = (int64_t)(t + 1) * KT;
-        stage_tile<T, DP, KT, WAVES>(k + j * a.k.stride, keys - (int)j, a.k.stride, a.dim_in, base + ((t + 1) & 1) * BYTES, wave, lane);
-        stage_tile<T, DP, KT, WAVES>(v + j * a.v.stride, keys - (int)j, a.v.stride, a.dim_in, base + ((t + 1) & 1) * BYTES + 2 * BYTES, wave, lane);
+      const unsigned kt = base + t % BUFS * BYTES, vt = kt + BUFS * BYTES;
+      if (BUFS == 1 && t > 0) {
+        __syncthreads();
+        stage(t);
       }
+      wait_direct_loads();
+      __syncthreads();                              // tile t is there, and t - 1 is read
+      if (BUFS == 2 && t + 1 < tiles) stage(t + 1);
       const int j0 = t * KT;
       if (j0 >= any_sees) continue;
       const bool whole = j0 + KT <= all_see;
@@ -129,18 +132,21 @@ __device__ __forceinline__ void stage_floats(const float *p, int n, unsigned lds
 #pragma clang diagnostic pop
 }
 
-// dk and dv: one block has 32 WAVES keys of one sequence and one head of keys, a key a lane, and goes over the queries that see them, 32 rows at a time, of all
-// heads that share the keys, in order: no sum is taken by two blocks.
-template <typename T, int DP, int WAVES, bool DK, bool DV>
-__global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const AttnArgs a) {
+// dk and dv: one block has 32 WAVES keys of one sequence and one head of keys, a key a lane, and goes over the queries that see them, QT rows at a time, of all
+// heads that share the keys, in order. HALVES: so many times WAVES waves each go over their part of these queries, and their sums are added at the end, in order: no sum is taken
+// by two blocks. IN_LDS: the block's keys and values stay in LDS, where registers for them as well would leave one wave a SIMD.
+template <typename T, int DP, int WAVES, int QT, int HALVES, bool IN_LDS, bool DK, bool DV>
+__global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
   using vec = typename L::vec;
-  constexpr int BM = 32 * WAVES, QT = 32, BYTES = QT * L::RB;
-  __shared__ __attribute__((aligned(16))) char lds[4 * BYTES + 4 * 256];
+  constexpr int BM = 32 * WAVES, BYTES = QT * L::RB, BUFS = kBuffers<WAVES>, EACH = 2 * BUFS * (BYTES + 256), SUMS = BM * DP * 4;   // of a half: two tiles of q and of dout, and the rows' statistics
+  constexpr int KEYS = IN_LDS ? 2 * BM * L::RB : 0, ALL = HALVES * EACH + KEYS, JOIN = HALVES > 1 ? (DK + DV) * SUMS : 0;
+  __shared__ __attribute__((aligned(16))) char lds[ALL > JOIN ? ALL : JOIN];
   touch_args(a);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES : 0, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
   Place at;
-  if (!place_of(a, a.k_ptr, a.n_k, a.kv_heads, BM, lane, at)) return;
+  if (!place_of(a, a.k_ptr, a.n_k, a.kv_heads, BM, false, lane, at)) return;
   const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
   const int j0 = __builtin_amdgcn_readfirstlane(at.tile < (ks.len + BM - 1) / BM ? at.tile * BM : -1);
   if (j0 < 0) return;
@@ -152,17 +158,20 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Attn
   const int w0 = j0 + 32 * wave, w1 = w0 + 31;
   const int begin = __builtin_amdgcn_readfirstlane(first_of(j0)) / QT * QT;
   const int any_sees = __builtin_amdgcn_readfirstlane(first_of(w0)), all_see = __builtin_amdgcn_readfirstlane(first_of(w1)), mine = first_of(j);
-  const int per_head = (len_q - begin + QT - 1) / QT, tiles = per_head * group;
+  const int per_head = (len_q - begin + QT - 1) / QT, all_tiles = per_head * group, share = (all_tiles + HALVES - 1) / HALVES;
+  const int first = half * share, tiles = first < all_tiles ? (all_tiles - first < share ? all_tiles - first : share) : 0;   // of this half
   vec k[L::SLABS], v[L::SLABS];
-  load_row<T, DP>(k, head_at<T>(a.k, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
-  if (DK) load_row<T, DP>(v, head_at<T>(a.v, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
-  const unsigned base = lds_address(lds), stats = base + 4 * BYTES;
+  const unsigned base = lds_address(lds) + half * EACH, stats = base + 2 * BUFS * BYTES, keys = lds_address(lds) + HALVES * EACH, values = keys + BM * L::RB;
+  if constexpr (!IN_LDS) {
+    load_row<T, DP>(k, head_at<T>(a.k, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
+    if (DK) load_row<T, DP>(v, head_at<T>(a.v, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
+  }
   const float c = a.scale * kLog2e;
-  auto stage = [&](int t) {
-    const int head = at.head * group + t / per_head, i = begin + t % per_head * QT, b = t & 1;
+  auto stage = [&](int e, int i, int b) {             // rows i on of the group's head e
+    const int head = at.head * group + e;
     const int64_t row = qs.begin + i;
     stage_tile<T, DP, QT, WAVES>(head_at<T>(a.q, row, head), len_q - i, a.q.stride, a.dim_in, base + b * BYTES, wave, lane);
-    stage_tile<T, DP, QT, WAVES>(head_at<T>(a.dout, row, head), len_q - i, a.dout.stride, a.dim_in, base + (2 + b) * BYTES, wave, lane);
+    stage_tile<T, DP, QT, WAVES>(head_at<T>(a.dout, row, head), len_q - i, a.dout.stride, a.dim_in, base + (BUFS + b) * BYTES, wave, lane);
     const int n = len_q - i < QT ? len_q - i : QT;
     if (wave == 0) stage_floats(a.stat_lse + head * a.n_q + row, n, stats + b * 512, lane);
     if (DK && wave == WAVES - 1) stage_floats(a.stat_delta + head * a.n_q + row, n, stats + b * 512 + 256, lane);
@@ -172,60 +181,115 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dkv_kernel(const Attn
     constexpr int NB = sizeof(dk) / sizeof(f32x16);
     for (auto &x : dk) x = zero_acc();
     for (auto &x : dv) x = zero_acc();
-    if (tiles > 0) stage(0);
-    for (int t = 0; t < tiles; ++t) {
-      const unsigned qt = base + (t & 1) * BYTES, dt = qt + 2 * BYTES, st = stats + (t & 1) * 512;
+    const int e0 = per_head > 0 ? first / per_head : 0;
+    int next_e = e0, next_i = begin + (first - e0 * per_head) * QT, i = next_i;
+    if constexpr (IN_LDS) {
+      stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.k, ks.begin + j0, at.head), ks.len - j0, a.k.stride, a.dim_in, keys, half * WAVES + wave, lane);
+      if (DK) stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.v, ks.begin + j0, at.head), ks.len - j0, a.v.stride, a.dim_in, values, half * WAVES + wave, lane);
+    }
+    if (tiles > 0) stage(next_e, next_i, 0);
+    for (int t = 0; t < share; ++t) {
+      const unsigned qt = base + t % BUFS * BYTES, dt = qt + BUFS * BYTES, st = stats + t % BUFS * 512;
+      if (BUFS == 1 && t > 0) {
+        __syncthreads();
+        stage(next_e, next_i, 0);
+      }
       wait_direct_loads();
       __syncthreads();
-      if (t + 1 < tiles) stage(t + 1);
-      const int i0 = begin + t % per_head * QT;
-      if (i0 + QT <= any_sees) continue;
-      const bool whole = i0 >= all_see && i0 + QT <= len_q;
-      f32x16 s = zero_acc(), dp = zero_acc();
-#pragma unroll
-      for (int x = 0; x < L::SLABS; ++x) {
-        Operand<T>::mma(L::along(qt, 0, x, lane), k[x], s);
-        if (DK) Operand<T>::mma(L::along(dt, 0, x, lane), v[x], dp);
+      i = next_i;
+      next_i += QT;
+      if (next_i >= len_q) {
+        next_i = begin;
+        ++next_e;
       }
+      if (BUFS == 2 && t + 1 < tiles) stage(next_e, next_i, (t + 1) & 1);
+      if (t >= tiles || i + QT <= any_sees) continue;
+      const bool whole = i >= all_see && i + QT <= len_q;
+      f32x16 s[QT / 32], dp[QT / 32];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const f32x4 lse2 = *lds_at<const f32x4>(st + (8 * n + 4 * g) * 4), delta = *lds_at<const f32x4>(st + 256 + (8 * n + 4 * g) * 4);
+      for (int qb = 0; qb < QT / 32; ++qb) {
+        s[qb] = zero_acc();
+        dp[qb] = zero_acc();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * n + r], c, -lse2[r]));
-          s[4 * n + r] = p;
-          if (DK) dp[4 * n + r] = p * (dp[4 * n + r] - delta[r]);
-        }
-      }
-      auto counts = [&](int r) { const int i = i0 + acc_row(r, g); return i >= mine && i < len_q; };
-      if (!whole) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[r] = counts(r) ? s[r] : 0.f;
-          if (DK) dp[r] = counts(r) ? dp[r] : 0.f;
+        for (int x = 0; x < L::SLABS; ++x) {
+          Operand<T>::mma(L::along(qt, 32 * qb, x, lane), IN_LDS ? L::along(keys, 32 * wave, x, lane) : k[x], s[qb]);
+          if (DK) Operand<T>::mma(L::along(dt, 32 * qb, x, lane), IN_LDS ? L::along(values, 32 * wave, x, lane) : v[x], dp[qb]);
         }
       }
 #pragma unroll
-      for (int x = 0; x < 32 / L::STEP; ++x) {
-        const vec p = acc_operand<T>(s, x), ds = acc_operand<T>(dp, x);
-        if (SAFE && !whole) {
-          vec seen;
+      for (int qb = 0; qb < QT / 32; ++qb) {
 #pragma unroll
-          for (int n = 0; n < L::V; ++n) seen[n] = (T)(counts(x * L::V + n) ? 1.f : 0.f);
+        for (int n = 0; n < 4; ++n) {
+          const unsigned at_row = st + (32 * qb + 8 * n + 4 * g) * 4;
+          const f32x4 lse2 = *lds_at<const f32x4>(at_row), delta = *lds_at<const f32x4>(at_row + 256);
 #pragma unroll
-          for (int db = 0; db < NB; ++db) {
-            if (DV) mma_seen<T>(L::across(dt, x * L::STEP, db0 + db, lane), p, seen, dv[db]);
-            if (DK) mma_seen<T>(L::across(qt, x * L::STEP, db0 + db, lane), ds, seen, dk[db]);
+          for (int r = 0; r < 4; ++r) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[qb][4 * n + r], c, -lse2[r]));
+            s[qb][4 * n + r] = p;
+            if (DK) dp[qb][4 * n + r] = p * (dp[qb][4 * n + r] - delta[r]);
           }
-        } else {
+        }
+        auto counts = [&](int r) { const int n = 32 * qb + acc_row(r, 0); return n >= mine - i - 4 * g && n < len_q - i - 4 * g; };
+        if (!whole) {
 #pragma unroll
-          for (int db = 0; db < NB; ++db) {
-            if (DV) Operand<T>::mma(L::across(dt, x * L::STEP, db0 + db, lane), p, dv[db]);
-            if (DK) Operand<T>::mma(L::across(qt, x * L::STEP, db0 + db, lane), ds, dk[db]);
+          for (int r = 0; r < 16; ++r) {
+            s[qb][r] = counts(r) ? s[qb][r] : 0.f;
+            if (DK) dp[qb][r] = counts(r) ? dp[qb][r] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 32 / L::STEP; ++x) {
+          const vec p = acc_operand<T>(s[qb], x), ds = acc_operand<T>(dp[qb], x);
+          if (SAFE && !whole) {
+            vec seen;
+#pragma unroll
+            for (int n = 0; n < L::V; ++n) seen[n] = (T)(counts(x * L::V + n) ? 1.f : 0.f);
+#pragma unroll
+            for (int db = 0; db < NB; ++db) {
+              if (DV) mma_seen<T>(L::across(dt, 32 * qb + x * L::STEP, db0 + db, lane), p, seen, dv[db]);
+              if (DK) mma_seen<T>(L::across(qt, 32 * qb + x * L::STEP, db0 + db, lane), ds, seen, dk[db]);
+            }
+          } else {
+#pragma unroll
+            for (int db = 0; db < NB; ++db) {
+              if (DV) Operand<T>::mma(L::across(dt, 32 * qb + x * L::STEP, db0 + db, lane), p, dv[db]);
+              if (DK) Operand<T>::mma(L::across(qt, 32 * qb + x * L::STEP, db0 + db, lane), ds, dk[db]);
+            }
           }
         }
       }
     }
+    if constexpr (HALVES > 1) {
+      // the second half's sums through LDS to the first
+      static_assert(HALVES == 2);
+      const unsigned at_dk = lds_address(lds) + (unsigned)(wave * 64 + lane) * 16, at_dv = at_dk + (DK ? SUMS : 0);
+      auto exchange = [&](unsigned p, auto &x) {
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            auto *to = lds_at<f32x4>(p + (unsigned)((db * 4 + n) * WAVES * 64 * 16));
+            if (half) {
+              *to = f32x4{x[db][4 * n], x[db][4 * n + 1], x[db][4 * n + 2], x[db][4 * n + 3]};
+            } else {
+              const f32x4 y = *to;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) x[db][4 * n + r] += y[r];
+            }
+          }
+      };
+      __syncthreads();                              // (the last tiles are read)
+      if (half) {
+        if (DK) exchange(at_dk, dk);
+        if (DV) exchange(at_dv, dv);
+      }
+      __syncthreads();
+      if (!half) {
+        if (DK) exchange(at_dk, dk);
+        if (DV) exchange(at_dv, dv);
+      }
+    }
+    if (half) return;
     if (DK) store_row<T>(head_at<T>(a.dk, ks.begin + j, at.head), there, a.dim, a.quads, dk, a.scale, g, db0);
     if (DV) store_row<T>(head_at<T>(a.dv, ks.begin + j, at.head), there, a.dim, a.quads, dv, 1.f, g, db0);
   };
@@ -249,14 +313,14 @@ void launch(const xrl_ctx *c, AttnArgs &a) {
   if (a.n_q <= 64 * a.seqs) launch_tiles(c, a, attention_dq_kernel<T, DP, 1, 32>, a.n_q, a.q_heads, 32, 64);
   else launch_tiles(c, a, attention_dq_kernel<T, DP, 4, 32>, a.n_q, a.q_heads, 128, 256);
   // One launch for both where both sums fit in the registers with their operands, else one for each, which computes the scores once more.
-  constexpr bool BOTH = DP * sizeof(T) <= 256;
+  constexpr bool BOTH = DP * sizeof(T) <= 256, BF16 = sizeof(T) == 2;
   if constexpr (!BOTH) {
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, true, false>, a.n_k, a.kv_heads, 128, 256);
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, false, true>, a.n_k, a.kv_heads, 128, 256);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, 32, 1, false, true, false>, a.n_k, a.kv_heads, 128, 256);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, 32, 1, false, false, true>, a.n_k, a.kv_heads, 128, 256);
   } else if (a.n_k <= 64 * a.seqs) {
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 1, true, true>, a.n_k, a.kv_heads, 32, 64);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 1, 32, 1, false, true, true>, a.n_k, a.kv_heads, 32, 64);
   } else {
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, true, true>, a.n_k, a.kv_heads, 128, 256);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, BF16 && DP < 128 ? 64 : 32, 2, BF16 && DP == 128, true, true>, a.n_k, a.kv_heads, 128, 512);
   }
 }
 template <typename T>
