@@ -342,6 +342,7 @@ class Encoder:
             raise ValueError(f"weights has {w.size} entries, the model needs {self.n_weights}")
         self.stream = torch.cuda.current_stream() if stream is None else stream
         self._raw_stream, self._device = self.stream.cuda_stream, self.stream.device
+        self._index = self._device.index
         self._types = {torch.float32: 0, torch.bfloat16: 1}
         self.handle = C.c_void_p()
         _check(self.lib.xrl_create(C.byref(model_desc(model)), w.ctypes.data,
@@ -449,6 +450,8 @@ class Encoder:
             return self.torch.empty_strided(shape, (1,), dtype=dtype, device=self._device)
         if len(shape) == 2:
             return self.torch.empty_strided(shape, (shape[1] or 1, 1), dtype=dtype, device=self._device)
+        if len(shape) == 3:
+            return self.torch.empty_strided(shape, ((shape[1] or 1) * (shape[2] or 1), shape[2] or 1, 1), dtype=dtype, device=self._device)
         return self.torch.empty(shape, dtype=dtype, device=self._device)
 
     def _made(self, *specs):
@@ -621,22 +624,29 @@ class Encoder:
 
     def _heads(self, x, name, shape=None, type=None):
         """A tensor [n, heads, dim] on the context's GPU, dim contiguous, as the library takes it."""
-        if x.dim() != 3 or x.device != self._device:
+        if x.dim() != 3 or x.get_device() != self._index:
             raise ValueError(f"{name}: a tensor [n, heads, dim] on {self._device} is needed")
         if shape is not None and x.shape != shape:
             raise ValueError(f"{name}: shape {tuple(x.shape)}, {tuple(shape)} is needed")
         if type is not None and x.dtype != type:
             raise ValueError(f"{name}: {x.dtype}, {type} is needed")
         stride, head_stride, step = x.stride()
-        if step != 1 and x.shape[2] > 1:
+        if step != 1 and x.size(2) > 1:
             raise ValueError(f"{name}: heads of contiguous columns are needed")
         return Heads(x.data_ptr(), stride, head_stride)
 
+    def _made_heads(self, *like):
+        """Tensors of the shapes and type of the given ones, each with the library's view of it."""
+        made = self._made(*((x.shape, x.dtype) for x in like))
+        return made, [Heads(x.data_ptr(), *x.stride()[:2]) for x in made]
+
     def _here(self, x, name, dtype, n):
         """As _flat, on the context's GPU."""
-        if x is not None and x.device != self._device:
-            raise ValueError(f"{name}: a tensor on {self._device} is needed")
-        return self._flat(x, name, dtype, n)
+        if x is None:
+            return None
+        if x.get_device() != self._index or x.dtype != dtype or x.numel() != n or not x.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous elements of {dtype} on {self._device} are needed")
+        return x.data_ptr()
 
     def _rotary(self, q, k, positions, freqs, q_weight, k_weight, eps, interleaved):
         t = self.torch
@@ -653,6 +663,14 @@ class Encoder:
                           self._here(freqs, "freqs", f, pairs), self._here(q_weight, "q_weight", f, dim),
                           self._here(k_weight, "k_weight", f, dim)), hq, hk
 
+    def _rotary_out(self, q, k, out):
+        """What is written, like q and k (k None: none), and the library's views of it."""
+        if out is None:
+            made, views = self._made_heads(q) if k is None else self._made_heads(q, k)
+            return (made, views) if k is not None else ((made[0], None), (views[0], None))
+        oq, ok = out
+        return out, (self._heads(oq, "out", q.shape, q.dtype), None if k is None else self._heads(ok, "out", k.shape, q.dtype))
+
     @staticmethod
     def _maybe(h):
         return None if h is None else C.byref(h)
@@ -662,13 +680,8 @@ class Encoder:
         [n, heads, dim], k [n, kv heads, dim] or None, positions [n] int32, freqs float32 (see rotary_freqs); out: two tensors to write
         to, the inputs themselves among others. See xrl_head_rotary."""
         d, hq, hk = self._rotary(q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
-        if out is None:
-            out = self._made((q.shape, q.dtype), *([] if k is None else [(k.shape, k.dtype)]))
-            if k is None:
-                out.append(None)
-        oq, ok = out
-        _check(self.lib.xrl_head_rotary(self.handle, C.byref(d), C.byref(hq), self._maybe(hk), C.byref(self._heads(oq, "out", q.shape, q.dtype)),
-                                        None if k is None else C.byref(self._heads(ok, "out", k.shape, q.dtype))))
+        (oq, ok), (gq, gk) = self._rotary_out(q, k, out)
+        _check(self.lib.xrl_head_rotary(self.handle, C.byref(d), C.byref(hq), self._maybe(hk), C.byref(gq), self._maybe(gk)))
         return oq, ok
 
     def head_rotary_backward(self, q, k, positions, freqs, dq_out, dk_out, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
@@ -676,16 +689,12 @@ class Encoder:
         """(dq, dk) from the inputs and the gradients to the results; dq_weight, dk_weight [dim] float32 are added to; out: two tensors to write
         to, dq_out and dk_out among others. See xrl_head_rotary_backward."""
         d, hq, hk = self._rotary(q, k, positions, freqs, q_weight, k_weight, eps, interleaved)
-        if out is None:
-            out = self._made((q.shape, q.dtype), *([] if k is None else [(k.shape, k.dtype)]))
-            if k is None:
-                out.append(None)
-        oq, ok = out
+        (oq, ok), (wq, wk) = self._rotary_out(q, k, out)
         f, dim = self.torch.float32, q.shape[2]
-        gk, wk = (None, None) if k is None else (self._heads(dk_out, "dk_out", k.shape, q.dtype), self._heads(ok, "out", k.shape, q.dtype))
+        gk = None if k is None else self._heads(dk_out, "dk_out", k.shape, q.dtype)
         _check(self.lib.xrl_head_rotary_backward(
             self.handle, C.byref(d), C.byref(hq), self._maybe(hk), C.byref(self._heads(dq_out, "dq_out", q.shape, q.dtype)), self._maybe(gk),
-            C.byref(self._heads(oq, "out", q.shape, q.dtype)), self._maybe(wk),
+            C.byref(wq), self._maybe(wk),
             self._here(dq_weight, "dq_weight", f, dim), self._here(dk_weight, "dk_weight", f, dim)))
         return oq, ok
 
@@ -716,8 +725,9 @@ class Encoder:
         d, hq, hk, hv = self._attention(q, k, v, q_ptr, k_ptr, causal, scale)
         if out is None:
             o, lse = self._made((q.shape, q.dtype), (q.shape[:2], f))
-            out = dict(out=o, lse=lse)
-        ho = self._heads(out["out"], "out", q.shape, q.dtype)
+            out, ho = dict(out=o, lse=lse), Heads(o.data_ptr(), *o.stride()[:2])
+        else:
+            ho = self._heads(out["out"], "out", q.shape, q.dtype)
         _check(self.lib.xrl_attention(self.handle, C.byref(d), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho),
                                       self._here(out["lse"], "lse", f, q.shape[0] * q.shape[1])))
         return out
@@ -727,24 +737,25 @@ class Encoder:
         xrl_attention_backward."""
         d, hq, hk, hv = self._attention(q, k, v, q_ptr, k_ptr, causal, scale)
         if out is None:
-            out = self._made((q.shape, q.dtype), (k.shape, k.dtype), (v.shape, v.dtype))
+            out, (gq, gk, gv) = self._made_heads(q, k, v)
+        else:
+            gq, gk, gv = (self._heads(g, name, x.shape, x.dtype) for g, name, x in zip(out, ("dq", "dk", "dv"), (q, k, v)))
         dq, dk, dv = out
         _check(self.lib.xrl_attention_backward(
             self.handle, C.byref(d), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(self._heads(forward["out"], "out", q.shape, q.dtype)),
             self._here(forward["lse"], "lse", self.torch.float32, q.shape[0] * q.shape[1]),
-            C.byref(self._heads(dout, "dout", q.shape, q.dtype)), C.byref(self._heads(dq, "dq", q.shape, q.dtype)),
-            C.byref(self._heads(dk, "dk", k.shape, k.dtype)), C.byref(self._heads(dv, "dv", v.shape, v.dtype))))
+            C.byref(self._heads(dout, "dout", q.shape, q.dtype)), C.byref(gq), C.byref(gk), C.byref(gv)))
         return dq, dk, dv
 
     def _cache(self, n, heads, q_ptr, k_cache, v_cache, table, lengths, type):
         t = self.torch
         for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-            if x.dim() != 4 or x.device != self._device or x.dtype != type or x.shape != k_cache.shape:
+            if x.dim() != 4 or x.get_device() != self._index or x.dtype != type or x.shape != k_cache.shape:
                 raise ValueError(f"{name}: a tensor [pages, page, kv heads, dim] of {type} on {self._device} is needed, both of one shape")
             if x.stride(3) != 1 and x.shape[3] > 1:
                 raise ValueError(f"{name}: heads of contiguous columns are needed")
         pages, page, kv, dim = k_cache.shape
-        if q_ptr.numel() < 1 or table.dim() != 2 or table.device != self._device or table.dtype != t.int32 or table.shape[0] != q_ptr.numel() - 1:
+        if q_ptr.numel() < 1 or table.dim() != 2 or table.get_device() != self._index or table.dtype != t.int32 or table.shape[0] != q_ptr.numel() - 1:
             raise ValueError("table: a matrix of int32 on the GPU with a row for each sequence of q_ptr is needed")
         if table.stride(1) != 1 and table.shape[1] > 1:
             raise ValueError("table: contiguous rows are needed")
@@ -773,9 +784,11 @@ class Encoder:
         if dim != d.dim or heads < 1 or heads % max(d.kv_heads, 1):
             raise ValueError(f"q: shape {tuple(q.shape)} with a cache of {tuple(k_cache.shape)}")
         if out is None:
-            out, = self._made((q.shape, q.dtype))
+            (out,), (ho,) = self._made_heads(q)
+        else:
+            ho = self._heads(out, "out", q.shape, q.dtype)
         _check(self.lib.xrl_cache_attention(self.handle, C.byref(d), dim ** -0.5 if scale is None else scale, C.byref(hq), C.byref(pk), C.byref(pv),
-                                            C.byref(self._heads(out, "out", q.shape, q.dtype))))
+                                            C.byref(ho)))
         return out
 
     def get_activation(self, batch, what, rnd=0):
