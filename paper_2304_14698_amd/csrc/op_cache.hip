@@ -171,6 +171,12 @@ __device__ __forceinline__ void load_query(Vec<T> *x, const T *p, bool there, in
   }
 }
 
+// A lane's column: a new token and a head.
+struct Column {
+  bool there;
+  int token, head;
+};
+
 template <typename T, int DP, int WAVES, int KT, bool WHOLE>
 struct CacheWalk {
   using L = Tile<T, DP>;
@@ -189,18 +195,20 @@ struct CacheWalk {
     kv = __builtin_amdgcn_readfirstlane(kv);
     t0 = __builtin_amdgcn_readfirstlane(t0);
     t1 = __builtin_amdgcn_readfirstlane(t1);
-    const int l32 = lane & 31, g = lane >> 5;
-    const int col = block * BM + 32 * wave + l32, token = col / a.group, head = kv * a.group + col % a.group;
-    const bool there = token < seq.rows;
-    const int64_t row = seq.begin + (there ? token : 0);
+    const int g = lane >> 5;
+    auto column = [&](int l) {                        // of lane l
+      const int col = block * BM + 32 * wave + (l & 31), token = col / a.group;
+      return Column{token < seq.rows, token < seq.rows ? token : 0, kv * a.group + col % a.group};
+    };
+    const Column mine_at = column(lane);
     // keys that a token sees
     auto keys_of = [&](int i) { const int e = seq.length - seq.rows + i + 1; return e < 0 ? 0 : e < seq.keys ? e : seq.keys; };
     const int columns = seq.rows * a.group, w0 = block * BM + 32 * wave, last = columns - 1 < w0 + 31 ? columns - 1 : w0 + 31;
-    const int all_see = w0 < columns ? keys_of(w0 / a.group) : 0, any_sees = w0 < columns ? keys_of(last / a.group) : 0, mine = there ? keys_of(token) : 0;
+    const int all_see = w0 < columns ? keys_of(w0 / a.group) : 0, any_sees = w0 < columns ? keys_of(last / a.group) : 0, mine = mine_at.there ? keys_of(mine_at.token) : 0;
     const int end = columns - 1 < block * BM + BM - 1 ? columns - 1 : block * BM + BM - 1, keys = keys_of(end / a.group);
     const int stop = t1 < (keys + KT - 1) / KT ? t1 : (keys + KT - 1) / KT;
     vec q[L::SLABS];
-    load_query<T, DP, WHOLE>(q, (const T *)a.q.p + row * a.q.stride + head * a.q.head_stride, there, a.dim, g);
+    load_query<T, DP, WHOLE>(q, (const T *)a.q.p + (seq.begin + mine_at.token) * a.q.stride + mine_at.head * a.q.head_stride, mine_at.there, a.dim, g);
     const float c = a.scale * kLog2e;
     const T *kb = (const T *)a.kc.p + kv * a.kc.head_stride, *vb = (const T *)a.vc.p + kv * a.vc.head_stride;
     // Keys that are not there stand for the sequence's first one, or for the cache's first row: their scores do not count.
@@ -253,12 +261,15 @@ struct CacheWalk {
       }
       __syncthreads();                                // (the next tiles go where the last ones are read)
       l = half_sum(l);
+      int now = lane;
+      asm volatile("" : "+v"(now));                   // (computed anew: kept over the loop it is spilled)
+      const Column c_at = column(now);
       if (slot < 0) {
-        store_row<T>((T *)a.out.p + row * a.out.stride + head * a.out.head_stride, there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, g, db0);
+        store_row<T>((T *)a.out.p + (seq.begin + c_at.token) * a.out.stride + c_at.head * a.out.head_stride, c_at.there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, now >> 5, db0);
       } else {
-        const int64_t at = slot * BM + 32 * wave + l32;
-        store_row<float>(a.part + at * DP, there, DP, true, o, 1.f, g, db0);
-        if (there && g == 0) {
+        const int64_t at = slot * BM + 32 * wave + (now & 31);
+        store_row<float>(a.part + at * DP, c_at.there, DP, true, o, 1.f, now >> 5, db0);
+        if (c_at.there && now < 32) {
           a.part_sums[2 * at] = mc;
           a.part_sums[2 * at + 1] = l;
         }
@@ -299,7 +310,7 @@ __global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 || (WAVES == 1 && 
   for (int64_t s = lane; s < a.seqs; s += 64) total += weight(s);
   total = uniform64(__shfl(sum_scan(total, lane), 63));
   const int64_t piece = (total + a.blocks - 1) / a.blocks, x0 = piece * blockIdx.x, x1 = x0 + piece < total ? x0 + piece : total;
-  Split split = {0, 0, 0, 0};
+  if (threadIdx.x == 0) a.splits[blockIdx.x] = {0, 0, 0, 0};
   if (x0 < x1) {
     // the sequence of the piece's first tile
     int64_t s = 0, start = 0;
@@ -326,14 +337,13 @@ __global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 || (WAVES == 1 && 
         // (units of one block of columns follow each other by heads of keys)
         const int block = (int)(n / a.kv_heads), kv = (int)(n % a.kv_heads);
         const bool cut = t0 > 0 || t1 < q.tiles;
+        if (t0 == 0 && cut && threadIdx.x == 0) a.splits[blockIdx.x] = {s, block, kv, (int)((q.tiles - t1 + piece - 1) / piece)};
         walk.unit(s, q, block, kv, t0, t1, cut ? 2 * (int64_t)blockIdx.x + (t0 > 0 ? 0 : 1) : -1);
-        if (t0 == 0 && cut) split = {s, block, kv, (int)((q.tiles - t1 + piece - 1) / piece)};
         x += t1 - t0;
       }
       start = stop;
     }
   }
-  if (threadIdx.x == 0) a.splits[blockIdx.x] = split;
 }
 
 // Where units are short: a whole one a block.
@@ -362,7 +372,7 @@ __global__ __launch_bounds__(WAVES * 64, DP * sizeof(T) > 256 || (WAVES == 1 && 
   walk.unit(lo, q, (int)block, (int)(b % a.kv_heads), 0, q.tiles, -1);
 }
 
-// The units that end behind the piece they begin in: a column's parts, in order.
+// The units that end behind the piece they begin in: a column's parts, in order; 32 columns a block.
 template <typename T, int DP, int BM>
 __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a) {
   const int64_t b = blockIdx.x;
@@ -372,9 +382,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const CacheArgs a) {
   const int columns = r.len * a.group - s.block * BM < BM ? r.len * a.group - s.block * BM : BM;
   // part 0: the second place of b, then the first places of the blocks behind it
   auto at = [&](int i) { return (i == 0 ? 2 * b + 1 : 2 * (b + i)) * BM; };
-  for (int e = threadIdx.x; e < columns * (DP / 4); e += 256) {
-    const int col = e / (DP / 4), d = e % (DP / 4) * 4;
-    if (d >= a.dim) continue;
+  for (int e = threadIdx.x; e < 32 * (DP / 4); e += 256) {
+    const int col = blockIdx.y * 32 + e / (DP / 4), d = e % (DP / 4) * 4;
+    if (col >= columns || d >= a.dim) continue;
     // (eight parts' loads together: each by itself is a round trip to memory)
     float m = kLowest, l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 <= s.follow; i0 += 8) {
@@ -494,7 +504,7 @@ int launch(xrl_ctx *c, CacheArgs &a, const char *who) {
   a.part_sums = (float *)(ws + part);
   a.splits = (Split *)(ws + part + sums);
   cache_attention_kernel<T, DP, WAVES, KT, WHOLE><<<dim3((unsigned)a.blocks), dim3(WAVES * 64), 0, op_stream(c)>>>(a);
-  cache_join_kernel<T, DP, BM><<<dim3((unsigned)a.blocks), dim3(256), 0, op_stream(c)>>>(a);
+  cache_join_kernel<T, DP, BM><<<dim3((unsigned)a.blocks, WAVES), dim3(256), 0, op_stream(c)>>>(a);
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
