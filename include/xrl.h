@@ -485,6 +485,7 @@ typedef struct xrl_attention_desc {
 int xrl_attention(xrl_ctx *ctx, const xrl_attention_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out, float *d_lse);
 
 /* xrl_attention_backward: from the inputs, xrl_attention's results and dout = dJ/dout the gradients dq, dk, dv, of the inputs' shapes and type, written (not added to).
+ * In bf16 the exponentials are rounded to it as factors of dout, dJ/ds_ij once as a factor of q_i, and as a sum of two bf16 numbers as a factor of k_j.
  * The gradients of a key head are sums over the query heads that share it, in a fixed order. Rows of no sequence are left as they were; keys that no row sees get 0.
  * Errors: as above, OOM. */
 int xrl_attention_backward(xrl_ctx *ctx, const xrl_attention_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *v, const xrl_heads *out,

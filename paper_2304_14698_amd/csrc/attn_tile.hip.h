@@ -71,6 +71,19 @@ __device__ __forceinline__ Vec<T> acc_operand(const f32x16 &a, int slab) {
   }
 }
 
+// What that operand's rounding left out, rounded in turn (bf16; fp32 leaves nothing out).
+template <typename T>
+__device__ __forceinline__ Vec<T> acc_rest(const f32x16 &a, int slab, const Vec<T> &rounded) {
+  if constexpr (sizeof(T) == 2) {
+    float rest[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) rest[n] = a[8 * slab + n] - (float)rounded[n];
+    return pack_bf16x8(rest[0], rest[1], rest[2], rest[3], rest[4], rest[5], rest[6], rest[7]);
+  } else {
+    return rounded;
+  }
+}
+
 // Rows of a tensor [rows, heads, dim] that a wave's scalar registers describe: loads behind the last one give zeros.
 __device__ __forceinline__ u32x4 rows_descriptor(const void *p, unsigned bytes) {
   const uint64_t a = (uint64_t)(uintptr_t)p;
