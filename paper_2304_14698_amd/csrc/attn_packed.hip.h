@@ -45,11 +45,13 @@ struct Place {
   int64_t seq;
   int head, tile;
 };
+__device__ __forceinline__ int head_of(const AttnArgs &a, int heads, int h) {
+  const int group = heads / a.kv_heads;
+  return h % a.kv_heads * group + h / a.kv_heads;
+}
 __device__ __forceinline__ bool place_of(const AttnArgs &a, const int32_t *ptr, int64_t n, int heads, int bm, bool last_first, int lane, Place &o) {
   const int64_t b = a.block0 + blockIdx.x;
-  const int h = (int)(b % heads);
-  const int group = heads / a.kv_heads;
-  o.head = h % a.kv_heads * group + h / a.kv_heads;
+  o.head = head_of(a, heads, (int)(b % heads));
   if (a.seqs <= 64) {
     const Span mine = lane < a.seqs ? span_of(ptr, lane, n) : Span{0, 0};
     const int tiles = (mine.len + bm - 1) / bm;
@@ -82,8 +84,109 @@ __device__ __forceinline__ bool place_of(const AttnArgs &a, const int32_t *ptr, 
   return true;
 }
 
-// Bits of a wave's tile that count: keys [j0, j0 + 32) against row i, which sees those below `end`.
-__device__ __forceinline__ bool sees(int j, int end) { return j < end; }
+// Short sequences: a tile is 32 rows that follow each other in the packed tensor, of whatever sequences, a row a lane, and goes over the rows of the other side that any of
+// them meets. A sequence by itself would leave most of a tile empty. (Where in a tile its keys lie then depends on its place among the others, and so do the last bits of its sums.)
+// us, forward and backward of 1024 sequences of 1 to 24 rows with 4 heads of 32 in fp32: 60 by a tile a sequence, 35 by mixed ones.
+//
+// Taken where sequences have at most 128 rows on average on both sides. 16384 rows in sequences of one length, mixed tiles and (>) tiles of 128 rows of one sequence, forward + backward in
+// us: 4 heads of 32 in fp32 16 + 44 > 22 + 72 at 96 rows, 20 + 56 > 29 + 111 at 128, 22 + 66 > 29 + 92 at 192, 29 + 88 > 25 + 79 at 256; 32 heads of 128 in bf16 118 + 304 > 137 + 318, 125 + 358 >
+// 126 + 395, 137 + 378 > 143 + 356, 148 + 445 > 131 + 357.
+inline bool mixes(const AttnArgs &a) { return a.n_q <= 128 * a.seqs && a.n_k <= 128 * a.seqs; }
+// Few rows over many of the other side: a wave a tile of 32 of one sequence's rows.
+// us, attention of 8192 queries over 600 keys a sequence, by such waves and by blocks of four: 16 heads of 64 in bf16, 8 queries a sequence 243 and 415, 64: 51 and 61, 128: 48 and 39.
+inline bool few_rows(const AttnArgs &a, int64_t n) { return n <= 64 * a.seqs; }
+
+// What the lane's row meets: rows [lo, hi) of the other tensor (keys that a query sees; queries that see a key); and over the wave the first and the last of these, and what all
+// rows meet.
+struct Meets {
+  bool there;                                       // the row is one of a sequence
+  int lo, hi, first, last, all_lo, all_hi;
+};
+// The row's own tensor has the ends `ptr` and n rows, the other one `other` and m; `keys`: the row is a key.
+__device__ __forceinline__ Meets meets_of(const AttnArgs &a, const int32_t *ptr, int64_t n, const int32_t *other, int64_t m, bool keys, int64_t tile, int lane) {
+  const int64_t row0 = 32 * tile, row = row0 + (lane & 31);
+  int64_t s0 = last_begun(ptr, a.seqs, n, row0, lane), s = -1;
+  if (s0 < 0) s0 = 0;
+  // so many of the sequences behind it have begun at the lane's row or in front of it, 64 of them at a time
+  for (bool more = true; __ballot(more); s0 += 64) {
+    const int64_t end = s0 + 1 + lane < a.seqs ? end_at(ptr, s0 + 1 + lane, n) : INT64_MAX;
+    const int e = end <= INT32_MAX ? (int)end : INT32_MAX;
+    int count = 0;                                  // (the ends do not fall: by halves)
+#pragma unroll
+    for (int step = 32; step > 0; step /= 2) count += __shfl(e, count + step - 1) <= row ? step : 0;
+    count += __shfl(e, count) <= row ? 1 : 0;
+    if (more && count < 64) s = s0 + count;
+    more = more && count == 64;
+  }
+  Meets o;
+  const Span mine = span_of(ptr, s, n), that = span_of(other, s, m);
+  const int at = (int)(row - mine.begin);
+  o.there = row >= mine.begin && at < mine.len;
+  int lo = 0, hi = that.len;
+  if (a.causal && keys) {                           // from the first row that sees the key on
+    const int i = at - (mine.len - that.len);
+    lo = i < 0 ? 0 : i < hi ? i : hi;
+  } else if (a.causal) {
+    const int e = at + 1 + that.len - mine.len;
+    hi = e < 0 ? 0 : e < hi ? e : hi;
+  }
+  const bool some = o.there && lo < hi;
+  o.lo = some ? (int)that.begin + lo : 0;
+  o.hi = some ? (int)that.begin + hi : 0;
+  o.first = wave_min(some ? o.lo : INT32_MAX);
+  o.last = -wave_min(-o.hi);
+  o.all_lo = -wave_min(o.there ? some ? -o.lo : -INT32_MAX : 0);
+  o.all_hi = wave_min(o.there ? o.hi : INT32_MAX);
+  if (o.first > o.last) o.first = o.last;
+  return o;
+}
+
+// A lane's row of queries, and the keys that its block goes over: `keys` of them from row key0 of their tensor on, of which the row sees [from, mine); all rows of the wave see
+// [all_from, all_see), and any of them keys below any_sees.
+struct Queries {
+  int head;
+  int64_t row, key0;
+  bool there;
+  int keys, from, mine, all_from, all_see, any_sees;
+};
+template <int WAVES, bool MIXED>
+__device__ __forceinline__ bool queries_of(const AttnArgs &a, int wave, int lane, Queries &o) {
+  constexpr int BM = 32 * WAVES;
+  if constexpr (MIXED) {
+    static_assert(WAVES == 1);
+    const int64_t b = a.block0 + blockIdx.x;
+    const Meets x = meets_of(a, a.q_ptr, a.n_q, a.k_ptr, a.n_k, false, b / a.q_heads, lane);
+    o.head = head_of(a, a.q_heads, (int)(b % a.q_heads));
+    o.there = x.there;
+    o.row = x.there ? 32 * (b / a.q_heads) + (lane & 31) : 0;
+    o.key0 = x.first;
+    o.keys = o.any_sees = __builtin_amdgcn_readfirstlane(x.last - x.first);
+    o.from = x.lo - x.first;
+    o.mine = x.hi - x.first;
+    o.all_from = x.all_lo - x.first;
+    o.all_see = x.all_hi - x.first;
+    return true;
+  } else {
+    Place at;
+    if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, true, lane, at)) return false;
+    const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
+    const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
+    if (i0 < 0) return false;
+    const int len_k = __builtin_amdgcn_readfirstlane(ks.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len);
+    auto keys_of = [&](int i) { const int e = a.causal ? i + 1 + off : len_k; return e < 0 ? 0 : e < len_k ? e : len_k; };
+    const int last = (i0 + BM < qs.len ? i0 + BM : qs.len) - 1, w0 = i0 + 32 * wave, w1 = w0 + 31 < last ? w0 + 31 : last, i = w0 + (lane & 31);
+    o.head = at.head;
+    o.there = i < qs.len;
+    o.row = qs.begin + (o.there ? i : 0);
+    o.key0 = ks.begin;
+    o.keys = __builtin_amdgcn_readfirstlane(keys_of(last));
+    o.from = o.all_from = 0;
+    o.mine = keys_of(i);
+    o.all_see = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w0) : 0);
+    o.any_sees = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w1) : 0);
+    return true;
+  }
+}
 
 // Rows [n, heads, dim] that are written must lie apart; rows that are read may not (broadcast inputs).
 inline bool lies_apart(const xrl_heads &x, int64_t n, int heads, int dim) {
@@ -174,6 +277,13 @@ struct Inputs {
   }
 };
 
+// Launches `kernel` over the tiles of 32 rows of n that follow each other, for each of `heads` heads.
+template <typename K>
+void launch_mixed(const xrl_ctx *c, AttnArgs &a, K kernel, int64_t n, int heads) {
+  a.blocks = (n + 31) / 32 * heads;
+  for (a.block0 = 0; a.block0 < a.blocks; a.block0 += kMaxBlocks)
+    kernel<<<dim3((unsigned)std::min(a.blocks - a.block0, kMaxBlocks)), dim3(64), 0, op_stream(c)>>>(a);
+}
 // Launches `kernel` over all tiles of bm rows of n, in seqs sequences, for each of `heads` heads.
 template <typename K>
 void launch_tiles(const xrl_ctx *c, AttnArgs &a, K kernel, int64_t n, int heads, int bm, int threads) {

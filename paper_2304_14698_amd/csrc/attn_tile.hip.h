@@ -232,7 +232,7 @@ __device__ __forceinline__ void add_tile(unsigned kt, unsigned vt, const Vec<T> 
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
   mx = half_max(mx) * c;
   // The reference of the exponentials follows the maximum only where that has grown by 2^8: until then sums and results are up to 2^8 times as large, and nothing is
-  // multiplied. Each row by its own maximum: what shares its wave changes none of its bits.
+  // multiplied. Each row by its own maximum, whatever shares its wave.
   const bool grown = mx > mc + 8.f;
   if (__ballot(grown)) {
     const float m = grown ? mx : mc, f = __builtin_amdgcn_exp2f(mc - m);
@@ -282,8 +282,8 @@ __device__ __forceinline__ Span span_of(const int32_t *ptr, int64_t s, int64_t n
   const int64_t b = end_at(ptr, s, n), e = end_at(ptr, s + 1, n);
   return {b, e > b ? (int)(e - b) : 0};
 }
-// The sequence of a row, or -1.
-__device__ __forceinline__ int64_t sequence_of_row(const int32_t *ptr, int64_t seqs, int64_t n, int64_t row, int lane) {
+// The last sequence that begins at a row or in front of it, or -1.
+__device__ __forceinline__ int64_t last_begun(const int32_t *ptr, int64_t seqs, int64_t n, int64_t row, int lane) {
   int64_t lo = 0, hi = seqs;
   do {
     const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
@@ -293,7 +293,12 @@ __device__ __forceinline__ int64_t sequence_of_row(const int32_t *ptr, int64_t s
     lo += (c - 1) * step;
     hi = lo + step < hi ? lo + step : hi;
   } while (hi - lo > 1);
-  return row < end_at(ptr, lo + 1, n) ? lo : -1;
+  return lo;
+}
+// The sequence of a row, or -1.
+__device__ __forceinline__ int64_t sequence_of_row(const int32_t *ptr, int64_t seqs, int64_t n, int64_t row, int lane) {
+  const int64_t s = last_begun(ptr, seqs, n, row, lane);
+  return s >= 0 && row < end_at(ptr, s + 1, n) ? s : -1;
 }
 // The sequence that tile number u belongs to, or -1; 64 of them are looked at at once.
 __device__ __forceinline__ int64_t sequence_of(const int32_t *ptr, int64_t seqs, int64_t n, int bm, int64_t u, int lane) {

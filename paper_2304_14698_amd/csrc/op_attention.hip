@@ -9,32 +9,21 @@
 
 namespace {
 
-// One block: BM = 32 WAVES rows of one sequence and one head, KT keys at a time.
-template <typename T, int DP, int WAVES, int KT>
+// One block: BM = 32 WAVES rows of one sequence (MIXED: of whatever sequences) and one head, KT keys at a time.
+template <typename T, int DP, int WAVES, int KT, bool MIXED>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 : 2) void attention_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
   using vec = typename L::vec;
-  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB, BUFS = kBuffers<WAVES>;
+  constexpr int BYTES = KT * L::RB, BUFS = kBuffers<WAVES>;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUFS * BYTES];
   touch_args(a);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
-  Place at;
-  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, true, lane, at)) return;
-  const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
-  const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
-  if (i0 < 0) return;
-  const int len_k = __builtin_amdgcn_readfirstlane(ks.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len);
-  const int kv = at.head / (a.q_heads / a.kv_heads);
-  // keys that rows i0 .. i0 + BM - 1 see, and that this wave's rows see, all of them and any
-  auto keys_of = [&](int i) { const int e = a.causal ? i + 1 + off : len_k; return e < 0 ? 0 : e < len_k ? e : len_k; };
-  const int last = (i0 + BM < qs.len ? i0 + BM : qs.len) - 1, w0 = i0 + 32 * wave, w1 = w0 + 31 < last ? w0 + 31 : last;
-  const int keys = __builtin_amdgcn_readfirstlane(keys_of(last)), tiles = (keys + KT - 1) / KT;
-  const int all_see = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w0) : 0), any_sees = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w1) : 0);
-  const int i = w0 + l32, mine = keys_of(i);        // keys that the lane's row sees
-  const bool there = i < qs.len;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  Queries w;
+  if (!queries_of<WAVES, MIXED>(a, wave, lane, w)) return;
+  const int kv = w.head / (a.q_heads / a.kv_heads), keys = w.keys, tiles = (keys + KT - 1) / KT;
   vec q[L::SLABS];
-  load_row<T, DP>(q, head_at<T>(a.q, qs.begin + (there ? i : 0), at.head), there, a.dim_in, g);
-  const T *k = head_at<T>(a.k, ks.begin, kv), *v = head_at<T>(a.v, ks.begin, kv);
+  load_row<T, DP>(q, head_at<T>(a.q, w.row, w.head), w.there, a.dim_in, g);
+  const T *k = head_at<T>(a.k, w.key0, kv), *v = head_at<T>(a.v, w.key0, kv);
   const unsigned base = lds_address(lds);
   const float c = a.scale * kLog2e;
   float mc, l;
@@ -60,16 +49,17 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
       __syncthreads();                              // tile t is there, and t - 1 is read
       if (BUFS == 2 && t + 1 < tiles) stage(t + 1);
       const int j0 = t * KT;
-      if (j0 >= any_sees) continue;
-      add_tile<T, DP, KT, SAFE>(kt, vt, q, c, j0 + KT <= all_see, [&](int n) { return n < mine - j0 - 4 * g; }, o, mc, l, lane, db0);
+      if (j0 >= w.any_sees) continue;
+      const int from = w.from - j0 - 4 * g, mine = w.mine - j0 - 4 * g;
+      add_tile<T, DP, KT, SAFE>(kt, vt, q, c, (!MIXED || j0 >= w.all_from) && j0 + KT <= w.all_see, [&](int n) { return n < mine && (!MIXED || n >= from); }, o, mc, l, lane, db0);
     }
     l = half_sum(l);
-    store_row<T>(head_at<T>(a.out, qs.begin + i, at.head), there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, g, db0);
+    store_row<T>(head_at<T>(a.out, w.row, w.head), w.there, a.dim, a.quads, o, l == 0.f ? 0.f : 1.f / l, g, db0);
   };
   f32x16 o[L::BLOCKS];
   pass(std::false_type(), o, 0);
-  if (there && g == 0) a.lse[(qs.begin + i) * a.q_heads + at.head] = l == 0.f ? -INFINITY : mc * kLn2 + logf(l);
-  if (!a.causal) return;
+  if (w.there && g == 0) a.lse[w.row * a.q_heads + w.head] = l == 0.f ? -INFINITY : mc * kLn2 + logf(l);
+  if (!MIXED && !a.causal) return;
   bool fine = true;
 #pragma unroll
   for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(o[db]);
@@ -85,8 +75,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
 template <typename T, int DP>
 void launch(const xrl_ctx *c, AttnArgs &a) {
   constexpr int KT = sizeof(T) == 2 ? 64 : 32;
-  if (a.n_q <= 64 * a.seqs) launch_tiles(c, a, attention_kernel<T, DP, 1, 32>, a.n_q, a.q_heads, 32, 64);
-  else launch_tiles(c, a, attention_kernel<T, DP, 4, KT>, a.n_q, a.q_heads, 128, 256);
+  if (mixes(a)) launch_mixed(c, a, attention_kernel<T, DP, 1, 32, true>, a.n_q, a.q_heads);
+  else if (few_rows(a, a.n_q)) launch_tiles(c, a, attention_kernel<T, DP, 1, 32, false>, a.n_q, a.q_heads, 32, 64);
+  else launch_tiles(c, a, attention_kernel<T, DP, 4, KT, false>, a.n_q, a.q_heads, 128, 256);
 }
 template <typename T>
 void launch_dim(const xrl_ctx *c, AttnArgs &a) {

@@ -14,44 +14,33 @@ namespace {
 // bf16: ds is a difference of nearly equal numbers, and rounding it once to the products' 8 bits would cost dq 1.8e-3 of its size, as much as dq's own rounding. So its rest, ds - bf16(ds), is a
 // second operand of the same product. D from the rounded out is off as well, by delta_i = sum_j ds_ij, as sum_j p_ij = 1: the keys' gradients take D + delta. Relative errors of two sequences of 4096
 // tokens with heads of 128: dq 2.7e-3 to 2.1e-3, dk 2.6e-3 to 2.3e-3, where a rounded output alone has 1.7e-3; 6 % of the backward pass. (The rest of ds for dk too: 2.0e-3, 9 % more; left out.)
-template <typename T, int DP, int WAVES, int KT>
+template <typename T, int DP, int WAVES, int KT, bool MIXED>
 __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
   using vec = typename L::vec;
-  constexpr int BM = 32 * WAVES, BYTES = KT * L::RB, BUFS = kBuffers<WAVES>;
+  constexpr int BYTES = KT * L::RB, BUFS = kBuffers<WAVES>;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUFS * BYTES];
   touch_args(a);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, g = lane >> 5;
-  Place at;
-  if (!place_of(a, a.q_ptr, a.n_q, a.q_heads, BM, true, lane, at)) return;
-  const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
-  const int i0 = __builtin_amdgcn_readfirstlane(at.tile < (qs.len + BM - 1) / BM ? at.tile * BM : -1);
-  if (i0 < 0) return;
-  const int len_k = __builtin_amdgcn_readfirstlane(ks.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len);
-  const int kv = at.head / (a.q_heads / a.kv_heads);
-  auto keys_of = [&](int i) { const int e = a.causal ? i + 1 + off : len_k; return e < 0 ? 0 : e < len_k ? e : len_k; };
-  const int last = (i0 + BM < qs.len ? i0 + BM : qs.len) - 1, w0 = i0 + 32 * wave, w1 = w0 + 31 < last ? w0 + 31 : last;
-  const int keys = __builtin_amdgcn_readfirstlane(keys_of(last)), tiles = (keys + KT - 1) / KT;
-  const int all_see = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w0) : 0), any_sees = __builtin_amdgcn_readfirstlane(w0 <= last ? keys_of(w1) : 0);
-  const int i = w0 + l32, mine = keys_of(i);
-  const bool there = i < qs.len;
-  const int64_t row = qs.begin + (there ? i : 0);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5;
+  Queries w;
+  if (!queries_of<WAVES, MIXED>(a, wave, lane, w)) return;
+  const int kv = w.head / (a.q_heads / a.kv_heads), keys = w.keys, tiles = (keys + KT - 1) / KT;
   vec q[L::SLABS], dout[L::SLABS];
   float delta = 0.f;
   {
-    load_row<T, DP>(q, head_at<T>(a.out, row, at.head), there, a.dim_in, g);
-    load_row<T, DP>(dout, head_at<T>(a.dout, row, at.head), there, a.dim_in, g);
+    load_row<T, DP>(q, head_at<T>(a.out, w.row, w.head), w.there, a.dim_in, g);
+    load_row<T, DP>(dout, head_at<T>(a.dout, w.row, w.head), w.there, a.dim_in, g);
 #pragma unroll
     for (int x = 0; x < L::SLABS; ++x)
 #pragma unroll
       for (int j = 0; j < L::V; ++j) delta = fmaf((float)q[x][j], (float)dout[x][j], delta);
     delta = half_sum(delta);
   }
-  load_row<T, DP>(q, head_at<T>(a.q, row, at.head), there, a.dim_in, g);
+  load_row<T, DP>(q, head_at<T>(a.q, w.row, w.head), w.there, a.dim_in, g);
   // (a row without keys, or with scores of -inf alone: every exponential below is 0)
-  const float lse = a.lse[row * a.q_heads + at.head], lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
-  if (there && g == 0) a.stat_lse[at.head * a.n_q + row] = lse2;
-  const T *k = head_at<T>(a.k, ks.begin, kv), *v = head_at<T>(a.v, ks.begin, kv);
+  const float lse = a.lse[w.row * a.q_heads + w.head], lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  if (w.there && g == 0) a.stat_lse[w.head * a.n_q + w.row] = lse2;
+  const T *k = head_at<T>(a.k, w.key0, kv), *v = head_at<T>(a.v, w.key0, kv);
   const unsigned base = lds_address(lds);
   const float c = a.scale * kLog2e;
   constexpr bool REST = sizeof(T) == 2;
@@ -77,8 +66,10 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
       __syncthreads();                              // tile t is there, and t - 1 is read
       if (BUFS == 2 && t + 1 < tiles) stage(t + 1);
       const int j0 = t * KT;
-      if (j0 >= any_sees) continue;
-      const bool whole = j0 + KT <= all_see;
+      if (j0 >= w.any_sees) continue;
+      const bool whole = (!MIXED || j0 >= w.all_from) && j0 + KT <= w.all_see;
+      const int from = w.from - j0 - 4 * g, mine = w.mine - j0 - 4 * g;
+      auto sees = [&](int n) { return n < mine && (!MIXED || n >= from); };
 #pragma unroll
       for (int kb = 0; kb < KT / 32; ++kb) {
         f32x16 s = zero_acc(), dp = zero_acc();
@@ -91,7 +82,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - delta);
         if (!whole) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = sees(j0 + 32 * kb + acc_row(r, g), mine) ? s[r] : 0.f;
+          for (int r = 0; r < 16; ++r) s[r] = sees(32 * kb + acc_row(r, 0)) ? s[r] : 0.f;
         }
         if (REST && !SAFE) {
 #pragma unroll
@@ -103,7 +94,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
           if (SAFE && !whole) {
             vec seen;
 #pragma unroll
-            for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(j0 + 32 * kb + acc_row(x * L::V + n, g), mine) ? 1.f : 0.f);
+            for (int n = 0; n < L::V; ++n) seen[n] = (T)(sees(32 * kb + acc_row(x * L::V + n, 0)) ? 1.f : 0.f);
 #pragma unroll
             for (int db = 0; db < NB; ++db) {
               const vec key = L::across(kt, 32 * kb + x * L::STEP, db0 + db, lane);
@@ -121,13 +112,13 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
         }
       }
     }
-    store_row<T>(head_at<T>(a.dq, row, at.head), there, a.dim, a.quads, dq, a.scale, g, db0);
+    store_row<T>(head_at<T>(a.dq, w.row, w.head), w.there, a.dim, a.quads, dq, a.scale, g, db0);
   };
   f32x16 dq[L::BLOCKS];
   pass(std::false_type(), dq, 0);
   more = half_sum(more);
-  if (there && g == 0) a.stat_delta[at.head * a.n_q + row] = delta + more;
-  if (!a.causal) return;
+  if (w.there && g == 0) a.stat_delta[w.head * a.n_q + w.row] = delta + more;
+  if (!MIXED && !a.causal) return;
   bool fine = true;
 #pragma unroll
   for (int db = 0; db < L::BLOCKS; ++db) fine = fine && all_finite(dq[db]);
@@ -149,10 +140,65 @@ __device__ __forceinline__ void stage_floats(const float *p, int n, unsigned lds
 #pragma clang diagnostic pop
 }
 
+// A lane's key, and the rows of queries that its block goes over: `rows` of them from row row0 of their tensor on, from the multiple `begin` of QT on. Rows [mine, end) see the
+// key, rows [all_see, all_end) all keys of the wave, and rows below any_sees none. A block's keys are key0 + j0 on, of `keys` from key0 on.
+struct Keys {
+  int head;
+  int64_t row, row0, key0;
+  bool there;
+  int j0, keys, rows, begin, mine, end, any_sees, all_see, all_end;
+};
+template <int WAVES, bool MIXED>
+__device__ __forceinline__ bool keys_of(const AttnArgs &a, int qt, int wave, int lane, Keys &o) {
+  constexpr int BM = 32 * WAVES;
+  if constexpr (MIXED) {
+    static_assert(WAVES == 1);
+    const int64_t b = a.block0 + blockIdx.x, tile = b / a.kv_heads;
+    const Meets x = meets_of(a, a.k_ptr, a.n_k, a.q_ptr, a.n_q, true, tile, lane);
+    o.head = (int)(b % a.kv_heads);
+    o.there = x.there;
+    o.row = x.there ? 32 * tile + (lane & 31) : 0;
+    o.row0 = x.first;
+    o.key0 = 32 * tile;
+    o.j0 = 0;
+    o.keys = a.n_k - o.key0 < 32 ? (int)(a.n_k - o.key0) : 32;
+    o.rows = __builtin_amdgcn_readfirstlane(x.last - x.first);
+    o.begin = o.any_sees = 0;
+    o.mine = x.lo - x.first;
+    o.end = x.hi - x.first;
+    o.all_see = x.all_lo - x.first;
+    o.all_end = x.all_hi - x.first;
+    return true;
+  } else {
+    Place at;
+    if (!place_of(a, a.k_ptr, a.n_k, a.kv_heads, BM, false, lane, at)) return false;
+    const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
+    o.j0 = __builtin_amdgcn_readfirstlane(at.tile < (ks.len + BM - 1) / BM ? at.tile * BM : -1);
+    if (o.j0 < 0) return false;
+    const int len_q = __builtin_amdgcn_readfirstlane(qs.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len);
+    const int w0 = o.j0 + 32 * wave, j = w0 + (lane & 31);
+    // the first row that sees a key
+    auto first_of = [&](int j) { const int i = a.causal ? j - off : 0; return i < 0 ? 0 : i < len_q ? i : len_q; };
+    o.head = at.head;
+    o.there = j < ks.len;
+    o.row = ks.begin + (o.there ? j : 0);
+    o.row0 = qs.begin;
+    o.key0 = ks.begin;
+    o.keys = ks.len;
+    o.rows = len_q;
+    o.begin = __builtin_amdgcn_readfirstlane(first_of(o.j0)) / qt * qt;
+    o.any_sees = __builtin_amdgcn_readfirstlane(first_of(w0));
+    o.all_see = __builtin_amdgcn_readfirstlane(first_of(w0 + 31));
+    o.mine = first_of(j);
+    o.end = o.all_end = len_q;
+    return true;
+  }
+}
+
 // dk and dv: one block has 32 WAVES keys of one sequence and one head of keys, a key a lane, and goes over the queries that see them, QT rows at a time, of all
 // heads that share the keys, in order. HALVES: so many times WAVES waves each go over their part of these queries, and their sums are added at the end, in order: no sum is taken
 // by two blocks. IN_LDS: the block's keys and values stay in LDS, where registers for them as well would leave one wave a SIMD.
-template <typename T, int DP, int WAVES, int QT, int HALVES, bool IN_LDS, bool DK, bool DV>
+template <typename T, int DP, int WAVES, int QT, int HALVES, bool IN_LDS, bool DK, bool DV, bool MIXED>
 __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
   using vec = typename L::vec;
@@ -162,31 +208,22 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
   touch_args(a);
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int half = HALVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES : 0, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % WAVES;
-  Place at;
-  if (!place_of(a, a.k_ptr, a.n_k, a.kv_heads, BM, false, lane, at)) return;
-  const Span qs = span_of(a.q_ptr, at.seq, a.n_q), ks = span_of(a.k_ptr, at.seq, a.n_k);
-  const int j0 = __builtin_amdgcn_readfirstlane(at.tile < (ks.len + BM - 1) / BM ? at.tile * BM : -1);
-  if (j0 < 0) return;
-  const int len_q = __builtin_amdgcn_readfirstlane(qs.len), off = __builtin_amdgcn_readfirstlane(ks.len - qs.len), group = a.q_heads / a.kv_heads;
-  const int j = j0 + 32 * wave + l32;
-  const bool there = j < ks.len;
-  // the first row that sees a key
-  auto first_of = [&](int j) { const int i = a.causal ? j - off : 0; return i < 0 ? 0 : i < len_q ? i : len_q; };
-  const int w0 = j0 + 32 * wave, w1 = w0 + 31;
-  const int begin = __builtin_amdgcn_readfirstlane(first_of(j0)) / QT * QT;
-  const int any_sees = __builtin_amdgcn_readfirstlane(first_of(w0)), all_see = __builtin_amdgcn_readfirstlane(first_of(w1)), mine = first_of(j);
+  Keys w;
+  if (!keys_of<WAVES, MIXED>(a, QT, wave, lane, w)) return;
+  const int group = a.q_heads / a.kv_heads, len_q = w.rows, begin = w.begin, j0 = w.j0;
+  const bool there = w.there;
   const int per_head = (len_q - begin + QT - 1) / QT, all_tiles = per_head * group, share = (all_tiles + HALVES - 1) / HALVES;
   const int first = half * share, tiles = first < all_tiles ? (all_tiles - first < share ? all_tiles - first : share) : 0;   // of this half
   vec k[L::SLABS], v[L::SLABS];
   const unsigned base = lds_address(lds) + half * EACH, stats = base + 2 * BUFS * BYTES, keys = lds_address(lds) + HALVES * EACH, values = keys + BM * L::RB;
   if constexpr (!IN_LDS) {
-    load_row<T, DP>(k, head_at<T>(a.k, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
-    if (DK) load_row<T, DP>(v, head_at<T>(a.v, ks.begin + (there ? j : 0), at.head), there, a.dim_in, g);
+    load_row<T, DP>(k, head_at<T>(a.k, w.row, w.head), there, a.dim_in, g);
+    if (DK) load_row<T, DP>(v, head_at<T>(a.v, w.row, w.head), there, a.dim_in, g);
   }
   const float c = a.scale * kLog2e;
   auto stage = [&](int e, int i, int b) {             // rows i on of the group's head e
-    const int head = at.head * group + e;
-    const int64_t row = qs.begin + i;
+    const int head = w.head * group + e;
+    const int64_t row = w.row0 + i;
     stage_tile<T, DP, QT, WAVES>(head_at<T>(a.q, row, head), len_q - i, a.q.stride, a.dim_in, base + b * BYTES, wave, lane);
     stage_tile<T, DP, QT, WAVES>(head_at<T>(a.dout, row, head), len_q - i, a.dout.stride, a.dim_in, base + (BUFS + b) * BYTES, wave, lane);
     const int n = len_q - i < QT ? len_q - i : QT;
@@ -201,8 +238,8 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
     const int e0 = per_head > 0 ? first / per_head : 0;
     int next_e = e0, next_i = begin + (first - e0 * per_head) * QT, i = next_i;
     if constexpr (IN_LDS) {
-      stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.k, ks.begin + j0, at.head), ks.len - j0, a.k.stride, a.dim_in, keys, half * WAVES + wave, lane);
-      if (DK) stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.v, ks.begin + j0, at.head), ks.len - j0, a.v.stride, a.dim_in, values, half * WAVES + wave, lane);
+      stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.k, w.key0 + j0, w.head), w.keys - j0, a.k.stride, a.dim_in, keys, half * WAVES + wave, lane);
+      if (DK) stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.v, w.key0 + j0, w.head), w.keys - j0, a.v.stride, a.dim_in, values, half * WAVES + wave, lane);
     }
     if (tiles > 0) stage(next_e, next_i, 0);
     for (int t = 0; t < share; ++t) {
@@ -220,8 +257,8 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
         ++next_e;
       }
       if (BUFS == 2 && t + 1 < tiles) stage(next_e, next_i, (t + 1) & 1);
-      if (t >= tiles || i + QT <= any_sees) continue;
-      const bool whole = i >= all_see && i + QT <= len_q;
+      if (t >= tiles || i + QT <= w.any_sees) continue;
+      const bool whole = i >= w.all_see && i + QT <= (MIXED ? w.all_end : len_q);
       f32x16 s[QT / 32], dp[QT / 32];
 #pragma unroll
       for (int qb = 0; qb < QT / 32; ++qb) {
@@ -246,7 +283,7 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
             if (DK) dp[qb][4 * n + r] = p * (dp[qb][4 * n + r] - delta[r]);
           }
         }
-        auto counts = [&](int r) { const int n = 32 * qb + acc_row(r, 0); return n >= mine - i - 4 * g && n < len_q - i - 4 * g; };
+        auto counts = [&](int r) { const int n = 32 * qb + acc_row(r, 0); return n >= w.mine - i - 4 * g && n < (MIXED ? w.end : len_q) - i - 4 * g; };
         if (!whole) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -307,12 +344,12 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
       }
     }
     if (half) return;
-    if (DK) store_row<T>(head_at<T>(a.dk, ks.begin + j, at.head), there, a.dim, a.quads, dk, a.scale, g, db0);
-    if (DV) store_row<T>(head_at<T>(a.dv, ks.begin + j, at.head), there, a.dim, a.quads, dv, 1.f, g, db0);
+    if (DK) store_row<T>(head_at<T>(a.dk, w.row, w.head), there, a.dim, a.quads, dk, a.scale, g, db0);
+    if (DV) store_row<T>(head_at<T>(a.dv, w.row, w.head), there, a.dim, a.quads, dv, 1.f, g, db0);
   };
   f32x16 dk[L::BLOCKS], dv[L::BLOCKS];
   pass(std::false_type(), dk, dv, 0);
-  if (!a.causal) return;
+  if (!MIXED && !a.causal) return;
   bool fine = true;
 #pragma unroll
   for (int db = 0; db < L::BLOCKS; ++db) fine = fine && (!DK || all_finite(dk[db])) && (!DV || all_finite(dv[db]));
@@ -327,17 +364,20 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
 
 template <typename T, int DP>
 void launch(const xrl_ctx *c, AttnArgs &a) {
-  if (a.n_q <= 64 * a.seqs) launch_tiles(c, a, attention_dq_kernel<T, DP, 1, 32>, a.n_q, a.q_heads, 32, 64);
-  else launch_tiles(c, a, attention_dq_kernel<T, DP, 4, 32>, a.n_q, a.q_heads, 128, 256);
+  if (mixes(a)) launch_mixed(c, a, attention_dq_kernel<T, DP, 1, 32, true>, a.n_q, a.q_heads);
+  else if (few_rows(a, a.n_q)) launch_tiles(c, a, attention_dq_kernel<T, DP, 1, 32, false>, a.n_q, a.q_heads, 32, 64);
+  else launch_tiles(c, a, attention_dq_kernel<T, DP, 4, 32, false>, a.n_q, a.q_heads, 128, 256);
   // One launch for both where both sums fit in the registers with their operands, else one for each, which computes the scores once more.
   constexpr bool BOTH = DP * sizeof(T) <= 256, BF16 = sizeof(T) == 2;
   if constexpr (!BOTH) {
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, 32, 1, false, true, false>, a.n_k, a.kv_heads, 128, 256);
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, 32, 1, false, false, true>, a.n_k, a.kv_heads, 128, 256);
-  } else if (a.n_k <= 64 * a.seqs) {
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 1, 32, 1, false, true, true>, a.n_k, a.kv_heads, 32, 64);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, 32, 1, false, true, false, false>, a.n_k, a.kv_heads, 128, 256);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, 32, 1, false, false, true, false>, a.n_k, a.kv_heads, 128, 256);
+  } else if (mixes(a)) {
+    launch_mixed(c, a, attention_dkv_kernel<T, DP, 1, 32, 1, false, true, true, true>, a.n_k, a.kv_heads);
+  } else if (few_rows(a, a.n_k)) {
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 1, 32, 1, false, true, true, false>, a.n_k, a.kv_heads, 32, 64);
   } else {
-    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, BF16 && DP < 128 ? 64 : 32, 2, BF16 && DP == 128, true, true>, a.n_k, a.kv_heads, 128, 512);
+    launch_tiles(c, a, attention_dkv_kernel<T, DP, 4, BF16 && DP < 128 ? 64 : 32, 2, BF16 && DP == 128, true, true, false>, a.n_k, a.kv_heads, 128, 512);
   }
 }
 template <typename T>
