@@ -692,22 +692,40 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_k
     }
     __syncthreads();
     float sum = 0.f;
-    u64 mass = 0;
-    for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int col, const float *x) {
-      for_entries<VEC>(x, [&](int j, float xj) {
-        if (few || !by_p) sum += __builtin_amdgcn_exp2f((xj - m) * c);
-        if (few) {
+    if (few) {
+      for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int col, const float *x) {
+        for_entries<VEC>(x, [&](int j, float xj) {
+          sum += __builtin_amdgcn_exp2f((xj - m) * c);
           if (xj != -INFINITY && bin_of(s, xj) <= bin) t.push(xj, col + j, weight_of(s, xj));
-        } else {
-          const double w = weight_of(s, xj);
-          if (by_p) mass += xj != -INFINITY ? whole_of(s, w) : 0;
-          if (xj != -INFINITY && w >= a.min_p) t.push(xj, col + j, w);
+        });
+      });
+      sum = t.block_sum(sum);                          // (its barriers: the list is there)
+    } else {
+      // (four weights at once and one branch for the few that are kept; a masked entry's is 2^-100, whose multiple of 2^-S is 0)
+      u64 mass = 0;
+      for_pieces<T>(row, t.odd, t.begin, t.end, lane, [&](int col, const float *x) {
+        float y[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) y[j] = x[j];
+#pragma unroll 1
+        for (int j = 0; j < VEC; j += 4) {
+          double w[4];
+          bool any = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            w[i] = weight_of(s, y[i]);
+            mass += whole_of(s, w[i]);
+            any = any | (w[i] >= a.min_p);
+          }
+          if (any)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (w[i] >= a.min_p && y[i] != -INFINITY) t.push(y[i], col + j + i, w[i]);
+#pragma unroll
+          for (int i = 0; i + 4 < VEC; ++i) y[i] = y[i + 4];
         }
       });
-    });
-    sum = t.block_sum(sum);                            // (its barriers: the list is there)
-    if (!few && by_p) {
-      t.over_waves(wave_sum64(mass), whole);
+      t.over_waves(wave_sum64(mass), whole);           // (its barriers as well)
       sum = (float)((double)whole / s.one);
     }
     // (by min-p alone the first top_k have to be there for top-p to take its share of them)
