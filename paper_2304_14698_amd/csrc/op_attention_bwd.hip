@@ -12,8 +12,13 @@ namespace {
 // dq, and of every row what the keys' gradients need besides: lse log2(e) and D. Rows and tiles as in the forward kernel.
 //
 // bf16: ds is a difference of nearly equal numbers, and rounding it once to the products' 8 bits would cost dq 1.8e-3 of its size, as much as dq's own rounding. So its rest, ds - bf16(ds), is a
-// second operand of the same product. D from the rounded out is off as well, by delta_i = sum_j ds_ij, as sum_j p_ij = 1: the keys' gradients take D + delta. Relative errors of two sequences of 4096
-// tokens with heads of 128: dq 2.7e-3 to 2.1e-3, dk 2.6e-3 to 2.3e-3, where a rounded output alone has 1.7e-3; 6 % of the backward pass. (The rest of ds for dk too: 2.0e-3, 9 % more; left out.)
+// second operand of the same product. D from the rounded out is off as well, by delta_i = sum_j ds_ij, as sum_j p_ij = 1: the keys' gradients take D + delta. For dq, whose sums run before delta is
+// known, a pass over the keys takes D = sum_j p_ij (dout_i . v_j) first, where a block has at most kExact of them: what the rounded out does to a row's dq falls as the number of
+// keys that it spreads over grows, and the pass would cost half of the kernel's time again.
+// Relative errors of dq, a result's rounding alone being 1.66e-3, without any of this, with the rests, and with the pass up to 512 keys, 1024 and all: two sequences of 4096 with heads of 128 2.69e-3,
+// 2.08e-3, 1.90e-3, 1.82e-3, 1.66e-3 in 1133, 1200, 1247, 1270 and 1544 us (with dk and dv); 16 episodes of 330 to 3300 with heads of 64 2.90e-3, 2.32e-3, 1.87e-3, 1.75e-3, 1.66e-3; sequences of
+// 1 to 24 up to 3.6e-3 without the pass. dk: 2.7e-3, and 2.3e-3 with D + delta (its own rests: 1.7e-3 and 9 % more; left out).
+constexpr int kExact = 512;
 template <typename T, int DP, int WAVES, int KT, bool MIXED>
 __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnArgs a) {
   using L = Tile<T, DP>;
@@ -44,11 +49,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
   const unsigned base = lds_address(lds);
   const float c = a.scale * kLog2e;
   constexpr bool REST = sizeof(T) == 2;
-  float more = 0.f;
-  auto pass = [&](auto safe, auto &dq, int db0) {
-    constexpr bool SAFE = decltype(safe)::value;
-    constexpr int NB = sizeof(dq) / sizeof(f32x16);
-    for (auto &x : dq) x = zero_acc();
+  // f(tiles of keys and values, first key, whether all rows of the wave see all of it, whether this lane's row sees its key n + 4 g)
+  auto over_keys = [&](auto f) {
     auto stage = [&](int t) {
       const int64_t j = (int64_t)t * KT;
       const unsigned to = base + t % BUFS * BYTES;
@@ -67,17 +69,47 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
       if (BUFS == 2 && t + 1 < tiles) stage(t + 1);
       const int j0 = t * KT;
       if (j0 >= w.any_sees) continue;
-      const bool whole = (!MIXED || j0 >= w.all_from) && j0 + KT <= w.all_see;
       const int from = w.from - j0 - 4 * g, mine = w.mine - j0 - 4 * g;
-      auto sees = [&](int n) { return n < mine && (!MIXED || n >= from); };
+      f(kt, vt, (!MIXED || j0 >= w.all_from) && j0 + KT <= w.all_see, [&](int n) { return n < mine && (!MIXED || n >= from); });
+    }
+  };
+  // scores, and dout . v, of 32 keys
+  auto products = [&](unsigned kt, unsigned vt, int kb, f32x16 &s, f32x16 &dp) {
+    s = zero_acc();
+    dp = zero_acc();
+#pragma unroll
+    for (int x = 0; x < L::SLABS; ++x) {
+      Operand<T>::mma(L::along(kt, 32 * kb, x, lane), q[x], s);
+      Operand<T>::mma(L::along(vt, 32 * kb, x, lane), dout[x], dp);
+    }
+  };
+  if (REST && keys <= kExact) {
+    float sum = 0.f;
+    over_keys([&](unsigned kt, unsigned vt, bool whole, auto sees) {
 #pragma unroll
       for (int kb = 0; kb < KT / 32; ++kb) {
-        f32x16 s = zero_acc(), dp = zero_acc();
+        f32x16 s, dp;
+        products(kt, vt, kb, s, dp);
 #pragma unroll
-        for (int x = 0; x < L::SLABS; ++x) {
-          Operand<T>::mma(L::along(kt, 32 * kb, x, lane), q[x], s);
-          Operand<T>::mma(L::along(vt, 32 * kb, x, lane), dout[x], dp);
+        for (int r = 0; r < 16; ++r) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * dp[r];
+          sum += whole || sees(32 * kb + acc_row(r, 0)) ? x : 0.f;
         }
+      }
+    });
+    delta = half_sum(sum);
+    __syncthreads();                                // (the last tiles are read)
+  }
+  float more = 0.f;
+  auto pass = [&](auto safe, auto &dq, int db0) {
+    constexpr bool SAFE = decltype(safe)::value;
+    constexpr int NB = sizeof(dq) / sizeof(f32x16);
+    for (auto &x : dq) x = zero_acc();
+    over_keys([&](unsigned kt, unsigned vt, bool whole, auto sees) {
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb) {
+        f32x16 s, dp;
+        products(kt, vt, kb, s, dp);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)) * (dp[r] - delta);
         if (!whole) {
@@ -111,7 +143,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
           }
         }
       }
-    }
+    });
     store_row<T>(head_at<T>(a.dq, w.row, w.head), w.there, a.dim, a.quads, dq, a.scale, g, db0);
   };
   f32x16 dq[L::BLOCKS];
