@@ -488,6 +488,8 @@ template <typename T, int DP, int WAVES, bool WHOLE>
 int launch(xrl_ctx *c, CacheArgs &a, const char *who) {
   constexpr int KT = WAVES == 1 || sizeof(T) == 4 ? 32 : 64, BM = 32 * WAVES, LDS = 4 * KT * DP * (int)sizeof(T) + WAVES * KT * 16 + 256;
   const int64_t most = ((int64_t)a.table_cols * a.page + KT - 1) / KT;
+  // (us, one new token each in fp32, 4 heads of 32, whole units and pieces: 64 sequences of up to 64 keys 13.5 and 15.6, 192 16.0 and 16.7, 256 20.4 and 15.7; 512 of 64 15.8 and 22.4, of 128
+  // 26 and 30, of 512 75 and 67)
   if (most <= 4) {
     a.blocks = (a.n_q * a.group / BM + a.seqs) * a.kv_heads;
     for (a.block0 = 0; a.block0 < a.blocks; a.block0 += kMaxBlocks)
@@ -511,8 +513,9 @@ int launch(xrl_ctx *c, CacheArgs &a, const char *who) {
 template <typename T, int DP>
 int launch_waves(xrl_ctx *c, CacheArgs &a, bool whole, const char *who) {
   if (!whole) return launch<T, DP, 1, false>(c, a, who);
-  // blocks of 128 columns where the sequences have that many on average
-  return a.n_q * a.group >= 128 * a.seqs ? launch<T, DP, 4, true>(c, a, who) : launch<T, DP, 1, true>(c, a, who);
+  // Blocks of 128 columns, whose four waves share the keys' tiles, where the sequences have half as many on average, else a wave by itself. us, 32768 cached tokens of 4 sequences, 8 heads of keys
+  // of 128 in bf16, a wave and four: 64 columns 70 and 54, 96 86 and 62, 192 140 and 85, 2036 1020 and 422; of 512 sequences with 4 columns and 500 keys of 64 60 and 96.
+  return a.n_q * a.group >= 64 * a.seqs ? launch<T, DP, 4, true>(c, a, who) : launch<T, DP, 1, true>(c, a, who);
 }
 template <typename T>
 int launch_dim(xrl_ctx *c, CacheArgs &a, bool whole, const char *who) {

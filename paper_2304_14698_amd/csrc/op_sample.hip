@@ -31,9 +31,15 @@ struct SampleArgs {
   float *part_stats;            // [rows][parts][2]: the largest logit, and the sum of exponentials relative to it
 };
 
-constexpr int kBins = 2048, kList = 1024, kListBins = 1024;         // of a histogram; entries that are ranked against each other
+// Bins of a histogram, entries that are ranked against each other, and bins of these: fewer for a row a wave, so that 16 of them fit on a compute unit.
+template <int WAVES>
+constexpr int kBins = WAVES == 1 ? 256 : 2048;
+template <int WAVES>
+constexpr int kList = WAVES == 1 ? 256 : 1024;
+template <int WAVES>
+constexpr int kListBins = kList<WAVES>;
 constexpr int kPart = 8192, kGroups = 256;          // entries of a part, and its groups: what one thread has of it
-constexpr float kBinsATurn = 64.f;                 // bins for a factor e in weight: 32 of these, the last bin has all below
+constexpr float kTurns = 32.f;                     // factors of e in weight that the bins cover; the last bin has all below
 
 // 2^t, t <= 0, in 64 bits: the integer part by the exponent, the rest in [-1/2, 1/2] by Taylor's sum of thirteen terms, whose rest is below 2^-52. Below 2^-100: of no weight.
 constexpr double kExp2[13] = {2.5678435993488206e-11, 4.4455382718708116e-10, 7.054911620801123e-09, 1.01780860092397e-07, 1.321548679014431e-06, 1.5252733804059841e-05, 0.0001540353039338161, 0.0013333558146428443, 0.009618129107628477, 0.05550410866482158, 0.24022650695910072, 0.6931471805599453, 1.0};   // ln(2)^k / k!, k = 12 .. 0
@@ -60,19 +66,20 @@ struct RowScale {
   float m;                      // largest logit
   double c;
   double one;                   // 2^S
-  float bins;
+  float bins, last;             // bins for a unit of the logits; the last one
 };
 __device__ __forceinline__ double weight_of(const RowScale &s, float x) { return exp2_64(((double)x - (double)s.m) * s.c); }
 // w as a multiple of 2^-S: in the sum with 2^52 the last place is 1.
 __device__ __forceinline__ unsigned long long whole_of(const RowScale &s, double w) {
   return (unsigned long long)__double_as_longlong(fma(w, s.one, 4503599627370496.0)) & 0xfffffffffffffull;
 }
+template <int WAVES>
 __device__ __forceinline__ RowScale scale_of(const SampleArgs &a, float m, int len) {
   const int bits = 32 - __clz(len - 1);
-  return {m, a.c, __longlong_as_double((long long)(1023 + 51 - (bits > 11 ? bits - 11 : 0)) << 52), a.inv_t * kBinsATurn};
+  return {m, a.c, __longlong_as_double((long long)(1023 + 51 - (bits > 11 ? bits - 11 : 0)) << 52), a.inv_t * (kBins<WAVES> / kTurns), (float)(kBins<WAVES> - 1)};
 }
 // Falls as x rises, so a bin is an interval of keys.
-__device__ __forceinline__ int bin_of(const RowScale &s, float x) { return (int)fminf((s.m - x) * s.bins, (float)(kBins - 1)); }
+__device__ __forceinline__ int bin_of(const RowScale &s, float x) { return (int)fminf((s.m - x) * s.bins, s.last); }
 
 typedef unsigned long long u64;
 __device__ __forceinline__ u64 wave_sum64(u64 x) {
@@ -97,11 +104,11 @@ struct Entry {
 
 template <int WAVES>
 struct Shared {
-  u64 mass[kBins];
-  unsigned count[kBins];
-  u64 list_mass[kListBins];     // bins over the list
-  unsigned list_count[kListBins];
-  Entry list[kList];
+  u64 mass[kBins<WAVES>];
+  unsigned count[kBins<WAVES>];
+  u64 list_mass[kListBins<WAVES>];     // bins over the list
+  unsigned list_count[kListBins<WAVES>];
+  Entry list[kList<WAVES>];
   int members[64], few;
   u64 sums[WAVES];
   float floats[WAVES];
@@ -260,18 +267,18 @@ struct Sampler {
         lo = min(lo, key);
         hi = max(hi, key);
         const int at = atomicAdd(&sh.n, 1);
-        if (at < kList) sh.list[at] = {whole_of(s, weight_of(s, xj)), key, col + j};
+        if (at < kList<WAVES>) sh.list[at] = {whole_of(s, weight_of(s, xj)), key, col + j};
       });
     });
     __syncthreads();
     n = sh.n;
-    while (n > kList) {
+    while (n > kList<WAVES>) {
       // too many: bins over their keys
       lo = block_min(lo);
       hi = ~block_min(~hi);
       if (lo == hi) return cut_of_equal(by_mass, limit, before, in_front, lo);
       int shift = 0;
-      while ((hi - lo) >> shift >= kBins) ++shift;
+      while ((hi - lo) >> shift >= kBins<WAVES>) ++shift;
       clear_bins(sh.count, sh.mass);
       spoiled = true;
       for_pieces<T>(row, odd, begin, end, lane, [&](int, const float *x) {
@@ -301,7 +308,7 @@ struct Sampler {
           lo = min(lo, key);
           hi = max(hi, key);
           const int at = atomicAdd(&sh.n, 1);
-          if (at < kList) sh.list[at] = {whole_of(s, weight_of(s, xj)), key, col + j};
+          if (at < kList<WAVES>) sh.list[at] = {whole_of(s, weight_of(s, xj)), key, col + j};
         });
       });
       __syncthreads();
@@ -316,7 +323,7 @@ struct Sampler {
   // One more entry of the list, if there is room: sh.n counts all.
   __device__ __forceinline__ void push(float x, int id, double w) {
     const int at = atomicAdd(&sh.n, 1);
-    if (at < kList) sh.list[at] = {whole_of(s, w) | (w >= a.min_p ? 0 : kBelow), key_of(x), id};
+    if (at < kList<WAVES>) sh.list[at] = {whole_of(s, w) | (w >= a.min_p ? 0 : kBelow), key_of(x), id};
   }
 
   // Of those of the list's n entries that count(i), in the order of the cuts (by_index: of their indices), the one at which the sum of counts (by_mass: weights) reaches `limit`: its key and
@@ -324,7 +331,7 @@ struct Sampler {
   // few are left, which are ranked against each other. (Ranking all against all took 230 us for 200 to 700 entries.)
   template <typename Counts>
   __device__ __forceinline__ u64 select(int n, bool by_mass, bool by_index, u64 limit, Counts counts) {
-    constexpr int EACH = kList / (WAVES * 64);
+    constexpr int EACH = kList<WAVES> / (WAVES * 64);
     Entry e[EACH];
     u64 place[EACH];
     bool in[EACH];
@@ -344,8 +351,9 @@ struct Sampler {
     least = block_min(least);
     most = ~block_min(~most);
     u64 lo = by_index ? least : (u64)least << 32, hi = by_index ? most : (u64)most << 32 | 0xffffffffu, before = 0, mass = 0;
-    for (int step = 0; step < 7; ++step) {            // (64 bits by ten each time)
-      const int bits = 64 - __clzll((long long)(hi - lo)), shift = bits > 10 ? bits - 10 : 0;
+    constexpr int BITS = __builtin_ctz(kListBins<WAVES>);
+    for (int step = 0; step < (63 + BITS) / BITS; ++step) {   // (64 bits by BITS each time)
+      const int bits = 64 - __clzll((long long)(hi - lo)), shift = bits > BITS ? bits - BITS : 0;
       clear_bins(sh.list_count, sh.list_mass);
 #pragma unroll
       for (int q = 0; q < EACH; ++q) {
@@ -395,7 +403,7 @@ struct Sampler {
   // The list's n entries are the row's n first in the order of the cuts, and all that can be kept are among them. sum: of all weights that may be chosen (without top-k, top-p
   // takes its share of `whole`).
   __device__ __forceinline__ void draw_from_list(int64_t r, float u, bool by_k, bool by_p, u64 whole, float sum) {
-    constexpr int EACH = kList / (WAVES * 64);
+    constexpr int EACH = kList<WAVES> / (WAVES * 64);
     const int n = sh.n;
     Cut cut = {0, 0x7fffffff};
     auto all_of = [](int) { return true; };
@@ -450,14 +458,14 @@ struct Sampler {
     constexpr int PIECES = kPart / (kGroups * VEC);
     const bool by_k = a.top_k > 0;
     const int groups = a.parts * kGroups;
-    unsigned *chosen = (unsigned *)sh.mass;            // [kList]
+    unsigned *chosen = (unsigned *)sh.mass;            // [kList<WAVES>]
     clear_bins(sh.count, sh.mass);
     if (threadIdx.x == 0) {
       sh.n = 0;
       sh.few = 0;
-      sh.bin = kBins - 1;
+      sh.bin = kBins<WAVES> - 1;
     }
-    int bin = kBins - 1;
+    int bin = kBins<WAVES> - 1;
     if (by_k) {
       for (int i = threadIdx.x; i < groups; i += WAVES * 64)
         if (tops[i] > -INFINITY) atomicAdd(&sh.count[bin_of(s, tops[i])], 1u);
@@ -469,11 +477,11 @@ struct Sampler {
     for (int i = threadIdx.x; i < groups; i += WAVES * 64) {
       if (tops[i] == -INFINITY || bin_of(s, tops[i]) > bin || (!by_k && !(weight_of(s, tops[i]) >= a.min_p))) continue;
       const int at = atomicAdd(&sh.few, 1);
-      if (at < kList) chosen[at] = i;
+      if (at < kList<WAVES>) chosen[at] = i;
     }
     __syncthreads();
     const int n = sh.few;
-    if (n > kList) return false;
+    if (n > kList<WAVES>) return false;
     for (int i = threadIdx.x; i < n * PIECES; i += WAVES * 64) {
       const int g = chosen[i / PIECES], col = g / kGroups * kPart + (i % PIECES * kGroups + g % kGroups) * VEC;
       float x[VEC];
@@ -485,7 +493,7 @@ struct Sampler {
       });
     }
     __syncthreads();
-    if (sh.n > kList) return false;
+    if (sh.n > kList<WAVES>) return false;
     draw_from_list(r, u, by_k, a.top_p < 1.0, 0, sum);
     return true;
   }
@@ -644,7 +652,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_k
       }
       return;
     }
-    t.s = scale_of(a, m, row.len);
+    t.s = scale_of<WAVES>(a, m, row.len);
     if (t.draw_from_groups(r, u, tops, sum)) return;
     __syncthreads();
   }
@@ -671,7 +679,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_k
     }
     return;
   }
-  t.s = scale_of(a, m, row.len);
+  t.s = scale_of<WAVES>(a, m, row.len);
   const RowScale s = t.s;
   Cut cut = {0, 0x7fffffff};
   const bool by_k = a.top_k > 0 && a.top_k < row.len, by_p = a.top_p < 1.0;
@@ -680,12 +688,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_k
   // the top_k-th of these.
   const bool few = by_k && a.top_k <= WAVES * 16;
   if (few || a.min_p > 0.0) {
-    int bin = kBins - 1;
+    int bin = kBins<WAVES> - 1;
     t.clear_bins(sh.count, sh.mass);
     if (threadIdx.x == 0) sh.n = 0;
     if (few) {
       if (mine > -INFINITY) atomicAdd(&sh.count[bin_of(s, mine)], 1u);
-      if (threadIdx.x == 0) sh.bin = kBins - 1;
+      if (threadIdx.x == 0) sh.bin = kBins<WAVES> - 1;
       __syncthreads();
       t.find_bin(sh.count, sh.mass, false, a.top_k);                      // (where fewer threads have an entry the last bin stays)
       bin = sh.bin;
@@ -729,7 +737,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_k
       sum = (float)((double)whole / s.one);
     }
     // (by min-p alone the first top_k have to be there for top-p to take its share of them)
-    if (sh.n <= kList && (few || !(by_k && by_p) || sh.n >= a.top_k)) {
+    if (sh.n <= kList<WAVES> && (few || !(by_k && by_p) || sh.n >= a.top_k)) {
       t.draw_from_list(r, u, by_k, by_p, whole, sum);
       return;
     }
@@ -750,11 +758,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 3 : 4) void token_sample_k
   };
   if (by_k || by_p) {
     histogram(by_k);
-    if (by_p) whole = t.mass_before(sh.mass, kBins);
+    if (by_p) whole = t.mass_before(sh.mass, kBins<WAVES>);
     u64 share = whole;                                 // what top-p takes its part of
     if (by_k) {
       u64 n = 0, all;
-      for (int i = threadIdx.x; i < kBins; i += WAVES * 64) n += sh.count[i];
+      for (int i = threadIdx.x; i < kBins<WAVES>; i += WAVES * 64) n += sh.count[i];
       t.over_waves(wave_sum64(n), all);
       if ((u64)a.top_k < all) {
         cut = t.cut_at(false, a.top_k);
@@ -840,7 +848,8 @@ void launch(const xrl_ctx *c, SampleArgs &a, int waves) {
   for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += most) {
     const dim3 grid((unsigned)std::min(a.n_rows - a.row0, most));
     if (a.parts) token_sample_groups_kernel<T><<<dim3((unsigned)(grid.x * a.parts)), dim3(256), 0, op_stream(c)>>>(a);
-    if (waves == 4) token_sample_kernel<T, 4><<<grid, dim3(256), 0, op_stream(c)>>>(a);
+    if (waves == 1) token_sample_kernel<T, 1><<<grid, dim3(64), 0, op_stream(c)>>>(a);
+    else if (waves == 4) token_sample_kernel<T, 4><<<grid, dim3(256), 0, op_stream(c)>>>(a);
     else if (waves == 8) token_sample_kernel<T, 8><<<grid, dim3(512), 0, op_stream(c)>>>(a);
     else token_sample_kernel<T, 16><<<grid, dim3(1024), 0, op_stream(c)>>>(a);
   }
@@ -862,8 +871,13 @@ extern "C" int xrl_token_sample(xrl_ctx *c, const xrl_logits_desc *logits, const
   a.top_k = how->top_k; a.top_p = how->top_p; a.min_p = how->min_p;
   a.uniforms = d_uniforms; a.ids = d_ids; a.logp = d_logp;
   const int64_t cols = a.row_ptr ? a.n_cols / a.n_rows : a.n_cols;
-  const int waves = cols <= 4096 ? 4 : a.n_rows > op_compute_units(c) ? 8 : 16;
-  // Long rows of which few entries can be kept: by groups.
+  // A wave a row where rows are short, or so many that they fill the chip; else a block of as many waves as pay for its barriers. us, fp32, no filter and the best 100 with top-p and min-p: 4000 x 64 by
+  // a wave 17 and 20, by four 58 and 80; 4000 x 2000 63 and 104, 71 and 202; 32 x 500 10.8 and 27, 10.5 and 23. bf16, top-p alone, by 4, 8 and 16 waves: 200 x 4000 24, 21, 26; 2048 x 16000 224, 169,
+  // 279; 200 x 32003 100, 59, 57; 8 x 128256 336, 175, 133.
+  const bool many = a.n_rows > 2 * op_compute_units(c);
+  const int waves = cols <= 256 || (many && cols <= 2048) ? 1 : cols <= 2048 ? 4 : a.n_rows > op_compute_units(c) || cols <= 16384 ? 8 : 16;
+  // Long rows of which few entries can be kept: by groups. us, with top-p, without and with: the best 50 of 8 x 128256 51 and 35, of 2048 x 32003 140 and 118; 20 of 512 x 32003 38 and 35, of
+  // 8 x 16384 28 and 30.
   const int64_t parts = (cols + kPart - 1) / kPart;
   if (!a.row_ptr && cols > kPart && (a.top_k > 0 ? a.top_k * 16 <= parts * kGroups : a.top_p == 1.0 && a.min_p > 0.0) && parts <= 1024) {
     const size_t tops = op_align((size_t)a.n_rows * parts * kGroups * 4);

@@ -9,6 +9,7 @@ from test_gpu_token_sample import check, draw
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
+INF = math.inf
 HEADS, KV, DIM, VOCAB, PAGE = 6, 2, 40, 700, 7
 
 
@@ -321,3 +322,46 @@ def test_drawing_of_more_rows_than_compute_units():
         check(enc, x, u, top_k=40, top_p=0.9)
         check(enc, x, u, temperature=0.8)
     enc.close()
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("cols", [257, 1025, 2043])
+@pytest.mark.parametrize("how", [dict(), dict(top_k=3), dict(top_k=700), dict(top_p=0.6), dict(min_p=0.02), dict(top_k=300, top_p=0.9, min_p=0.01), dict(top_k=16, top_p=0.5)])
+def test_drawing_of_many_middling_rows(type, cols, how):
+    """So many rows that each has one wave: random ones, ties, masked ones, what is not finite."""
+    import torch
+    enc = encoder()
+    rows = 530
+    x, u, g = draw(61 + cols, rows, cols, type)
+    mask = torch.rand(rows, cols, generator=g, device="cuda") < 0.7
+    x[3] = 0.5
+    x[4, :cols // 2] = 2.0
+    x[4, cols // 2:] = -INF
+    x[5] = -INF
+    x[6, cols - 1] = math.nan
+    x[7, 0] = INF
+    mask[8] = False
+    mask[9] = False
+    mask[9, cols - 1] = True
+    keep = torch.cat([torch.arange(40, device="cuda"), torch.arange(rows - 20, rows, device="cuda")])
+    for m in (None, mask.to(torch.uint8)):
+        got = enc.token_sample(x, u, mask=m, **how)
+        check_rows(enc, x, u, m, got, keep, how)
+    enc.close()
+
+
+def check_rows(enc, x, u, mask, got, keep, how):
+    """Some rows of a call against the oracle."""
+    import torch
+    from test_gpu_token_sample import one_row
+    torch.cuda.synchronize()
+    kw = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) | how
+    for r in keep.tolist():
+        X = x[r].double().cpu().numpy()
+        id, lp, _ = one_row(X, None if mask is None else mask[r].cpu().numpy(), float(u[r]), kw["top_k"], kw["top_p"], kw["min_p"], kw["temperature"])
+        assert int(got["ids"][r]) == id, r
+        g, n = float(got["logp"][r]), max(2, len(X))
+        if math.isfinite(lp):
+            assert abs(g - lp) <= (3 * (n / 64 + 8) + 64 + 4 * math.log2(n)) * U + 6 * U * (abs(lp) + math.log(n)), r
+        else:
+            assert g == lp or (math.isnan(lp) and math.isnan(g)), r
