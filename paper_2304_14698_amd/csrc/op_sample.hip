@@ -7,6 +7,9 @@
 // A row's cut (the smallest kept entry, by falling logit, then rising index) comes from a histogram over the distance from the largest logit, of counts for top-k and of
 // weights for top-p, and then from the entries of one bin, ranked against each other. Both cuts are monotone in the same order, so that one entry describes
 // what is kept.
+//
+// Bound by instructions for many long rows, each entry's exponential in 64 bits first (2048 x 32003 in bf16 with top-p and min-p: 137 us, 58 vector instructions for 64 entries, where reading them takes
+// 25), and by a row's chain of barriers and memory round trips for few (8 x 128256, the best 50: 4 + 29 us; 32 rows of 65 slots: 9).
 #include "logits_rows.hip.h"
 
 #include <algorithm>
