@@ -46,6 +46,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 1 || DP * sizeof(T) > 256 ? 1 
     };
     if (tiles > 0) stage(0);
     for (int t = 0; t < tiles; ++t) {
+      if (MIXED && !__ballot(w.from < t * KT + KT && w.mine > t * KT)) continue;   // (a sequence without queries)
       const unsigned kt = base + t % BUFS * BYTES, vt = kt + BUFS * BYTES;
       if (BUFS == 1 && t > 0) {
         __syncthreads();

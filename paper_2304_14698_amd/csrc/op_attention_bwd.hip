@@ -62,6 +62,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void attention_dq_kernel(const AttnA
     };
     if (tiles > 0) stage(0);
     for (int t = 0; t < tiles; ++t) {
+      if (MIXED && !__ballot(w.from < t * KT + KT && w.mine > t * KT)) continue;   // (a sequence without queries)
       const unsigned kt = base + t % BUFS * BYTES, vt = kt + BUFS * BYTES;
       if (BUFS == 1 && t > 0) {
         __syncthreads();
@@ -280,18 +281,20 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
     if (tiles > 0) stage(next_e, next_i, 0);
     for (int t = 0; t < share; ++t) {
       const unsigned qt = base + t % BUFS * BYTES, dt = qt + BUFS * BYTES, st = stats + t % BUFS * 512;
-      if (BUFS == 1 && t > 0) {
-        __syncthreads();
-        stage(next_e, next_i, 0);
-      }
-      wait_direct_loads();
-      __syncthreads();
+      const int e = next_e;
       i = next_i;
       next_i += QT;
       if (next_i >= len_q) {
         next_i = begin;
         ++next_e;
       }
+      if (MIXED && !__ballot(w.mine < i + QT && w.end > i)) continue;   // (a sequence without keys)
+      if (BUFS == 1 && t > 0) {
+        __syncthreads();
+        stage(e, i, 0);
+      }
+      wait_direct_loads();
+      __syncthreads();
       if (BUFS == 2 && t + 1 < tiles) stage(next_e, next_i, (t + 1) & 1);
       if (t >= tiles || i + QT <= w.any_sees) continue;
       const bool whole = i >= w.all_see && i + QT <= (MIXED ? w.all_end : len_q);

@@ -63,3 +63,14 @@ def test_neighbours_that_are_not_finite(enc, type, causal, what):  # noqa: F811
     torch.cuda.synchronize()
     for a, b, p in zip(*res, (qp, qp, qp, kp, kp)):
         assert torch.equal(a[:p[2]], b[:p[2]]) and torch.equal(a[p[3]:], b[p[3]:])
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("far", ["keys", "queries"])
+def test_long_sequences_without_the_other_side(enc, type, causal, far):  # noqa: F811
+    """Keys that no query has, or queries without keys, lie between the rows of a tile, whole tiles of them."""
+    few, many = [3, 0, 2] * 8, [4, 300, 6] * 8
+    nq, nk = (few, many) if far == "keys" else (many, few)
+    q, k, v, d = tensors(9, sum(nq), sum(nk), 4, 2, 32, type)
+    check(enc, q, k, v, d, ptr(nq), ptr(nk), causal)
