@@ -757,9 +757,9 @@ class Encoder:
         pages, page, kv, dim = k_cache.shape
         if q_ptr.numel() < 1 or table.dim() != 2 or table.get_device() != self._index or table.dtype != t.int32 or table.shape[0] != q_ptr.numel() - 1:
             raise ValueError("table: a matrix of int32 on the GPU with a row for each sequence of q_ptr is needed")
-        if table.stride(1) != 1 and table.shape[1] > 1:
-            raise ValueError("table: contiguous rows are needed")
         seqs, cols = table.shape
+        if (table.stride(1) != 1 and cols > 1) or (table.stride(0) < cols and seqs > 1):
+            raise ValueError("table: contiguous rows that lie apart are needed")
         d = CacheDesc(seqs, n, pages, max(cols, table.stride(0)), self._here(q_ptr, "q_ptr", t.int32, seqs + 1),
                       self._here(lengths, "lengths", t.int32, seqs), table.data_ptr(), cols, page, heads or kv, kv, dim, self._type(k_cache, "k_cache"))
         return d, *(Pages(x.data_ptr(), *x.stride()[:3]) for x in (k_cache, v_cache))

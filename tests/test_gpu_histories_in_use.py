@@ -263,6 +263,25 @@ def test_a_workspace_that_would_have_to_grow_is_refused_in_a_capture():
         enc.close()
 
 
+def test_tables_whose_rows_share_memory_are_refused():
+    """A row of a table for all sequences (stride 0), and rows that overlap: the library takes rows at least their length apart."""
+    import torch
+    enc, s = encoder(), state(13, torch.float32)
+    wide = s["table"].contiguous()
+    for bad in (wide[:1].expand(5, -1), wide.as_strided((5, wide.shape[1]), (wide.shape[1] - 1, 1)), wide.T.contiguous().T):
+        how = dict(table=bad, lengths=s["lengths"])
+        with pytest.raises(ValueError, match="table"):
+            enc.cache_attention(s["q1"], s["ptr1"], s["kc"], s["vc"], **how)
+        with pytest.raises(ValueError, match="table"):
+            enc.cache_write(s["k1"], s["v1"], s["ptr1"], s["kc"], s["vc"], **how)
+    apart = torch.full((5, wide.shape[1] + 3), -1, dtype=torch.int32, device="cuda")
+    apart[:, :wide.shape[1]] = wide
+    a, b = (enc.cache_attention(s["q1"], s["ptr1"], s["kc"], s["vc"], table=t, lengths=s["lengths"]) for t in (wide, apart[:, :wide.shape[1]]))
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+    enc.close()
+
+
 @pytest.mark.parametrize("type", ["fp32", "bf16"])
 @pytest.mark.parametrize("how", [dict(), dict(top_k=3), dict(top_k=40, top_p=0.8), dict(min_p=0.1), dict(top_p=0.7), dict(top_k=9, min_p=0.2)])
 @pytest.mark.parametrize("masked", ["own", "shared", "odd"])
