@@ -274,7 +274,8 @@ __global__ __launch_bounds__(HALVES * WAVES * 64, HALVES) void attention_dkv_ker
     for (auto &x : dv) x = zero_acc();
     const int e0 = per_head > 0 ? first / per_head : 0;
     int next_e = e0, next_i = begin + (first - e0 * per_head) * QT, i = next_i;
-    if constexpr (IN_LDS) {
+    // (without queries nothing is read, and no step below would wait for these loads before the sums go to the places that they write)
+    if (IN_LDS && share > 0) {
       stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.k, w.key0 + j0, w.head), w.keys - j0, a.k.stride, a.dim_in, keys, half * WAVES + wave, lane);
       if (DK) stage_tile<T, DP, BM, HALVES * WAVES>(head_at<T>(a.v, w.key0 + j0, w.head), w.keys - j0, a.v.stride, a.dim_in, values, half * WAVES + wave, lane);
     }
