@@ -127,7 +127,9 @@ struct Places {
   int64_t k, v;
 };
 
-// KT rows of both caches into two tiles. WHOLE: in pieces of 16 bytes past the registers, there behind wait_direct_loads() and a barrier; else element by element.
+// KT rows of both caches into two tiles, zeros behind dim (0 times an infinity would make a score no number). WHOLE: in pieces of 16 bytes past the registers, there behind
+// wait_direct_loads() and a barrier; else element by element.
+__device__ const u32x4 kZeroPiece = {0, 0, 0, 0};
 template <typename T, int DP, int KT, int WAVES, bool WHOLE>
 __device__ __forceinline__ void stage_pages(const T *k, const T *v, unsigned places, int dim, unsigned kt, unsigned vt, int wave, int lane) {
   using L = Tile<T, DP>;
@@ -140,10 +142,10 @@ __device__ __forceinline__ void stage_pages(const T *k, const T *v, unsigned pla
     typedef int64_t i64x2 __attribute__((ext_vector_type(2)));
     const i64x2 at = *lds_at<const i64x2>(places + row * 16);
     if constexpr (WHOLE) {
-      // (pieces behind dim: any that is there; q has zeros for them, and results there are not stored)
-      const int d = piece * L::V < dim ? piece * L::V : 0;
-      lds_direct_load16(k + at[0] + d, __builtin_amdgcn_readfirstlane(kt + n * 1024));
-      lds_direct_load16(v + at[1] + d, __builtin_amdgcn_readfirstlane(vt + n * 1024));
+      const int d = piece * L::V;
+      const T *zeros = (const T *)&kZeroPiece;
+      lds_direct_load16(d < dim ? k + at[0] + d : zeros, __builtin_amdgcn_readfirstlane(kt + n * 1024));
+      lds_direct_load16(d < dim ? v + at[1] + d : zeros, __builtin_amdgcn_readfirstlane(vt + n * 1024));
     } else {
       typename L::vec x, y;
 #pragma unroll
