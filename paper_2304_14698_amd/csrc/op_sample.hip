@@ -882,7 +882,7 @@ extern "C" int xrl_token_sample(xrl_ctx *c, const xrl_logits_desc *logits, const
   // Long rows of which few entries can be kept: by groups. us, with top-p, without and with: the best 50 of 8 x 128256 51 and 35, of 2048 x 32003 140 and 118; 20 of 512 x 32003 38 and 35, of
   // 8 x 16384 28 and 30.
   const int64_t parts = (cols + kPart - 1) / kPart;
-  if (!a.row_ptr && cols > kPart && (a.top_k > 0 ? a.top_k * 16 <= parts * kGroups : a.top_p == 1.0 && a.min_p > 0.0) && parts <= 1024) {
+  if (!a.row_ptr && cols > kPart && (a.top_k > 0 ? (int64_t)a.top_k * 16 <= parts * kGroups : a.top_p == 1.0 && a.min_p > 0.0) && parts <= 1024) {
     const size_t tops = op_align((size_t)a.n_rows * parts * kGroups * 4);
     char *ws = nullptr;
     if (int rc = op_workspace(c, tops + (size_t)a.n_rows * parts * 8, &ws, who)) return rc;
