@@ -602,6 +602,7 @@ class Encoder:
         if out is None:
             ids, logp = self._made(((n,), t.int32), ((n,), f))
             out = dict(ids=ids, logp=logp)
+        top_k = max(-1, min(top_k, 2 ** 31 - 1))           # (what passes 32 bits would be read without its upper ones)
         _check(self.lib.xrl_token_sample(self.handle, C.byref(d), C.byref(SampleDesc(top_k, top_p, min_p)), self._flat(uniforms, "uniforms", f, n),
                                          self._flat(out["ids"], "ids", t.int32, n), self._flat(out["logp"], "logp", f, n)))
         return out

@@ -45,3 +45,16 @@ def test_no_workspace_is_taken_for_them(k):
             stream.synchronize()
             assert torch.equal(out["ids"], want["ids"]) and torch.equal(out["logp"], want["logp"])
         enc.close()
+
+
+def test_numbers_past_32_bits(enc):  # noqa: F811
+    """Are not read without their upper bits: no limit, and refused below 0."""
+    import paper_2304_14698_amd as xrl
+    x, u, _ = draw(7, 8, 500, "fp32")
+    want = check(enc, x, u)
+    for k in (1 << 31, (1 << 32) + 1, (1 << 40) + 3):
+        assert np.array_equal(check(enc, x, u, top_k=k), want), k
+    for k in (-(1 << 31), 1 - (1 << 32), -(1 << 40)):
+        with pytest.raises(xrl.XrlError) as e:
+            enc.token_sample(x, u, top_k=k)
+        assert e.value.code == xrl.ERR["VALUE"]
