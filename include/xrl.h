@@ -393,8 +393,8 @@ int xrl_token_logp_backward(xrl_ctx *ctx, const xrl_logits_desc *logits, const i
  * temperature and w = exp(x - largest x): in the order of falling logits, the lowest index first among equals, the first top_k (0: all); of these the ones in front of
  * which less than top_p of their weight lies (1: all); of these the ones with w >= min_p. The first of them by index up to whose end more than d_uniforms[row] of their weight
  * lies is drawn: d_ids [n_rows] its index inside the row, d_logp [n_rows] its log-probability among all entries that may be chosen, as xrl_token_logp gives it for
- * the same temperature. Weights and their sums are exact to some 2^-45 of the largest weight (rows of 2^17 entries; 2^-51 up to 2^11). A random number outside [0, 1) counts as
- * the nearest inside (NaN: 0). A row with nothing to choose: -1 and -inf; one with a NaN or +inf that may be chosen: -1 and NaN.
+ * the same temperature. A weight is held to within 1.5 2^-S of the largest one, S = 51 for rows of up to 2^11 entries and one less for every doubling (45 for 2^17); a sum of n of them
+ * is off by at most n times that, whatever their order, and a border (of top_p's share, of the random number's place) by 2 n 2^-S. A random number outside [0, 1) counts as the nearest inside (NaN: 0). A row with nothing to choose: -1 and -inf; one with a NaN or +inf that may be chosen: -1 and NaN.
  * Errors: NULL, SHAPE, UNSUPPORTED (type), VALUE (temperature; top_k < 0, top_p outside (0, 1], min_p outside [0, 1]), HIP. */
 typedef struct xrl_sample_desc {
   int32_t top_k;

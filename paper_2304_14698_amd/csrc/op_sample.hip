@@ -1,8 +1,10 @@
 // One entry drawn from every row of logits by a given random number, after temperature, top-k, top-p and min-p.
 //
 // Weights w = exp((x - largest) / temperature) are computed in 64 bits and held as whole multiples of 2^-S, S = 51 for rows of up to 2048 entries and one less for every
-// doubling: sums of them are exact in 64 bits whatever their order, so what is kept and drawn does not depend on how a row is shared out, and differs from exact
-// arithmetic only where a border lies within some 2^-S of a sum. (fp32 sums would draw another entry in one row of a few hundred.)
+// doubling: adding them up is exact in 64 bits whatever their order, so what is kept and drawn does not depend on how a row is shared out. A weight is off by at most 1.5 2^-S: 1/2 for the multiple, 0.38
+// for the rest of the exponential's sum and the rest for the roundings of its argument and terms (1.1 is the most of 4 10^7 on the host). A sum of n of them is off by n times that, and with the
+// rounding of its product with top_p or the random number what is drawn differs from exact arithmetic only where a border lies within 2 n 2^-S of a sum. (fp32 sums would draw another entry
+// in one row of a few hundred.)
 //
 // A row's cut (the smallest kept entry, by falling logit, then rising index) comes from a histogram over the distance from the largest logit, of counts for top-k and of
 // weights for top-p, and then from the entries of one bin, ranked against each other. Both cuts are monotone in the same order, so that one entry describes
