@@ -453,7 +453,8 @@ typedef struct xrl_rotary_desc {
 int xrl_head_rotary(xrl_ctx *ctx, const xrl_rotary_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *q_out, const xrl_heads *k_out);
 
 /* xrl_head_rotary_backward: from the inputs (not read, and may be NULL, where there is no weight) and the gradients to the results, dq_out and dk_out, the gradients dq and dk,
- * written (they may lie in dq_out's and dk_out's own memory), and d_dq_weight, d_dk_weight [dim] fp32, added to in a fixed order (NULL: not wanted).
+ * written (they may lie in dq_out's and dk_out's own memory), and d_dq_weight, d_dk_weight [dim] fp32, added to in a fixed order (NULL: not wanted; a weight that both share
+ * may have one vector: q's sum is added first).
  * Errors: as above, OOM. */
 int xrl_head_rotary_backward(xrl_ctx *ctx, const xrl_rotary_desc *desc, const xrl_heads *q, const xrl_heads *k, const xrl_heads *dq_out, const xrl_heads *dk_out,
                              const xrl_heads *dq, const xrl_heads *dk, float *d_dq_weight, float *d_dk_weight);

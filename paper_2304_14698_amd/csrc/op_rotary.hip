@@ -532,6 +532,8 @@ int xrl_head_rotary_backward(xrl_ctx *c, const xrl_rotary_desc *d, const xrl_hea
   if (a.n == 0 || a.heads == 0) return XRL_OK;
   a.dweight[0] = d->d_q_weight ? d_dq_weight : nullptr;
   a.dweight[1] = d->d_k_weight ? d_dk_weight : nullptr;
+  if (a.dweight[0] && a.dweight[1] && a.dweight[0] != a.dweight[1] && a.dweight[0] < a.dweight[1] + a.dim && a.dweight[1] < a.dweight[0] + a.dim)
+    return fail(XRL_ERR_SHAPE, "%s: the weights' gradients lie in a part of each other", who);
   const int lanes = lanes_of(a, v, aligned);
   a.tokens = rows_of_block(c, a.n);
   a.partials = (int)std::min<int64_t>((a.n + a.tokens - 1) / a.tokens, 4 * (int64_t)op_compute_units(c));
@@ -541,7 +543,12 @@ int xrl_head_rotary_backward(xrl_ctx *c, const xrl_rotary_desc *d, const xrl_hea
     a.partial = (float *)ws;
   }
   es == 2 ? launch_lanes<bf16_t>(c, a, aligned, lanes, true) : launch_lanes<float>(c, a, aligned, lanes, true);
-  if (a.partial) head_rotary_weights_kernel<<<dim3((unsigned)((2 * a.dim + 15) / 16)), dim3(1024), 0, op_stream(c)>>>(a);
+  const bool shared = a.dweight[0] && a.dweight[0] == a.dweight[1];   // one vector for both: in turn, as each entry is read and written
+  for (int k = 0; a.partial && k <= (shared ? 1 : 0); ++k) {
+    RotaryArgs w = a;
+    if (shared) w.dweight[1 - k] = nullptr;
+    head_rotary_weights_kernel<<<dim3((unsigned)((2 * a.dim + 15) / 16)), dim3(1024), 0, op_stream(c)>>>(w);
+  }
   OP_TRY(hipGetLastError());
   return XRL_OK;
 }
