@@ -2,7 +2,8 @@
 //
 // A tile's row is cut into pieces of 16 bytes, and piece p of row r lies at place p ^ swizzle(r). Read along rows (the contraction runs over columns),
 // eight neighbouring lanes read one piece each of eight rows; read across rows (it runs over the rows), sixteen lanes read 32 bytes each of four rows.
-// The swizzle gives both eight places in different banks.
+// The swizzle spreads both over eight places, 128 bytes; the LDS has banks for 256, and reads still meet in them: with heads of 128 in bf16 conflicts are 46 to 50 % of the LDS's busy
+// cycles in the kernels of packed attention, and 38 % in the cache's for single tokens.
 #pragma once
 #include "op_common.h"
 

@@ -4,8 +4,8 @@
 // of which computes the scores anew: one has a query a lane and sums over keys, the other a key a lane and sums over queries. That is seven products where one kernel
 // would do with five, but no sum is shared by blocks: no float atomics, the same bits from run to run. (bf16: an eighth for the rests of ds, see below.)
 //
-// Bound by the matrix cores and what feeds them from LDS, each score tile's exponentials between. Two causal sequences of 4096, 32 heads of 128 in bf16: dq 553 to 595 us, dk and dv 672 to
-// 728, that is 830 to 900 TFLOP/s of the eight products, the matrix cores busy for 52 and 40 % of the cycles, the LDS for 39 and 65; 16 sequences of 330 to 3300 rows, 16 heads of 64: 169 and 241. p and ds are rounded to bf16 as factors of dv and dk, half a step of 2^-8 each.
+// Bound by the matrix cores and what feeds them from LDS, each score tile's exponentials between. Two causal sequences of 4096, 32 heads of 128 in bf16: dq 553 to 602 us, dk and dv 672 to
+// 736, that is 820 to 900 TFLOP/s of the eight products, the matrix cores busy for 52 and 40 % of the cycles, the LDS for 39 and 65; 16 sequences of 330 to 3300 rows, 16 heads of 64: 169 to 179 and 241 to 256. p and ds are rounded to bf16 as factors of dv and dk, half a step of 2^-8 each.
 #include "attn_packed.hip.h"
 
 #include <type_traits>

@@ -7,7 +7,8 @@
 // cache line that a neighbour has just read. A block has up to eight tokens, computes their
 // cosines and sines, of angles in 64 bits, once, while its first rows are on their way, and goes over all their heads with the next rows' loads ahead.
 //
-// 16384 rows of 40 heads of 128 in bf16, half of each rotated: forward 88 us, 3.8 TB/s; backward 102 and 5 for the weights' sums, 4.7 TB/s. (A large copy reaches 5.18.) 32 rows: 8.3.
+// 16384 rows of 40 heads of 128 in bf16, half of each rotated: forward 87 to 91 us, 3.8 TB/s; backward 101 to 105 and 5 for the weights' sums, 4.7 TB/s; in fp32 166, and 202 with the sums. (A large copy
+// reaches 5.18.) 32 rows: 8.3. Rows at odd addresses, one column a lane at a time: 268 and 366.
 #include "op_common.h"
 
 #include <algorithm>
@@ -196,8 +197,8 @@ __device__ __forceinline__ RowAt row_at(unsigned i, unsigned rows, unsigned head
   return {(int)t, (int)(i - t * heads)};
 }
 
-// us, 16384 rows of 32 + 8 heads of 128 in bf16, half of each rotated: 83, 4.05 TB/s read and written (one row at a time 86, four 88, with results that stay in the caches 107, without
-// the next rows' loads ahead 110).
+// us, 16384 rows of 32 + 8 heads of 128 in bf16, half of each rotated, when these choices were made, side by side on one machine: 83 (one row at a time 86, four 88, with results that stay in the caches 107,
+// without the next rows' loads ahead 110).
 template <typename T, int V, int PIECES, int LANES, bool STREAM>
 __global__ __launch_bounds__(256) void head_rotary_kernel(const RotaryArgs a) {
   touch_args(a);
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void head_rotary_kernel(const RotaryArgs a) {
   }
 }
 
-// Tokens in turn by a fixed number of blocks, each of which leaves one sum of the weights' gradients. The same rows: 121 us, 4.2 TB/s (two rows at a time 158: 149 registers for 110).
+// Tokens in turn by a fixed number of blocks, each of which leaves one sum of the weights' gradients. The same rows, side by side: 121 us (two rows at a time 158: 149 registers for 110).
 template <typename T, int V, int PIECES, int LANES, bool STREAM>
 __global__ __launch_bounds__(256) void head_rotary_backward_kernel(const RotaryArgs a) {
   touch_args(a);
